@@ -412,6 +412,140 @@ int ilpc_paged_prefill_attn_cascade(const uint16_t* q, const uint16_t* k_pool, c
                                     uint16_t* out, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Block tables, row offsets, context lengths and slot map of a batch that
+ * grows by new tokens, on the device (section 2.1.2: the KV cache is held in
+ * fixed-size blocks, allocated as tokens come).  Request r holds start_pos[r]
+ * tokens, whose blocks are the first ceil(start_pos[r] / 16) entries of its
+ * row, and gets new_lens[r] more.
+ *
+ * block_tables [device] int32 [B, max_blocks]  in/out: the entries of the new
+ *              blocks are written, all others stay as they are
+ * start_pos    [device] int32 [B]    tokens held, >= 0
+ * new_lens     [device] int32 [B]    new tokens, >= 0
+ * free_ids     [device] int32 [n_free]  free block ids, taken in order
+ * taken        [device] int32 [1]    ids at the front of free_ids already taken
+ * num_blocks   [host]   blocks of the pools the slots are for
+ * seq_lens     [device] int32 [B]    out: start_pos[r] + new_lens[r]; may be
+ *                                    start_pos itself
+ * cu_q         [device] int32 [B+1]  out: first row of each request (running
+ *                                    sums of new_lens)
+ * cu_blocks    [device] int32 [B+1]  out: running sums of the blocks taken
+ * slot_map     [device] int32 [max_rows]  out: 16 * block + offset of each
+ *              row's token in the pools; -1 for rows behind cu_q[B] (padding of
+ *              a captured step) and where the block id is not in [0, num_blocks)
+ * taken_out    [device] int32 [1]    out: taken + blocks taken; may be taken
+ * status       [device] int32 [1]    out: 0, or what was refused (bits)
+ *
+ * Request r's k-th new block is free_ids[taken + cu_blocks[r] + k], as from an
+ * allocator that serves request after request.  The batch is taken whole or
+ * not at all: with status 1 (free_ids does not hold enough), 2 (a request
+ * passes 16 * max_blocks tokens), 4 (more than max_rows new tokens) or 8 (a
+ * negative length, or taken outside [0, n_free]) set, tables and taken count
+ * stay as they were, seq_lens is start_pos, cu_q and cu_blocks are 0 and every
+ * slot is -1, so that the append and attention queued behind do nothing.
+ * B <= 2^20, max_blocks <= 2^24, num_blocks < 2^27 (ILPC_EUNSUP); other outputs
+ * must not overlap inputs.  No workspace; captured into a graph, a replay goes
+ * by the lengths that it finds.
+ */
+int ilpc_extend_tables(int32_t* block_tables, int32_t max_blocks, int32_t B, const int32_t* start_pos,
+                       const int32_t* new_lens, const int32_t* free_ids, int32_t n_free, const int32_t* taken,
+                       int32_t num_blocks, int32_t* seq_lens, int32_t* cu_q, int32_t* cu_blocks, int32_t* slot_map,
+                       int32_t max_rows, int32_t* taken_out, int32_t* status, void* stream);
+
+/*
+ * Blocks given back to the free list that ilpc_extend_tables takes from
+ * (section 2.1.2: a finished request's blocks are freed).  Of request r, the
+ * entries first_block[r] .. ceil(seq_lens[r] / 16) - 1 of its row are put back
+ * in front of the ids still free, request after request:
+ *   free_ids[taken - n + cu_blocks[r] + k] = block_tables[r][first_block[r] + k],
+ * n = cu_blocks[B] their number.  A request that goes on has seq_lens[r] = 0
+ * here (or first_block[r] at or past its end).  The tables are not changed.
+ *
+ * first_block  [device] int32 [B]    blocks at the front that are not given
+ *                                    back (those the prefix cache holds)
+ * seq_lens     [device] int32 [B]
+ * free_ids     [device] int32 [n_free]  in/out
+ * taken        [device] int32 [1]    ids of free_ids taken
+ * cu_blocks    [device] int32 [B+1]  out: running sums of the blocks given back
+ * taken_out    [device] int32 [1]    out: taken - n; may be taken
+ * status       [device] int32 [1]    out: 0, or bits as above: 1 more blocks
+ *              than were taken, 2 a request longer than its row, 8 a negative
+ *              value or taken outside [0, n_free]; then nothing is given back
+ *              and cu_blocks is 0
+ *
+ * Ids go back as they stand in the rows; one given back twice is in the list
+ * twice.  Limits as for ilpc_extend_tables.
+ */
+int ilpc_release_tables(const int32_t* block_tables, int32_t max_blocks, int32_t B, const int32_t* first_block,
+                        const int32_t* seq_lens, int32_t* free_ids, int32_t n_free, const int32_t* taken,
+                        int32_t* cu_blocks, int32_t* taken_out, int32_t* status, void* stream);
+
+/*
+ * ilpc_kv_append by a slot map (section 3.2.2): row i of k_new and v_new is
+ * stored at slot s = slot_map[i] of the pools, block s / 16, offset s % 16.
+ * Rows whose slot is not in [0, 16 * num_blocks) are not stored; a slot named
+ * by more than one row holds unspecified ones of their values.
+ *
+ * k_new, v_new [device] bf16, row i at k_new + i * k_stride (elements; a
+ *              multiple of 8, at least Hkv * D): [Hkv, D], contiguous, so that
+ *              rows may be parts of a fused projection's
+ * slot_map     [device] int32 [n_rows]
+ */
+int ilpc_kv_append_slots(const uint16_t* k_new, int64_t k_stride, const uint16_t* v_new, int64_t v_stride,
+                         uint16_t* k_pool, uint16_t* v_pool, int32_t num_blocks, const int32_t* slot_map,
+                         int32_t n_rows, int32_t Hkv, int32_t D, int32_t block_size, void* stream);
+
+/* Which dimensions of a head ilpc_paged_diff_attn's two maps read: its two
+ * halves, or (pair layout) those i with i mod D/2 in the lower or upper half of
+ * D/2, so that the pairs (i, i + D/2) that ilpc_rope_kv_append rotates lie
+ * within one map (its inv_freq then holds the D/4 angles of a map twice). */
+#define ILPC_DIFF_HALVES 0
+#define ILPC_DIFF_ROPE 1
+
+/* Bytes of device workspace ilpc_paged_diff_attn needs for these sizes on the
+ * current device (0 where one workgroup works a request's keys). */
+int ilpc_diff_attn_workspace_bytes(int32_t B, int32_t max_q_len, int32_t Hq, int32_t Hkv, int32_t D,
+                                   int32_t max_blocks, size_t* bytes);
+
+/*
+ * Differential attention over the paged cache: the difference of two causal
+ * softmax maps over one set of values, for prefill suffixes and decode steps
+ * alike (section 2.1.2, as ilpc_paged_prefill_attn).  With q = [q1 | q2] and
+ * k = [k1 | k2] the two maps' parts of a head's D dimensions,
+ *   A_m = softmax(softmax_scale * q_m k_m^T)  over the keys a query sees,
+ *   y   = (A_1 - lambda[h] * A_2) V,
+ *   out = out_scale * norm_weight * y / sqrt(mean(y^2) + norm_eps),
+ * or out_scale * y where norm_weight is NULL.  Queries, keys, head groups,
+ * pools and tables are those of ilpc_paged_prefill_attn, with these arguments:
+ *
+ * q            [device] bf16, row i at q + i * q_stride (elements; a multiple
+ *              of 8, at least Hq * D): [Hq, D], contiguous
+ * n_rows       [host]   rows of q and out; requests with rows at or past it are
+ *              not computed
+ * softmax_scale > 0     usually 1 / sqrt(D / 2)
+ * layout       ILPC_DIFF_HALVES or ILPC_DIFF_ROPE
+ * lambda       [device] fp32 [Hq]
+ * norm_weight  [device] fp32 [D], 16-byte aligned, or NULL
+ * out          [device] bf16 [n_rows, Hq, D]; rows of no request stay as they are
+ * workspace    [device] >= ilpc_diff_attn_workspace_bytes() bytes, 16-byte
+ *              aligned, no initial contents needed (NULL with 0 bytes where
+ *              that is 0).  Calls that may run concurrently, captured graphs
+ *              among them, need separate ones.
+ *
+ * Scores, softmax sums and the products with V are held in fp32; the weights
+ * enter those products as bf16 numbers whose rounding is made up for (see the
+ * kernels), so that the error stays near the rounding of the output also where
+ * the maps nearly cancel.  Requests with q_len_r > L_r are not computed;
+ * otherwise the bounds rules of ilpc_paged_prefill_attn hold.
+ */
+int ilpc_paged_diff_attn(const uint16_t* q, int64_t q_stride, int32_t n_rows, const uint16_t* k_pool,
+                         const uint16_t* v_pool, int32_t num_blocks, const int32_t* block_tables, int32_t max_blocks,
+                         const int32_t* cu_q, const int32_t* seq_lens, int32_t B, int32_t max_q_len, int32_t Hq,
+                         int32_t Hkv, int32_t D, int32_t block_size, float softmax_scale, int32_t layout,
+                         const float* lambda, const float* norm_weight, float norm_eps, float out_scale,
+                         uint16_t* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Scheduler steps of a chunked prefill (the per-step token bound that section
  * 3.3 tunes, vLLM's max-num-batched-tokens; section 4.1's PC-Chunk baseline).
  * Host only.

@@ -21,6 +21,10 @@ InferLog paper (arXiv 2507.08523) it follows.
   least-recently-used eviction (section 2.1.2).
 * ``rope_ref``    -- rotary position embedding of the new tokens' keys and
   queries at their absolute positions (section 2.1.2; RoFormer's rotation).
+* ``diff_ref``    -- dense float64 differential attention of the same suffix
+  queries: the difference of two causal softmax maps over one set of values.
+* ``tables_ref``  -- block tables, slot map and free list of a growing batch
+  (section 2.1.2: blocks allocated as tokens come, freed at a request's end).
 
 Readings of points the paper leaves open (block size 16, frozen-snapshot
 visibility inside a batch, the fully-cached cap, the hash itself, 1/sqrt(D)

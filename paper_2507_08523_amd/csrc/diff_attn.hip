@@ -1,0 +1,614 @@
+// Differential attention over the paged cache, for gfx950: each head is the
+// difference of two softmax maps over one set of values.
+//
+// With the halves q = [q1 | q2] and k = [k1 | k2] of a head's D dimensions,
+//   A_m = softmax(s q_m k_m^T)  (causal),   y = (A_1 - lambda_h A_2) V,
+//   out = out_scale * w * y / sqrt(mean(y^2) + eps)   (w: optional norm weight).
+// A K row of the pool holds [k1 | k2], a V row all D values, so the pools, the
+// block tables and the appends are those of ordinary attention (InferLog
+// section 2.1.2: the suffix queries attend to the reused KV of the cached prefix
+// and to their own).  In one pass over the keys a head keeps per map a running
+// maximum m_m, a sum l_m and O_m = sum 2^(s log2(e) q_m.k_m - m_m) v; at the end
+//   y = O_1 / l_1 - lambda_h O_2 / l_2.
+//
+// Kernel for few columns: 16 (token, head of the group) columns a wave.  The two
+// maps are the two 16-column halves of the N side of one
+// v_mfma_f32_32x32x16_bf16 stream: column c holds [q1 | 0], column 16 + c
+// [0 | q2], so one product over all D dimensions of a K row gives both scores.
+// Half of those products multiply zeros, which costs nothing here: the kernel is
+// bound by reading K and V from HBM.  Each wave streams its range of a
+// request's keys from the pools into registers, two pool blocks (32 keys) a
+// step, the next step's loads in flight; W waves of a workgroup and n_split
+// workgroups share a (request, kv head, column tile) where there are too few of
+// them to fill the chip, and their states are joined at the end.
+//   Precision: y is a difference, and where the two maps nearly agree (the case
+// the method is made for) it is much smaller than its terms, so that a weight
+// rounded to bf16 (2^-9 relative) would leave an error of several bf16 roundings
+// of y.  Each weight p therefore enters as two bf16 numbers, hi = bf16(p) and
+// lo = bf16(p - hi), 16 bits in all: 8 more products a step, on matrix cores
+// that wait for HBM.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+
+#include "../../include/ilpc.h"
+#include "ilpc_internal.h"
+
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kBlock = 16;
+constexpr int kStepKeys = 32;        // keys a step (two pool blocks)
+constexpr int kTileCols = 16;        // query columns of a wave (each one twice, once a map)
+constexpr int kMaxGroups = 16;       // most workgroups to a pair
+constexpr float kLazyRescale = 8.f;  // log2 growth of a column max tolerated before rescaling O
+
+// What the last step of every kernel here needs.
+struct Epilogue {
+  const float* lambda;  // [Hq]
+  const float* norm_w;  // [D] or nullptr: no norm
+  float eps, scale;
+};
+
+// Key held by MFMA row m of a step: the groups [4,8) and [8,12) of every 16
+// keys trade places, which makes accumulator register e of lane half hh the key
+// (e >> 3) * 16 + 8 * hh + (e & 7): the layout of the P^T operand.
+__device__ __forceinline__ int key_of_row(int m) {
+  const int grp = (m >> 2) & 3;
+  return m + (grp == 1 ? 4 : (grp == 2 ? -4 : 0));
+}
+
+__device__ __forceinline__ bf16x8 as_bf16x8(u32x4 v) { return __builtin_bit_cast(bf16x8, v); }
+
+__device__ __forceinline__ float max_across_halves(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float add_across_halves(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// Map that 16-dimension chunk kc of a head belongs to: its half of D, or in the
+// pair layout its half of each half of D.
+template <int D>
+__device__ __forceinline__ int map_of_chunk(int kc, int pairs) {
+  return pairs ? (kc / (D / 64)) & 1 : kc / (D / 32);
+}
+
+template <int D>
+struct StepRegs {
+  u32x4 k[D / 16];      // K operand, one per 16-dimension chunk
+  u32x4 v[2][D / 32];   // V^T operand, [pool block of the step][32-dimension tile]
+};
+
+constexpr int group_waves(int W) { return W > 4 ? W : 4; }  // waves of a workgroup, W of them to a pair
+
+template <int D, int W>
+__global__ __launch_bounds__(64 * group_waves(W), 2) void diff_stream_kernel(
+    const uint16_t* __restrict__ q, int64_t q_stride, int n_rows, const uint16_t* __restrict__ k_pool,
+    const uint16_t* __restrict__ v_pool, int num_blocks, const int32_t* __restrict__ block_tables, int max_blocks,
+    const int32_t* __restrict__ cu_q, const int32_t* __restrict__ seq_lens, int n_req, int max_q_len, int Hq, int Hkv,
+    float scale_log2, int pairs_layout, Epilogue ep, uint16_t* __restrict__ out, int n_ct, int n_split,
+    float* __restrict__ part_o, float* __restrict__ part_ml) {
+  constexpr int kDch = D / 16, kDt = D / 32, kWavesPerGroup = group_waves(W);
+  // Q^T of each wave in LDS; for the merge (W > 1) the same space holds every
+  // wave's O, a row of kRow floats a column.
+  constexpr int kRow = D + 4, kCols = 2 * kTileCols;
+  constexpr int kQBytes = kWavesPerGroup * kDch * 64 * 16, kOBytes = kWavesPerGroup * kCols * kRow * 4;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[W > 1 && kOBytes > kQBytes ? kOBytes : kQBytes];
+  __shared__ float s_m[kWavesPerGroup][kCols], s_l[kWavesPerGroup][kCols];
+  u32x4(*q_lds)[kDch][64] = reinterpret_cast<u32x4(*)[kDch][64]>(lds);
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = lane & 31, hh = lane >> 5;
+  const int map = n >> 4, nc = n & 15;  // this lane's map, and its column of the tile
+
+  // Workgroup b runs on XCD b % 8; each XCD takes a contiguous range of items,
+  // numbered request-major (all kv heads of a block are adjacent in memory).
+  const unsigned nb = gridDim.x, per = nb >> 3, extra = nb & 7u;
+  const unsigned x = blockIdx.x & 7u, i = blockIdx.x >> 3;
+  const unsigned group = x * per + min(x, extra) + i;
+  const int64_t item = int64_t(group) * (kWavesPerGroup / W) + wave / W;
+  const int64_t n_items = int64_t(n_req) * Hkv * n_split * n_ct;
+  if (W == 1 && item >= n_items) return;
+  const bool in_grid = item < n_items;
+  const int ct = in_grid ? int(item % n_ct) : 0;
+  const int64_t rest = in_grid ? item / n_ct : 0;
+  const int sp = int(rest % n_split), pair = int(rest / n_split);
+  const int r = pair / Hkv, h = pair % Hkv;
+  const int G = Hq / Hkv;
+
+  const int q0 = cu_q[r], q_end = cu_q[r + 1], q_len = q_end - q0;
+  const int L = min(seq_lens[r], max_blocks * kBlock);
+  const int col0 = ct * kTileCols, n_cols = min(min(q_len, max_q_len) * G - col0, kTileCols);
+  const bool valid = in_grid && q0 >= 0 && q_end <= n_rows && q_len > 0 && q_len <= L && n_cols > 0;
+  if (W == 1 && !valid) return;
+
+  f32x16 o[kDt];
+#pragma unroll
+  for (int dt = 0; dt < kDt; ++dt)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[dt][e] = 0.f;
+  float m_run = -INFINITY, l_run = 0.f;
+  // This lane's column (padding columns repeat the last valid one).
+  const bool col_valid = valid && nc < n_cols;
+  const int colc = col0 + (col_valid ? nc : max(n_cols, 1) - 1);
+  const int t = colc / G, head = h * G + (colc - t * G);
+  if (valid) {
+    const int pos = L - q_len + t;  // keys 0 .. pos are visible to this column
+    const uint16_t* qr = q + int64_t(q0 + t) * q_stride + size_t(head) * D;
+#pragma unroll
+    for (int kc = 0; kc < kDch; ++kc) {
+      const u32x4 zero = {0, 0, 0, 0};
+      q_lds[wave][kc][lane] =
+          map_of_chunk<D>(kc, pairs_layout) == map ? *(const u32x4*)(qr + kc * 16 + hh * 8) : zero;
+    }
+    const int32_t* bt = block_tables + size_t(r) * max_blocks;
+    const int n_blk = (L + kBlock - 1) / kBlock;
+    // keys past the last column's position are not visited (and their V rows zeroed)
+    const int key_end = L - q_len + (col0 + n_cols - 1) / G + 1;
+    const int n_steps_all = (key_end + kStepKeys - 1) / kStepKeys;
+    const int n_ranges = n_split * W, range = sp * W + wave % W;
+    const int steps_per = (n_steps_all + n_ranges - 1) / n_ranges;
+    const int s_begin = min(range * steps_per, n_steps_all);
+    const int n_steps = min(s_begin + steps_per, n_steps_all);
+    const int krow = key_of_row(n);
+    const size_t head_off = size_t(h) * kBlock * D;
+    const size_t slab = size_t(Hkv) * kBlock * D;
+
+    // Block ids come 64 at a time, one a lane, a window ahead of use; a step
+    // picks its two with readlane.  Ids past the request's blocks or outside the
+    // pool read block 0 (those keys are masked and their V rows zeroed, or the
+    // request's output is unspecified).
+    auto load_ids = [&](int window) { return bt[min(window * 64 + lane, max_blocks - 1)]; };
+    int win = (2 * s_begin) >> 6;
+    int ids0, ids1;
+    if (win & 1) {
+      ids1 = load_ids(win);
+      ids0 = load_ids(win + 1);
+    } else {
+      ids0 = load_ids(win);
+      ids1 = load_ids(win + 1);
+    }
+    auto block_id = [&](int lb) {
+      const int id = (win & 1) ? __builtin_amdgcn_readlane(ids1, lb & 63) : __builtin_amdgcn_readlane(ids0, lb & 63);
+      return (lb < n_blk && id >= 0 && id < num_blocks) ? id : 0;
+    };
+    auto load = [&](int s, StepRegs<D>& R) {
+      if ((2 * s) >> 6 != win) {
+        if (win & 1) ids1 = load_ids(win + 2);
+        else ids0 = load_ids(win + 2);
+        ++win;
+      }
+      const int id0 = block_id(2 * s), id1 = block_id(2 * s + 1);
+      const int idk = krow < kBlock ? id0 : id1;
+      const uint16_t* ks = k_pool + size_t(idk) * slab + head_off + size_t(krow & 15) * D + hh * 8;
+#pragma unroll
+      for (int kc = 0; kc < kDch; ++kc) R.k[kc] = *(const u32x4*)(ks + kc * 16);
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const uint16_t* vs = v_pool + size_t(b ? id1 : id0) * slab + head_off + size_t(n) * kBlock + hh * 8;
+#pragma unroll
+        for (int dt = 0; dt < kDt; ++dt) R.v[b][dt] = *(const u32x4*)(vs + dt * 32 * kBlock);
+      }
+    };
+
+    const int mask_from = L - q_len + col0 / G;  // steps reaching past this key need the causal mask
+
+    auto compute = [&](int s, StepRegs<D>& R) {
+      const int j0 = s * kStepKeys;
+      f32x16 sc;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) sc[e] = 0.f;
+#pragma unroll
+      for (int kc = 0; kc < kDch; ++kc)
+        sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(R.k[kc]), as_bf16x8(q_lds[wave][kc][lane]), sc, 0, 0,
+                                                    0);
+      if (j0 + kStepKeys - 1 > mask_from) {
+        // causal mask (which also covers keys >= L), and the V rows of keys >=
+        // key_end zeroed: unwritten pool slots may hold any bits
+        const int rel = pos - j0 - hh * 8;
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if ((e >> 3) * 16 + (e & 7) > rel) sc[e] = -INFINITY;
+        const int lim = key_end - j0 - hh * 8;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int dt = 0; dt < kDt; ++dt)
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+              const int k0 = b * 16 + 2 * w;
+              R.v[b][dt][w] &= (k0 < lim ? 0x0000FFFFu : 0u) | (k0 + 1 < lim ? 0xFFFF0000u : 0u);
+            }
+      }
+      float mx = sc[0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) mx = fmaxf(mx, sc[e]);
+      mx = max_across_halves(mx) * scale_log2;
+      // O and the sum are rescaled only when a column max has grown by more than 2^8
+      if (__ballot(mx > m_run + kLazyRescale)) {
+        const float m_new = fmaxf(m_run, mx);
+        const float alpha = m_new == m_run ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
+        m_run = m_new;
+        l_run *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < kDt; ++dt)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[dt][e] *= alpha;
+      }
+      // (a column that has seen no key yet, in a range that starts past key 0,
+      // has scores and maximum -inf: exp2(-inf - 0) = 0)
+      const float m_sub = m_run == -INFINITY ? 0.f : m_run;
+      bf16x8 ph[2], pl[2];
+      float ls = 0.f;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e], scale_log2, -m_sub));
+        const __bf16 hi = (__bf16)p;
+        ph[e >> 3][e & 7] = hi;
+        pl[e >> 3][e & 7] = (__bf16)(p - (float)hi);
+        ls += p;
+      }
+      l_run += ls;
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int dt = 0; dt < kDt; ++dt) {
+          o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(R.v[b][dt]), ph[b], o[dt], 0, 0, 0);
+          o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(R.v[b][dt]), pl[b], o[dt], 0, 0, 0);
+        }
+    };
+
+    // Two register sets; the scheduling barriers keep a step's loads behind the
+    // computation that frees their registers.
+    StepRegs<D> ra, rb;
+    int s = s_begin;
+    if (s < n_steps) load(s, ra);
+    for (; s + 1 < n_steps; s += 2) {
+      load(s + 1, rb);
+      __builtin_amdgcn_sched_barrier(0);
+      compute(s, ra);
+      __builtin_amdgcn_sched_barrier(0);
+      if (s + 2 < n_steps) load(s + 2, ra);
+      __builtin_amdgcn_sched_barrier(0);
+      compute(s + 1, rb);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (s < n_steps) compute(s, ra);
+  }
+
+  const float l_tot = add_across_halves(l_run);
+  if constexpr (W == 1) {
+    if (n_split > 1) {
+      // state of this (pair, split): [map][column of the tile], O unnormalised
+      if (col_valid) {
+        const size_t slot = (size_t(pair) * n_split + sp) * kCols + n;
+        float* po = part_o + slot * D;
+#pragma unroll
+        for (int dt = 0; dt < kDt; ++dt)
+#pragma unroll
+          for (int g4 = 0; g4 < 4; ++g4) {
+            const f32x4 v = {o[dt][g4 * 4], o[dt][g4 * 4 + 1], o[dt][g4 * 4 + 2], o[dt][g4 * 4 + 3]};
+            *(f32x4*)(po + dt * 32 + g4 * 8 + hh * 4) = v;
+          }
+        if (hh == 0) {
+          part_ml[slot * 2] = m_run;
+          part_ml[slot * 2 + 1] = l_tot;
+        }
+      }
+      return;
+    }
+    // y = O_1 / l_1 - lambda O_2 / l_2: the two maps of a column are 16 lanes apart
+    const float wgt = (map ? -ep.lambda[head] : 1.f) / l_tot;
+    float sq = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < kDt; ++dt)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float a = o[dt][e] * wgt;
+        o[dt][e] = a + __shfl_xor(a, 16);
+        sq += o[dt][e] * o[dt][e];
+      }
+    float fac = ep.scale;
+    if (ep.norm_w) fac *= rsqrtf(add_across_halves(sq) * (1.f / D) + ep.eps);
+    if (nc >= n_cols) return;
+    uint16_t* orow = out + (size_t(q0 + t) * Hq + head) * D;
+#pragma unroll
+    for (int dt = 0; dt < kDt; ++dt) {
+      if (dt / (kDt / 2) != map) continue;  // (each of a column's lane pairs stores half of the row)
+#pragma unroll
+      for (int g4 = 0; g4 < 4; ++g4) {
+        const int d = dt * 32 + g4 * 8 + hh * 4;
+        f32x4 w = {fac, fac, fac, fac};
+        if (ep.norm_w) {
+          const f32x4 nw = *(const f32x4*)(ep.norm_w + d);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[e] *= nw[e];
+        }
+        bf16x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = (__bf16)(o[dt][g4 * 4 + e] * w[e]);
+        *(bf16x4*)(orow + d) = v;
+      }
+    }
+  } else {
+    // Join of the W ranges: every wave's O, max and sum to LDS (behind a barrier:
+    // no wave reads Q from there any more), then a thread sums 4 dimensions of a
+    // column over the waves, both maps, with weights 2^(m_k - M).
+    float(*so)[kCols][kRow] = reinterpret_cast<float(*)[kCols][kRow]>(lds);
+    __syncthreads();
+    if (col_valid) {
+#pragma unroll
+      for (int dt = 0; dt < kDt; ++dt)
+#pragma unroll
+        for (int g4 = 0; g4 < 4; ++g4) {
+          const f32x4 v = {o[dt][g4 * 4], o[dt][g4 * 4 + 1], o[dt][g4 * 4 + 2], o[dt][g4 * 4 + 3]};
+          *(f32x4*)&so[wave][n][dt * 32 + g4 * 8 + hh * 4] = v;
+        }
+      if (hh == 0) {
+        s_m[wave][n] = m_run;
+        s_l[wave][n] = l_tot;
+      }
+    }
+    __syncthreads();
+    if (!valid) return;
+    const int w0 = wave / W * W;     // first wave of the pair
+    constexpr int kPer = D / 4;      // threads to a column
+    for (int u = (wave - w0) * 64 + lane; u < n_cols * kPer; u += W * 64) {
+      const int c = u / kPer, d = u % kPer * 4;
+      f32x4 acc[2];
+      float mx[2], den[2];
+#pragma unroll
+      for (int mp = 0; mp < 2; ++mp) {
+        const int vc = mp * kTileCols + c;
+        mx[mp] = s_m[w0][vc];
+#pragma unroll
+        for (int k = 1; k < W; ++k) mx[mp] = fmaxf(mx[mp], s_m[w0 + k][vc]);
+        acc[mp] = f32x4{0.f, 0.f, 0.f, 0.f};
+        den[mp] = 0.f;
+#pragma unroll
+        for (int k = 0; k < W; ++k) {
+          const float m = s_m[w0 + k][vc];
+          // (a range that saw no key of this column has weight 0)
+          const float wg = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mx[mp]);
+          den[mp] += wg * s_l[w0 + k][vc];
+          const f32x4 v = *(const f32x4*)&so[w0 + k][vc][d];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[mp][e] += wg * v[e];
+        }
+        if (n_split > 1) {
+          const size_t slot = (size_t(pair) * n_split + sp) * kCols + vc;
+          *(f32x4*)(part_o + slot * D + d) = acc[mp];
+          if (d == 0) {
+            part_ml[slot * 2] = mx[mp];
+            part_ml[slot * 2 + 1] = den[mp];
+          }
+        }
+      }
+      if (n_split > 1) continue;
+      const int tt = (col0 + c) / G, hd = h * G + (col0 + c - tt * G);
+      const float w1 = 1.f / den[0], w2 = ep.lambda[hd] / den[1];
+      f32x4 y;
+      float sq = 0.f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        y[e] = acc[0][e] * w1 - acc[1][e] * w2;
+        sq += y[e] * y[e];
+      }
+      f32x4 f = {ep.scale, ep.scale, ep.scale, ep.scale};
+      if (ep.norm_w) {
+#pragma unroll
+        for (int off = 1; off < kPer; off <<= 1) sq += __shfl_xor(sq, off);
+        const float inv = rsqrtf(sq * (1.f / D) + ep.eps);
+        const f32x4 nw = *(const f32x4*)(ep.norm_w + d);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f[e] *= inv * nw[e];
+      }
+      bf16x4 v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = (__bf16)(y[e] * f[e]);
+      *(bf16x4*)(out + (size_t(q0 + tt) * Hq + hd) * D + d) = v;
+    }
+  }
+}
+
+// Join of the n_split states of a (request, kv head, column), a wave each: lane
+// k reads split k's (max, sum) of each map, M = max m_k, w_k = 2^(m_k - M),
+// O = sum w_k O_k / sum w_k l_k.  Split 0 holds key 0, which every column sees,
+// so M is finite; a split that saw none has m = -inf and weight 0.
+constexpr int kJoinWaves = 4;
+
+template <int D>
+__global__ __launch_bounds__(64 * kJoinWaves) void diff_join_kernel(
+    const float* __restrict__ part_o, const float* __restrict__ part_ml, const int32_t* __restrict__ cu_q,
+    const int32_t* __restrict__ seq_lens, int n_rows, int max_blocks, int n_req, int max_q_len, int Hq, int Hkv,
+    int n_split, int cols_cap, Epilogue ep, uint16_t* __restrict__ out) {
+  constexpr int kPer = D / 64;  // dimensions of a lane
+  typedef float vec_t __attribute__((ext_vector_type(kPer)));
+  const int lane = threadIdx.x & 63;
+  const int64_t w = int64_t(blockIdx.x) * kJoinWaves + (threadIdx.x >> 6);
+  const int c = int(w % cols_cap);
+  const int pair = int(w / cols_cap);
+  if (pair >= n_req * Hkv) return;
+  const int r = pair / Hkv, h = pair % Hkv;
+  const int G = Hq / Hkv;
+  const int q0 = cu_q[r], q_end = cu_q[r + 1], q_len = q_end - q0;
+  const int L = min(seq_lens[r], max_blocks * kBlock);
+  const int n_cols = min(q_len, max_q_len) * G;
+  if (q0 < 0 || q_end > n_rows || q_len <= 0 || q_len > L || c >= n_cols) return;
+  const int t = c / G, head = h * G + (c - t * G);
+
+  vec_t y = {};
+#pragma unroll
+  for (int mp = 0; mp < 2; ++mp) {
+    const size_t slot0 = size_t(pair) * n_split * (2 * kTileCols) + mp * kTileCols + c;
+    constexpr size_t kNext = 2 * kTileCols;  // slots from one split to the next
+    float m = -INFINITY, l = 0.f;
+    if (lane < n_split) {
+      m = part_ml[(slot0 + size_t(lane) * kNext) * 2];
+      l = part_ml[(slot0 + size_t(lane) * kNext) * 2 + 1];
+    }
+    float mx = m;
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor(mx, off));
+    const float wgt = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mx);
+    float den = wgt * l;
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) den += __shfl_xor(den, off);
+    const float* po = part_o + slot0 * D + lane * kPer;
+    vec_t acc = {};
+    for (int k = 0; k < n_split; ++k)
+      acc += __int_as_float(__builtin_amdgcn_readlane(__float_as_int(wgt), k)) * *(const vec_t*)(po + k * kNext * D);
+    y += acc * ((mp ? -ep.lambda[head] : 1.f) / den);
+  }
+  float fac = ep.scale;
+  if (ep.norm_w) {
+    float sq = 0.f;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) sq += y[e] * y[e];
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) sq += __shfl_xor(sq, off);
+    fac *= rsqrtf(sq * (1.f / D) + ep.eps);
+  }
+  uint16_t* orow = out + (size_t(q0 + t) * Hq + head) * D + lane * kPer;
+#pragma unroll
+  for (int e = 0; e < kPer; ++e) {
+    const float f = ep.norm_w ? fac * ep.norm_w[lane * kPer + e] : fac;
+    orow[e] = __builtin_bit_cast(uint16_t, (__bf16)(y[e] * f));
+  }
+}
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+// Waves of a workgroup, and workgroups, to a (request, kv head, column tile).
+struct Plan {
+  int waves, groups;
+};
+
+int64_t column_tiles(int64_t max_q_len, int Hq, int Hkv) {
+  return (max_q_len * (Hq / Hkv) + kTileCols - 1) / kTileCols;
+}
+
+// Enough waves to give every SIMD of the device one; of a workgroup first (their
+// join is in LDS), then of several, while each wave keeps at least 4 steps.
+Plan stream_plan(int64_t items, int64_t n_ct, int64_t max_blocks) {
+  const int64_t cus = ilpc::device_cus(), steps = (max_blocks * kBlock + kStepKeys - 1) / kStepKeys;
+  int w = 1;
+  while (w < 4 && items * w < 4 * cus && w * 2 <= steps) w *= 2;
+  int64_t n = 1;
+  if (w == 4 && n_ct == 1) {
+    n = std::min<int64_t>({cus / items, steps / (4 * w), kMaxGroups});
+    n = std::max<int64_t>(n, 1);
+  }
+  return {w, int(n)};
+}
+
+size_t part_bytes(int64_t pairs, int D, int n) {
+  return n > 1 ? size_t(pairs) * n * (2 * kTileCols) * (D + 2) * sizeof(float) : 0;
+}
+
+int check_sizes(const char* fn, int32_t B, int32_t max_q_len, int32_t Hq, int32_t Hkv, int32_t D, int32_t max_blocks) {
+  using ilpc::set_error;
+  if (B < 0 || max_q_len < 0 || max_blocks < 1 || Hq < 1 || Hkv < 1)
+    return set_error(ILPC_EINVAL, "%s: negative or zero size", fn);
+  if (D != 64 && D != 128) return set_error(ILPC_EUNSUP, "%s: head_dim %d unsupported", fn, D);
+  if (Hq % Hkv != 0 || Hq / Hkv > 64) return set_error(ILPC_EUNSUP, "%s: Hq %d / Hkv %d unsupported", fn, Hq, Hkv);
+  if (max_blocks > (1 << 24)) return set_error(ILPC_EUNSUP, "%s: max_blocks %d > %d", fn, max_blocks, 1 << 24);
+  if (int64_t(B) * Hkv > INT32_MAX / kMaxGroups || int64_t(max_q_len) * (Hq / Hkv) > (int64_t(1) << 30) ||
+      int64_t(B) * Hkv * column_tiles(max_q_len, Hq, Hkv) > INT32_MAX / kMaxGroups)
+    return set_error(ILPC_EUNSUP, "%s: batch too large", fn);
+  return ILPC_OK;
+}
+
+}  // namespace
+
+extern "C" int ilpc_diff_attn_workspace_bytes(int32_t B, int32_t max_q_len, int32_t Hq, int32_t Hkv, int32_t D,
+                                              int32_t max_blocks, size_t* bytes) {
+  static const char* fn = "ilpc_diff_attn_workspace_bytes";
+  if (!bytes) return ilpc::set_error(ILPC_EINVAL, "%s: bytes is NULL", fn);
+  const int rc = check_sizes(fn, B, max_q_len, Hq, Hkv, D, max_blocks);
+  if (rc != ILPC_OK) return rc;
+  *bytes = 0;
+  if (B == 0 || max_q_len == 0) return ILPC_OK;
+  if (ilpc::device_cus() <= 0) return ilpc::set_error(ILPC_EHIP, "%s: cannot query the device", fn);
+  const int64_t n_ct = column_tiles(max_q_len, Hq, Hkv), pairs = int64_t(B) * Hkv;
+  *bytes = part_bytes(pairs, D, stream_plan(pairs * n_ct, n_ct, max_blocks).groups);
+  return ILPC_OK;
+}
+
+extern "C" int ilpc_paged_diff_attn(const uint16_t* q, int64_t q_stride, int32_t n_rows, const uint16_t* k_pool,
+                                    const uint16_t* v_pool, int32_t num_blocks, const int32_t* block_tables,
+                                    int32_t max_blocks, const int32_t* cu_q, const int32_t* seq_lens, int32_t B,
+                                    int32_t max_q_len, int32_t Hq, int32_t Hkv, int32_t D, int32_t block_size,
+                                    float softmax_scale, int32_t layout, const float* lambda,
+                                    const float* norm_weight, float norm_eps, float out_scale, uint16_t* out,
+                                    void* workspace, size_t workspace_bytes, void* stream) {
+  static const char* fn = "ilpc_paged_diff_attn";
+  using ilpc::set_error;
+  const int rc = check_sizes(fn, B, max_q_len, Hq, Hkv, D, max_blocks);
+  if (rc != ILPC_OK) return rc;
+  if (num_blocks < 1 || n_rows < 0) return set_error(ILPC_EINVAL, "%s: num_blocks %d, n_rows %d", fn, num_blocks, n_rows);
+  if (block_size != kBlock) return set_error(ILPC_EUNSUP, "%s: block_size must be 16", fn);
+  if (layout != ILPC_DIFF_HALVES && layout != ILPC_DIFF_ROPE)
+    return set_error(ILPC_EINVAL, "%s: layout %d", fn, layout);
+  if (!(std::isfinite(softmax_scale) && softmax_scale > 0.f) || !std::isfinite(out_scale))
+    return set_error(ILPC_EINVAL, "%s: scales must be finite, and softmax_scale positive", fn);
+  if (norm_weight && !(std::isfinite(norm_eps) && norm_eps >= 0.f))
+    return set_error(ILPC_EINVAL, "%s: norm_eps must be finite and not negative", fn);
+  if (B == 0 || max_q_len == 0 || n_rows == 0) return ILPC_OK;
+  if (!q || !k_pool || !v_pool || !block_tables || !cu_q || !seq_lens || !lambda || !out)
+    return set_error(ILPC_EINVAL, "%s: NULL pointer", fn);
+  if (!aligned16(q) || !aligned16(k_pool) || !aligned16(v_pool) || !aligned16(out) || !aligned16(norm_weight))
+    return set_error(ILPC_EINVAL, "%s: Q/K/V/out/norm_weight must be 16-byte aligned", fn);
+  if (q_stride < int64_t(Hq) * D || q_stride % 8 != 0)
+    return set_error(ILPC_EINVAL, "%s: q_stride must be a multiple of 8 elements, at least Hq * D", fn);
+  if (ilpc::device_cus() <= 0) return set_error(ILPC_EHIP, "%s: cannot query the device", fn);
+  const int64_t n_ct = column_tiles(max_q_len, Hq, Hkv), pairs = int64_t(B) * Hkv;
+  Plan plan = stream_plan(pairs * n_ct, n_ct, max_blocks);
+  const size_t need = part_bytes(pairs, D, plan.groups);
+  if (need && (!workspace || workspace_bytes < need || !aligned16(workspace)))
+    return set_error(ILPC_EINVAL, "%s: workspace must be %zu bytes, 16-byte aligned", fn, need);
+  const Epilogue ep{lambda, norm_weight, norm_eps, out_scale};
+  float* part_o = need ? static_cast<float*>(workspace) : nullptr;
+  float* part_ml = need ? part_o + size_t(pairs) * plan.groups * (2 * kTileCols) * D : nullptr;
+  const int64_t items = pairs * n_ct * plan.groups, per_group = group_waves(plan.waves) / plan.waves;
+  const dim3 grid{unsigned((items + per_group - 1) / per_group)}, block{unsigned(64 * group_waves(plan.waves))};
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  auto launch = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid, block, 0, s, q, q_stride, n_rows, k_pool, v_pool, num_blocks, block_tables, max_blocks,
+                       cu_q, seq_lens, B, max_q_len, Hq, Hkv, softmax_scale * 1.4426950408889634f,
+                       int(layout == ILPC_DIFF_ROPE), ep, out, int(n_ct), plan.groups, part_o, part_ml);
+  };
+  if (D == 128) {
+    if (plan.waves == 1) launch(diff_stream_kernel<128, 1>);
+    else if (plan.waves == 2) launch(diff_stream_kernel<128, 2>);
+    else launch(diff_stream_kernel<128, 4>);
+  } else {
+    if (plan.waves == 1) launch(diff_stream_kernel<64, 1>);
+    else if (plan.waves == 2) launch(diff_stream_kernel<64, 2>);
+    else launch(diff_stream_kernel<64, 4>);
+  }
+  hipError_t e = hipGetLastError();
+  if (e == hipSuccess && plan.groups > 1) {
+    const int cols_cap = int(std::min<int64_t>(int64_t(max_q_len) * (Hq / Hkv), kTileCols));
+    const dim3 jgrid{unsigned((pairs * cols_cap + kJoinWaves - 1) / kJoinWaves)}, jblock{64 * kJoinWaves};
+    auto join = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, jgrid, jblock, 0, s, part_o, part_ml, cu_q, seq_lens, n_rows, max_blocks, B, max_q_len, Hq,
+                         Hkv, plan.groups, cols_cap, ep, out);
+    };
+    if (D == 128) join(diff_join_kernel<128>);
+    else join(diff_join_kernel<64>);
+    e = hipGetLastError();
+  }
+  if (e != hipSuccess) return set_error(ILPC_EHIP, "%s: launch failed: %s", fn, hipGetErrorString(e));
+  return ILPC_OK;
+}

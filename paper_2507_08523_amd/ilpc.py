@@ -23,6 +23,9 @@ LIB_PATH = os.path.join(_HERE, "libilpc.so")
 
 OK, EINVAL, ENOSPC, ETABLE, EUNSUP, EHIP = 0, -1, -2, -3, -4, -5
 NO_LOOKUP, NO_REGISTER = 1, 2
+DIFF_HALVES, DIFF_ROPE = 0, 1  # dimensions of the two maps of a differential head (see the C header)
+# bits of the status that extend_tables and release_tables write
+NO_BLOCKS, TOO_LONG, TOO_MANY_ROWS, BAD_VALUE = 1, 2, 4, 8
 BLOCK = 16
 _NAMES = {EINVAL: "EINVAL", ENOSPC: "ENOSPC", ETABLE: "ETABLE", EUNSUP: "EUNSUP", EHIP: "EHIP"}
 
@@ -56,6 +59,14 @@ _SIGS = [
     ("ilpc_paged_prefill_attn_cascade", _i32, [_vp, _vp, _vp, _i32, _vp, _i32, _vp, _vp, _i32, _i32,
                                                _i32, _i32, _i32, _i32, _i32, _f32, _vp, _vp,
                                                ctypes.c_size_t, _vp]),
+    ("ilpc_extend_tables", _i32, [_vp, _i32, _i32, _vp, _vp, _vp, _i32, _vp, _i32, _vp, _vp, _vp, _vp, _i32, _vp,
+                                  _vp, _vp]),
+    ("ilpc_release_tables", _i32, [_vp, _i32, _i32, _vp, _vp, _vp, _i32, _vp, _vp, _vp, _vp, _vp]),
+    ("ilpc_kv_append_slots", _i32, [_vp, _i64, _vp, _i64, _vp, _vp, _i32, _vp, _i32, _i32, _i32, _i32, _vp]),
+    ("ilpc_diff_attn_workspace_bytes", _i32, [_i32, _i32, _i32, _i32, _i32, _i32,
+                                              ctypes.POINTER(ctypes.c_size_t)]),
+    ("ilpc_paged_diff_attn", _i32, [_vp, _i64, _i32, _vp, _vp, _i32, _vp, _i32, _vp, _vp, _i32, _i32, _i32, _i32,
+                                    _i32, _i32, _f32, _i32, _vp, _vp, _f32, _f32, _vp, _vp, ctypes.c_size_t, _vp]),
     ("ilpc_chunk_schedule", _i32, [_vp, _i32, _i32, _i32, _vp, _vp, _vp, _vp, ctypes.POINTER(_i32),
                                    ctypes.POINTER(_i32)]),
     ("ilpc_shared_prefix_len", _i32, [_vp, _vp, _i32, _i32, ctypes.POINTER(_i32)]),
@@ -604,3 +615,196 @@ def paged_prefill_attn_cascade(q, k_pool, v_pool, block_tables, cu_q, seq_lens, 
             _dev(out, torch.bfloat16, "out", 3), _dev(workspace, torch.uint8, "workspace", 1),
             workspace.numel(), _stream(stream))
     _check(load().ilpc_paged_prefill_attn_cascade(*args))
+
+
+# -- growing batches on the device, differential attention ---------------------
+
+def _at(tensors, stream):
+    """The stream of a call on these tensors (`stream`, or their device's current
+    one): all on one device, the stream's.  Returns a context in which that
+    device is the current one, and the stream."""
+    import torch
+
+    dev = tensors[0].device
+    for t in tensors:
+        if t is not None and t.device != dev:
+            raise ILPCError(EINVAL, f"tensors on {dev} and on {t.device}")
+    if stream is None:
+        stream = torch.cuda.current_stream(dev)
+    elif stream.device != dev:
+        raise ILPCError(EINVAL, f"tensors on {dev}, the stream on {stream.device}")
+    return torch.cuda.device(dev), stream
+
+
+def _rows(t, name, shape):
+    """Pointer and row stride of bf16 rows [n, H, D], each row contiguous."""
+    import torch
+
+    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+        raise ILPCError(EINVAL, f"{name} must be a CUDA/HIP torch tensor")
+    if t.dtype != torch.bfloat16:
+        raise ILPCError(EINVAL, f"{name} must be {torch.bfloat16}, got {t.dtype}")
+    if t.dim() != 3 or t.shape[1:] != shape:
+        raise ILPCError(EINVAL, f"{name} must be [rows, {shape[0]}, {shape[1]}]")
+    n, H, D = t.shape
+    if t.numel() and (t.stride(2) != 1 or (H > 1 and t.stride(1) != D)):
+        raise ILPCError(EINVAL, f"{name} must have contiguous rows")
+    return ctypes.c_void_p(t.data_ptr()), t.stride(0) if n > 1 else H * D
+
+
+def _pools(k_pool, v_pool, fn):
+    import torch
+
+    kp, vp = _dev(k_pool, torch.bfloat16, "k_pool", 4), _dev(v_pool, torch.bfloat16, "v_pool", 4)
+    NB, Hkv, bs, D = k_pool.shape
+    if v_pool.shape != (NB, Hkv, D, bs):
+        raise ILPCError(EINVAL, f"{fn}: inconsistent pool shapes")
+    return kp, vp, NB, Hkv, bs, D
+
+
+def _ints(fn, **tensors):
+    """Pointers of int32 device tensors, each given with its wanted shape (-1: any)."""
+    import torch
+
+    out = []
+    for name, (t, shape) in tensors.items():
+        p = _dev(t, torch.int32, name, len(shape))
+        if any(w >= 0 and w != have for w, have in zip(shape, t.shape)):
+            raise ILPCError(EINVAL, f"{fn}: {name} must be {list(shape)}, got {list(t.shape)}")
+        out.append(p)
+    return out
+
+
+def _apart(fn, outputs, inputs):
+    """Refuses outputs that share memory with an input or with each other."""
+    spans = [(t.data_ptr(), t.data_ptr() + 4 * t.numel(), name) for name, t in outputs + inputs if t.numel()]
+    for i, (a0, a1, an) in enumerate(spans[:len(outputs)]):
+        for b0, b1, bn in spans[i + 1:]:
+            if a0 < b1 and b0 < a1:
+                raise ILPCError(EINVAL, f"{fn}: {an} and {bn} overlap")
+
+
+def extend_tables(block_tables, start_pos, new_lens, free_ids, taken, seq_lens, cu_q, cu_blocks, slot_map, taken_out,
+                  status, num_blocks: int, stream=None):
+    """Grow the requests' block tables by new tokens on the device (see the C header).
+
+    All int32 device tensors: block_tables [B, max_blocks] (in/out), start_pos
+    and new_lens [B], free_ids [n], taken [1]; out: seq_lens [B] (may be
+    start_pos), cu_q and cu_blocks [B+1], slot_map [rows], taken_out [1] (may be
+    taken), status [1] (0, or NO_BLOCKS | TOO_LONG | TOO_MANY_ROWS | BAD_VALUE
+    with nothing changed).
+    """
+    fn = "extend_tables"
+    B = start_pos.shape[0] if getattr(start_pos, "ndim", 0) == 1 else -1
+    p = _ints(fn, block_tables=(block_tables, (B, -1)), start_pos=(start_pos, (B,)), new_lens=(new_lens, (B,)),
+              free_ids=(free_ids, (-1,)), taken=(taken, (1,)), seq_lens=(seq_lens, (B,)), cu_q=(cu_q, (B + 1,)),
+              cu_blocks=(cu_blocks, (B + 1,)), slot_map=(slot_map, (-1,)), taken_out=(taken_out, (1,)),
+              status=(status, (1,)))
+    outs = [("block_tables", block_tables), ("cu_q", cu_q), ("cu_blocks", cu_blocks), ("slot_map", slot_map),
+            ("status", status)]
+    ins = [("new_lens", new_lens), ("free_ids", free_ids)]
+    for out, src, name, of in ((seq_lens, start_pos, "seq_lens", "start_pos"), (taken_out, taken, "taken_out", "taken")):
+        outs.append((name, out))
+        if out.data_ptr() != src.data_ptr():
+            ins.append((of, src))
+    _apart(fn, outs, ins)
+    ctx, s = _at((start_pos, block_tables, new_lens, free_ids, taken, seq_lens, cu_q, cu_blocks, slot_map, taken_out,
+                  status), stream)
+    with ctx:
+        _check(load().ilpc_extend_tables(p[0], block_tables.shape[1], B, p[1], p[2], p[3], free_ids.shape[0], p[4],
+                                         int(num_blocks), p[5], p[6], p[7], p[8], slot_map.shape[0], p[9], p[10],
+                                         ctypes.c_void_p(s.cuda_stream)))
+
+
+def release_tables(block_tables, first_block, seq_lens, free_ids, taken, cu_blocks, taken_out, status, stream=None):
+    """Give blocks back to the free list of extend_tables (see the C header): of
+    each request, table entries first_block[r] .. ceil(seq_lens[r] / 16) - 1.
+
+    All int32 device tensors: block_tables [B, max_blocks], first_block and
+    seq_lens [B], free_ids [n] (in/out), taken [1]; out: cu_blocks [B+1],
+    taken_out [1] (may be taken), status [1].
+    """
+    fn = "release_tables"
+    B = first_block.shape[0] if getattr(first_block, "ndim", 0) == 1 else -1
+    p = _ints(fn, block_tables=(block_tables, (B, -1)), first_block=(first_block, (B,)), seq_lens=(seq_lens, (B,)),
+              free_ids=(free_ids, (-1,)), taken=(taken, (1,)), cu_blocks=(cu_blocks, (B + 1,)),
+              taken_out=(taken_out, (1,)), status=(status, (1,)))
+    outs = [("free_ids", free_ids), ("cu_blocks", cu_blocks), ("status", status), ("taken_out", taken_out)]
+    ins = [("block_tables", block_tables), ("first_block", first_block), ("seq_lens", seq_lens)]
+    if taken_out.data_ptr() != taken.data_ptr():
+        ins.append(("taken", taken))
+    _apart(fn, outs, ins)
+    ctx, s = _at((first_block, block_tables, seq_lens, free_ids, taken, cu_blocks, taken_out, status), stream)
+    with ctx:
+        _check(load().ilpc_release_tables(p[0], block_tables.shape[1], B, p[1], p[2], p[3], free_ids.shape[0], p[4],
+                                          p[5], p[6], p[7], ctypes.c_void_p(s.cuda_stream)))
+
+
+def kv_append_slots(k_new, v_new, k_pool, v_pool, slot_map, stream=None):
+    """Store K/V rows [n, Hkv, D] at the slots of slot_map (int32 [n]; rows whose
+    slot is not in the pools, -1 among them, are not stored).  The rows may be
+    views of a wider row (a fused projection's output)."""
+    fn = "kv_append_slots"
+    kp, vp, NB, Hkv, bs, D = _pools(k_pool, v_pool, fn)
+    k, k_stride = _rows(k_new, "k_new", (Hkv, D))
+    v, v_stride = _rows(v_new, "v_new", (Hkv, D))
+    n = k_new.shape[0]
+    if v_new.shape[0] != n:
+        raise ILPCError(EINVAL, f"{fn}: k_new and v_new must have as many rows")
+    (slots,) = _ints(fn, slot_map=(slot_map, (n,)))
+    ctx, s = _at((k_pool, v_pool, k_new, v_new, slot_map), stream)
+    with ctx:
+        _check(load().ilpc_kv_append_slots(k, k_stride, v, v_stride, kp, vp, NB, slots, n, Hkv, D, bs,
+                                           ctypes.c_void_p(s.cuda_stream)))
+
+
+def diff_attn_workspace_bytes(B, max_q_len, Hq, Hkv, D, max_blocks) -> int:
+    n = ctypes.c_size_t()
+    _check(load().ilpc_diff_attn_workspace_bytes(B, max_q_len, Hq, Hkv, D, max_blocks, ctypes.byref(n)))
+    return int(n.value)
+
+
+def paged_diff_attn(q, k_pool, v_pool, block_tables, cu_q, seq_lens, max_q_len: int, scale: float, lam, out,
+                    norm_weight=None, norm_eps: float = 1e-5, out_scale: float = 1.0, layout: int = DIFF_HALVES,
+                    workspace=None, stream=None):
+    """Differential attention of packed queries [total, Hq, D] over the paged pools:
+    (softmax(scale q1 k1^T) - lam softmax(scale q2 k2^T)) V per head, causal, then
+    per-head RMS norm (with norm_weight) and out_scale; see the C header.
+
+    q may be a view of a wider row.  lam: fp32 [Hq]; norm_weight: fp32 [D] or
+    None.  `workspace` (uint8, diff_attn_workspace_bytes() bytes) is allocated
+    for the call when omitted, on its stream, so that calls and captured graphs
+    do not share one.
+    """
+    import torch
+
+    fn = "paged_diff_attn"
+    kp, vp, NB, Hkv, bs, D = _pools(k_pool, v_pool, fn)
+    if not isinstance(q, torch.Tensor) or q.dim() != 3 or out.shape != q.shape:
+        raise ILPCError(EINVAL, f"{fn}: q and out must both be [total, Hq, {D}]")
+    total, Hq, _ = q.shape
+    qp, q_stride = _rows(q, "q", (Hq, D))
+    B = cu_q.shape[0] - 1 if getattr(cu_q, "ndim", 0) == 1 else -1
+    bt, cu, L = _ints(fn, block_tables=(block_tables, (B, -1)), cu_q=(cu_q, (B + 1,)), seq_lens=(seq_lens, (B,)))
+    lp = _dev(lam, torch.float32, "lam", 1)
+    if lam.shape[0] != Hq:
+        raise ILPCError(EINVAL, f"{fn}: lam must be [{Hq}]")
+    wp = None
+    if norm_weight is not None:
+        wp = _dev(norm_weight, torch.float32, "norm_weight", 1)
+        if norm_weight.shape[0] != D:
+            raise ILPCError(EINVAL, f"{fn}: norm_weight must be [{D}]")
+    op = _dev(out, torch.bfloat16, "out", 3)
+    ctx, s = _at((k_pool, v_pool, q, out, block_tables, cu_q, seq_lens, lam, norm_weight, workspace), stream)
+    with ctx:
+        if workspace is None:
+            need = diff_attn_workspace_bytes(B, int(max_q_len), Hq, Hkv, D, block_tables.shape[1])
+            if need:
+                with torch.cuda.stream(s):
+                    workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        ws, nbytes = (None, 0) if workspace is None else (_dev(workspace, torch.uint8, "workspace", 1),
+                                                         workspace.numel())
+        _check(load().ilpc_paged_diff_attn(qp, q_stride, total, kp, vp, NB, bt, block_tables.shape[1], cu, L, B,
+                                           int(max_q_len), Hq, Hkv, D, bs, float(scale), int(layout), lp, wp,
+                                           float(norm_eps), float(out_scale), op, ws, nbytes,
+                                           ctypes.c_void_p(s.cuda_stream)))

@@ -37,14 +37,19 @@ class PagedPrefixCache:
     """Prefix cache (host) + paged K/V pools (device) for one attention layer."""
 
     def __init__(self, n_kv_heads: int, head_dim: int, num_blocks: int, max_blocks: int,
-                 max_batch: int, table_log2_cap: int = 20, device="cuda", lru: bool = False):
+                 max_batch: int, table_log2_cap: int = 20, device="cuda", lru: bool = False, spare_blocks: int = 0):
+        """``spare_blocks``: blocks of the pools behind the prefix cache's ``num_blocks`` that
+        DeviceTables takes for the tokens of growing requests, and gives back, on the device."""
         import torch
 
         self.n_kv_heads, self.head_dim = n_kv_heads, head_dim
         self.num_blocks, self.max_blocks, self.max_batch = num_blocks, max_blocks, max_batch
         self.device = torch.device(device)
         self.cache = ilpc.PrefixCache(num_blocks, table_log2_cap, lru=lru)
-        self.k_pool, self.v_pool = ilpc.alloc_pools(num_blocks, n_kv_heads, head_dim, self.device)
+        self.k_pool, self.v_pool = ilpc.alloc_pools(num_blocks + spare_blocks, n_kv_heads, head_dim, self.device)
+        # the free list on the device: ids, and how many at its front are taken
+        self.free_ids = torch.arange(num_blocks, num_blocks + spare_blocks, dtype=torch.int32, device=self.device)
+        self.free_taken = torch.zeros(1, dtype=torch.int32, device=self.device)
         n = max_batch * max_blocks + 3 * max_batch + 1
         self._host = [torch.empty(n, dtype=torch.int32, pin_memory=True) for _ in range(2)]
         self._host_np = [h.numpy() for h in self._host]
@@ -221,6 +226,18 @@ class PagedPrefixCache:
                                         batch.seq_lens, batch.max_q_len, shared_len, scale, out,
                                         workspace, stream)
 
+    def append_slots(self, slot_map, k_new, v_new, stream=None):
+        """K/V rows to the slots of a device slot map (DeviceTables.extend); -1: not stored."""
+        ilpc.kv_append_slots(k_new, v_new, self.k_pool, self.v_pool, slot_map, stream)
+
+    def attend_diff(self, batch: DeviceBatch, q, out, scale: float, lam, norm_weight=None, norm_eps: float = 1e-5,
+                    out_scale: float = 1.0, layout: int = ilpc.DIFF_HALVES, workspace=None, stream=None):
+        """Differential attention: the difference of two softmax maps, whose queries and keys are the
+        two parts of each head's dimensions (ilpc.paged_diff_attn)."""
+        ilpc.paged_diff_attn(q, self.k_pool, self.v_pool, batch.block_tables, batch.cu_q, batch.seq_lens,
+                             batch.max_q_len, scale, lam, out, norm_weight, norm_eps, out_scale, layout, workspace,
+                             stream)
+
     def cascade_workspace(self, batch: DeviceBatch, n_q_heads: int):
         """A workspace for attend_cascade on this batch shape (first 128 bytes zeroed)."""
         import torch
@@ -230,6 +247,68 @@ class PagedPrefixCache:
         ws = torch.empty(n, dtype=torch.uint8, device=self.device)
         ws[:128].zero_()
         return ws
+
+
+class DeviceTables:
+    """A batch whose metadata stays on the device while its requests grow.
+
+    Starts from a matched batch (host tables, context lengths).  ``extend``
+    adds new tokens: block tables, lengths, row offsets and slot map are built
+    on the device (ilpc.extend_tables), new blocks come from ``pc``'s spare
+    ones, so a decode loop needs no host step and can be captured: a replay
+    goes on from where the last one left the lengths.  ``release`` gives the
+    blocks of ended requests back.  Calls are ordered on one stream; batches
+    that share ``pc`` share its free list and that order.
+
+    ``status`` (device, 1 value) holds what the last extend or release refused
+    (0: nothing): a refused extend changes nothing, and the append and attention
+    queued behind it do nothing.
+    """
+
+    def __init__(self, pc: PagedPrefixCache, tables, seq_lens, max_rows: int):
+        import torch
+
+        tables = np.ascontiguousarray(tables, dtype=np.int32)
+        L = np.ascontiguousarray(seq_lens, dtype=np.int32)
+        if tables.ndim != 2 or tables.shape[1] != pc.max_blocks or L.shape != (tables.shape[0],):
+            raise ilpc.ILPCError(ilpc.EINVAL, "DeviceTables: tables must be [B, max_blocks], seq_lens [B]")
+        self.pc, self.B, self.max_rows = pc, int(tables.shape[0]), int(max_rows)
+
+        def dev(a):
+            return torch.from_numpy(np.array(a, dtype=np.int32, order="C")).to(pc.device)
+
+        def empty(n):
+            return torch.zeros(n, dtype=torch.int32, device=pc.device)
+
+        self.block_tables, self.seq_lens = dev(tables), dev(L)
+        self.start_pos, self.first_block = dev(L), dev(-(-L // BLOCK))
+        self.cu_q, self.cu_blocks = empty(self.B + 1), empty(self.B + 1)
+        self.slot_map, self.status = empty(self.max_rows).fill_(-1), empty(1)
+
+    def extend(self, new_lens, max_new: int) -> DeviceBatch:
+        """Every request r gets new_lens[r] (device int32, at most max_new) tokens.
+
+        The rows of the returned batch are the new tokens', in request order,
+        ``max_rows`` at most; its views hold until the next extend."""
+        import torch
+
+        torch.add(self.seq_lens, 0, out=self.start_pos)
+        ilpc.extend_tables(self.block_tables, self.start_pos, new_lens, self.pc.free_ids, self.pc.free_taken,
+                           self.seq_lens, self.cu_q, self.cu_blocks, self.slot_map, self.pc.free_taken, self.status,
+                           self.pc.k_pool.shape[0])
+        return DeviceBatch(block_tables=self.block_tables, cu_q=self.cu_q, seq_lens=self.seq_lens,
+                           start_pos=self.start_pos, max_q_len=int(max_new), total_q=self.max_rows, B=self.B)
+
+    def append(self, k_new, v_new):
+        """K/V of the last extend's tokens [max_rows, Hkv, D] into the pools."""
+        self.pc.append_slots(self.slot_map, k_new, v_new)
+
+    def release(self, ended):
+        """Requests with ended[r] (device int32) = 1, not 0, have finished: the blocks that they
+        took by extend are free again, and their context length is 0."""
+        ilpc.release_tables(self.block_tables, self.first_block, self.seq_lens * ended, self.pc.free_ids,
+                            self.pc.free_taken, self.cu_blocks, self.pc.free_taken, self.status)
+        self.seq_lens.mul_(1 - ended)
 
 
 class DecodeGraph:

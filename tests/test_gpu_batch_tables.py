@@ -1,0 +1,398 @@
+"""GPU: block tables, slot maps and free list of growing batches, the append by slots,
+and a decode loop of them with differential attention, against plain lists and the
+fp64 oracles.  Integers have to be equal, stored rows the same bits."""
+import numpy as np
+import pytest
+import torch
+
+from oracle.diff_ref import diff_attention_ref
+from oracle.rope_ref import rope
+from oracle.tables_ref import extend_ref, release_ref
+from paper_2507_08523_amd import ilpc, pipeline
+
+pytestmark = pytest.mark.gpu
+
+BLOCK = 16
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a ROCm GPU (run with -m 'not gpu' on the CPU)")
+    ilpc.load()
+    yield
+    torch.cuda.synchronize()
+
+
+def dev(a):
+    return torch.from_numpy(np.array(a, dtype=np.int32, order="C")).cuda()
+
+
+def ints(t):
+    return t.cpu().numpy().tolist()
+
+
+def make(B, lo, hi, new_hi, seed, spare=5, width=None):
+    """(tables, start, new, free ids, taken) of a random batch; ids of the whole pool once."""
+    rng = np.random.default_rng(seed)
+    start = rng.integers(lo, hi + 1, B)
+    new = rng.integers(0, new_hi + 1, B)
+    held, end = -(-start // BLOCK), -(-(start + new) // BLOCK)
+    mb = width or int(end.max()) + 1 if B else 1
+    taken = 2
+    n = int(held.sum()) + int((end - held).sum()) + spare + taken
+    ids = rng.permutation(n).astype(np.int32)
+    tables, at = np.full((B, mb), -1, np.int32), 0
+    for r in range(B):
+        tables[r, :held[r]] = ids[at:at + held[r]]
+        at += held[r]
+    return tables, start, new, ids[at:], taken, n
+
+
+class State:
+    def __init__(self, tables, start, new, free, taken, num_blocks, rows):
+        B = len(start)
+        self.t, self.s, self.n, self.f, self.k = dev(tables), dev(start), dev(new), dev(free), dev([taken])
+        self.seq, self.cu, self.cb = dev([9] * B), dev([9] * (B + 1)), dev([9] * (B + 1))
+        self.slots, self.k2, self.st, self.nb = dev([9] * rows), dev([9]), dev([9]), num_blocks
+
+    def extend(self, in_place=False, stream=None):
+        seq, k2 = (self.s, self.k) if in_place else (self.seq, self.k2)
+        ilpc.extend_tables(self.t, self.s, self.n, self.f, self.k, seq, self.cu, self.cb, self.slots, k2, self.st,
+                           self.nb, stream=stream)
+        return [self.t, seq, self.cu, self.cb, self.slots, k2, self.st]
+
+
+def same(got, want):
+    torch.cuda.synchronize()
+    for name, g, w in zip(("tables", "seq_lens", "cu_q", "cu_blocks", "slots", "taken", "status"), got, want):
+        assert ints(g) == ([w] if isinstance(w, int) else [list(map(int, x)) if isinstance(x, (list, np.ndarray))
+                                                           else int(x) for x in w]), name
+
+
+@pytest.mark.parametrize("B,lo,hi,new_hi,pad", [
+    (1, 0, 0, 1, 0), (1, 0, 0, 40, 3), (1, 31, 33, 1, 0), (3, 0, 70, 5, 2), (64, 0, 300, 1, 0), (63, 15, 17, 2, 7),
+    (512, 0, 90, 1, 1), (1000, 0, 40, 3, 0), (1025, 0, 40, 3, 5), (3000, 0, 20, 2, 0), (5, 0, 100, 5000, 11),
+    (300, 0, 50, 200, 100), (2049, 0, 5, 30, 0)])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_extend(B, lo, hi, new_hi, pad, in_place):
+    tables, start, new, free, taken, nb = make(B, lo, hi, new_hi, B + new_hi)
+    rows = int(new.sum()) + pad
+    want = extend_ref(tables, start.tolist(), new.tolist(), free.tolist(), taken, nb, rows)
+    assert want[-1] == 0
+    same(State(tables, start, new, free, taken, nb, rows).extend(in_place), want)
+
+
+def test_a_long_request_among_short_ones_and_none_at_all():
+    tables, start, new, free, taken, nb = make(200, 0, 30, 1, 1)
+    new[77] = 20000
+    tables = np.full((200, 1300), -1, np.int32)
+    for r in range(200):
+        tables[r, :-(-start[r] // BLOCK)] = r
+    free = np.arange(3000)
+    rows = int(new.sum()) + 1
+    same(State(tables, start, new, free, 0, 3000, rows).extend(),
+         extend_ref(tables, start.tolist(), new.tolist(), free.tolist(), 0, 3000, rows))
+    none = np.zeros(200, int)
+    same(State(tables, start, none, free, 5, 3000, 6).extend(),
+         extend_ref(tables, start.tolist(), none.tolist(), free.tolist(), 5, 3000, 6))
+    # no request at all, no rows at all
+    s = State(np.zeros((0, 4)), [], [], [1, 2], 1, 8, 3)
+    s.extend()
+    torch.cuda.synchronize()
+    assert (ints(s.cu), ints(s.cb), ints(s.slots), ints(s.k2), ints(s.st)) == ([0], [0], [-1] * 3, [1], [0])
+    same(State(tables, start, none, free, 5, 3000, 0).extend(),
+         extend_ref(tables, start.tolist(), none.tolist(), free.tolist(), 5, 3000, 0))
+
+
+@pytest.mark.parametrize("kind", ["blocks", "long", "rows", "negative start", "negative new", "taken", "taken low",
+                                  "huge"])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_refused_batches_change_nothing(kind, in_place):
+    tables, start, new, free, taken, nb = make(70, 0, 60, 20, 3)
+    rows = int(new.sum())
+    if kind == "blocks":
+        free = free[:-8]
+    elif kind == "long":
+        new[5] = 16 * tables.shape[1] - start[5] + 1
+        rows += 1000
+    elif kind == "rows":
+        rows -= 1
+    elif kind == "negative start":
+        start[69] = -1
+    elif kind == "negative new":
+        new[0] = -3
+    elif kind == "taken":
+        taken = len(free) + 1
+    elif kind == "taken low":
+        taken = -1
+    else:
+        new[:] = (1 << 31) - 1
+    want = extend_ref(tables, start.tolist(), new.tolist(), free.tolist(), taken, nb, rows)
+    bits = {"blocks": 1, "long": 2, "rows": 4}
+    s = State(tables, start, new, free, taken, nb, rows)
+    got = s.extend(in_place)
+    torch.cuda.synchronize()
+    status = ints(s.st)[0]
+    assert status & bits.get(kind, 8 if kind != "huge" else 2)
+    same(got[:-1], want[:-1])
+
+
+def test_ids_outside_the_pool_give_no_slot():
+    tables = np.array([[3, 1 << 30, -1], [-5, 2, -1]], np.int32)
+    start, new, free = [20, 10], [20, 4], [99, 1]
+    want = extend_ref(tables, start, new, free, 0, 4, 24)
+    assert want[4].count(-1) == 20 + 4
+    same(State(tables, start, new, free, 0, 4, 24).extend(), want)
+
+
+@pytest.mark.parametrize("B,lo,hi", [(1, 1, 16), (7, 0, 100), (64, 0, 2000), (1025, 0, 60), (3000, 0, 40)])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_release(B, lo, hi, in_place):
+    rng = np.random.default_rng(B)
+    seq = rng.integers(lo, hi + 1, B) * (rng.random(B) < 0.7)
+    first = rng.integers(0, 4, B)
+    mb = -(-hi // BLOCK) + 1
+    tables = rng.integers(0, 1 << 20, (B, mb))
+    gone = int(np.maximum(-(-seq // BLOCK) - first, 0).sum())
+    free = rng.integers(0, 1 << 20, gone + 9)
+    for taken in (gone, gone + 9, gone - 1):
+        if taken < 0:
+            continue
+        want = release_ref(tables.tolist(), first.tolist(), seq.tolist(), free.tolist(), taken)
+        assert want[-1] == (1 if taken < gone else 0)
+        f, k, cb, k2, st = dev(free), dev([taken]), dev([9] * (B + 1)), dev([9]), dev([9])
+        k2 = k if in_place else k2
+        ilpc.release_tables(dev(tables), dev(first), dev(seq), f, k, cb, k2, st)
+        torch.cuda.synchronize()
+        assert (ints(f), ints(cb), ints(k2)[0], ints(st)[0]) == tuple(map(lambda x: x if isinstance(x, int) else
+                                                                        list(map(int, x)), want))
+
+
+def test_release_refuses_bad_values():
+    tables = np.arange(12).reshape(3, 4)
+    for first, seq, free, taken, bit in (([0, -1, 0], [4, 4, 4], [9] * 8, 3, 8), ([0, 0, 0], [4, -4, 4], [9] * 8, 3, 8),
+                                         ([0, 0, 0], [4, 65, 4], [9] * 8, 8, 2), ([0, 0, 0], [4, 4, 4], [9] * 2, 3, 8),
+                                         ([0, 0, 0], [64, 64, 64], [9] * 8, 8, 1)):
+        f, k, cb, st = dev(free), dev([taken]), dev([9] * 4), dev([0])
+        ilpc.release_tables(dev(tables), dev(first), dev(seq), f, k, cb, k, st)
+        torch.cuda.synchronize()
+        assert ints(st)[0] & bit and ints(f) == free and ints(k) == [taken] and ints(cb) == [0] * 4
+
+
+def pools(nb, Hkv, D, seed=0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    rnd = lambda *s: torch.randn(*s, generator=g, device="cuda").to(torch.bfloat16)  # noqa: E731
+    return rnd(nb, Hkv, 16, D), rnd(nb, Hkv, D, 16)
+
+
+def stored(kp, vp, k, v, slots):
+    kp, vp = kp.clone(), vp.clone()
+    for i, s in enumerate(slots):
+        if 0 <= s < 16 * kp.shape[0]:
+            kp[s // 16, :, s % 16] = k[i]
+            vp[s // 16, :, :, s % 16] = v[i]
+    return kp, vp
+
+
+def slot_patterns(nb, rng):
+    yield "one", [5]
+    yield "decode", rng.permutation(16 * nb)[:50].tolist()
+    yield "all padding", [-1] * 33
+    yield "outside", [16 * nb, -7, 3, (1 << 31) - 1, -(1 << 31), 4]
+    yield "whole blocks", list(range(32, 32 + 64))
+    yield "odd starts", [*range(7, 16), *range(48, 64), *range(80, 83), -1, -1, *range(16, 48)]
+    yield "runs at every phase", sum(([*range(16 * b + b, 16 * b + 16)] for b in range(12)), [])
+    yield "broken runs", [0, 1, 2, 4, 5, 6, 7, 8, 9, 10, 11, 12, 13, 14, 15, 33, 32, 40, 41, 42, 43, 44, 45, 46, 47]
+    yield "seventeen after one", [3, *range(64, 80), *range(100, 117)]
+    yield "descending", list(range(60, 20, -1))
+
+
+@pytest.mark.parametrize("Hkv,D", [(1, 64), (3, 64), (2, 128), (8, 128)])
+@pytest.mark.parametrize("fused", [False, True])
+def test_append_by_slots(Hkv, D, fused):
+    nb = 16
+    for name, slots in slot_patterns(nb, np.random.default_rng(1)):
+        n = len(slots)
+        x = torch.randn(n, 5 + 2 * Hkv, D, device="cuda").to(torch.bfloat16)
+        k, v = x[:, 5:5 + Hkv], x[:, 5 + Hkv:]
+        if not fused:
+            k, v = k.contiguous(), v.contiguous()
+        kp, vp = pools(nb, Hkv, D)
+        want = stored(kp, vp, k, v, slots)
+        ilpc.kv_append_slots(k, v, kp, vp, dev(slots))
+        torch.cuda.synchronize()
+        assert torch.equal(kp, want[0]) and torch.equal(vp, want[1]), name
+
+
+def test_append_equals_the_append_by_tables():
+    lens, start = np.array([100, 33, 250, 17]), np.array([32, 0, 17, 16])
+    B, Hkv, D = 4, 2, 128
+    new = lens - start
+    n, mb = int(new.sum()), 16
+    tables = np.random.default_rng(0).permutation(B * mb).reshape(B, mb).astype(np.int32)
+    k, v = (torch.randn(n, Hkv, D, device="cuda").to(torch.bfloat16) for _ in range(2))
+    cu = np.concatenate([[0], np.cumsum(new)])
+    pos = np.concatenate([np.arange(a, b) for a, b in zip(start, lens)])
+    slots = tables[np.repeat(np.arange(B), new), pos // 16] * 16 + pos % 16
+    a, b = pools(B * mb, Hkv, D), pools(B * mb, Hkv, D)
+    ilpc.kv_append(k, v, *a, dev(tables), dev(cu), dev(start), int(new.max()))
+    ilpc.kv_append_slots(k, v, *b, dev(slots))
+    torch.cuda.synchronize()
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_append_far_into_a_large_pool():
+    # element offsets past 2^32 of the pools
+    Hkv, D, nb = 8, 128, 300000  # 4.9e9 elements each
+    kp, vp = (torch.zeros(nb, Hkv, *s, dtype=torch.bfloat16, device="cuda") for s in ((16, D), (D, 16)))
+    k, v = (torch.randn(20, Hkv, D, device="cuda").to(torch.bfloat16) for _ in range(2))
+    slots = np.concatenate([np.arange(16 * (nb - 1), 16 * nb), [16 * 262144 + 5, 16 * 131072 + 9, 3, 16 * nb]])
+    ilpc.kv_append_slots(k, v, kp, vp, dev(slots))
+    torch.cuda.synchronize()
+    for i, s in enumerate(slots[:-1].tolist()):
+        assert torch.equal(kp[s // 16, :, s % 16], k[i]) and torch.equal(vp[s // 16, :, :, s % 16], v[i])
+    assert int(kp.view(torch.int16).count_nonzero()) == int(k[:-1].contiguous().view(torch.int16).count_nonzero())
+    # and attention over keys that far
+    q, out = torch.randn(1, 8, D, device="cuda").to(torch.bfloat16), torch.empty(1, 8, D, dtype=torch.bfloat16,
+                                                                                 device="cuda")
+    ilpc.paged_diff_attn(q, kp, vp, dev([[nb - 1]]), dev([0, 1]), dev([16]), 1, 0.1, torch.full((8,), 0.5).cuda(), out)
+    torch.cuda.synchronize()
+    ref = diff_attention_ref(q.float().cpu(), k[:16].float().cpu(), v[:16].float().cpu(), 0.1, [0.5] * 8)
+    err = np.abs(out.float().cpu().numpy() - ref)
+    assert (err <= 2.0 ** -8 * np.abs(ref) + 2.0 ** -8 * 2 * float(v.abs().max())).all()
+
+
+def refused(call, **kw):
+    with pytest.raises(ilpc.ILPCError):
+        call(**kw)
+
+
+def test_binding_refusals():
+    i, cu, one = dev([1, 2, 3]), dev([0] * 4), dev([0])
+    a = dict(block_tables=dev(np.zeros((3, 4))), start_pos=i, new_lens=dev([1] * 3), free_ids=dev([1, 2]), taken=one,
+             seq_lens=dev([0] * 3), cu_q=cu, cu_blocks=dev([0] * 4), slot_map=dev([0] * 5), taken_out=dev([0]),
+             status=dev([0]), num_blocks=8)
+    call = lambda **kw: ilpc.extend_tables(**dict(a, **kw))  # noqa: E731
+    for kw in (dict(start_pos=i.long()), dict(new_lens=i[:2]), dict(cu_q=i), dict(cu_blocks=cu[:3]), dict(taken=i),
+               dict(block_tables=dev(np.zeros((2, 4)))), dict(block_tables=dev(np.zeros((4, 3))).t()),
+               dict(status=i), dict(free_ids=i[None]), dict(slot_map=i.cpu()), dict(start_pos=i[None]),
+               dict(cu_blocks=cu), dict(seq_lens=a["new_lens"]), dict(slot_map=a["free_ids"]), dict(status=one),
+               dict(num_blocks=-1), dict(num_blocks=1 << 27)):
+        refused(call, **kw)
+    buf = dev([0] * 8)
+    refused(call, start_pos=buf[:3], seq_lens=buf[1:4])  # (overlapping, and not the same)
+    call()
+    b = dict(block_tables=a["block_tables"], first_block=i, seq_lens=a["seq_lens"], free_ids=a["free_ids"], taken=one,
+             cu_blocks=cu, taken_out=dev([0]), status=dev([0]))
+    call = lambda **kw: ilpc.release_tables(**dict(b, **kw))  # noqa: E731
+    for kw in (dict(first_block=i[:2]), dict(seq_lens=i.short()), dict(free_ids=a["block_tables"]), dict(status=cu),
+               dict(cu_blocks=i), dict(taken_out=cu), dict(free_ids=a["seq_lens"]), dict(status=one)):
+        refused(call, **kw)
+    call()
+    kp, vp = pools(4, 2, 64)
+    k = torch.zeros(3, 2, 64, dtype=torch.bfloat16, device="cuda")
+    c = dict(k_new=k, v_new=k, k_pool=kp, v_pool=vp, slot_map=i)
+    call = lambda **kw: ilpc.kv_append_slots(**dict(c, **kw))  # noqa: E731
+    for kw in (dict(k_new=k.half()), dict(v_new=k[:2]), dict(k_new=k.transpose(0, 1)), dict(k_new=k[..., :32]),
+               dict(slot_map=i[:2]), dict(slot_map=i.long()), dict(v_pool=kp), dict(k_pool=kp.transpose(2, 3)),
+               dict(v_new=torch.zeros(3, 130, dtype=torch.bfloat16, device="cuda")[:, 1:129].view(3, 2, 64)),
+               dict(k_new=k.cpu())):
+        refused(call, **kw)
+    call()
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("captured", [False, True])
+def test_decode_loop_on_the_device(captured):
+    """A matched batch, prefilled with rotated keys, then decode steps whose tables, appends and
+    differential attention never meet the host; two requests end on the way."""
+    Hq, Hkv, D, B, steps = 4, 2, 128, 3, 40
+    rng = np.random.default_rng(2)
+    L0 = np.array([50, 16, 77])
+    freq = np.concatenate([pipeline.rope_inv_freq(D // 2, 10000.0)] * 2)
+    prompts = [rng.integers(0, 1000, n).astype(np.int32) for n in L0]
+    pc = pipeline.PagedPrefixCache(Hkv, D, 16, 10, B, 8, spare_blocks=12)
+    rnd = lambda *s: torch.randn(*s, device="cuda").to(torch.bfloat16)  # noqa: E731
+    lam, w, scale = torch.rand(Hq, device="cuda"), 1 + 0.1 * torch.randn(D, device="cuda"), (D // 2) ** -0.5
+    cached, tables = pc.match(prompts)
+    batch = pc.upload_prefill(cached, tables, L0)
+    n0 = int(L0.sum())
+    q0, k0, v0 = rnd(n0, Hq, D), rnd(n0, Hkv, D), rnd(n0, Hkv, D)
+    qr, out0 = torch.empty_like(q0), torch.empty_like(q0)
+    fr = torch.from_numpy(freq).cuda()
+    pc.append_rope(batch, k0, v0, fr, q0, qr)
+    pc.attend_diff(batch, qr, out0, scale, lam, w, out_scale=0.2, layout=ilpc.DIFF_ROPE)
+
+    dt = pipeline.DeviceTables(pc, tables, L0, max_rows=B + 2)
+    new, ended = dev([1] * B), dev([0] * B)
+    q, k, v, out = (rnd(B + 2, h, D) for h in (Hq, Hkv, Hkv, Hq))
+
+    def step():
+        b = dt.extend(new, 1)
+        dt.append(k, v)
+        pc.attend_diff(b, q, out, scale, lam, w, out_scale=0.2)
+
+    # what the requests hold: rotated keys of the prompt, then the steps' as they come
+    cu = np.concatenate([[0], np.cumsum(L0)])
+    keys = [list(rope(k0[a:b].float().cpu().numpy(), np.arange(b - a), freq)) for a, b in zip(cu, cu[1:])]
+    vals = [list(v0[a:b].float().cpu().numpy()) for a, b in zip(cu, cu[1:])]
+    lam64, w64 = lam.double().cpu().numpy(), w.double().cpu().numpy()
+
+    def close(got, ref):
+        # (keys rounded to bf16 after the rotation: 2^-8 of each product's terms on top, within the sum below)
+        err = np.linalg.norm(got - ref) / np.linalg.norm(ref)
+        assert err <= 0.02, err
+
+    for r in range(B):
+        a, b = int(cu[r]), int(cu[r + 1])
+        ref = diff_attention_ref(rope(q0[a:b].float().cpu().numpy(), np.arange(b - a), freq), np.array(keys[r]),
+                                 np.array(vals[r]), scale, lam64, w64, out_scale=0.2, layout="rope")
+        close(out0[a:b].float().cpu().numpy(), ref)
+    if captured:
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step()
+    live, free0 = [0, 1, 2], ints(pc.free_ids)
+    for s in range(steps):
+        if s in (15, 30):  # a request ends; the blocks it took are free again
+            gone = live.pop(1)
+            ended.zero_()
+            ended[gone] = 1
+            new[gone] = 0
+            before = ints(pc.free_taken)[0]
+            dt.release(ended)
+            mine = -(-len(keys[gone]) // BLOCK) - -(-int(L0[gone]) // BLOCK)
+            assert ints(pc.free_taken)[0] == before - mine and ints(dt.status) == [0] and ints(dt.seq_lens)[gone] == 0
+        for x, h in ((q, Hq), (k, Hkv), (v, Hkv)):
+            x.copy_(rnd(B + 2, h, D))
+        out.fill_(7.0)
+        graph.replay() if captured else step()
+        torch.cuda.synchronize()
+        assert ints(dt.status) == [0] and ints(dt.cu_q)[-1] == len(live)
+        for i, r in enumerate(live):
+            keys[r].append(k[i].float().cpu().numpy())
+            vals[r].append(v[i].float().cpu().numpy())
+            if s % 7 == 0 or s > steps - 3:
+                # halves of decode rows against keys rotated as pairs: any fixed split of the dimensions
+                ref = diff_attention_ref(q[i:i + 1].float().cpu().numpy(), np.array(keys[r]), np.array(vals[r]),
+                                         scale, lam64, w64, out_scale=0.2)
+                close(out[i:i + 1].float().cpu().numpy(), ref)
+        assert (out[len(live):] == 7.0).all()
+        # blocks in use are distinct
+        ids = [int(x) for r in live for x in dt.block_tables[r, :-(-len(keys[r]) // BLOCK)]]
+        assert len(set(ids)) == len(ids)
+    # every spare block is free (behind the taken ones at the list's front) or in one request's row
+    assert sorted(ints(pc.free_ids)[ints(pc.free_taken)[0]:] + [x for x in ids if x >= pc.num_blocks]) == sorted(free0)
+    # out of blocks: refused on the device, nothing stored, nothing computed
+    pool, seq = pc.k_pool.clone(), ints(dt.seq_lens)
+    new.fill_(0)
+    new[live[0]] = 4 * BLOCK * 12
+    pc.k_pool.copy_(pool)
+    out.fill_(7.0)
+    graph.replay() if captured else step()
+    torch.cuda.synchronize()
+    assert ints(dt.status)[0] & (ilpc.NO_BLOCKS | ilpc.TOO_LONG | ilpc.TOO_MANY_ROWS)
+    assert ints(dt.seq_lens) == seq and torch.equal(pc.k_pool.view(torch.int16), pool.view(torch.int16))
+    assert (out == 7.0).all()

@@ -1,0 +1,318 @@
+"""GPU: differential attention over the paged cache against the fp64 oracle.
+
+Tolerances.  The output is rounded to bf16 once: half a step, 2^-8 of its value,
+2^-8 / sqrt(3) = 0.0023 in the 2-norm at most.  The weights enter the products with
+V as bf16 numbers, again half a step each: independent roundings of the combined
+weights leave at most as much again in the 2-norm, so 0.0045 is the sum of both
+(NORM).  Element by element a weight's rounding is at most 2^-8 of the map that it
+belongs to as normalised over the keys seen when it was rounded, mass 1 (A_1) and
+|lam| (A_2, and as much again where its share was still being corrected):
+2^-8 (1 + 2 |lam|) max |v| times the norm's factor.  Sums and scores in fp32 add
+less than 2^-16 of the same.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle.diff_ref import diff_attention_ref
+from paper_2507_08523_amd import ilpc
+
+pytestmark = pytest.mark.gpu
+
+HALF, NORM = 2.0 ** -8, 0.0045
+NAMES = {"halves": ilpc.DIFF_HALVES, "rope": ilpc.DIFF_ROPE}
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a ROCm GPU (run with -m 'not gpu' on the CPU)")
+    ilpc.load()
+    yield
+    torch.cuda.synchronize()
+
+
+class Batch:
+    """Requests of `lens` keys whose last `new` are queries, in permuted blocks of pools
+    whose other slots hold NaN."""
+
+    def __init__(self, lens, new, Hq=4, Hkv=2, D=128, std=1.0, seed=0, norm=True, layout="halves", extra=0,
+                 near=None, spare_cols=0, fused=False, lam=None):
+        rng = np.random.default_rng(seed)
+        g = torch.Generator().manual_seed(seed)
+        self.lens, self.new, self.D, self.Hq, self.Hkv, self.layout = list(lens), list(new), D, Hq, Hkv, layout
+        B, n = len(lens), sum(new)
+        bf = lambda *s: torch.randn(*s, generator=g).to(torch.bfloat16)  # noqa: E731
+        nb = sum(-(-x // 16) for x in lens) + 3
+        mb = max(max(-(-x // 16) for x in lens), 1) + spare_cols
+        ids = rng.permutation(nb)
+        self.kd, self.vd = [bf(x, Hkv, D) for x in lens], [bf(x, Hkv, D) for x in lens]
+        q = (bf(n, Hq, D) * std).to(torch.bfloat16)
+        if near is not None:  # the second map's queries and keys near the first's
+            half = D // 2
+            q[..., half:] = (q[..., :half].float() + near * torch.randn(n, Hq, half, generator=g)).to(torch.bfloat16)
+            for k in self.kd:
+                k[..., half:] = k[..., :half]
+        kp, vp = torch.full((nb, Hkv, 16, D), float("nan")), torch.full((nb, Hkv, D, 16), float("nan"))
+        bt = np.full((B, mb), -1, np.int32)
+        at = 0
+        for r, x in enumerate(lens):
+            m = -(-x // 16)
+            bt[r, :m] = ids[at:at + m]
+            at += m
+            for j in range(m):
+                a, b = 16 * j, min(16 * j + 16, x)
+                kp[bt[r, j], :, :b - a] = self.kd[r][a:b].float().permute(1, 0, 2)
+                vp[bt[r, j], :, :, :b - a] = self.vd[r][a:b].float().permute(1, 2, 0)
+        dev = lambda a: torch.from_numpy(np.asarray(a, np.int32)).cuda()  # noqa: E731
+        self.kp, self.vp = kp.to(torch.bfloat16).cuda(), vp.to(torch.bfloat16).cuda()
+        self.bt, self.cu, self.L = dev(bt), dev(np.concatenate([[0], np.cumsum(new)])), dev(lens)
+        self.q = q.cuda()
+        if fused:  # rows of a wider projection
+            wide = torch.full((n, Hq + 2 * Hkv, D), float("nan"), dtype=torch.bfloat16, device="cuda")
+            wide[:, :Hq] = self.q
+            self.q = wide[:, :Hq]
+        if extra:
+            pad = torch.full((extra, *self.q.shape[1:]), float("nan"), dtype=torch.bfloat16, device="cuda")
+            self.q = torch.cat([self.q, pad])
+        lam = torch.rand(Hq, generator=g) * 0.8 + 0.1 if lam is None else torch.full((Hq,), float(lam))
+        self.lam = lam.cuda()
+        self.w = (1 + 0.2 * torch.randn(D, generator=g)).cuda() if norm else None
+        self.out_scale = 0.2 if norm else 1.0
+        self.scale = (D // 2) ** -0.5
+        self.max_q = max(new)
+
+    def run(self, out=None, **kw):
+        out = torch.full(self.q.shape, 7.0, dtype=torch.bfloat16, device="cuda") if out is None else out
+        a = dict(norm_weight=self.w, out_scale=self.out_scale, layout=NAMES[self.layout])
+        ilpc.paged_diff_attn(self.q, self.kp, self.vp, self.bt, self.cu, self.L, self.max_q, self.scale, self.lam,
+                             out, **dict(a, **kw))
+        return out
+
+    def check(self, out, norm=NORM, rows_of=None):
+        torch.cuda.synchronize()
+        got, cu = out.float().cpu().numpy(), np.concatenate([[0], np.cumsum(self.new)])
+        q, lam = self.q.float().cpu().numpy(), self.lam.double().cpu().numpy()
+        w = None if self.w is None else self.w.double().cpu().numpy()
+        num = den = 0.0
+        for r, (L, S) in enumerate(zip(self.lens, self.new)):
+            if S == 0 or (rows_of is not None and r not in rows_of):
+                continue
+            k, v = self.kd[r].float().numpy(), self.vd[r].float().numpy()
+            plain = diff_attention_ref(q[cu[r]:cu[r + 1]], k, v, self.scale, lam, layout=self.layout)
+            fac = np.full((S, self.Hq, 1), self.out_scale)
+            if w is not None:
+                fac = fac / np.sqrt((plain ** 2).mean(-1, keepdims=True) + 1e-5)
+            ref = plain * fac * (1 if w is None else w)
+            fac = fac * (1 if w is None else np.abs(w))
+            err = np.abs(got[cu[r]:cu[r + 1]] - ref)
+            vmax = np.repeat(np.abs(v).max(0), self.Hq // self.Hkv, axis=0)[None]
+            bound = HALF * np.abs(ref) + HALF * (1 + 2 * np.abs(lam))[None, :, None] * fac * vmax
+            assert np.isfinite(got[cu[r]:cu[r + 1]]).all(), f"request {r}"
+            assert (err <= bound).all(), f"request {r}: {(err / bound).max()}"
+            num, den = num + (err ** 2).sum(), den + (ref ** 2).sum()
+        rel = (num / max(den, 1e-30)) ** 0.5
+        print(f"lens {self.lens[:4]} new {self.new[:4]} {self.Hq}/{self.Hkv}/{self.D}: rel {rel:.2e}", flush=True)
+        if norm is not None:
+            assert rel <= norm
+        return rel
+
+
+HEADS = [(1, 1, 64), (4, 1, 64), (6, 2, 64), (8, 8, 128), (4, 2, 128), (7, 1, 128), (16, 2, 128), (20, 1, 64),
+         (64, 1, 128)]
+
+
+@pytest.mark.parametrize("heads", HEADS)
+@pytest.mark.parametrize("new", [1, 3])
+def test_decode_shapes(heads, new):
+    Hq, Hkv, D = heads
+    b = Batch([3, 16, 17, 63, 64, 65, 130], [min(new, 3)] * 7, Hq, Hkv, D, seed=Hq)
+    b.check(b.run())
+
+
+@pytest.mark.parametrize("heads", HEADS)
+def test_prefill_shapes(heads):
+    Hq, Hkv, D = heads
+    b = Batch([1, 40, 100, 129, 33], [1, 40, 36, 128, 33], Hq, Hkv, D, seed=Hq)
+    b.check(b.run())
+
+
+@pytest.mark.parametrize("layout", ["halves", "rope"])
+@pytest.mark.parametrize("norm", [False, True])
+@pytest.mark.parametrize("fused", [False, True])
+@pytest.mark.parametrize("D", [64, 128])
+def test_layouts_norm_and_row_strides(layout, norm, fused, D):
+    for lens, new in (([50, 7], [1, 2]), ([150, 77], [90, 65])):
+        b = Batch(lens, new, 4, 2, D, norm=norm, layout=layout, fused=fused, seed=D)
+        b.check(b.run())
+
+
+@pytest.mark.parametrize("S", [1, 2, 15, 16, 17, 31, 32, 33, 64, 65, 127, 128, 129, 200, 257])
+@pytest.mark.parametrize("D", [64, 128])
+def test_row_counts(S, D):
+    # one request of S rows over a cached prefix, beside one without rows and one of a row
+    b = Batch([S + 48, 30, 5], [S, 0, 1], 4, 1, D, seed=S)
+    b.check(b.run())
+
+
+@pytest.mark.parametrize("L", [1, 2, 15, 31, 32, 33, 127, 128, 500, 1023, 1024, 1025, 4000, 9001])
+@pytest.mark.parametrize("new", [1, 40])
+def test_context_lengths(L, new):
+    # one request alone (its keys go over many workgroups), with spare table columns
+    b = Batch([L], [min(new, L)], 8, 1, 128, seed=L, spare_cols=37)
+    b.check(b.run())
+
+
+@pytest.mark.parametrize("B", [1, 2, 5, 33, 70, 140, 300])
+def test_batch_sizes(B):
+    # the plan of waves and workgroups to a request changes with their number
+    rng = np.random.default_rng(B)
+    lens = [int(x) for x in rng.integers(1, 700, B)]
+    b = Batch(lens, [1] * B, 8, 8, 64, seed=B)
+    b.check(b.run())
+    new = [int(rng.integers(0, min(x, 40) + 1)) for x in lens]
+    new[0] = max(new[0], 1)
+    b = Batch(lens, new, 2, 1, 128, seed=B)
+    b.check(b.run())
+
+
+@pytest.mark.parametrize("std", [128 ** -0.5, 0.3, 4.0, 30.0])
+@pytest.mark.parametrize("new", [1, 140])
+def test_flat_and_peaked_maps(std, new):
+    b = Batch([300, 1200], [new, new], 4, 2, 128, std=std, seed=3)
+    b.check(b.run())
+
+
+@pytest.mark.parametrize("near", [0.02, 0.2])
+@pytest.mark.parametrize("new", [1, 140])
+def test_maps_that_nearly_cancel(near, new):
+    # the case the method is made for: the output is a small difference
+    b = Batch([300, 700], [new, new], 4, 2, 128, near=near, lam=0.95, seed=4)
+    b.check(b.run())
+
+
+@pytest.mark.parametrize("new", [1, 140])
+def test_equal_maps_leave_nothing(new):
+    b = Batch([300], [new], 4, 2, 128, near=0.0, lam=1.0, seed=5, norm=False)
+    b.check(b.run(), norm=None)  # (the reference is 0: the bound by element alone)
+
+
+@pytest.mark.parametrize("lam", [0.0, -0.5, 1.5])
+@pytest.mark.parametrize("new", [1, 70])
+def test_lambda_values(lam, new):
+    b = Batch([100, 260], [new, new], 4, 2, 64, lam=lam, seed=6)
+    b.check(b.run())
+
+
+@pytest.mark.parametrize("new", [1, 130])
+def test_a_key_that_takes_all_late_and_early(new):
+    # maxima that grow by hundreds at one key: first, in the middle, last before the queries
+    for at in (0, 77, 200 - new):
+        b = Batch([200], [new], 2, 1, 128, seed=7)
+        b.kd[0][at, :, :64] *= 20
+        j = b.bt[0, at // 16]
+        b.kp[j, :, at % 16] = b.kd[0][at].cuda()
+        b.check(b.run(), norm=None if at else NORM)
+
+
+def test_rows_behind_the_last_request_and_uncomputed_requests_stay():
+    for new in ([2, 0, 1], [70, 0, 3]):
+        b = Batch([80, 9, 40], new, 4, 2, 128, extra=5, seed=8)
+        out = b.run()
+        b.check(out)
+        assert (out[sum(new):] == 7.0).all()
+    # more rows than keys, rows past q, rows past max_q_len: not computed
+    b = Batch([80, 40, 50], [3, 2, 4], 4, 2, 128, seed=9)
+    b.L[1] = 1
+    out = b.run()
+    b.check(out, rows_of=(0, 2))
+    assert (out[3:5] == 7.0).all()
+    b.L[1] = 40
+    b.cu[3] = 50
+    out = b.run()
+    b.check(out, rows_of=(0, 1))
+    assert (out[5:] == 7.0).all()
+    b = Batch([80], [70], 4, 2, 128, seed=9)
+    b.max_q = 33
+    out = b.run()
+    assert (out[33:] == 7.0).all() and not (out[:33] == 7.0).all()
+
+
+@pytest.mark.parametrize("new", [1, 60])
+def test_bad_block_ids_touch_nothing_else(new):
+    b = Batch([100, 90, 110], [new] * 3, 4, 2, 128, seed=10)
+    b.bt[1, 2], b.bt[1, 3], b.bt[1, 4] = -1, 1 << 30, -(1 << 31)
+    out = b.run()
+    b.check(out, rows_of=(0, 2))
+    b.L[1] = (1 << 31) - 1  # far past its row of the table
+    b.check(b.run(), rows_of=(0, 2))
+
+
+def test_own_streams_and_short_workspaces():
+    b = Batch([2000, 1500], [1, 1], 8, 1, 128, seed=11)
+    want = b.run()
+    need = ilpc.diff_attn_workspace_bytes(2, 1, 8, 1, 128, b.bt.shape[1])
+    assert need > 0
+    for ws in (torch.zeros(need - 16, dtype=torch.uint8, device="cuda"),
+               torch.zeros(need + 8, dtype=torch.uint8, device="cuda")[8:]):
+        with pytest.raises(ilpc.ILPCError, match="workspace"):
+            b.run(workspace=ws)
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    torch.cuda.synchronize()
+    outs = [torch.empty_like(want) for _ in streams]
+    for s, o in zip(streams, outs):  # at once, each call with scratch of its own
+        b.run(out=o, stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) for o in outs)
+
+
+def test_two_captured_graphs_replayed_at_once():
+    b = [Batch([2000, 900], [1, 1], 8, 1, 128, seed=12), Batch([1800], [1], 8, 1, 128, seed=13)]
+    want = [x.run() for x in b]
+    torch.cuda.synchronize()
+    outs, graphs = [torch.zeros_like(w) for w in want], []
+    for x, o in zip(b, outs):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            x.run(out=o)
+        graphs.append(g)
+    streams = [torch.cuda.Stream() for _ in b]
+    for _ in range(4):
+        for o in outs:
+            o.zero_()
+        torch.cuda.synchronize()
+        for s, g in zip(streams, graphs):
+            with torch.cuda.stream(s):
+                g.replay()
+        extra = b[0].run()  # eager work between the replays
+        torch.cuda.synchronize()
+        assert torch.equal(extra, want[0]) and all(torch.equal(o, w) for o, w in zip(outs, want))
+
+
+def test_same_bits_every_time():
+    for new in ([1, 1], [130, 60]):
+        b = Batch([900, 300], new, 16, 2, 128, seed=14)
+        want = b.run()
+        for _ in range(3):
+            assert torch.equal(b.run(), want)
+
+
+def test_binding_refusals():
+    b = Batch([40, 30], [3, 2], 4, 2, 128)
+    out = torch.empty(b.q.shape, dtype=torch.bfloat16, device="cuda")
+
+    def call(**kw):
+        a = dict(q=b.q, kp=b.kp, vp=b.vp, bt=b.bt, cu=b.cu, L=b.L, lam=b.lam, out=out, w=b.w, layout=0, stream=None)
+        a.update(kw)
+        ilpc.paged_diff_attn(a["q"], a["kp"], a["vp"], a["bt"], a["cu"], a["L"], 3, 0.1, a["lam"], a["out"],
+                             norm_weight=a["w"], layout=a["layout"], stream=a["stream"])
+
+    for kw in (dict(q=b.q.float()), dict(q=b.q[:, :3]), dict(q=b.q[..., ::2]), dict(q=b.q.transpose(0, 1)),
+               dict(q=b.q[..., :64]), dict(out=out[:4]), dict(out=out.cpu()), dict(vp=b.vp.transpose(2, 3)),
+               dict(kp=b.kp[..., :64].contiguous()), dict(bt=b.bt.long()), dict(bt=b.bt[:1]), dict(cu=b.cu[:2]),
+               dict(L=b.L[:1]), dict(lam=b.lam[:3]), dict(lam=b.lam.double()), dict(w=b.w[:64]), dict(w=b.w.half()),
+               dict(layout=5), dict(q=b.q[0]), dict(q=None)):
+        with pytest.raises(ilpc.ILPCError):
+            call(**kw)
+    call()
+    torch.cuda.synchronize()
