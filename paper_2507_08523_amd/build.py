@@ -21,7 +21,7 @@ SOURCES = [os.path.join(PKG, "csrc", "prefix_cache.cpp"), os.path.join(PKG, "csr
            os.path.join(PKG, "csrc", "paged_attn.hip"), os.path.join(PKG, "csrc", "rope_append.hip"),
            os.path.join(PKG, "csrc", "decode_attn.hip"),
            os.path.join(PKG, "csrc", "attn_noalloc.hip"), os.path.join(PKG, "csrc", "batch_tables.hip"),
-           os.path.join(PKG, "csrc", "diff_attn.hip")]
+           os.path.join(PKG, "csrc", "diff_attn.hip"), os.path.join(PKG, "csrc", "diff_prefill.hip")]
 BINDING = os.path.join(PKG, "_binding.so")
 BINDING_SOURCE = os.path.join(PKG, "csrc", "binding.cpp")
 ARCH = "gfx950"

@@ -34,54 +34,18 @@
 #include <cstdint>
 
 #include "../../include/ilpc.h"
+#include "diff_attn.h"
 #include "ilpc_internal.h"
 
 namespace {
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
+using namespace ilpc;
 
 constexpr int kBlock = 16;
 constexpr int kStepKeys = 32;        // keys a step (two pool blocks)
 constexpr int kTileCols = 16;        // query columns of a wave (each one twice, once a map)
 constexpr int kMaxGroups = 16;       // most workgroups to a pair
 constexpr float kLazyRescale = 8.f;  // log2 growth of a column max tolerated before rescaling O
-
-// What the last step of every kernel here needs.
-struct Epilogue {
-  const float* lambda;  // [Hq]
-  const float* norm_w;  // [D] or nullptr: no norm
-  float eps, scale;
-};
-
-// Key held by MFMA row m of a step: the groups [4,8) and [8,12) of every 16
-// keys trade places, which makes accumulator register e of lane half hh the key
-// (e >> 3) * 16 + 8 * hh + (e & 7): the layout of the P^T operand.
-__device__ __forceinline__ int key_of_row(int m) {
-  const int grp = (m >> 2) & 3;
-  return m + (grp == 1 ? 4 : (grp == 2 ? -4 : 0));
-}
-
-__device__ __forceinline__ bf16x8 as_bf16x8(u32x4 v) { return __builtin_bit_cast(bf16x8, v); }
-
-__device__ __forceinline__ float max_across_halves(float x) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ __forceinline__ float add_across_halves(float x) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-
-// Map that 16-dimension chunk kc of a head belongs to: its half of D, or in the
-// pair layout its half of each half of D.
-template <int D>
-__device__ __forceinline__ int map_of_chunk(int kc, int pairs) {
-  return pairs ? (kc / (D / 64)) & 1 : kc / (D / 32);
-}
 
 template <int D>
 struct StepRegs {
@@ -96,7 +60,7 @@ __global__ __launch_bounds__(64 * group_waves(W), 2) void diff_stream_kernel(
     const uint16_t* __restrict__ q, int64_t q_stride, int n_rows, const uint16_t* __restrict__ k_pool,
     const uint16_t* __restrict__ v_pool, int num_blocks, const int32_t* __restrict__ block_tables, int max_blocks,
     const int32_t* __restrict__ cu_q, const int32_t* __restrict__ seq_lens, int n_req, int max_q_len, int Hq, int Hkv,
-    float scale_log2, int pairs_layout, Epilogue ep, uint16_t* __restrict__ out, int n_ct, int n_split,
+    float scale_log2, int pairs_layout, DiffEpilogue ep, uint16_t* __restrict__ out, int n_ct, int n_split,
     float* __restrict__ part_o, float* __restrict__ part_ml) {
   constexpr int kDch = D / 16, kDt = D / 32, kWavesPerGroup = group_waves(W);
   // Q^T of each wave in LDS; for the merge (W > 1) the same space holds every
@@ -149,7 +113,7 @@ __global__ __launch_bounds__(64 * group_waves(W), 2) void diff_stream_kernel(
     for (int kc = 0; kc < kDch; ++kc) {
       const u32x4 zero = {0, 0, 0, 0};
       q_lds[wave][kc][lane] =
-          map_of_chunk<D>(kc, pairs_layout) == map ? *(const u32x4*)(qr + kc * 16 + hh * 8) : zero;
+          diff_map_of_chunk<D>(kc, pairs_layout) == map ? *(const u32x4*)(qr + kc * 16 + hh * 8) : zero;
     }
     const int32_t* bt = block_tables + size_t(r) * max_blocks;
     const int n_blk = (L + kBlock - 1) / kBlock;
@@ -160,7 +124,7 @@ __global__ __launch_bounds__(64 * group_waves(W), 2) void diff_stream_kernel(
     const int steps_per = (n_steps_all + n_ranges - 1) / n_ranges;
     const int s_begin = min(range * steps_per, n_steps_all);
     const int n_steps = min(s_begin + steps_per, n_steps_all);
-    const int krow = key_of_row(n);
+    const int krow = diff_key_of_row(n);
     const size_t head_off = size_t(h) * kBlock * D;
     const size_t slab = size_t(Hkv) * kBlock * D;
 
@@ -431,7 +395,7 @@ template <int D>
 __global__ __launch_bounds__(64 * kJoinWaves) void diff_join_kernel(
     const float* __restrict__ part_o, const float* __restrict__ part_ml, const int32_t* __restrict__ cu_q,
     const int32_t* __restrict__ seq_lens, int n_rows, int max_blocks, int n_req, int max_q_len, int Hq, int Hkv,
-    int n_split, int cols_cap, Epilogue ep, uint16_t* __restrict__ out) {
+    int n_split, int cols_cap, DiffEpilogue ep, uint16_t* __restrict__ out) {
   constexpr int kPer = D / 64;  // dimensions of a lane
   typedef float vec_t __attribute__((ext_vector_type(kPer)));
   const int lane = threadIdx.x & 63;
@@ -512,6 +476,11 @@ Plan stream_plan(int64_t items, int64_t n_ct, int64_t max_blocks) {
   return {w, int(n)};
 }
 
+// Whether the kernel for many columns takes a batch.
+bool many_columns(int64_t B, int64_t max_q_len, int Hq, int Hkv, int64_t max_blocks) {
+  return max_q_len * (Hq / Hkv) > 32;
+}
+
 size_t part_bytes(int64_t pairs, int D, int n) {
   return n > 1 ? size_t(pairs) * n * (2 * kTileCols) * (D + 2) * sizeof(float) : 0;
 }
@@ -540,6 +509,7 @@ extern "C" int ilpc_diff_attn_workspace_bytes(int32_t B, int32_t max_q_len, int3
   *bytes = 0;
   if (B == 0 || max_q_len == 0) return ILPC_OK;
   if (ilpc::device_cus() <= 0) return ilpc::set_error(ILPC_EHIP, "%s: cannot query the device", fn);
+  if (many_columns(B, max_q_len, Hq, Hkv, max_blocks)) return ILPC_OK;
   const int64_t n_ct = column_tiles(max_q_len, Hq, Hkv), pairs = int64_t(B) * Hkv;
   *bytes = part_bytes(pairs, D, stream_plan(pairs * n_ct, n_ct, max_blocks).groups);
   return ILPC_OK;
@@ -572,12 +542,20 @@ extern "C" int ilpc_paged_diff_attn(const uint16_t* q, int64_t q_stride, int32_t
   if (q_stride < int64_t(Hq) * D || q_stride % 8 != 0)
     return set_error(ILPC_EINVAL, "%s: q_stride must be a multiple of 8 elements, at least Hq * D", fn);
   if (ilpc::device_cus() <= 0) return set_error(ILPC_EHIP, "%s: cannot query the device", fn);
+  if (many_columns(B, max_q_len, Hq, Hkv, max_blocks)) {
+    const DiffArgs a{q, q_stride, n_rows, k_pool, v_pool, num_blocks, block_tables, max_blocks, cu_q, seq_lens, B,
+                     max_q_len, Hq, Hkv, D, softmax_scale * 1.4426950408889634f, int(layout == ILPC_DIFF_ROPE),
+                     DiffEpilogue{lambda, norm_weight, norm_eps, out_scale}, out};
+    if (!launch_diff_prefill(a, static_cast<hipStream_t>(stream)))
+      return set_error(ILPC_EHIP, "%s: launch failed", fn);
+    return ILPC_OK;
+  }
   const int64_t n_ct = column_tiles(max_q_len, Hq, Hkv), pairs = int64_t(B) * Hkv;
   Plan plan = stream_plan(pairs * n_ct, n_ct, max_blocks);
   const size_t need = part_bytes(pairs, D, plan.groups);
   if (need && (!workspace || workspace_bytes < need || !aligned16(workspace)))
     return set_error(ILPC_EINVAL, "%s: workspace must be %zu bytes, 16-byte aligned", fn, need);
-  const Epilogue ep{lambda, norm_weight, norm_eps, out_scale};
+  const DiffEpilogue ep{lambda, norm_weight, norm_eps, out_scale};
   float* part_o = need ? static_cast<float*>(workspace) : nullptr;
   float* part_ml = need ? part_o + size_t(pairs) * plan.groups * (2 * kTileCols) * D : nullptr;
   const int64_t items = pairs * n_ct * plan.groups, per_group = group_waves(plan.waves) / plan.waves;

@@ -1,0 +1,450 @@
+// Differential attention of many query columns, for gfx950 (the mathematics and
+// the kernel for few columns are in diff_attn.hip).
+//
+// A workgroup of four waves works 128 columns -- (token, head of the group) pairs
+// of one (request, kv head) -- against 64-key tiles of K and V in LDS, each wave
+// 32 columns with both of their maps.  Per 32 keys and wave, on
+// v_mfma_f32_32x32x16_bf16:
+//   S_m^T = K_m Q_m^T            D/32 products a map,
+//   O_m^T += V^T P_m^T           2 * D/32 products a map,
+// six D-wide products a column and key in all: both maps have to meet V in one
+// pass, since their sums are known only at the end.  Both maps in one wave: every
+// V operand read from LDS feeds two products.
+//
+// Precision.  y = O_1 / l_1 - lambda O_2 / l_2 is a difference, and where the maps
+// nearly agree it is much smaller than its terms; weights rounded to bf16 would
+// leave an error of 2^-9 of the terms.  What is accumulated is therefore
+//   A = sum (p_1 - beta p_2) v,   B = sum p_2 v,   beta ~ lambda l_1 / l_2,
+// with the difference of the weights taken in fp32 before it is rounded: beta is
+// lambda l_1 / l_2 as of the last time a running maximum was taken, and in the end
+//   y = (A + (beta - lambda l_1 / l_2) B) / l_1,
+// exact in beta.  A's rounding is relative to the combined weights, B's is scaled
+// by how far beta was off.  When a maximum grows (factors a_1, a_2) and beta is
+// set anew: A <- a_1 A + (a_1 beta - a_2 beta') B, B <- a_2 B.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+#include <type_traits>
+
+#include "diff_attn.h"
+#include "ilpc_internal.h"
+
+namespace {
+
+using namespace ilpc;
+
+constexpr int kBlock = 16;
+constexpr int kWaves = 4;
+constexpr int kCols = 32 * kWaves;  // columns of a workgroup
+constexpr int kKeys = 64;           // keys of a tile: two steps of 32
+constexpr int kTileBlocks = kKeys / kBlock;
+// Largest sum of a lane's exponentials of a step accepted without taking the
+// step's maximum.
+constexpr float kSumLimit = 256.f;
+
+// 16-byte slot of chunk c in LDS K row m: XOR-swizzled so that the lanes an LDS
+// cycle serves (consecutive rows, one chunk each) hit distinct banks.
+template <int D>
+__device__ __forceinline__ int k_slot(int m, int c) {
+  return D == 128 ? (c ^ (m & 15)) : (c ^ ((m >> 1) & 7));
+}
+// 16-byte half (keys 0-7 or 8-15) of V row d of a [D][16] block in LDS.
+__device__ __forceinline__ int v_slot(int d, int hf) { return hf ^ ((d >> 2) & 1) ^ ((d >> 3) & 1); }
+
+// 16-byte chunk of a K or Q row in memory that is logical chunk c, in an order in
+// which map 1's dimensions come first: the same, or in the pair layout quarters
+// 0, 2, 1, 3 of the row.
+template <int D>
+__device__ __forceinline__ int source_chunk(int c, int pairs) {
+  constexpr int kQuarter = D / 32;  // 16-byte chunks of a quarter row
+  const int quarter = c / kQuarter;
+  return pairs && (quarter == 1 || quarter == 2) ? c + (quarter == 1 ? kQuarter : -kQuarter) : c;
+}
+
+// One (block, kv head) slab of a pool straight into LDS: instruction i moves 16
+// bytes a lane from base + off[i] + i KiB (base wave-uniform) to lds + i KiB + 16
+// * lane.  Inline assembly, so that the compiler does not wait for such loads
+// before every LDS read; callers wait with an explicit vmcnt.  M0 carries the LDS
+// address; nothing else in these kernels uses it.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void load_slab4(uint32_t o0, uint32_t o1, uint32_t o2, uint32_t o3, uint64_t base,
+                                           uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %5\n\ts_nop 0\n\t"
+               "global_load_lds_dwordx4 %0, %4\n\t"
+               "global_load_lds_dwordx4 %1, %4 offset:1024\n\t"
+               "global_load_lds_dwordx4 %2, %4 offset:2048\n\t"
+               "global_load_lds_dwordx4 %3, %4 offset:3072"
+               :
+               : "v"(o0), "v"(o1), "v"(o2), "v"(o3), "s"(base), "s"(lds)
+               : "memory", "m0");
+}
+__device__ __forceinline__ void load_slab2(uint32_t o0, uint32_t o1, uint64_t base, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\t"
+               "global_load_lds_dwordx4 %0, %2\n\t"
+               "global_load_lds_dwordx4 %1, %2 offset:1024"
+               :
+               : "v"(o0), "v"(o1), "s"(base), "s"(lds)
+               : "memory", "m0");
+}
+// (outside the kernel templates: the cast in their host pass would drop the stubs)
+__device__ __forceinline__ uint32_t lds_offset(uint8_t* p) {
+  return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint8_t*)p));
+}
+#pragma clang diagnostic pop
+__device__ __forceinline__ uint32_t scalar(uint32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ uint64_t scalar(uint64_t x) {
+  return uint64_t(scalar(uint32_t(x >> 32))) << 32 | scalar(uint32_t(x));
+}
+// A word that no kernel writes meanwhile, at a wave-uniform address, through the
+// scalar cache.
+__device__ __forceinline__ int32_t scalar_load(const int32_t* p) {
+  return *(const __attribute__((address_space(4))) int32_t*)scalar(reinterpret_cast<uint64_t>(p));
+}
+__device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0F70); }  // vmcnt(0)
+__device__ __forceinline__ void wait_lds() { __builtin_amdgcn_s_waitcnt(0xC07F); }    // lgkmcnt(0)
+// Barrier without the fence of __syncthreads: the caller has waited for what it needs.
+__device__ __forceinline__ void bare_barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+constexpr int wgs_per_cu(int D) { return D == 64 ? 3 : 2; }
+
+template <int D>
+__global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void diff_prefill_kernel(DiffArgs a, int n_ct) {
+  constexpr int kDch = D / 16;                          // 16-dimension chunks of a row: half of them map 1's
+  constexpr int kDt = D / 32;                           // 32-row tiles of O^T
+  constexpr int kRowBytes = D * 2, kKch = D / 8;
+  constexpr int kSlabBytes = kBlock * D * 2;
+  constexpr int kTileBytes = kTileBlocks * kSlabBytes;
+  constexpr int kInsts = kSlabBytes / 1024;
+  __shared__ __attribute__((aligned(16))) uint8_t ring[4 * kTileBytes];  // two K tiles, two V tiles
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = lane & 31, hh = lane >> 5;
+  const int G = a.Hq / a.Hkv;
+
+  // Workgroup b runs on XCD b % 8, which takes every eighth (request, kv head),
+  // its column tiles one after the other, the heaviest first: they read the same
+  // keys through one L2.
+  const unsigned x = blockIdx.x & 7u, at = blockIdx.x >> 3;
+  const unsigned pair = at / unsigned(n_ct) * 8u + x;
+  if (pair >= unsigned(a.B) * unsigned(a.Hkv)) return;
+  const int tile = n_ct - 1 - int(at % unsigned(n_ct));
+  const int r = int(pair / unsigned(a.Hkv)), h = int(pair % unsigned(a.Hkv));
+  const int q0 = scalar_load(a.cu_q + r), q_end = scalar_load(a.cu_q + r + 1);
+  const int L = min(scalar_load(a.seq_lens + r), a.max_blocks * kBlock);
+  const int q_len = q_end - q0;
+  const int64_t all_cols = int64_t(min(q_len, a.max_q_len)) * G;
+  const int64_t col0 = int64_t(tile) * kCols;
+  if (q0 < 0 || q_end > a.n_rows || q_len <= 0 || q_len > L || col0 >= all_cols) return;
+  const int row_a = int(col0 / G), rem0 = int(col0 - int64_t(row_a) * G);
+  const int n_valid = int(min(all_cols - col0, int64_t(kCols)));
+  const int wave_first = wave * 32;
+  const bool active = wave_first < n_valid;
+  // This lane's column (padding columns repeat the last valid one).
+  const int co = min(wave_first + n, n_valid - 1);
+  const int t_off = (rem0 + co) / G, head = h * G + (rem0 + co - t_off * G);
+  const int pos0 = L - q_len + row_a;
+  const int pos = pos0 + t_off;
+  const int wave_pos_min = pos0 + (rem0 + min(wave_first, n_valid - 1)) / G;
+  const int wave_pos_max = pos0 + (rem0 + min(wave_first + 32, n_valid) - 1) / G;
+  const int key_lim = pos0 + (rem0 + n_valid - 1) / G + 1;  // keys from here on are hidden from all columns
+  const int n_tiles = (key_lim + kKeys - 1) / kKeys;
+  const int n_blk = (key_lim + kBlock - 1) / kBlock;
+  const int last_step = active ? wave_pos_max / 32 : -1;  // last step with a key that some column of the wave sees
+
+  // A wave loads one pool block of every K tile and of every V tile.  K runs half
+  // a tile ahead: tile j holds the blocks 4j+2 .. 4j+5, whose scores are taken
+  // while V blocks 4j .. 4j+3 are multiplied, so that both are free at the same
+  // barrier; tile -1 holds the first two blocks.
+  uint32_t koff[kInsts];
+#pragma unroll
+  for (int i = 0; i < kInsts; ++i) {
+    const int m = i * (1024 / kRowBytes) + lane / kKch;
+    const int c = source_chunk<D>(k_slot<D>(m, lane % kKch), a.pairs);
+    koff[i] = uint32_t(diff_key_of_row(m) * kRowBytes + c * 16 + 1024 - i * 1024);
+  }
+  const uint32_t voff = uint32_t((lane >> 1) * 32 + v_slot(lane >> 1, lane & 1) * 16);
+  const uint32_t ring0 = lds_offset(ring) + wave * kSlabBytes;
+  const size_t slab_stride = size_t(a.Hkv) * kSlabBytes;
+  const int32_t* bt = a.block_tables + size_t(r) * a.max_blocks;
+  const uint64_t kbase = reinterpret_cast<uint64_t>(a.k_pool) - 1024 + size_t(h) * kSlabBytes;
+  const uint64_t vbase = reinterpret_cast<uint64_t>(a.v_pool) + size_t(h) * kSlabBytes;
+  auto raw_id = [&](int blk) { return scalar_load(bt + min(blk, a.max_blocks - 1)); };
+  // (ids past the last block, or outside the pool, read block 0: masked keys)
+  auto usable = [&](int blk, int id) { return (blk < n_blk && id >= 0 && id < a.num_blocks) ? id : 0; };
+  auto k_buf = [&](int j) { return unsigned(j & 1) * kTileBytes; };
+  auto v_buf = [&](int j) { return unsigned(2 + (j & 1)) * kTileBytes; };
+  auto issue_k = [&](int j, int id) {
+    const uint64_t base = scalar(kbase + size_t(id) * slab_stride);
+    const uint32_t to = scalar(ring0 + k_buf(j));
+    if constexpr (kInsts == 4) load_slab4(koff[0], koff[1], koff[2], koff[3], base, to);
+    else load_slab2(koff[0], koff[1], base, to);
+  };
+  auto issue_v = [&](int j, int id) {
+    const uint64_t base = scalar(vbase + size_t(id) * slab_stride);
+    const uint32_t to = scalar(ring0 + v_buf(j));
+    if constexpr (kInsts == 4) load_slab4(voff, voff, voff, voff, base, to);
+    else load_slab2(voff, voff, base, to);
+  };
+
+  const int first_k = raw_id(max(wave - 2, 0)), k0 = raw_id(2 + wave), v0 = raw_id(wave);
+  if (wave >= 2) issue_k(-1, usable(wave - 2, first_k));
+  issue_k(0, usable(2 + wave, k0));
+  issue_v(0, usable(wave, v0));
+  bf16x8 qf[kDch];  // Q operand, map 1's chunks first
+  {
+    const uint16_t* qr = a.q + int64_t(q0 + row_a + t_off) * a.q_stride + size_t(head) * D;
+#pragma unroll
+    for (int kc = 0; kc < kDch; ++kc)
+      qf[kc] = as_bf16x8(*(const u32x4*)(qr + source_chunk<D>(kc * 2, a.pairs) * 8 + hh * 8));
+  }
+  const float lam = a.ep.lambda[head];
+
+  f32x16 oa[kDt], ob[kDt];  // A^T and B^T
+#pragma unroll
+  for (int dt = 0; dt < kDt; ++dt)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) oa[dt][e] = 0.f, ob[dt][e] = 0.f;
+  f32x16 s1, s2;                     // scores of the next step
+  bf16x8 pc[2], p2[2];               // p_1 - beta p_2 and p_2 of the step whose products with V are due
+  float m1 = -INFINITY, m2 = -INFINITY, l1 = 0.f, l2 = 0.f, beta = 0.f;  // l: this lane half's share
+
+  auto mask = [&](int step) {
+    const int j0 = step * 32;
+    if (j0 + 31 <= wave_pos_min) return;
+    const int rel = pos - j0 - hh * 8;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const bool hide = (e >> 3) * 16 + (e & 7) > rel;
+      s1[e] = hide ? -INFINITY : s1[e];
+      s2[e] = hide ? -INFINITY : s2[e];
+    }
+  };
+
+  // Weights of a masked step against the running maxima; where a lane's sum of them
+  // leaves [0, 2^8] (the first step; a maximum that grew), or beta is off by more than
+  // a factor of 2, the maxima are taken and A, B, the sums and beta brought in line.
+  // (A beta left too large would scale up the rounding of every p_2 behind it.)
+  auto softmax = [&](bool first) __attribute__((always_inline)) {
+    float t1, t2;
+    auto exps = [&]() __attribute__((always_inline)) {
+      float u1[2], u2[2];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float a1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s1[e], a.scale_log2, -m1));
+        const float a2 = __builtin_amdgcn_exp2f(__builtin_fmaf(s2[e], a.scale_log2, -m2));
+        u1[e & 1] = e < 2 ? a1 : u1[e & 1] + a1;
+        u2[e & 1] = e < 2 ? a2 : u2[e & 1] + a2;
+        pc[e >> 3][e & 7] = (__bf16)__builtin_fmaf(-beta, a2, a1);
+        p2[e >> 3][e & 7] = (__bf16)a2;
+      }
+      t1 = u1[0] + u1[1];
+      t2 = u2[0] + u2[1];
+      // (formed here, not behind the test below, across which 32 weights would stay live)
+      asm volatile("" : "+v"(pc[0]), "+v"(pc[1]), "+v"(p2[0]), "+v"(p2[1]));
+    };
+    bool slow = first;
+    if (!first) {
+      exps();
+      // beta within a factor of 2 of what it stands for: |beta| L_2 against |lambda| L_1
+      const float w1 = fabsf(lam) * add_across_halves(l1 + t1), w2 = fabsf(beta) * add_across_halves(l2 + t2);
+      slow = __ballot(!(t1 <= kSumLimit) || !(t2 <= kSumLimit) || w2 > 2.f * w1 || w1 > 2.f * w2) != 0;
+    }
+    if (slow) {
+      float x1 = s1[0], x2 = s2[0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) x1 = fmaxf(x1, s1[e]), x2 = fmaxf(x2, s2[e]);
+      const float n1 = fmaxf(m1, max_across_halves(x1) * a.scale_log2);
+      const float n2 = fmaxf(m2, max_across_halves(x2) * a.scale_log2);
+      const float f1 = __builtin_amdgcn_exp2f(m1 - n1), f2 = __builtin_amdgcn_exp2f(m2 - n2);
+      m1 = n1, m2 = n2;
+      l1 *= f1, l2 *= f2;
+      const float old = f1 * beta;
+      // the sums of this step, for beta's ratio, before the weights that it enters
+      float y1 = 0.f, y2 = 0.f;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        y1 += __builtin_amdgcn_exp2f(__builtin_fmaf(s1[e], a.scale_log2, -m1));
+        y2 += __builtin_amdgcn_exp2f(__builtin_fmaf(s2[e], a.scale_log2, -m2));
+      }
+      beta = lam * add_across_halves(l1 + y1) / add_across_halves(l2 + y2);
+      const float k = old - f2 * beta;
+#pragma unroll
+      for (int dt = 0; dt < kDt; ++dt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          oa[dt][e] = f1 * oa[dt][e] + k * ob[dt][e];
+          ob[dt][e] *= f2;
+        }
+      exps();
+    }
+    l1 += t1;
+    l2 += t2;
+  };
+
+  // Products: A, B += V P of a step (the two V blocks at sV), then the scores of the
+  // next (the 32 K rows at sK), the LDS operands read kPrefetch ahead.
+  constexpr int kPv = 2 * kDt, kQk = kDch, kPrefetch = 4;
+  auto products = [&](auto with_pv, auto with_qk, const uint8_t* sV, const uint8_t* sK)
+                      __attribute__((always_inline)) {
+    constexpr int first = decltype(with_pv)::value ? 0 : kPv;
+    constexpr int last = decltype(with_qk)::value ? kPv + kQk : kPv;
+    // score products alternate between the maps, which are independent chains
+    auto chunk_of = [](int u) { return (u & 1) * (kDch / 2) + (u >> 1); };
+    auto operand = [&](int st) -> bf16x8 {
+      if (st < kPv) {
+        const int b = st / kDt, d = (st % kDt) * 32 + n;
+        return *(const bf16x8*)(sV + b * kSlabBytes + d * 32 + (v_slot(d, hh) << 4));
+      }
+      return *(const bf16x8*)(sK + n * kRowBytes + (k_slot<D>(n, chunk_of(st - kPv) * 2 + hh) << 4));
+    };
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_setprio(1);
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (decltype(with_qk)::value) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s1[e] = 0.f, s2[e] = 0.f;
+    }
+    bf16x8 buf[kPrefetch];
+#pragma unroll
+    for (int st = first; st < first + kPrefetch && st < last; ++st) buf[st % kPrefetch] = operand(st);
+#pragma unroll
+    for (int st = first; st < last; ++st) {
+      const bf16x8 op = buf[st % kPrefetch];
+      if (st + kPrefetch < last) buf[st % kPrefetch] = operand(st + kPrefetch);
+      if (st < kPv) {
+        const int dt = st % kDt, b = st / kDt;
+        oa[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op, pc[b], oa[dt], 0, 0, 0);
+        ob[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op, p2[b], ob[dt], 0, 0, 0);
+      } else {
+        const int u = st - kPv;
+        if (u & 1) s2 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op, qf[chunk_of(u)], s2, 0, 0, 0);
+        else s1 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op, qf[chunk_of(u)], s1, 0, 0, 0);
+      }
+    }
+    // pin that order: kPrefetch reads, then the product(s) of one operand a read
+    constexpr int steps = last - first, lead = steps < kPrefetch ? steps : kPrefetch;
+    constexpr int pv = first < kPv ? kPv : 0, qk = steps - pv;  // operands of each kind
+    constexpr int pv_reads = pv < steps - lead ? pv : steps - lead, qk_reads = steps - lead - pv_reads;
+    __builtin_amdgcn_sched_group_barrier(0x100, lead, 0);
+#pragma unroll
+    for (int st = 0; st < pv; ++st) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+      if (st < pv_reads) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+#pragma unroll
+    for (int st = 0; st < qk; ++st) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      if (st < qk_reads) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_setprio(0);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  using yes = std::true_type;
+  using no = std::false_type;
+
+  // Zero the V rows of keys >= key_lim in this wave's block of V tile j (its own
+  // loads of it have landed; others read it behind the next barrier): unwritten
+  // slots may hold any bits, and a weight of 0 does not hide a NaN.
+  auto zero_v_tail = [&](int j) {
+    const int nv = key_lim - (j * kKeys + wave * kBlock);
+    if (nv >= kBlock) return;
+    uint8_t* sV = ring + v_buf(j) + wave * kSlabBytes;
+    const int keep = nv - v_slot(lane >> 1, lane & 1) * 8;
+#pragma unroll
+    for (int i = 0; i < kInsts; ++i) {
+      u32x4* p = (u32x4*)(sV + i * 1024 + lane * 16);
+      u32x4 v = *p;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] &= (2 * e < keep ? 0x0000FFFFu : 0u) | (2 * e + 1 < keep ? 0xFFFF0000u : 0u);
+      *p = v;
+    }
+    wait_lds();
+  };
+
+  // Two steps a tile.  Before the first of tile j: wait for this wave's loads of
+  // K(j), V(j); barrier; issue K(j+1) and V(j+1) into the buffers of tile j-1, which
+  // every wave has left behind.  The scores of a step past the wave's last one are
+  // computed and ignored.
+  wait_loads();
+  bare_barrier();
+  if (active) products(no(), yes(), ring, ring + k_buf(-1) + 32 * kRowBytes);
+  for (int u = 0; u < 2 * n_tiles; ++u) {
+    const int j = u >> 1;
+    if (!(u & 1)) {
+      if (j > 0) wait_loads();
+      zero_v_tail(j);
+      bare_barrier();
+      if (j + 1 < n_tiles) {
+        const int kb = (j + 1) * kTileBlocks + 2 + wave, vb = (j + 1) * kTileBlocks + wave;
+        const int kid = raw_id(kb), vid = raw_id(vb);
+        issue_k(j + 1, usable(kb, kid));
+        issue_v(j + 1, usable(vb, vid));
+      }
+    }
+    if (u <= last_step) {
+      mask(u);
+      int uu = u;
+      asm volatile("" : "+s"(uu));  // (one body for the first step and the others)
+      softmax(uu == 0);
+      products(yes(), yes(), ring + v_buf(j) + (u & 1) * 2 * kSlabBytes, ring + k_buf(j) + (u & 1) * 32 * kRowBytes);
+    }
+  }
+  if (!active) return;
+
+  const float t1 = add_across_halves(l1), t2 = add_across_halves(l2);
+  const float k = beta - lam * t1 / t2, inv = 1.f / t1;
+  float sq = 0.f;
+#pragma unroll
+  for (int dt = 0; dt < kDt; ++dt)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const float y = (oa[dt][e] + k * ob[dt][e]) * inv;
+      oa[dt][e] = y;
+      sq += y * y;
+    }
+  float fac = a.ep.scale;
+  if (a.ep.norm_w) fac *= rsqrtf(add_across_halves(sq) * (1.f / D) + a.ep.eps);
+  if (wave_first + n >= n_valid) return;
+  uint16_t* orow = a.out + (size_t(q0 + row_a + t_off) * a.Hq + head) * D;
+#pragma unroll
+  for (int dt = 0; dt < kDt; ++dt)
+#pragma unroll
+    for (int g4 = 0; g4 < 4; ++g4) {
+      const int d = dt * 32 + g4 * 8 + hh * 4;
+      f32x4 w = {fac, fac, fac, fac};
+      if (a.ep.norm_w) {
+        const f32x4 nw = *(const f32x4*)(a.ep.norm_w + d);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] *= nw[e];
+      }
+      bf16x4 v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = (__bf16)(oa[dt][g4 * 4 + e] * w[e]);
+      *(bf16x4*)(orow + d) = v;
+    }
+}
+
+}  // namespace
+
+namespace ilpc {
+
+bool launch_diff_prefill(const DiffArgs& a, hipStream_t stream) {
+  const int64_t n_ct = (int64_t(a.max_q_len) * (a.Hq / a.Hkv) + kCols - 1) / kCols;
+  const int64_t grid = (int64_t(a.B) * a.Hkv + 7) / 8 * 8 * n_ct;
+  if (a.D == 128)
+    hipLaunchKernelGGL(diff_prefill_kernel<128>, dim3(unsigned(grid)), dim3(64 * kWaves), 0, stream, a, int(n_ct));
+  else
+    hipLaunchKernelGGL(diff_prefill_kernel<64>, dim3(unsigned(grid)), dim3(64 * kWaves), 0, stream, a, int(n_ct));
+  return hipGetLastError() == hipSuccess;
+}
+
+}  // namespace ilpc
