@@ -13,9 +13,13 @@
 // is kept from one call to the next but the library's entry points.
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <ATen/ops/empty.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 
 #include <climits>
+#include <initializer_list>
+#include <type_traits>
 
 #include "../../include/ilpc.h"
 
@@ -27,6 +31,11 @@ decltype(&ilpc_rope_kv_append) rope_kv_append = nullptr;
 decltype(&ilpc_attn_workspace_bytes) attn_workspace_bytes = nullptr;
 decltype(&ilpc_paged_prefill_attn) prefill_attn = nullptr;
 decltype(&ilpc_paged_prefill_attn_cascade) prefill_attn_cascade = nullptr;
+decltype(&ilpc_extend_tables) extend_tables = nullptr;
+decltype(&ilpc_release_tables) release_tables = nullptr;
+decltype(&ilpc_kv_append_slots) kv_append_slots = nullptr;
+decltype(&ilpc_diff_attn_workspace_bytes) diff_attn_workspace_bytes = nullptr;
+decltype(&ilpc_paged_diff_attn) paged_diff_attn = nullptr;
 
 constexpr int kNotHere = INT_MIN;  // what a body returns for a call it does not take
 
@@ -139,20 +148,20 @@ int call(int (*fn)(P...), A... args) {
   return rc;
 }
 
-// bind(addresses of kv_append, rope_kv_append, attn_workspace_bytes, paged_prefill_attn, paged_prefill_attn_cascade)
+// bind(addresses of the entry points above, in their order)
 PyObject* py_bind(PyObject*, PyObject* const* argv, Py_ssize_t n) {
-  void* p[5];
-  if (n != 5) {
-    PyErr_SetString(PyExc_TypeError, "bind() takes 5 addresses");
+  constexpr int kEntries = 10;
+  void* p[kEntries];
+  if (n != kEntries) {
+    PyErr_Format(PyExc_TypeError, "bind() takes %d addresses", kEntries);
     return nullptr;
   }
-  for (int i = 0; i < 5; ++i) p[i] = PyLong_AsVoidPtr(argv[i]);
+  for (int i = 0; i < kEntries; ++i) p[i] = PyLong_AsVoidPtr(argv[i]);
   if (PyErr_Occurred()) return nullptr;
-  kv_append = reinterpret_cast<decltype(kv_append)>(p[0]);
-  rope_kv_append = reinterpret_cast<decltype(rope_kv_append)>(p[1]);
-  attn_workspace_bytes = reinterpret_cast<decltype(attn_workspace_bytes)>(p[2]);
-  prefill_attn = reinterpret_cast<decltype(prefill_attn)>(p[3]);
-  prefill_attn_cascade = reinterpret_cast<decltype(prefill_attn_cascade)>(p[4]);
+  int i = 0;
+  auto set = [&](auto& fn) { fn = reinterpret_cast<std::decay_t<decltype(fn)>>(p[i++]); };
+  set(kv_append), set(rope_kv_append), set(attn_workspace_bytes), set(prefill_attn), set(prefill_attn_cascade);
+  set(extend_tables), set(release_tables), set(kv_append_slots), set(diff_attn_workspace_bytes), set(paged_diff_attn);
   Py_RETURN_NONE;
 }
 
@@ -277,11 +286,166 @@ PyObject* py_prefill_attn_cascade(PyObject*, PyObject* const* argv, Py_ssize_t n
   });
 }
 
+// Tensors of one call: all on the stream's device, which is the current one (the
+// general path makes another one current), the stream's pointer in *s.
+bool placed(std::initializer_list<const at::Tensor*> tensors, PyObject* so, void** s) {
+  int dev;
+  if (!stream_of(so, s, &dev) || dev != c10::hip::current_device()) return false;
+  for (const at::Tensor* t : tensors)
+    if (t && t->device().index() != dev) return false;
+  return true;
+}
+
+struct Span {
+  const char *from, *to;
+  explicit Span(const at::Tensor* t)
+      : from(static_cast<const char*>(t->data_ptr())), to(from + t->numel() * t->element_size()) {}
+  bool meets(const Span& o) const { return from < o.to && o.from < to && from < to && o.from < o.to; }
+};
+
+// Whether outputs share memory with an input or with each other.
+bool apart(std::initializer_list<const at::Tensor*> outputs, std::initializer_list<const at::Tensor*> inputs) {
+  for (auto a = outputs.begin(); a != outputs.end(); ++a) {
+    const Span s(*a);
+    for (auto b = a + 1; b != outputs.end(); ++b)
+      if (s.meets(Span(*b))) return false;
+    for (const at::Tensor* b : inputs)
+      if (b && s.meets(Span(b))) return false;
+  }
+  return true;
+}
+
+// extend_tables(block_tables, start_pos, new_lens, free_ids, taken, seq_lens, cu_q, cu_blocks, slot_map, taken_out,
+//               status, num_blocks, stream)
+PyObject* py_extend_tables(PyObject*, PyObject* const* argv, Py_ssize_t n) {
+  return guarded([&]() -> int {
+    Args a{argv, n};
+    auto ints = [&](int64_t dim) { return a.tensor(at::kInt, dim); };
+    const at::Tensor *bt = ints(2), *start = ints(1), *add = ints(1), *free = ints(1), *taken = ints(1), *seq = ints(1),
+                     *cu = ints(1), *cb = ints(1), *slots = ints(1), *out = ints(1), *status = ints(1);
+    const int32_t nb = a.integer();
+    PyObject* so = a.next();
+    if (!a.ok) return kNotHere;
+    const int64_t B = start->size(0);
+    if (bt->size(0) != B || add->size(0) != B || seq->size(0) != B || cu->size(0) != B + 1 || cb->size(0) != B + 1 ||
+        taken->size(0) != 1 || out->size(0) != 1 || status->size(0) != 1)
+      return kNotHere;
+    if (!apart({bt, cu, cb, slots, status, seq, out},
+               {add, free, seq->data_ptr() == start->data_ptr() ? nullptr : start,
+                out->data_ptr() == taken->data_ptr() ? nullptr : taken}))
+      return kNotHere;
+    void* s;
+    if (!placed({bt, start, add, free, taken, seq, cu, cb, slots, out, status}, so, &s)) return kNotHere;
+    return call(extend_tables, i32(bt), int32_t(bt->size(1)), int32_t(B), i32(start), i32(add), i32(free),
+                int32_t(free->size(0)), i32(taken), nb, i32(seq), i32(cu), i32(cb), i32(slots),
+                int32_t(slots->size(0)), i32(out), i32(status), s);
+  });
+}
+
+// release_tables(block_tables, first_block, seq_lens, free_ids, taken, cu_blocks, taken_out, status, stream)
+PyObject* py_release_tables(PyObject*, PyObject* const* argv, Py_ssize_t n) {
+  return guarded([&]() -> int {
+    Args a{argv, n};
+    auto ints = [&](int64_t dim) { return a.tensor(at::kInt, dim); };
+    const at::Tensor *bt = ints(2), *first = ints(1), *seq = ints(1), *free = ints(1), *taken = ints(1), *cb = ints(1),
+                     *out = ints(1), *status = ints(1);
+    PyObject* so = a.next();
+    if (!a.ok) return kNotHere;
+    const int64_t B = first->size(0);
+    if (bt->size(0) != B || seq->size(0) != B || cb->size(0) != B + 1 || taken->size(0) != 1 || out->size(0) != 1 ||
+        status->size(0) != 1)
+      return kNotHere;
+    if (!apart({free, cb, status, out},
+               {bt, first, seq, out->data_ptr() == taken->data_ptr() ? nullptr : taken}))
+      return kNotHere;
+    void* s;
+    if (!placed({bt, first, seq, free, taken, cb, out, status}, so, &s)) return kNotHere;
+    return call(release_tables, i32(bt), int32_t(bt->size(1)), int32_t(B), i32(first), i32(seq), i32(free),
+                int32_t(free->size(0)), i32(taken), i32(cb), i32(out), i32(status), s);
+  });
+}
+
+// bf16 rows [n, H, D], each contiguous, *stride elements apart (nullptr: others).
+const at::Tensor* rows(Args& a, int64_t* stride) {
+  PyObject* o = a.next();
+  a.ok = a.ok && THPVariable_CheckExact(o);
+  if (!a.ok) return nullptr;
+  const at::Tensor& t = THPVariable_Unpack(o);
+  a.ok = t.is_cuda() && t.scalar_type() == at::kBFloat16 && t.layout() == at::kStrided && t.dim() == 3 &&
+         (t.numel() == 0 || (t.stride(2) == 1 && (t.size(1) <= 1 || t.stride(1) == t.size(2))));
+  if (!a.ok) return nullptr;
+  *stride = t.size(0) > 1 ? t.stride(0) : t.size(1) * t.size(2);
+  return &t;
+}
+
+// kv_append_slots(k_new, v_new, k_pool, v_pool, slot_map, stream)
+PyObject* py_kv_append_slots(PyObject*, PyObject* const* argv, Py_ssize_t n) {
+  return guarded([&]() -> int {
+    Args a{argv, n};
+    int64_t ks = 0, vs = 0;
+    const at::Tensor *k = rows(a, &ks), *v = rows(a, &vs), *kp = a.tensor(at::kBFloat16, 4),
+                     *vp = a.tensor(at::kBFloat16, 4), *slots = a.tensor(at::kInt, 1);
+    PyObject* so = a.next();
+    if (!a.ok) return kNotHere;
+    const int64_t Hkv = kp->size(1), D = kp->size(3);
+    if (!pools_fit(*kp, *vp) || k->size(1) != Hkv || k->size(2) != D || v->sizes() != k->sizes() ||
+        slots->size(0) != k->size(0))
+      return kNotHere;
+    void* s;
+    if (!placed({k, v, kp, vp, slots}, so, &s)) return kNotHere;
+    return call(kv_append_slots, bf16(k), ks, bf16(v), vs, bf16(kp), bf16(vp), int32_t(kp->size(0)), i32(slots),
+                int32_t(slots->size(0)), int32_t(Hkv), int32_t(D), int32_t(kp->size(2)), s);
+  });
+}
+
+// paged_diff_attn(q, k_pool, v_pool, block_tables, cu_q, seq_lens, max_q_len, scale, lam, out, norm_weight, norm_eps,
+//                 out_scale, layout, workspace, stream)
+PyObject* py_paged_diff_attn(PyObject*, PyObject* const* argv, Py_ssize_t n) {
+  return guarded([&]() -> int {
+    Args a{argv, n};
+    int64_t qs = 0;
+    const at::Tensor *q = rows(a, &qs), *kp = a.tensor(at::kBFloat16, 4), *vp = a.tensor(at::kBFloat16, 4),
+                     *bt = a.tensor(at::kInt, 2), *cu = a.tensor(at::kInt, 1), *L = a.tensor(at::kInt, 1);
+    const int32_t max_q = a.integer();
+    const float scale = a.real();
+    const at::Tensor *lam = a.tensor(at::kFloat, 1), *out = a.tensor(at::kBFloat16, 3),
+                     *w = a.tensor_or_none(at::kFloat, 1);
+    const float eps = a.real(), out_scale = a.real();
+    const int32_t layout = a.integer();
+    const at::Tensor* ws = a.tensor_or_none(at::kByte, 1);
+    PyObject* so = a.next();
+    if (!a.ok) return kNotHere;
+    const int64_t B = cu->size(0) - 1, Hq = q->size(1), Hkv = kp->size(1), D = kp->size(3);
+    if (!pools_fit(*kp, *vp) || q->size(2) != D || out->sizes() != q->sizes() || bt->size(0) != B ||
+        L->size(0) != B || lam->size(0) != Hq || (w && w->size(0) != D))
+      return kNotHere;
+    void* s;
+    if (!placed({q, kp, vp, bt, cu, L, lam, out, w, ws}, so, &s)) return kNotHere;
+    at::Tensor own;  // the call's scratch, from the current stream's memory
+    if (!ws) {
+      size_t need = 0;
+      if (diff_attn_workspace_bytes(int32_t(B), max_q, int32_t(Hq), int32_t(Hkv), int32_t(D), int32_t(bt->size(1)),
+                                    &need) != ILPC_OK ||
+          (need && so != Py_None))
+        return kNotHere;
+      if (need) own = at::empty({int64_t(need)}, q->options().dtype(at::kByte));
+    }
+    const at::Tensor* scratch = ws ? ws : own.defined() ? &own : nullptr;
+    return call(paged_diff_attn, bf16(q), qs, int32_t(q->size(0)), bf16(kp), bf16(vp), int32_t(kp->size(0)), i32(bt),
+                int32_t(bt->size(1)), i32(cu), i32(L), int32_t(B), max_q, int32_t(Hq), int32_t(Hkv), int32_t(D),
+                int32_t(kp->size(2)), scale, layout, static_cast<float*>(lam->data_ptr()),
+                w ? static_cast<float*>(w->data_ptr()) : nullptr, eps, out_scale, bf16(out),
+                scratch ? scratch->data_ptr() : nullptr, scratch ? size_t(scratch->numel()) : size_t(0), s);
+  });
+}
+
 #define FAST(name, fn) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(fn)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST("bind", py_bind),
                          FAST("kv_append", py_kv_append), FAST("rope_kv_append", py_rope_kv_append),
                          FAST("paged_prefill_attn", py_prefill_attn),
                          FAST("paged_prefill_attn_cascade", py_prefill_attn_cascade),
+                         FAST("extend_tables", py_extend_tables), FAST("release_tables", py_release_tables),
+                         FAST("kv_append_slots", py_kv_append_slots), FAST("paged_diff_attn", py_paged_diff_attn),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

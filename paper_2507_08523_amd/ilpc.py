@@ -137,7 +137,8 @@ def _native():
             return _binding
         mod.bind(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in (
             "ilpc_kv_append", "ilpc_rope_kv_append", "ilpc_attn_workspace_bytes", "ilpc_paged_prefill_attn",
-            "ilpc_paged_prefill_attn_cascade")))
+            "ilpc_paged_prefill_attn_cascade", "ilpc_extend_tables", "ilpc_release_tables", "ilpc_kv_append_slots",
+            "ilpc_diff_attn_workspace_bytes", "ilpc_paged_diff_attn")))
         _binding = mod
     return _binding
 
@@ -694,6 +695,11 @@ def extend_tables(block_tables, start_pos, new_lens, free_ids, taken, seq_lens, 
     taken), status [1] (0, or NO_BLOCKS | TOO_LONG | TOO_MANY_ROWS | BAD_VALUE
     with nothing changed).
     """
+    rc = (_binding or _native()).extend_tables(block_tables, start_pos, new_lens, free_ids, taken, seq_lens, cu_q,
+                                               cu_blocks, slot_map, taken_out, status, num_blocks, stream)
+    if rc is not None:
+        return _check(rc)
+
     fn = "extend_tables"
     B = start_pos.shape[0] if getattr(start_pos, "ndim", 0) == 1 else -1
     p = _ints(fn, block_tables=(block_tables, (B, -1)), start_pos=(start_pos, (B,)), new_lens=(new_lens, (B,)),
@@ -724,6 +730,11 @@ def release_tables(block_tables, first_block, seq_lens, free_ids, taken, cu_bloc
     seq_lens [B], free_ids [n] (in/out), taken [1]; out: cu_blocks [B+1],
     taken_out [1] (may be taken), status [1].
     """
+    rc = (_binding or _native()).release_tables(block_tables, first_block, seq_lens, free_ids, taken, cu_blocks,
+                                                taken_out, status, stream)
+    if rc is not None:
+        return _check(rc)
+
     fn = "release_tables"
     B = first_block.shape[0] if getattr(first_block, "ndim", 0) == 1 else -1
     p = _ints(fn, block_tables=(block_tables, (B, -1)), first_block=(first_block, (B,)), seq_lens=(seq_lens, (B,)),
@@ -744,6 +755,10 @@ def kv_append_slots(k_new, v_new, k_pool, v_pool, slot_map, stream=None):
     """Store K/V rows [n, Hkv, D] at the slots of slot_map (int32 [n]; rows whose
     slot is not in the pools, -1 among them, are not stored).  The rows may be
     views of a wider row (a fused projection's output)."""
+    rc = (_binding or _native()).kv_append_slots(k_new, v_new, k_pool, v_pool, slot_map, stream)
+    if rc is not None:
+        return _check(rc)
+
     fn = "kv_append_slots"
     kp, vp, NB, Hkv, bs, D = _pools(k_pool, v_pool, fn)
     k, k_stride = _rows(k_new, "k_new", (Hkv, D))
@@ -777,6 +792,11 @@ def paged_diff_attn(q, k_pool, v_pool, block_tables, cu_q, seq_lens, max_q_len: 
     do not share one.
     """
     import torch
+
+    rc = (_binding or _native()).paged_diff_attn(q, k_pool, v_pool, block_tables, cu_q, seq_lens, max_q_len, scale, lam,
+                                                 out, norm_weight, norm_eps, out_scale, layout, workspace, stream)
+    if rc is not None:
+        return _check(rc)
 
     fn = "paged_diff_attn"
     kp, vp, NB, Hkv, bs, D = _pools(k_pool, v_pool, fn)

@@ -268,7 +268,44 @@ def refused(call, **kw):
         call(**kw)
 
 
-def test_binding_refusals():
+class Taken:
+    """The native binding, noting what it answers (None: left to the general path)."""
+
+    def __init__(self):
+        self.native, self.rc = ilpc._native(), []
+        assert not isinstance(self.native, ilpc._NoNative)
+
+    def __getattr__(self, name):
+        return lambda *a: (self.rc.append(getattr(self.native, name)(*a)), self.rc[-1])[1]
+
+
+def test_native_calls_equal_the_general_path(monkeypatch):
+    tables, start, new, free, taken, nb = make(40, 0, 70, 20, 8)
+    rows = int(new.sum()) + 3
+    got, native = [], Taken()
+    for stand_in in (ilpc._NoNative(), native):
+        monkeypatch.setattr(ilpc, "_binding", stand_in)
+        s = State(tables, start, new, free, taken, nb, rows)
+        res = s.extend()
+        f, k2, cb, st = dev(free), dev([0]), dev([0] * 41), dev([9])
+        ilpc.release_tables(s.t, dev(-(-start // BLOCK)), s.seq, f, s.k2, cb, k2, st)
+        kp, vp = pools(nb, 2, 64)
+        x = torch.ones(rows, 5, 64, dtype=torch.bfloat16, device="cuda") * torch.arange(rows, device="cuda")[:, None, None]
+        ilpc.kv_append_slots(x[:, 1:3], x[:, 3:], kp, vp, s.slots)
+        out = torch.zeros(rows, 2, 64, dtype=torch.bfloat16, device="cuda")
+        for w, split in ((None, False), (torch.ones(64, device="cuda"), True)):
+            ilpc.paged_diff_attn(x[:, :2], kp, vp, s.t, s.cu, s.seq, 1 if split else 20, 0.1,
+                                 torch.ones(2, device="cuda"), out, norm_weight=w)
+        torch.cuda.synchronize()
+        got.append([t.clone() for t in (*res, f, k2, cb, st, kp, vp, out)])
+    assert native.rc == [0] * 5
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_binding_refusals(native, monkeypatch):
+    if not native:
+        monkeypatch.setattr(ilpc, "_binding", ilpc._NoNative())
     i, cu, one = dev([1, 2, 3]), dev([0] * 4), dev([0])
     a = dict(block_tables=dev(np.zeros((3, 4))), start_pos=i, new_lens=dev([1] * 3), free_ids=dev([1, 2]), taken=one,
              seq_lens=dev([0] * 3), cu_q=cu, cu_blocks=dev([0] * 4), slot_map=dev([0] * 5), taken_out=dev([0]),

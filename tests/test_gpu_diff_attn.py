@@ -297,7 +297,10 @@ def test_same_bits_every_time():
             assert torch.equal(b.run(), want)
 
 
-def test_binding_refusals():
+@pytest.mark.parametrize("native", [True, False])
+def test_binding_refusals(native, monkeypatch):
+    if not native:
+        monkeypatch.setattr(ilpc, "_binding", ilpc._NoNative())
     b = Batch([40, 30], [3, 2], 4, 2, 128)
     out = torch.empty(b.q.shape, dtype=torch.bfloat16, device="cuda")
 
