@@ -25,6 +25,12 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr int kBlock = 16;
 constexpr int kScanThreads = 1024;
 constexpr int kMaxRequests = 1 << 20;
+// Most rows (of extend; blocks that there can be, of release) that the workgroup of
+// the sums fills in itself.  us in one launch, in two: 512 requests of a row 5.2, 9.3;
+// one request of 4096 rows 5.3, 7.5; 64 requests of 128 rows 10.3, 10.9, of 256 17.2,
+// 10.5.  Released ids (of a table of as many or more): 512 3.7, 5.8; 4096 5.4, 5.9;
+// 8192 8.1, 6.0.
+constexpr int kOneFill = 4096, kOneRelease = 8192;
 
 // What is refused on the device (bits of *status).
 enum { kNoBlocks = 1, kTooLong = 2, kTooManyRows = 4, kBadValue = 8 };
@@ -71,19 +77,47 @@ __device__ __forceinline__ int owner(const int32_t* sums, int lo, int hi, int x)
   return lo;
 }
 
+// What the fill needs of a request: start, first row, first new block.
+struct Growth {
+  const int32_t *seq_lens, *cu_q, *cu_blocks;  // B, B + 1, B + 1
+  __device__ __forceinline__ int start(int r) const { return seq_lens[r] - (cu_q[r + 1] - cu_q[r]); }
+};
+
+// Table entry of the e-th block taken (a block of request r).
+__device__ __forceinline__ void put_block(int e, int r, const Growth& g, int32_t* block_tables, int max_blocks,
+                                          const int32_t* free_ids, int first_id) {
+  block_tables[size_t(r) * max_blocks + blocks_of(g.start(r)) + (e - g.cu_blocks[r])] = free_ids[first_id + e];
+}
+
+// Slot of row i (a row of request r).
+__device__ __forceinline__ int slot_of(int i, int r, const Growth& g, const int32_t* block_tables, int max_blocks,
+                                       const int32_t* free_ids, int first_id, int num_blocks) {
+  const int start = g.start(r), pos = start + (i - g.cu_q[r]), lb = pos / kBlock, had = blocks_of(start);
+  const int id = lb < had ? block_tables[size_t(r) * max_blocks + lb] : free_ids[first_id + g.cu_blocks[r] + lb - had];
+  return id >= 0 && id < num_blocks ? id * kBlock + pos % kBlock : -1;
+}
+
 // Lengths and sums, by one workgroup: a thread takes a run of requests, adds it
 // up, and behind the sum over the threads before it writes the run's results.
 // Reads of a request's lengths come before the same thread's write, so seq_lens
-// may be start_pos.
+// may be start_pos.  FILL: the same workgroup then writes the table entries and
+// slots, from sums that it keeps in LDS: a decode step's tables are one launch.
+constexpr int kFillRequests = 2048;  // FILL: at most
+
+template <bool FILL>
 __global__ __launch_bounds__(kScanThreads) void extend_scan_kernel(
-    const int32_t* start_pos, const int32_t* __restrict__ new_lens, int B, int n_free, const int32_t* taken,
-    int max_blocks, int max_rows, int32_t* seq_lens, int32_t* __restrict__ cu_q, int32_t* __restrict__ cu_blocks,
-    int32_t* taken_out, int32_t* __restrict__ status) {
+    int32_t* block_tables, const int32_t* start_pos, const int32_t* __restrict__ new_lens, int B,
+    const int32_t* __restrict__ free_ids, int n_free, const int32_t* taken, int num_blocks, int max_blocks,
+    int max_rows, int32_t* seq_lens, int32_t* __restrict__ cu_q, int32_t* __restrict__ cu_blocks,
+    int32_t* __restrict__ slot_map, int32_t* taken_out, int32_t* __restrict__ status) {
+  constexpr int kKeep = FILL ? kFillRequests : 1;
+  __shared__ int32_t k_seq[kKeep], k_cu[kKeep + 1], k_cb[kKeep + 1];
   const int per = (B + kScanThreads - 1) / kScanThreads;
   const int r0 = min(int(threadIdx.x) * per, B), r1 = min(r0 + per, B);
   const int64_t had = *taken;
   int64_t rows = 0, blocks = 0;
   int bad = 0;
+#pragma unroll 4
   for (int r = r0; r < r1; ++r) {
     const int64_t s = start_pos[r], n = new_lens[r];
     if (s < 0 || n < 0) bad |= kBadValue;
@@ -97,61 +131,79 @@ __global__ __launch_bounds__(kScanThreads) void extend_scan_kernel(
   if (had + t.tb > n_free) refused |= kNoBlocks;
   if (t.ta > max_rows) refused |= kTooManyRows;
   int64_t a = t.a, b = t.b;
+#pragma unroll 4
   for (int r = r0; r < r1; ++r) {
     const int64_t s = start_pos[r], n = new_lens[r];
-    cu_q[r] = refused ? 0 : int32_t(a);
-    cu_blocks[r] = refused ? 0 : int32_t(b);
-    seq_lens[r] = int32_t(refused ? s : s + n);
+    const int32_t row = refused ? 0 : int32_t(a), block = refused ? 0 : int32_t(b), len = int32_t(refused ? s : s + n);
+    cu_q[r] = row;
+    cu_blocks[r] = block;
+    seq_lens[r] = len;
+    if (FILL) k_cu[r] = row, k_cb[r] = block, k_seq[r] = len;
     a += n;
     b += blocks_of(s + n) - blocks_of(s);
   }
+  const int n_rows = refused ? 0 : int(t.ta), n_new = refused ? 0 : int(t.tb);
   if (threadIdx.x == 0) {
-    cu_q[B] = refused ? 0 : int32_t(t.ta);
-    cu_blocks[B] = refused ? 0 : int32_t(t.tb);
-    *taken_out = int32_t(refused ? had : had + t.tb);
+    cu_q[B] = n_rows;
+    cu_blocks[B] = n_new;
+    if (FILL) k_cu[B] = n_rows, k_cb[B] = n_new;
+    *taken_out = int32_t(had + n_new);
     *status = refused;
+  }
+  if constexpr (FILL) {
+    __syncthreads();
+    const Growth g{k_seq, k_cu, k_cb};
+    for (int e = threadIdx.x; e < n_new; e += kScanThreads)
+      put_block(e, owner(k_cb, 0, B, e), g, block_tables, max_blocks, free_ids, int(had));
+    for (int i = threadIdx.x; i < max_rows; i += kScanThreads)
+      slot_map[i] = i < n_rows ? slot_of(i, owner(k_cu, 0, B, i), g, block_tables, max_blocks, free_ids, int(had),
+                                         num_blocks)
+                               : -1;
   }
 }
 
-constexpr int kFillThreads = 256, kFillRows = 1024;  // rows of a workgroup
+// Table entries and slots from the sums, for many rows: 1024 rows a workgroup, whose
+// requests it looks up once.  What bounds the two launches is their latency (512
+// requests, 1.0 M rows 12 us, 16 K rows 13 us); sums copied to LDS first changed nothing.
+constexpr int kFillThreads = 256, kFillRows = 1024;
 
-// Table entries and slots from the sums.
 __global__ __launch_bounds__(kFillThreads) void extend_fill_kernel(
-    int32_t* __restrict__ block_tables, int B, int max_blocks, const int32_t* __restrict__ free_ids, int n_free,
+    int32_t* __restrict__ block_tables, int B, int max_blocks, const int32_t* __restrict__ free_ids,
     const int32_t* __restrict__ taken_out, int num_blocks, const int32_t* __restrict__ seq_lens,
     const int32_t* __restrict__ cu_q, const int32_t* __restrict__ cu_blocks, int32_t* __restrict__ slot_map,
     int max_rows) {
+  __shared__ int s_of[2];
   const int n_rows = cu_q[B], n_new = cu_blocks[B];
   const int first_id = *taken_out - n_new;
-  auto held = [&](int r) { return blocks_of(seq_lens[r] - (cu_q[r + 1] - cu_q[r])); };
-  for (int e = blockIdx.x * kFillThreads + threadIdx.x; e < n_new; e += gridDim.x * kFillThreads) {
-    const int r = owner(cu_blocks, 0, B, e);
-    block_tables[size_t(r) * max_blocks + held(r) + (e - cu_blocks[r])] = free_ids[first_id + e];
-  }
-  const int64_t i0 = int64_t(blockIdx.x) * kFillRows;
-  for (int64_t j = i0 + threadIdx.x; j < min(i0 + kFillRows, int64_t(max_rows)); j += kFillThreads) {
+  const Growth g{seq_lens, cu_q, cu_blocks};
+  for (int64_t e = int64_t(blockIdx.x) * kFillThreads + threadIdx.x; e < n_new; e += int64_t(gridDim.x) * kFillThreads)
+    put_block(int(e), owner(cu_blocks, 0, B, int(e)), g, block_tables, max_blocks, free_ids, first_id);
+  const int64_t i0 = int64_t(blockIdx.x) * kFillRows, i1 = min(i0 + kFillRows, int64_t(max_rows));
+  if (threadIdx.x < 2 && i0 < n_rows)
+    s_of[threadIdx.x] = owner(cu_q, 0, B, threadIdx.x ? int(min(i1, int64_t(n_rows))) - 1 : int(i0));
+  __syncthreads();
+  for (int64_t j = i0 + threadIdx.x; j < i1; j += kFillThreads) {
     const int i = int(j);
-    int slot = -1;
-    if (i < n_rows) {
-      const int r = owner(cu_q, 0, B, i);
-      const int start = seq_lens[r] - (cu_q[r + 1] - cu_q[r]);
-      const int pos = start + (i - cu_q[r]), lb = pos / kBlock, had = blocks_of(start);
-      const int id = lb < had ? block_tables[size_t(r) * max_blocks + lb] : free_ids[first_id + cu_blocks[r] + lb - had];
-      if (id >= 0 && id < num_blocks) slot = id * kBlock + pos % kBlock;
-    }
-    slot_map[i] = slot;
+    slot_map[i] = i < n_rows ? slot_of(i, owner(cu_q, s_of[0], s_of[1] + 1, i), g, block_tables, max_blocks, free_ids,
+                                       first_id, num_blocks)
+                             : -1;
   }
 }
 
+template <bool FILL>
 __global__ __launch_bounds__(kScanThreads) void release_scan_kernel(
-    const int32_t* __restrict__ first_block, const int32_t* __restrict__ seq_lens, int B, int max_blocks, int n_free,
-    const int32_t* taken, int32_t* __restrict__ cu_blocks, int32_t* taken_out, int32_t* __restrict__ status) {
+    const int32_t* __restrict__ block_tables, const int32_t* __restrict__ first_block,
+    const int32_t* __restrict__ seq_lens, int B, int max_blocks, int n_free, const int32_t* taken,
+    int32_t* __restrict__ free_ids, int32_t* __restrict__ cu_blocks, int32_t* taken_out,
+    int32_t* __restrict__ status) {
+  __shared__ int32_t k_cb[FILL ? kFillRequests + 1 : 1];
   const int per = (B + kScanThreads - 1) / kScanThreads;
   const int r0 = min(int(threadIdx.x) * per, B), r1 = min(r0 + per, B);
   const int64_t had = *taken;
   auto count = [&](int r) { return max(blocks_of(seq_lens[r]) - max(first_block[r], 0), 0); };
   int64_t blocks = 0;
   int bad = 0;
+#pragma unroll 4
   for (int r = r0; r < r1; ++r) {
     if (first_block[r] < 0 || seq_lens[r] < 0) bad |= kBadValue;
     if (seq_lens[r] > int64_t(max_blocks) * kBlock) bad |= kTooLong;
@@ -162,14 +214,25 @@ __global__ __launch_bounds__(kScanThreads) void release_scan_kernel(
   if (had < 0 || had > n_free) refused |= kBadValue;
   if (t.tb > had) refused |= kNoBlocks;
   int64_t b = t.b;
+#pragma unroll 4
   for (int r = r0; r < r1; ++r) {
     cu_blocks[r] = refused ? 0 : int32_t(b);
+    if (FILL) k_cb[r] = cu_blocks[r];
     b += count(r);
   }
+  const int n = refused ? 0 : int(t.tb);
   if (threadIdx.x == 0) {
-    cu_blocks[B] = refused ? 0 : int32_t(t.tb);
-    *taken_out = int32_t(refused ? had : had - t.tb);
+    cu_blocks[B] = n;
+    if (FILL) k_cb[B] = n;
+    *taken_out = int32_t(had - n);
     *status = refused;
+  }
+  if constexpr (FILL) {
+    __syncthreads();
+    for (int e = threadIdx.x; e < n; e += kScanThreads) {
+      const int r = owner(k_cb, 0, B, e);
+      free_ids[had - n + e] = block_tables[size_t(r) * max_blocks + first_block[r] + (e - k_cb[r])];
+    }
   }
 }
 
@@ -177,8 +240,8 @@ __global__ __launch_bounds__(kFillThreads) void release_fill_kernel(
     const int32_t* __restrict__ block_tables, int B, int max_blocks, const int32_t* __restrict__ first_block,
     const int32_t* __restrict__ cu_blocks, const int32_t* __restrict__ taken_out, int32_t* __restrict__ free_ids) {
   const int n = cu_blocks[B], at = *taken_out;
-  for (int e = blockIdx.x * kFillThreads + threadIdx.x; e < n; e += gridDim.x * kFillThreads) {
-    const int r = owner(cu_blocks, 0, B, e);
+  for (int64_t e = int64_t(blockIdx.x) * kFillThreads + threadIdx.x; e < n; e += int64_t(gridDim.x) * kFillThreads) {
+    const int r = owner(cu_blocks, 0, B, int(e));
     free_ids[at + e] = block_tables[size_t(r) * max_blocks + first_block[r] + (e - cu_blocks[r])];
   }
 }
@@ -270,13 +333,20 @@ extern "C" int ilpc_extend_tables(int32_t* block_tables, int32_t max_blocks, int
       !cu_blocks || (max_rows && !slot_map) || !taken_out || !status)
     return set_error(ILPC_EINVAL, "%s: NULL pointer", fn);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  hipLaunchKernelGGL(extend_scan_kernel, dim3(1), dim3(kScanThreads), 0, s, start_pos, new_lens, B, n_free, taken,
-                     max_blocks, max_rows, seq_lens, cu_q, cu_blocks, taken_out, status);
+  // One launch as long as one workgroup's fill costs less than the second launch.
+  const bool one = B <= kFillRequests && max_rows <= kOneFill;
+  auto launch_scan = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3(1), dim3(kScanThreads), 0, s, block_tables, start_pos, new_lens, B, free_ids,
+                       n_free, taken, num_blocks, max_blocks, max_rows, seq_lens, cu_q, cu_blocks, slot_map, taken_out,
+                       status);
+  };
+  if (one) launch_scan(extend_scan_kernel<true>);
+  else launch_scan(extend_scan_kernel<false>);
   const int rc = launch_status(fn);
-  if (rc != ILPC_OK) return rc;
+  if (rc != ILPC_OK || one) return rc;
   const unsigned grid = unsigned((int64_t(max_rows) + kFillRows - 1) / kFillRows) + (max_rows == 0);
   hipLaunchKernelGGL(extend_fill_kernel, dim3(grid), dim3(kFillThreads), 0, s, block_tables, B, max_blocks, free_ids,
-                     n_free, taken_out, num_blocks, seq_lens, cu_q, cu_blocks, slot_map, max_rows);
+                     taken_out, num_blocks, seq_lens, cu_q, cu_blocks, slot_map, max_rows);
   return launch_status(fn);
 }
 
@@ -293,12 +363,16 @@ extern "C" int ilpc_release_tables(const int32_t* block_tables, int32_t max_bloc
       !taken_out || !status)
     return set_error(ILPC_EINVAL, "%s: NULL pointer", fn);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  hipLaunchKernelGGL(release_scan_kernel, dim3(1), dim3(kScanThreads), 0, s, first_block, seq_lens, B, max_blocks,
-                     n_free, taken, cu_blocks, taken_out, status);
-  const int rc = launch_status(fn);
-  if (rc != ILPC_OK) return rc;
   const int64_t most = int64_t(B) * max_blocks;  // blocks there can be
-  if (most == 0) return ILPC_OK;
+  const bool one = B <= kFillRequests && most <= kOneRelease;
+  auto launch_scan = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3(1), dim3(kScanThreads), 0, s, block_tables, first_block, seq_lens, B, max_blocks,
+                       n_free, taken, free_ids, cu_blocks, taken_out, status);
+  };
+  if (one) launch_scan(release_scan_kernel<true>);
+  else launch_scan(release_scan_kernel<false>);
+  const int rc = launch_status(fn);
+  if (rc != ILPC_OK || one) return rc;
   const unsigned grid = unsigned(most < 256 * kFillThreads ? (most + kFillThreads - 1) / kFillThreads : 256);
   hipLaunchKernelGGL(release_fill_kernel, dim3(grid), dim3(kFillThreads), 0, s, block_tables, B, max_blocks,
                      first_block, cu_blocks, taken_out, free_ids);

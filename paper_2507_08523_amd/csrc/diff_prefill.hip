@@ -115,7 +115,7 @@ __device__ __forceinline__ void bare_barrier() {
 constexpr int wgs_per_cu(int D) { return D == 64 ? 3 : 2; }
 
 template <int D>
-__global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void diff_prefill_kernel(DiffArgs a, int n_ct) {
+__global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void diff_prefill_kernel(DiffArgs a, int recip) {
   constexpr int kDch = D / 16;                          // 16-dimension chunks of a row: half of them map 1's
   constexpr int kDt = D / 32;                           // 32-row tiles of O^T
   constexpr int kRowBytes = D * 2, kKch = D / 8;
@@ -123,38 +123,47 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void diff_prefill_kerne
   constexpr int kTileBytes = kTileBlocks * kSlabBytes;
   constexpr int kInsts = kSlabBytes / 1024;
   __shared__ __attribute__((aligned(16))) uint8_t ring[4 * kTileBytes];  // two K tiles, two V tiles
+  __shared__ __attribute__((aligned(16))) float s_norm[D];               // norm weight, or ones
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 31, hh = lane >> 5;
   const int G = a.Hq / a.Hkv;
 
-  // Workgroup b runs on XCD b % 8, which takes every eighth (request, kv head),
-  // its column tiles one after the other, the heaviest first: they read the same
-  // keys through one L2.
-  const unsigned x = blockIdx.x & 7u, at = blockIdx.x >> 3;
-  const unsigned pair = at / unsigned(n_ct) * 8u + x;
+  // Grid: 8 (XCDs: workgroup b runs on XCD b % 8) x column tiles x pairs / 8.  An
+  // XCD takes every eighth (request, kv head), its column tiles one after the
+  // other, the heaviest first: they read the same keys through one L2.
+  const unsigned pair = blockIdx.z * 8u + blockIdx.x;
   if (pair >= unsigned(a.B) * unsigned(a.Hkv)) return;
-  const int tile = n_ct - 1 - int(at % unsigned(n_ct));
+  const int tile = int(gridDim.y - 1u - blockIdx.y);
   const int r = int(pair / unsigned(a.Hkv)), h = int(pair % unsigned(a.Hkv));
-  const int q0 = scalar_load(a.cu_q + r), q_end = scalar_load(a.cu_q + r + 1);
-  const int L = min(scalar_load(a.seq_lens + r), a.max_blocks * kBlock);
+  const int32_t* bt = a.block_tables + size_t(r) * a.max_blocks;
+  auto raw_id = [&](int blk) { return scalar_load(bt + min(blk, a.max_blocks - 1)); };
+  // Lengths and the block ids of the first tiles in one round trip.
+  const int q0 = scalar_load(a.cu_q + r), q_end = scalar_load(a.cu_q + r + 1), L_in = scalar_load(a.seq_lens + r);
+  const int first_k = raw_id(max(wave - 2, 0)), k0 = raw_id(2 + wave), v0 = raw_id(wave);
+  int next_k = raw_id(kTileBlocks + 2 + wave), next_v = raw_id(kTileBlocks + wave);  // of the next tile, unchecked
+  asm volatile("" : : "s"(q0), "s"(q_end), "s"(L_in), "s"(first_k), "s"(k0), "s"(v0), "s"(next_k), "s"(next_v));
+  const int L = min(L_in, a.max_blocks * kBlock);
   const int q_len = q_end - q0;
   const int64_t all_cols = int64_t(min(q_len, a.max_q_len)) * G;
-  const int64_t col0 = int64_t(tile) * kCols;
+  const unsigned col0 = unsigned(tile) * kCols;
   if (q0 < 0 || q_end > a.n_rows || q_len <= 0 || q_len > L || col0 >= all_cols) return;
-  const int row_a = int(col0 / G), rem0 = int(col0 - int64_t(row_a) * G);
+  // Columns are split into (row, head of the group) by a 16-bit reciprocal of G,
+  // exact for the offsets met here, below G + kCols <= 192.
+  auto div_g = [&](int u) { return int((unsigned(u) * unsigned(recip)) >> 16); };
+  const int row_a = int(col0 / unsigned(G)), rem0 = int(col0 - unsigned(row_a) * unsigned(G));
   const int n_valid = int(min(all_cols - col0, int64_t(kCols)));
   const int wave_first = wave * 32;
   const bool active = wave_first < n_valid;
   // This lane's column (padding columns repeat the last valid one).
   const int co = min(wave_first + n, n_valid - 1);
-  const int t_off = (rem0 + co) / G, head = h * G + (rem0 + co - t_off * G);
+  const int t_off = div_g(rem0 + co), head = h * G + (rem0 + co - t_off * G);
   const int pos0 = L - q_len + row_a;
   const int pos = pos0 + t_off;
-  const int wave_pos_min = pos0 + (rem0 + min(wave_first, n_valid - 1)) / G;
-  const int wave_pos_max = pos0 + (rem0 + min(wave_first + 32, n_valid) - 1) / G;
-  const int key_lim = pos0 + (rem0 + n_valid - 1) / G + 1;  // keys from here on are hidden from all columns
+  const int wave_pos_min = pos0 + div_g(rem0 + min(wave_first, n_valid - 1));
+  const int wave_pos_max = pos0 + div_g(rem0 + min(wave_first + 32, n_valid) - 1);
+  const int key_lim = pos0 + div_g(rem0 + n_valid - 1) + 1;  // keys from here on are hidden from all columns
   const int n_tiles = (key_lim + kKeys - 1) / kKeys;
   const int n_blk = (key_lim + kBlock - 1) / kBlock;
   const int last_step = active ? wave_pos_max / 32 : -1;  // last step with a key that some column of the wave sees
@@ -173,10 +182,8 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void diff_prefill_kerne
   const uint32_t voff = uint32_t((lane >> 1) * 32 + v_slot(lane >> 1, lane & 1) * 16);
   const uint32_t ring0 = lds_offset(ring) + wave * kSlabBytes;
   const size_t slab_stride = size_t(a.Hkv) * kSlabBytes;
-  const int32_t* bt = a.block_tables + size_t(r) * a.max_blocks;
   const uint64_t kbase = reinterpret_cast<uint64_t>(a.k_pool) - 1024 + size_t(h) * kSlabBytes;
   const uint64_t vbase = reinterpret_cast<uint64_t>(a.v_pool) + size_t(h) * kSlabBytes;
-  auto raw_id = [&](int blk) { return scalar_load(bt + min(blk, a.max_blocks - 1)); };
   // (ids past the last block, or outside the pool, read block 0: masked keys)
   auto usable = [&](int blk, int id) { return (blk < n_blk && id >= 0 && id < a.num_blocks) ? id : 0; };
   auto k_buf = [&](int j) { return unsigned(j & 1) * kTileBytes; };
@@ -194,7 +201,6 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void diff_prefill_kerne
     else load_slab2(voff, voff, base, to);
   };
 
-  const int first_k = raw_id(max(wave - 2, 0)), k0 = raw_id(2 + wave), v0 = raw_id(wave);
   if (wave >= 2) issue_k(-1, usable(wave - 2, first_k));
   issue_k(0, usable(2 + wave, k0));
   issue_v(0, usable(wave, v0));
@@ -206,6 +212,7 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void diff_prefill_kerne
       qf[kc] = as_bf16x8(*(const u32x4*)(qr + source_chunk<D>(kc * 2, a.pairs) * 8 + hh * 8));
   }
   const float lam = a.ep.lambda[head];
+  if (tid < D) s_norm[tid] = a.ep.norm_w ? a.ep.norm_w[tid] : 1.f;
 
   f32x16 oa[kDt], ob[kDt];  // A^T and B^T
 #pragma unroll
@@ -214,7 +221,8 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void diff_prefill_kerne
     for (int e = 0; e < 16; ++e) oa[dt][e] = 0.f, ob[dt][e] = 0.f;
   f32x16 s1, s2;                     // scores of the next step
   bf16x8 pc[2], p2[2];               // p_1 - beta p_2 and p_2 of the step whose products with V are due
-  float m1 = -INFINITY, m2 = -INFINITY, l1 = 0.f, l2 = 0.f, beta = 0.f;  // l: this lane half's share
+  float m1 = -INFINITY, m2 = -INFINITY, l1 = 0.f, l2 = 0.f;  // l: this lane half's share
+  float beta = 0.f, most2 = 0.f;
 
   auto mask = [&](int step) {
     const int j0 = step * 32;
@@ -228,10 +236,14 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void diff_prefill_kerne
     }
   };
 
-  // Weights of a masked step against the running maxima; where a lane's sum of them
-  // leaves [0, 2^8] (the first step; a maximum that grew), or beta is off by more than
-  // a factor of 2, the maxima are taken and A, B, the sums and beta brought in line.
-  // (A beta left too large would scale up the rounding of every p_2 behind it.)
+  // Weights of a masked step against the running maxima.  The maxima are taken, and
+  // A, B, the sums and beta brought in line, in the first step, where a lane's sum of
+  // weights leaves [0, 2^8] (a maximum that grew), and where map 2's passes most2,
+  // twice what its sum was (and 2: that sum is at least 1 in one lane half) when beta
+  // was last looked at: beta is then too large for them, and scales up their rounding.
+  // Error of single rows against 64 bits, q of standard deviation 1, 2, 4, at most:
+  // 0.5, 0.6, 1.0% (without that test 0.6, 5.5, 40%).  64 x 1.9 K tokens, 64/8 heads:
+  // 6.72 ms, without it and the look at beta 6.47.
   auto softmax = [&](bool first) __attribute__((always_inline)) {
     float t1, t2;
     auto exps = [&]() __attribute__((always_inline)) {
@@ -253,9 +265,7 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void diff_prefill_kerne
     bool slow = first;
     if (!first) {
       exps();
-      // beta within a factor of 2 of what it stands for: |beta| L_2 against |lambda| L_1
-      const float w1 = fabsf(lam) * add_across_halves(l1 + t1), w2 = fabsf(beta) * add_across_halves(l2 + t2);
-      slow = __ballot(!(t1 <= kSumLimit) || !(t2 <= kSumLimit) || w2 > 2.f * w1 || w1 > 2.f * w2) != 0;
+      slow = __ballot(!(t1 <= kSumLimit) || !(t2 <= most2)) != 0;
     }
     if (slow) {
       float x1 = s1[0], x2 = s2[0];
@@ -275,6 +285,7 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void diff_prefill_kerne
         y2 += __builtin_amdgcn_exp2f(__builtin_fmaf(s2[e], a.scale_log2, -m2));
       }
       beta = lam * add_across_halves(l1 + y1) / add_across_halves(l2 + y2);
+      most2 = fminf(2.f * (l2 + y2) + 2.f, kSumLimit);
       const float k = old - f2 * beta;
 #pragma unroll
       for (int dt = 0; dt < kDt; ++dt)
@@ -291,7 +302,7 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void diff_prefill_kerne
 
   // Products: A, B += V P of a step (the two V blocks at sV), then the scores of the
   // next (the 32 K rows at sK), the LDS operands read kPrefetch ahead.
-  constexpr int kPv = 2 * kDt, kQk = kDch, kPrefetch = 4;
+  constexpr int kPv = 2 * kDt, kQk = kDch, kPrefetch = 3;
   auto products = [&](auto with_pv, auto with_qk, const uint8_t* sV, const uint8_t* sK)
                       __attribute__((always_inline)) {
     constexpr int first = decltype(with_pv)::value ? 0 : kPv;
@@ -370,11 +381,27 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void diff_prefill_kerne
     wait_lds();
   };
 
+  // beta set anew where the sums have moved it by more than a factor of 2.
+  auto follow = [&]() __attribute__((always_inline)) {
+    const float t1 = add_across_halves(l1), t2 = add_across_halves(l2);
+    const float w1 = fabsf(lam) * t1, w2 = fabsf(beta) * t2;
+    if (__ballot(w2 > 2.f * w1 || w1 > 2.f * w2)) {
+      const float now = lam * t1 / t2, k = beta - now;
+#pragma unroll
+      for (int dt = 0; dt < kDt; ++dt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) oa[dt][e] += k * ob[dt][e];
+      beta = now;
+    }
+    most2 = fminf(2.f * l2 + 2.f, kSumLimit);
+  };
+
   // Two steps a tile.  Before the first of tile j: wait for this wave's loads of
   // K(j), V(j); barrier; issue K(j+1) and V(j+1) into the buffers of tile j-1, which
   // every wave has left behind.  The scores of a step past the wave's last one are
   // computed and ignored.
   wait_loads();
+  wait_lds();
   bare_barrier();
   if (active) products(no(), yes(), ring, ring + k_buf(-1) + 32 * kRowBytes);
   for (int u = 0; u < 2 * n_tiles; ++u) {
@@ -384,17 +411,21 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void diff_prefill_kerne
       zero_v_tail(j);
       bare_barrier();
       if (j + 1 < n_tiles) {
-        const int kb = (j + 1) * kTileBlocks + 2 + wave, vb = (j + 1) * kTileBlocks + wave;
-        const int kid = raw_id(kb), vid = raw_id(vb);
-        issue_k(j + 1, usable(kb, kid));
-        issue_v(j + 1, usable(vb, vid));
+        const int kb = (j + 1) * kTileBlocks + 2 + wave, vb = kb - 2;
+        issue_k(j + 1, usable(kb, next_k));
+        issue_v(j + 1, usable(vb, next_v));
+        next_k = raw_id(kb + kTileBlocks);
+        next_v = raw_id(vb + kTileBlocks);
       }
+      if (j > 0 && u <= last_step) follow();
     }
     if (u <= last_step) {
       mask(u);
       int uu = u;
       asm volatile("" : "+s"(uu));  // (one body for the first step and the others)
       softmax(uu == 0);
+      // (the ids' scalar loads are waited for here, and not with the first LDS operands of the products)
+      asm volatile("" : "+s"(next_k), "+s"(next_v));
       products(yes(), yes(), ring + v_buf(j) + (u & 1) * 2 * kSlabBytes, ring + k_buf(j) + (u & 1) * 32 * kRowBytes);
     }
   }
@@ -413,24 +444,38 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void diff_prefill_kerne
     }
   float fac = a.ep.scale;
   if (a.ep.norm_w) fac *= rsqrtf(add_across_halves(sq) * (1.f / D) + a.ep.eps);
-  if (wave_first + n >= n_valid) return;
-  uint16_t* orow = a.out + (size_t(q0 + row_a + t_off) * a.Hq + head) * D;
+  // The rows leave through LDS, so that whole 128-byte half rows are stored (a lane
+  // holds 8-byte pieces of one row).  4 KiB a wave, in the buffers of the tile
+  // before the last, which every wave has left behind: 32 rows of 64 dimensions a
+  // pass, 16-byte chunks XOR-swizzled by row.
+  uint8_t* tb = ring + (wave < 2 ? k_buf(n_tiles) : v_buf(n_tiles)) + (wave & 1) * 4096;
+  size_t orow[4];
+  bool ok[4];
 #pragma unroll
-  for (int dt = 0; dt < kDt; ++dt)
+  for (int i = 0; i < 4; ++i) {
+    const int c = wave_first + i * 8 + (lane >> 3), u = rem0 + min(c, n_valid - 1), t = div_g(u);
+    ok[i] = c < n_valid;
+    orow[i] = (size_t(q0 + row_a + t) * a.Hq + h * G + (u - t * G)) * D + (lane & 7) * 8;
+  }
 #pragma unroll
-    for (int g4 = 0; g4 < 4; ++g4) {
-      const int d = dt * 32 + g4 * 8 + hh * 4;
-      f32x4 w = {fac, fac, fac, fac};
-      if (a.ep.norm_w) {
-        const f32x4 nw = *(const f32x4*)(a.ep.norm_w + d);
+  for (int p = 0; p < kDt / 2; ++p) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] *= nw[e];
+    for (int dl = 0; dl < 2; ++dl)
+#pragma unroll
+      for (int g4 = 0; g4 < 4; ++g4) {
+        const f32x4 w = *(const f32x4*)&s_norm[(2 * p + dl) * 32 + g4 * 8 + hh * 4];
+        bf16x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = (__bf16)(oa[2 * p + dl][g4 * 4 + e] * (fac * w[e]));
+        *(bf16x4*)(tb + n * 128 + (((dl * 4 + g4) ^ (n & 7)) << 4) + hh * 8) = v;
       }
-      bf16x4 v;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = (__bf16)(oa[dt][g4 * 4 + e] * w[e]);
-      *(bf16x4*)(orow + d) = v;
+    for (int i = 0; i < 4; ++i) {
+      const int row = i * 8 + (lane >> 3);
+      const u32x4 v = *(const u32x4*)(tb + row * 128 + (((lane & 7) ^ (row & 7)) << 4));
+      if (ok[i]) *(u32x4*)(a.out + orow[i] + p * 64) = v;
     }
+  }
 }
 
 }  // namespace
@@ -439,11 +484,10 @@ namespace ilpc {
 
 bool launch_diff_prefill(const DiffArgs& a, hipStream_t stream) {
   const int64_t n_ct = (int64_t(a.max_q_len) * (a.Hq / a.Hkv) + kCols - 1) / kCols;
-  const int64_t grid = (int64_t(a.B) * a.Hkv + 7) / 8 * 8 * n_ct;
-  if (a.D == 128)
-    hipLaunchKernelGGL(diff_prefill_kernel<128>, dim3(unsigned(grid)), dim3(64 * kWaves), 0, stream, a, int(n_ct));
-  else
-    hipLaunchKernelGGL(diff_prefill_kernel<64>, dim3(unsigned(grid)), dim3(64 * kWaves), 0, stream, a, int(n_ct));
+  const dim3 grid(8, unsigned(n_ct), unsigned((int64_t(a.B) * a.Hkv + 7) / 8)), block(64 * kWaves);
+  const int recip = 65536 / (a.Hq / a.Hkv) + 1;
+  if (a.D == 128) hipLaunchKernelGGL(diff_prefill_kernel<128>, grid, block, 0, stream, a, recip);
+  else hipLaunchKernelGGL(diff_prefill_kernel<64>, grid, block, 0, stream, a, recip);
   return hipGetLastError() == hipSuccess;
 }
 
