@@ -63,11 +63,12 @@ __global__ __launch_bounds__(64 * group_waves(W), 2) void diff_stream_kernel(
     float scale_log2, int pairs_layout, DiffEpilogue ep, uint16_t* __restrict__ out, int n_ct, int n_split,
     float* __restrict__ part_o, float* __restrict__ part_ml) {
   constexpr int kDch = D / 16, kDt = D / 32, kWavesPerGroup = group_waves(W);
-  // Q^T of each wave in LDS; for the merge (W > 1) the same space holds every
-  // wave's O, a row of kRow floats a column.
+  // Q^T of each wave in LDS; for the join the same space holds every wave's O, a row
+  // of kRow floats a column.
   constexpr int kRow = D + 4, kCols = 2 * kTileCols;
   constexpr int kQBytes = kWavesPerGroup * kDch * 64 * 16, kOBytes = kWavesPerGroup * kCols * kRow * 4;
-  __shared__ __attribute__((aligned(16))) uint8_t lds[W > 1 && kOBytes > kQBytes ? kOBytes : kQBytes];
+  static_assert(kOBytes >= kQBytes, "the join's rows are the larger");
+  __shared__ __attribute__((aligned(16))) uint8_t lds[kOBytes];
   __shared__ float s_m[kWavesPerGroup][kCols], s_l[kWavesPerGroup][kCols];
   u32x4(*q_lds)[kDch][64] = reinterpret_cast<u32x4(*)[kDch][64]>(lds);
   const int lane = threadIdx.x & 63;
@@ -82,11 +83,10 @@ __global__ __launch_bounds__(64 * group_waves(W), 2) void diff_stream_kernel(
   const unsigned group = x * per + min(x, extra) + i;
   const int64_t item = int64_t(group) * (kWavesPerGroup / W) + wave / W;
   const int64_t n_items = int64_t(n_req) * Hkv * n_split * n_ct;
-  if (W == 1 && item >= n_items) return;
   const bool in_grid = item < n_items;
-  const int ct = in_grid ? int(item % n_ct) : 0;
-  const int64_t rest = in_grid ? item / n_ct : 0;
-  const int sp = int(rest % n_split), pair = int(rest / n_split);
+  // item = ((request * Hkv + kv head) * n_ct + column tile) * n_split + range of the keys
+  const int sp = in_grid ? int(item % n_split) : 0, unit = in_grid ? int(item / n_split) : 0;
+  const int ct = unit % n_ct, pair = unit / n_ct;
   const int r = pair / Hkv, h = pair % Hkv;
   const int G = Hq / Hkv;
 
@@ -94,7 +94,6 @@ __global__ __launch_bounds__(64 * group_waves(W), 2) void diff_stream_kernel(
   const int L = min(seq_lens[r], max_blocks * kBlock);
   const int col0 = ct * kTileCols, n_cols = min(min(q_len, max_q_len) * G - col0, kTileCols);
   const bool valid = in_grid && q0 >= 0 && q_end <= n_rows && q_len > 0 && q_len <= L && n_cols > 0;
-  if (W == 1 && !valid) return;
 
   f32x16 o[kDt];
 #pragma unroll
@@ -251,137 +250,82 @@ __global__ __launch_bounds__(64 * group_waves(W), 2) void diff_stream_kernel(
   }
 
   const float l_tot = add_across_halves(l_run);
-  if constexpr (W == 1) {
-    if (n_split > 1) {
-      // state of this (pair, split): [map][column of the tile], O unnormalised
-      if (col_valid) {
-        const size_t slot = (size_t(pair) * n_split + sp) * kCols + n;
-        float* po = part_o + slot * D;
-#pragma unroll
-        for (int dt = 0; dt < kDt; ++dt)
-#pragma unroll
-          for (int g4 = 0; g4 < 4; ++g4) {
-            const f32x4 v = {o[dt][g4 * 4], o[dt][g4 * 4 + 1], o[dt][g4 * 4 + 2], o[dt][g4 * 4 + 3]};
-            *(f32x4*)(po + dt * 32 + g4 * 8 + hh * 4) = v;
-          }
-        if (hh == 0) {
-          part_ml[slot * 2] = m_run;
-          part_ml[slot * 2 + 1] = l_tot;
-        }
-      }
-      return;
-    }
-    // y = O_1 / l_1 - lambda O_2 / l_2: the two maps of a column are 16 lanes apart
-    const float wgt = (map ? -ep.lambda[head] : 1.f) / l_tot;
-    float sq = 0.f;
+  // Join of the W ranges: every wave's O, max and sum to LDS (behind a barrier:
+  // no wave reads Q from there any more), then a thread sums 4 dimensions of a
+  // column over the waves, both maps, with weights 2^(m_k - M).
+  float(*so)[kCols][kRow] = reinterpret_cast<float(*)[kCols][kRow]>(lds);
+  __syncthreads();
+  if (col_valid) {
 #pragma unroll
     for (int dt = 0; dt < kDt; ++dt)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float a = o[dt][e] * wgt;
-        o[dt][e] = a + __shfl_xor(a, 16);
-        sq += o[dt][e] * o[dt][e];
-      }
-    float fac = ep.scale;
-    if (ep.norm_w) fac *= rsqrtf(add_across_halves(sq) * (1.f / D) + ep.eps);
-    if (nc >= n_cols) return;
-    uint16_t* orow = out + (size_t(q0 + t) * Hq + head) * D;
-#pragma unroll
-    for (int dt = 0; dt < kDt; ++dt) {
-      if (dt / (kDt / 2) != map) continue;  // (each of a column's lane pairs stores half of the row)
-#pragma unroll
       for (int g4 = 0; g4 < 4; ++g4) {
-        const int d = dt * 32 + g4 * 8 + hh * 4;
-        f32x4 w = {fac, fac, fac, fac};
-        if (ep.norm_w) {
-          const f32x4 nw = *(const f32x4*)(ep.norm_w + d);
+        const f32x4 v = {o[dt][g4 * 4], o[dt][g4 * 4 + 1], o[dt][g4 * 4 + 2], o[dt][g4 * 4 + 3]};
+        *(f32x4*)&so[wave][n][dt * 32 + g4 * 8 + hh * 4] = v;
+      }
+    if (hh == 0) {
+      s_m[wave][n] = m_run;
+      s_l[wave][n] = l_tot;
+    }
+  }
+  __syncthreads();
+  if (!valid) return;
+  const int w0 = wave / W * W;     // first wave of the pair
+  constexpr int kPer = D / 4;      // threads to a column
+  for (int u = (wave - w0) * 64 + lane; u < n_cols * kPer; u += W * 64) {
+    const int c = u / kPer, d = u % kPer * 4;
+    f32x4 acc[2];
+    float mx[2], den[2];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) w[e] *= nw[e];
+    for (int mp = 0; mp < 2; ++mp) {
+      const int vc = mp * kTileCols + c;
+      mx[mp] = s_m[w0][vc];
+#pragma unroll
+      for (int k = 1; k < W; ++k) mx[mp] = fmaxf(mx[mp], s_m[w0 + k][vc]);
+      acc[mp] = f32x4{0.f, 0.f, 0.f, 0.f};
+      den[mp] = 0.f;
+#pragma unroll
+      for (int k = 0; k < W; ++k) {
+        const float m = s_m[w0 + k][vc];
+        // (a range that saw no key of this column has weight 0)
+        const float wg = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mx[mp]);
+        den[mp] += wg * s_l[w0 + k][vc];
+        const f32x4 v = *(const f32x4*)&so[w0 + k][vc][d];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[mp][e] += wg * v[e];
+      }
+      if (n_split > 1) {
+        const size_t slot = (size_t(unit) * n_split + sp) * kCols + vc;
+        *(f32x4*)(part_o + slot * D + d) = acc[mp];
+        if (d == 0) {
+          part_ml[slot * 2] = mx[mp];
+          part_ml[slot * 2 + 1] = den[mp];
         }
-        bf16x4 v;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = (__bf16)(o[dt][g4 * 4 + e] * w[e]);
-        *(bf16x4*)(orow + d) = v;
       }
     }
-  } else {
-    // Join of the W ranges: every wave's O, max and sum to LDS (behind a barrier:
-    // no wave reads Q from there any more), then a thread sums 4 dimensions of a
-    // column over the waves, both maps, with weights 2^(m_k - M).
-    float(*so)[kCols][kRow] = reinterpret_cast<float(*)[kCols][kRow]>(lds);
-    __syncthreads();
-    if (col_valid) {
+    if (n_split > 1) continue;
+    const int tt = (col0 + c) / G, hd = h * G + (col0 + c - tt * G);
+    const float w1 = 1.f / den[0], w2 = ep.lambda[hd] / den[1];
+    f32x4 y;
+    float sq = 0.f;
 #pragma unroll
-      for (int dt = 0; dt < kDt; ++dt)
-#pragma unroll
-        for (int g4 = 0; g4 < 4; ++g4) {
-          const f32x4 v = {o[dt][g4 * 4], o[dt][g4 * 4 + 1], o[dt][g4 * 4 + 2], o[dt][g4 * 4 + 3]};
-          *(f32x4*)&so[wave][n][dt * 32 + g4 * 8 + hh * 4] = v;
-        }
-      if (hh == 0) {
-        s_m[wave][n] = m_run;
-        s_l[wave][n] = l_tot;
-      }
+    for (int e = 0; e < 4; ++e) {
+      y[e] = acc[0][e] * w1 - acc[1][e] * w2;
+      sq += y[e] * y[e];
     }
-    __syncthreads();
-    if (!valid) return;
-    const int w0 = wave / W * W;     // first wave of the pair
-    constexpr int kPer = D / 4;      // threads to a column
-    for (int u = (wave - w0) * 64 + lane; u < n_cols * kPer; u += W * 64) {
-      const int c = u / kPer, d = u % kPer * 4;
-      f32x4 acc[2];
-      float mx[2], den[2];
+    f32x4 f = {ep.scale, ep.scale, ep.scale, ep.scale};
+    if (ep.norm_w) {
 #pragma unroll
-      for (int mp = 0; mp < 2; ++mp) {
-        const int vc = mp * kTileCols + c;
-        mx[mp] = s_m[w0][vc];
+      for (int off = 1; off < kPer; off <<= 1) sq += __shfl_xor(sq, off);
+      const float inv = rsqrtf(sq * (1.f / D) + ep.eps);
+      const f32x4 nw = *(const f32x4*)(ep.norm_w + d);
 #pragma unroll
-        for (int k = 1; k < W; ++k) mx[mp] = fmaxf(mx[mp], s_m[w0 + k][vc]);
-        acc[mp] = f32x4{0.f, 0.f, 0.f, 0.f};
-        den[mp] = 0.f;
-#pragma unroll
-        for (int k = 0; k < W; ++k) {
-          const float m = s_m[w0 + k][vc];
-          // (a range that saw no key of this column has weight 0)
-          const float wg = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mx[mp]);
-          den[mp] += wg * s_l[w0 + k][vc];
-          const f32x4 v = *(const f32x4*)&so[w0 + k][vc][d];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) acc[mp][e] += wg * v[e];
-        }
-        if (n_split > 1) {
-          const size_t slot = (size_t(pair) * n_split + sp) * kCols + vc;
-          *(f32x4*)(part_o + slot * D + d) = acc[mp];
-          if (d == 0) {
-            part_ml[slot * 2] = mx[mp];
-            part_ml[slot * 2 + 1] = den[mp];
-          }
-        }
-      }
-      if (n_split > 1) continue;
-      const int tt = (col0 + c) / G, hd = h * G + (col0 + c - tt * G);
-      const float w1 = 1.f / den[0], w2 = ep.lambda[hd] / den[1];
-      f32x4 y;
-      float sq = 0.f;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        y[e] = acc[0][e] * w1 - acc[1][e] * w2;
-        sq += y[e] * y[e];
-      }
-      f32x4 f = {ep.scale, ep.scale, ep.scale, ep.scale};
-      if (ep.norm_w) {
-#pragma unroll
-        for (int off = 1; off < kPer; off <<= 1) sq += __shfl_xor(sq, off);
-        const float inv = rsqrtf(sq * (1.f / D) + ep.eps);
-        const f32x4 nw = *(const f32x4*)(ep.norm_w + d);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) f[e] *= inv * nw[e];
-      }
-      bf16x4 v;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = (__bf16)(y[e] * f[e]);
-      *(bf16x4*)(out + (size_t(q0 + tt) * Hq + hd) * D + d) = v;
+      for (int e = 0; e < 4; ++e) f[e] *= inv * nw[e];
     }
+    bf16x4 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = (__bf16)(y[e] * f[e]);
+    *(bf16x4*)(out + (size_t(q0 + tt) * Hq + hd) * D + d) = v;
   }
 }
 
@@ -395,26 +339,27 @@ template <int D>
 __global__ __launch_bounds__(64 * kJoinWaves) void diff_join_kernel(
     const float* __restrict__ part_o, const float* __restrict__ part_ml, const int32_t* __restrict__ cu_q,
     const int32_t* __restrict__ seq_lens, int n_rows, int max_blocks, int n_req, int max_q_len, int Hq, int Hkv,
-    int n_split, int cols_cap, DiffEpilogue ep, uint16_t* __restrict__ out) {
+    int n_ct, int n_split, DiffEpilogue ep, uint16_t* __restrict__ out) {
   constexpr int kPer = D / 64;  // dimensions of a lane
   typedef float vec_t __attribute__((ext_vector_type(kPer)));
   const int lane = threadIdx.x & 63;
   const int64_t w = int64_t(blockIdx.x) * kJoinWaves + (threadIdx.x >> 6);
-  const int c = int(w % cols_cap);
-  const int pair = int(w / cols_cap);
+  const int c = int(w % kTileCols);
+  const int64_t unit = w / kTileCols;
+  const int ct = int(unit % n_ct), pair = int(unit / n_ct);
   if (pair >= n_req * Hkv) return;
   const int r = pair / Hkv, h = pair % Hkv;
   const int G = Hq / Hkv;
   const int q0 = cu_q[r], q_end = cu_q[r + 1], q_len = q_end - q0;
   const int L = min(seq_lens[r], max_blocks * kBlock);
-  const int n_cols = min(q_len, max_q_len) * G;
-  if (q0 < 0 || q_end > n_rows || q_len <= 0 || q_len > L || c >= n_cols) return;
-  const int t = c / G, head = h * G + (c - t * G);
+  const int n_cols = min(q_len, max_q_len) * G, col = ct * kTileCols + c;
+  if (q0 < 0 || q_end > n_rows || q_len <= 0 || q_len > L || col >= n_cols) return;
+  const int t = col / G, head = h * G + (col - t * G);
 
   vec_t y = {};
 #pragma unroll
   for (int mp = 0; mp < 2; ++mp) {
-    const size_t slot0 = size_t(pair) * n_split * (2 * kTileCols) + mp * kTileCols + c;
+    const size_t slot0 = size_t(unit) * n_split * (2 * kTileCols) + mp * kTileCols + c;
     constexpr size_t kNext = 2 * kTileCols;  // slots from one split to the next
     float m = -INFINITY, l = 0.f;
     if (lane < n_split) {
@@ -462,18 +407,32 @@ int64_t column_tiles(int64_t max_q_len, int Hq, int Hkv) {
   return (max_q_len * (Hq / Hkv) + kTileCols - 1) / kTileCols;
 }
 
-// Enough waves to give every SIMD of the device one; of a workgroup first (their
-// join is in LDS), then of several, while each wave keeps at least 4 steps.
-Plan stream_plan(int64_t items, int64_t n_ct, int64_t max_blocks) {
+// How a launch cuts its units (column tiles of the (request, kv head) pairs).  What a
+// launch waits for is the compute unit with most to do, and a wave's steps follow each
+// other at about 1 us: four waves to a unit, and several workgroups (whose states a
+// second launch joins, 3 to 4 us), while every workgroup has a CU to itself; else two;
+// and four again, quarters of the load, where twos leave some CUs twice the work of
+// others.  One wave to a unit is never better than two.  8 kv heads, D 128, us:
+//   units, keys       waves x workgroups
+//   8, 1000           4x1 13.8, 4x4 12.0     8, 4000     4x4 18.7, 4x12 15.0
+//   32, 600           4x1 11.0, 4x2 14.0     32, 2100    4x1 27, 4x6 17.1, 4x8 18.2
+//   64, 2100          4x1 26, 4x3 21.7       128, 2100   4x1 26.5, 4x2 29.7
+//   128, 8000         4x1 104, 4x2 94.9      264, 1000   2x1 26.0, 4x1 31.8
+//   576, 1000         1x1 53.6, 2x1 60.3, 4x1 51.2; of 300 21.9, 23.5, 22.4
+//   1024, 1000        2x1 90.0, 4x1 90.8 (60% of the keys shared by all 46.7, 48.5)
+//   1248, 1000        2x1 114, 4x1 107       4096, 2100  1x1 698, 2x1 683, 4x1 683
+// D 64, whose steps and join are shorter: 512 of 2100 2x1 41.8, 4x1 42.2 (shared 32.7,
+// 27.7); 1024 of 1000 40.8, 41.0 (25.9, 30.1); 128 of 2100 4x1 19.7, 8x1 17.3; 16 of
+// 1000 4x1 10.3, 4x4 12.2, of 2100 4x6 13.6.
+Plan stream_plan(int64_t units, int64_t max_blocks, int D) {
   const int64_t cus = ilpc::device_cus(), steps = (max_blocks * kBlock + kStepKeys - 1) / kStepKeys;
-  int w = 1;
-  while (w < 4 && items * w < 4 * cus && w * 2 <= steps) w *= 2;
-  int64_t n = 1;
-  if (w == 4 && n_ct == 1) {
-    n = std::min<int64_t>({cus / items, steps / (4 * w), kMaxGroups});
-    n = std::max<int64_t>(n, 1);
-  }
-  return {w, int(n)};
+  const bool four = units <= cus || (D == 64 && units <= 3 * cus) ||
+                    (steps >= 32 && ((units > 2 * cus && units <= 3 * cus) || (units > 4 * cus && units <= 5 * cus)));
+  if (!four) return {2, 1};
+  const int64_t room = std::min<int64_t>(cus / units, kMaxGroups);
+  if (room >= 3 && steps >= (D == 64 ? 48 : 32)) return {4, int(std::min(room, steps / 8))};
+  if (room == 2 && steps > 128) return {4, 2};
+  return {D == 64 && units <= cus && steps >= 32 ? 8 : 4, 1};
 }
 
 // Whether the kernel for many columns takes a batch.
@@ -481,8 +440,8 @@ bool many_columns(int64_t B, int64_t max_q_len, int Hq, int Hkv, int64_t max_blo
   return max_q_len * (Hq / Hkv) > 32;
 }
 
-size_t part_bytes(int64_t pairs, int D, int n) {
-  return n > 1 ? size_t(pairs) * n * (2 * kTileCols) * (D + 2) * sizeof(float) : 0;
+size_t part_bytes(int64_t units, int D, int n) {
+  return n > 1 ? size_t(units) * n * (2 * kTileCols) * (D + 2) * sizeof(float) : 0;
 }
 
 int check_sizes(const char* fn, int32_t B, int32_t max_q_len, int32_t Hq, int32_t Hkv, int32_t D, int32_t max_blocks) {
@@ -510,8 +469,8 @@ extern "C" int ilpc_diff_attn_workspace_bytes(int32_t B, int32_t max_q_len, int3
   if (B == 0 || max_q_len == 0) return ILPC_OK;
   if (ilpc::device_cus() <= 0) return ilpc::set_error(ILPC_EHIP, "%s: cannot query the device", fn);
   if (many_columns(B, max_q_len, Hq, Hkv, max_blocks)) return ILPC_OK;
-  const int64_t n_ct = column_tiles(max_q_len, Hq, Hkv), pairs = int64_t(B) * Hkv;
-  *bytes = part_bytes(pairs, D, stream_plan(pairs * n_ct, n_ct, max_blocks).groups);
+  const int64_t units = int64_t(B) * Hkv * column_tiles(max_q_len, Hq, Hkv);
+  *bytes = part_bytes(units, D, stream_plan(units, max_blocks, D).groups);
   return ILPC_OK;
 }
 
@@ -552,15 +511,15 @@ extern "C" int ilpc_paged_diff_attn(const uint16_t* q, int64_t q_stride, int32_t
       return set_error(ILPC_EHIP, "%s: launch failed", fn);
     return ILPC_OK;
   }
-  const int64_t n_ct = column_tiles(max_q_len, Hq, Hkv), pairs = int64_t(B) * Hkv;
-  Plan plan = stream_plan(pairs * n_ct, n_ct, max_blocks);
-  const size_t need = part_bytes(pairs, D, plan.groups);
+  const int64_t n_ct = column_tiles(max_q_len, Hq, Hkv), units = int64_t(B) * Hkv * n_ct;
+  const Plan plan = stream_plan(units, max_blocks, D);
+  const size_t need = part_bytes(units, D, plan.groups);
   if (need && (!workspace || workspace_bytes < need || !aligned16(workspace)))
     return set_error(ILPC_EINVAL, "%s: workspace must be %zu bytes, 16-byte aligned", fn, need);
   const DiffEpilogue ep{lambda, norm_weight, norm_eps, out_scale};
   float* part_o = need ? static_cast<float*>(workspace) : nullptr;
-  float* part_ml = need ? part_o + size_t(pairs) * plan.groups * (2 * kTileCols) * D : nullptr;
-  const int64_t items = pairs * n_ct * plan.groups, per_group = group_waves(plan.waves) / plan.waves;
+  float* part_ml = need ? part_o + size_t(units) * plan.groups * (2 * kTileCols) * D : nullptr;
+  const int64_t items = units * plan.groups, per_group = group_waves(plan.waves) / plan.waves;
   const dim3 grid{unsigned((items + per_group - 1) / per_group)}, block{unsigned(64 * group_waves(plan.waves))};
   hipStream_t s = static_cast<hipStream_t>(stream);
   auto launch = [&](auto kernel) {
@@ -569,21 +528,19 @@ extern "C" int ilpc_paged_diff_attn(const uint16_t* q, int64_t q_stride, int32_t
                        int(layout == ILPC_DIFF_ROPE), ep, out, int(n_ct), plan.groups, part_o, part_ml);
   };
   if (D == 128) {
-    if (plan.waves == 1) launch(diff_stream_kernel<128, 1>);
-    else if (plan.waves == 2) launch(diff_stream_kernel<128, 2>);
+    if (plan.waves == 2) launch(diff_stream_kernel<128, 2>);
     else launch(diff_stream_kernel<128, 4>);
   } else {
-    if (plan.waves == 1) launch(diff_stream_kernel<64, 1>);
-    else if (plan.waves == 2) launch(diff_stream_kernel<64, 2>);
-    else launch(diff_stream_kernel<64, 4>);
+    if (plan.waves == 2) launch(diff_stream_kernel<64, 2>);
+    else if (plan.waves == 4) launch(diff_stream_kernel<64, 4>);
+    else launch(diff_stream_kernel<64, 8>);
   }
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && plan.groups > 1) {
-    const int cols_cap = int(std::min<int64_t>(int64_t(max_q_len) * (Hq / Hkv), kTileCols));
-    const dim3 jgrid{unsigned((pairs * cols_cap + kJoinWaves - 1) / kJoinWaves)}, jblock{64 * kJoinWaves};
+    const dim3 jgrid{unsigned((units * kTileCols + kJoinWaves - 1) / kJoinWaves)}, jblock{64 * kJoinWaves};
     auto join = [&](auto kernel) {
-      hipLaunchKernelGGL(kernel, jgrid, jblock, 0, s, part_o, part_ml, cu_q, seq_lens, n_rows, max_blocks, B, max_q_len, Hq,
-                         Hkv, plan.groups, cols_cap, ep, out);
+      hipLaunchKernelGGL(kernel, jgrid, jblock, 0, s, part_o, part_ml, cu_q, seq_lens, n_rows, max_blocks, B, max_q_len,
+                         Hq, Hkv, int(n_ct), plan.groups, ep, out);
     };
     if (D == 128) join(diff_join_kernel<128>);
     else join(diff_join_kernel<64>);
