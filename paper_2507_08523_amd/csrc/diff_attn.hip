@@ -435,9 +435,14 @@ Plan stream_plan(int64_t units, int64_t max_blocks, int D) {
   return {D == 64 && units <= cus && steps >= 32 ? 8 : 4, 1};
 }
 
-// Whether the kernel for many columns takes a batch.
-bool many_columns(int64_t B, int64_t max_q_len, int Hq, int Hkv, int64_t max_blocks) {
-  return max_q_len * (Hq / Hkv) > 32;
+// Whether the kernel for many columns takes a batch: of more than one column tile a
+// pair, where there are more than two units to a CU (at D = 64, with its shorter steps,
+// four).  us here, there: D 128, contexts of 2100 keys, 256 units 28, 65; 384 46, 66;
+// 528 67, 68; 640 69, 68; 1056 103, 68; 2176 206, 88; of 100 keys, 320 11, 11; 576 14,
+// 12.  D 64, 2100 keys, 640 40, 55; 1056 59, 54; 2080 106, 69.
+bool many_columns(int64_t B, int64_t max_q_len, int Hq, int Hkv, int D) {
+  const int64_t n_ct = column_tiles(max_q_len, Hq, Hkv);
+  return n_ct > 1 && B * Hkv * n_ct > (D == 64 ? 4 : 2) * int64_t(ilpc::device_cus());
 }
 
 size_t part_bytes(int64_t units, int D, int n) {
@@ -468,7 +473,7 @@ extern "C" int ilpc_diff_attn_workspace_bytes(int32_t B, int32_t max_q_len, int3
   *bytes = 0;
   if (B == 0 || max_q_len == 0) return ILPC_OK;
   if (ilpc::device_cus() <= 0) return ilpc::set_error(ILPC_EHIP, "%s: cannot query the device", fn);
-  if (many_columns(B, max_q_len, Hq, Hkv, max_blocks)) return ILPC_OK;
+  if (many_columns(B, max_q_len, Hq, Hkv, D)) return ILPC_OK;
   const int64_t units = int64_t(B) * Hkv * column_tiles(max_q_len, Hq, Hkv);
   *bytes = part_bytes(units, D, stream_plan(units, max_blocks, D).groups);
   return ILPC_OK;
@@ -501,7 +506,7 @@ extern "C" int ilpc_paged_diff_attn(const uint16_t* q, int64_t q_stride, int32_t
   if (q_stride < int64_t(Hq) * D || q_stride % 8 != 0)
     return set_error(ILPC_EINVAL, "%s: q_stride must be a multiple of 8 elements, at least Hq * D", fn);
   if (ilpc::device_cus() <= 0) return set_error(ILPC_EHIP, "%s: cannot query the device", fn);
-  if (many_columns(B, max_q_len, Hq, Hkv, max_blocks)) {
+  if (many_columns(B, max_q_len, Hq, Hkv, D)) {
     if (int64_t(max_q_len) * (Hq / Hkv) > (int64_t(1) << 22) || int64_t(B) * Hkv > (1 << 18))
       return set_error(ILPC_EUNSUP, "%s: batch too large", fn);
     const DiffArgs a{q, q_stride, n_rows, k_pool, v_pool, num_blocks, block_tables, max_blocks, cu_q, seq_lens, B,
