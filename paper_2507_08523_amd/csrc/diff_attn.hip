@@ -507,7 +507,9 @@ extern "C" int ilpc_paged_diff_attn(const uint16_t* q, int64_t q_stride, int32_t
     return set_error(ILPC_EINVAL, "%s: q_stride must be a multiple of 8 elements, at least Hq * D", fn);
   if (ilpc::device_cus() <= 0) return set_error(ILPC_EHIP, "%s: cannot query the device", fn);
   if (many_columns(B, max_q_len, Hq, Hkv, D)) {
-    if (int64_t(max_q_len) * (Hq / Hkv) > (int64_t(1) << 22) || int64_t(B) * Hkv > (1 << 18))
+    // (grid limits: 65535 column tiles a request, rows / 16 numbers, and pairs / 8)
+    if (int64_t(max_q_len) * (Hq / Hkv) > (int64_t(1) << 22) || int64_t(B) * Hkv > (1 << 18) ||
+        int64_t(n_rows) * (Hq / Hkv) / 128 + B > (1 << 18))
       return set_error(ILPC_EUNSUP, "%s: batch too large", fn);
     const DiffArgs a{q, q_stride, n_rows, k_pool, v_pool, num_blocks, block_tables, max_blocks, cu_q, seq_lens, B,
                      max_q_len, Hq, Hkv, D, softmax_scale * 1.4426950408889634f, int(layout == ILPC_DIFF_ROPE),

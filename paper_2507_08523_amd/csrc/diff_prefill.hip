@@ -112,10 +112,12 @@ __device__ __forceinline__ void bare_barrier() {
   asm volatile("" ::: "memory");
 }
 
+enum { kByPair, kByRows };  // how workgroups find their column tile
+
 constexpr int wgs_per_cu(int D) { return D == 64 ? 3 : 2; }
 
 template <int D>
-__global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void diff_prefill_kernel(DiffArgs a, int recip) {
+__global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void diff_prefill_kernel(DiffArgs a, int recip, int numbering) {
   constexpr int kDch = D / 16;                          // 16-dimension chunks of a row: half of them map 1's
   constexpr int kDt = D / 32;                           // 32-row tiles of O^T
   constexpr int kRowBytes = D * 2, kKch = D / 8;
@@ -130,13 +132,37 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void diff_prefill_kerne
   const int n = lane & 31, hh = lane >> 5;
   const int G = a.Hq / a.Hkv;
 
-  // Grid: 8 (XCDs: workgroup b runs on XCD b % 8) x column tiles x pairs / 8.  An
-  // XCD takes every eighth (request, kv head), its column tiles one after the
-  // other, the heaviest first: they read the same keys through one L2.
-  const unsigned pair = blockIdx.z * 8u + blockIdx.x;
-  if (pair >= unsigned(a.B) * unsigned(a.Hkv)) return;
-  const int tile = int(gridDim.y - 1u - blockIdx.y);
-  const int r = int(pair / unsigned(a.Hkv)), h = int(pair % unsigned(a.Hkv));
+  int r, h, place;  // request, kv head, which of the request's column tiles (the heaviest first)
+  if (numbering == kByPair) {
+    // Grid: 8 (XCDs: workgroup b runs on XCD b % 8) x column tiles x pairs / 8.  An XCD
+    // takes every eighth (request, kv head), its column tiles one after the other: they
+    // read the same keys through one L2.
+    const unsigned pair = blockIdx.z * 8u + blockIdx.x;
+    if (pair >= unsigned(a.B) * unsigned(a.Hkv)) return;
+    r = int(pair / unsigned(a.Hkv)), h = int(pair % unsigned(a.Hkv));
+    place = int(blockIdx.y);
+  } else {
+    // Grid: 8 x numbers / 8 x kv heads.  Request r has the numbers from (columns before
+    // it) / 128 + r on, which is room for its tiles whatever the lengths; found eight
+    // probes a round trip.
+    const unsigned e = blockIdx.y * 8u + blockIdx.x;
+    auto first = [&](int i) { return unsigned(uint64_t(unsigned(max(scalar_load(a.cu_q + i), 0))) * unsigned(G) / kCols) + unsigned(i); };
+    int lo = 0, hi = a.B;  // first(lo) <= e < first(hi)
+    unsigned base = 0;
+    while (hi - lo > 1) {
+      const int st = (hi - lo + 7) >> 3;
+      unsigned f[7];
+#pragma unroll
+      for (int k = 0; k < 7; ++k) f[k] = first(min(lo + st * (k + 1), a.B));
+      int next = lo;
+#pragma unroll
+      for (int k = 0; k < 7; ++k)
+        if (lo + st * (k + 1) < hi && f[k] <= e) next = lo + st * (k + 1), base = f[k];
+      hi = min(next + st, hi);
+      lo = next;
+    }
+    r = lo, h = int(blockIdx.z), place = int(e - base);
+  }
   const int32_t* bt = a.block_tables + size_t(r) * a.max_blocks;
   auto raw_id = [&](int blk) { return scalar_load(bt + min(blk, a.max_blocks - 1)); };
   // Lengths and the block ids of the first tiles in one round trip.
@@ -147,8 +173,9 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void diff_prefill_kerne
   const int L = min(L_in, a.max_blocks * kBlock);
   const int q_len = q_end - q0;
   const int64_t all_cols = int64_t(min(q_len, a.max_q_len)) * G;
+  const int tile = int((all_cols + kCols - 1) / kCols) - 1 - place;
+  if (q0 < 0 || q_end > a.n_rows || q_len <= 0 || q_len > L || tile < 0) return;
   const unsigned col0 = unsigned(tile) * kCols;
-  if (q0 < 0 || q_end > a.n_rows || q_len <= 0 || q_len > L || col0 >= all_cols) return;
   // Columns are split into (row, head of the group) by a 16-bit reciprocal of G,
   // exact for the offsets met here, below G + kCols <= 192.
   auto div_g = [&](int u) { return int((unsigned(u) * unsigned(recip)) >> 16); };
@@ -483,11 +510,16 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void diff_prefill_kerne
 namespace ilpc {
 
 bool launch_diff_prefill(const DiffArgs& a, hipStream_t stream) {
-  const int64_t n_ct = (int64_t(a.max_q_len) * (a.Hq / a.Hkv) + kCols - 1) / kCols;
-  const dim3 grid(8, unsigned(n_ct), unsigned((int64_t(a.B) * a.Hkv + 7) / 8)), block(64 * kWaves);
-  const int recip = 65536 / (a.Hq / a.Hkv) + 1;
-  if (a.D == 128) hipLaunchKernelGGL(diff_prefill_kernel<128>, grid, block, 0, stream, a, recip);
-  else hipLaunchKernelGGL(diff_prefill_kernel<64>, grid, block, 0, stream, a, recip);
+  // By pair where that fills all XCDs evenly and most numbers hold rows (the host knows
+  // the longest request and the sum of all); else by rows.
+  const int64_t G = a.Hq / a.Hkv, n_ct = (a.max_q_len * G + kCols - 1) / kCols, pairs = int64_t(a.B) * a.Hkv;
+  const int64_t numbers = a.n_rows * G / kCols + a.B;
+  const bool by_pair = (pairs % 8 == 0 || pairs >= 64) && 2 * a.B * n_ct <= 3 * numbers;
+  const dim3 grid(8, unsigned(by_pair ? n_ct : (numbers + 7) / 8), unsigned(by_pair ? (pairs + 7) / 8 : a.Hkv));
+  const dim3 block(64 * kWaves);
+  const int recip = 65536 / int(G) + 1, numbering = by_pair ? kByPair : kByRows;
+  if (a.D == 128) hipLaunchKernelGGL(diff_prefill_kernel<128>, grid, block, 0, stream, a, recip, numbering);
+  else hipLaunchKernelGGL(diff_prefill_kernel<64>, grid, block, 0, stream, a, recip, numbering);
   return hipGetLastError() == hipSuccess;
 }
 

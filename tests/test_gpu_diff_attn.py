@@ -118,6 +118,16 @@ class Batch:
         return rel
 
 
+def wide(lens, new, Hq, Hkv, D=128):
+    """The same requests again and again, until the kernel for many columns takes the batch: more than
+    4 column tiles of 16 a pair to a compute unit (and more than one tile a pair)."""
+    cus = torch.cuda.get_device_properties(0).multi_processor_count
+    tiles = -(-max(new) * (Hq // Hkv) // 16)
+    assert tiles > 1
+    k = -(-(4 * cus + 1) // (len(lens) * Hkv * tiles))
+    return dict(lens=list(lens) * k, new=list(new) * k, Hq=Hq, Hkv=Hkv, D=D)
+
+
 HEADS = [(1, 1, 64), (4, 1, 64), (6, 2, 64), (8, 8, 128), (4, 2, 128), (7, 1, 128), (16, 2, 128), (20, 1, 64),
          (64, 1, 128)]
 
@@ -137,13 +147,45 @@ def test_prefill_shapes(heads):
     b.check(b.run())
 
 
+@pytest.mark.parametrize("heads", HEADS)
+def test_many_columns_shapes(heads):
+    Hq, Hkv, D = heads
+    b = Batch(**wide([1, 40, 100, 129, 60, 64], [1, 40, 36, 33, 17, 0], Hq, Hkv, D), seed=Hq)
+    b.check(b.run())
+
+
+@pytest.mark.parametrize("S", [17, 31, 32, 33, 64, 65, 127, 128, 129, 200, 257])
+@pytest.mark.parametrize("D", [64, 128])
+def test_many_columns_row_counts(S, D):
+    b = Batch(**wide([S + 48, S, S + 200], [S, S, S], 8, 4, D), seed=S)
+    b.check(b.run())
+
+
+@pytest.mark.parametrize("L", [40, 63, 64, 65, 96, 127, 128, 129, 191, 193, 1500])
+def test_many_columns_context_lengths(L):
+    b = Batch(**wide([L], [40], 16, 2), spare_cols=5, seed=L)
+    b.check(b.run())
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(32, 8), (28, 4), (3, 3), (16, 1)])
+def test_one_long_request_among_short_ones(Hq, Hkv):
+    # few of the numbers that the longest request would give every one hold rows
+    rng = np.random.default_rng(Hq)
+    lens = [int(x) for x in rng.integers(1, 60, 90)]
+    new = [int(rng.integers(0, min(x, 3) + 1)) for x in lens]
+    lens[50], new[50] = 700, 600
+    b = Batch(**wide(lens, new, Hq, Hkv), seed=Hq)
+    b.check(b.run())
+
+
 @pytest.mark.parametrize("layout", ["halves", "rope"])
 @pytest.mark.parametrize("norm", [False, True])
 @pytest.mark.parametrize("fused", [False, True])
 @pytest.mark.parametrize("D", [64, 128])
 def test_layouts_norm_and_row_strides(layout, norm, fused, D):
-    for lens, new in (([50, 7], [1, 2]), ([150, 77], [90, 65])):
-        b = Batch(lens, new, 4, 2, D, norm=norm, layout=layout, fused=fused, seed=D)
+    for kw in (dict(lens=[50, 7], new=[1, 2], Hq=4, Hkv=2, D=D), dict(lens=[150, 77], new=[90, 65], Hq=4, Hkv=2, D=D),
+               wide([150, 77], [90, 65], 16, 2, D)):
+        b = Batch(**kw, norm=norm, layout=layout, fused=fused, seed=D)
         b.check(b.run())
 
 
@@ -165,6 +207,7 @@ def test_context_lengths(L, new):
 
 @pytest.mark.parametrize("B", [1, 2, 5, 33, 70, 140, 300])
 def test_batch_sizes(B):
+    # (columns up to 40 rows: both kernels)
     # the plan of waves and workgroups to a request changes with their number
     rng = np.random.default_rng(B)
     lens = [int(x) for x in rng.integers(1, 700, B)]
@@ -176,51 +219,85 @@ def test_batch_sizes(B):
     b.check(b.run())
 
 
-@pytest.mark.parametrize("std", [128 ** -0.5, 0.3, 4.0, 30.0])
-@pytest.mark.parametrize("new", [1, 140])
+def sizes(new):
+    """The two kernels: few columns, and (new = 0) many."""
+    return wide([300, 700], [140, 33], 8, 2) if new == 0 else dict(lens=[300, 700], new=[new, new], Hq=4, Hkv=2, D=128)
+
+
+@pytest.mark.parametrize("std", [128 ** -0.5, 0.3, 2.0, 4.0, 30.0])
+@pytest.mark.parametrize("new", [1, 140, 0])
 def test_flat_and_peaked_maps(std, new):
-    b = Batch([300, 1200], [new, new], 4, 2, 128, std=std, seed=3)
+    b = Batch(**sizes(new), std=std, seed=3)
     b.check(b.run())
 
 
 @pytest.mark.parametrize("near", [0.02, 0.2])
-@pytest.mark.parametrize("new", [1, 140])
+@pytest.mark.parametrize("new", [1, 140, 0])
 def test_maps_that_nearly_cancel(near, new):
     # the case the method is made for: the output is a small difference
-    b = Batch([300, 700], [new, new], 4, 2, 128, near=near, lam=0.95, seed=4)
+    b = Batch(**sizes(new), near=near, lam=0.95, seed=4)
     b.check(b.run())
 
 
-@pytest.mark.parametrize("new", [1, 140])
+@pytest.mark.parametrize("new", [1, 140, 0])
 def test_equal_maps_leave_nothing(new):
-    b = Batch([300], [new], 4, 2, 128, near=0.0, lam=1.0, seed=5, norm=False)
+    b = Batch(**sizes(new), near=0.0, lam=1.0, seed=5, norm=False)
     b.check(b.run(), norm=None)  # (the reference is 0: the bound by element alone)
 
 
 @pytest.mark.parametrize("lam", [0.0, -0.5, 1.5])
-@pytest.mark.parametrize("new", [1, 70])
+@pytest.mark.parametrize("new", [1, 70, 0])
 def test_lambda_values(lam, new):
-    b = Batch([100, 260], [new, new], 4, 2, 64, lam=lam, seed=6)
+    b = Batch(**sizes(new), lam=lam, seed=6)
     b.check(b.run())
 
 
-@pytest.mark.parametrize("new", [1, 130])
-def test_a_key_that_takes_all_late_and_early(new):
-    # maxima that grow by hundreds at one key: first, in the middle, last before the queries
-    for at in (0, 77, 200 - new):
-        b = Batch([200], [new], 2, 1, 128, seed=7)
-        b.kd[0][at, :, :64] *= 20
-        j = b.bt[0, at // 16]
-        b.kp[j, :, at % 16] = b.kd[0][at].cuda()
-        b.check(b.run(), norm=None if at else NORM)
+@pytest.mark.parametrize("half", [0, 64])
+@pytest.mark.parametrize("new", [1, 130, 0])
+def test_a_key_that_takes_all_late_and_early(new, half):
+    # a map's maxima grow by hundreds at one key: first, in the middle, last before the queries
+    for at in (0, 37, 77, 60 if new == 0 else 200 - new):
+        b = Batch([200], [new], 2, 1, 128, seed=7) if new else Batch(**wide([200], [130], 8, 1), seed=7)
+        for r in range(len(b.lens)):
+            b.kd[r][at, :, half:half + 64] *= 20
+            b.kp[b.bt[r, at // 16], :, at % 16] = b.kd[r][at].cuda()
+        b.check(b.run(), norm=None)
+
+
+@pytest.mark.parametrize("rise", [0.5, 2.0])
+@pytest.mark.parametrize("half", [0, 64])
+def test_scores_that_rise_along_the_keys(half, rise):
+    # a map whose every 32 keys outweigh those before them (its weight ratio moves all the time)
+    b = Batch(**wide([500], [120], 8, 1), seed=15)
+    for r, L in enumerate(b.lens):
+        q, k = b.q[120 * r:120 * (r + 1)], b.kd[r]
+        q[..., half] = 4.0
+        k[..., half] = (torch.arange(L) * rise / 16)[:, None].to(torch.bfloat16)  # scores rise by that in 32 keys
+        for j in range(-(-L // 16)):
+            n = min(16, L - 16 * j)
+            b.kp[b.bt[r, j], :, :n] = k[16 * j:16 * j + n].permute(1, 0, 2).cuda()
+    b.check(b.run())
 
 
 def test_rows_behind_the_last_request_and_uncomputed_requests_stay():
-    for new in ([2, 0, 1], [70, 0, 3]):
-        b = Batch([80, 9, 40], new, 4, 2, 128, extra=5, seed=8)
+    for kw in (dict(lens=[80, 9, 40], new=[2, 0, 1], Hq=4, Hkv=2), dict(lens=[80, 9, 40], new=[70, 0, 3], Hq=4, Hkv=2),
+               wide([80, 9, 40], [70, 0, 3], 16, 4)):
+        b = Batch(**kw, extra=5, seed=8)
         out = b.run()
         b.check(out)
-        assert (out[sum(new):] == 7.0).all()
+        assert (out[sum(kw["new"]):] == 7.0).all()
+    kw = wide([80, 40, 50], [30, 20, 40], 16, 4)
+    b = Batch(**kw, seed=9)
+    ends = np.cumsum(kw["new"])
+    b.L[1] = 1                # more rows than keys
+    b.cu[len(ends)] += 1      # a row past q
+    out = b.run()
+    b.check(out, rows_of=[r for r in range(len(ends)) if r not in (1, len(ends) - 1)])
+    assert (out[ends[0]:ends[1]] == 7.0).all() and (out[ends[-2]:] == 7.0).all()
+    b = Batch(**kw, seed=9)
+    b.max_q = 25              # rows past it are not computed
+    out = b.run()
+    assert (out[25:30] == 7.0).all() and not (out[:25] == 7.0).all()
     # more rows than keys, rows past q, rows past max_q_len: not computed
     b = Batch([80, 40, 50], [3, 2, 4], 4, 2, 128, seed=9)
     b.L[1] = 1
@@ -238,14 +315,15 @@ def test_rows_behind_the_last_request_and_uncomputed_requests_stay():
     assert (out[33:] == 7.0).all() and not (out[:33] == 7.0).all()
 
 
-@pytest.mark.parametrize("new", [1, 60])
+@pytest.mark.parametrize("new", [1, 60, 0])
 def test_bad_block_ids_touch_nothing_else(new):
-    b = Batch([100, 90, 110], [new] * 3, 4, 2, 128, seed=10)
+    b = Batch(**(dict(lens=[100, 90, 110], new=[new] * 3) if new else wide([100, 90, 110], [60] * 3, 16, 4)), seed=10)
     b.bt[1, 2], b.bt[1, 3], b.bt[1, 4] = -1, 1 << 30, -(1 << 31)
+    others = [r for r in range(len(b.lens)) if r != 1]
     out = b.run()
-    b.check(out, rows_of=(0, 2))
+    b.check(out, rows_of=others)
     b.L[1] = (1 << 31) - 1  # far past its row of the table
-    b.check(b.run(), rows_of=(0, 2))
+    b.check(b.run(), rows_of=others)
 
 
 def test_own_streams_and_short_workspaces():
@@ -290,8 +368,9 @@ def test_two_captured_graphs_replayed_at_once():
 
 
 def test_same_bits_every_time():
-    for new in ([1, 1], [130, 60]):
-        b = Batch([900, 300], new, 16, 2, 128, seed=14)
+    for kw in (dict(lens=[900, 300], new=[1, 1], Hq=16, Hkv=2), dict(lens=[900, 300], new=[130, 60], Hq=16, Hkv=2),
+               wide([900, 300], [130, 60], 16, 2)):
+        b = Batch(**kw, seed=14)
         want = b.run()
         for _ in range(3):
             assert torch.equal(b.run(), want)
