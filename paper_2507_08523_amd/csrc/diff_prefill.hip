@@ -16,11 +16,26 @@
 // leave an error of 2^-9 of the terms.  What is accumulated is therefore
 //   A = sum (p_1 - beta p_2) v,   B = sum p_2 v,   beta ~ lambda l_1 / l_2,
 // with the difference of the weights taken in fp32 before it is rounded: beta is
-// lambda l_1 / l_2 as of the last time a running maximum was taken, and in the end
+// lambda l_1 / l_2 as of the last time the running maxima were taken, and in the end
 //   y = (A + (beta - lambda l_1 / l_2) B) / l_1,
 // exact in beta.  A's rounding is relative to the combined weights, B's is scaled
-// by how far beta was off.  When a maximum grows (factors a_1, a_2) and beta is
-// set anew: A <- a_1 A + (a_1 beta - a_2 beta') B, B <- a_2 B.
+// by how far beta was off.  When the maxima grow (factors a_1, a_2) and beta is
+// set anew: A <- a_1 A + (a_1 beta - a_2 beta') B, B <- a_2 B.  Where map 2 outgrows
+// beta by more than a factor of 2 the maps do not cancel, and roundings scaled by an
+// old beta would stay in A while the weights they belong to lose their share: beta is
+// given up (0) for that column, whose two maps are then simply summed apart.
+// Error against 64 bits (2-norm; the output's own rounding is 0.0017 of it), q of
+// standard deviation 0.09, 0.3, 1, 2, 4: 0.0024, 0.0024, 0.0023, 0.0021, 0.0018; keys
+// whose scores in map 2 rise by 0.5 every 32 of 8000: 0.0023 (with beta followed and
+// not given up 0.029, never looked at 0.16); second map near the first 0.0024.
+//
+// What bounds it: vector instructions and products of the two waves of a SIMD, about
+// 820 and 770 cycles a step and wave, at 2.05 GHz: 64 prompts of 1.9 K tokens (64/8 heads)
+// 6.7 to 7.1 ms (box to box), 0.95 to 1.0 PFLOP/s of products; an item's start and end, 11 K
+// of 114 K cycles there, 14 K of 57 K on prompts of 300 new tokens after 300 cached ones.
+// Tried and slower: one workgroup taking item after item with the next one's loads behind
+// the end of the one before (registers spill across the tile loop: 8.0 ms); 4 or 6 LDS
+// operands in flight instead of 3 (1, 4%); the products' raised priority left out (1%).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -267,10 +282,9 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void diff_prefill_kerne
   // A, B, the sums and beta brought in line, in the first step, where a lane's sum of
   // weights leaves [0, 2^8] (a maximum that grew), and where map 2's passes most2,
   // twice what its sum was (and 2: that sum is at least 1 in one lane half) when beta
-  // was last looked at: beta is then too large for them, and scales up their rounding.
-  // Error of single rows against 64 bits, q of standard deviation 1, 2, 4, at most:
-  // 0.5, 0.6, 1.0% (without that test 0.6, 5.5, 40%).  64 x 1.9 K tokens, 64/8 heads:
-  // 6.72 ms, without it and the look at beta 6.47.
+  // was last looked at: beta is then too large for them, and scales up their rounding
+  // (error of single rows, q of standard deviation 1, 2, 4, without that test 0.6, 5.5,
+  // 40%, with it 0.5, 0.9, 0.6%).  It costs 4%.
   auto softmax = [&](bool first) __attribute__((always_inline)) {
     float t1, t2;
     auto exps = [&]() __attribute__((always_inline)) {
@@ -311,7 +325,10 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void diff_prefill_kerne
         y1 += __builtin_amdgcn_exp2f(__builtin_fmaf(s1[e], a.scale_log2, -m1));
         y2 += __builtin_amdgcn_exp2f(__builtin_fmaf(s2[e], a.scale_log2, -m2));
       }
-      beta = lam * add_across_halves(l1 + y1) / add_across_halves(l2 + y2);
+      // beta' as long as beta was not more than twice it (nor given up: was = 0 < most)
+      const float now = lam * add_across_halves(l1 + y1) / add_across_halves(l2 + y2);
+      const float was = fabsf(old), most = 2.f * fabsf(f2 * now);
+      beta = bool(int(was <= most) & int(most <= was * 0x1p100f)) ? now : 0.f;
       most2 = fminf(2.f * (l2 + y2) + 2.f, kSumLimit);
       const float k = old - f2 * beta;
 #pragma unroll
@@ -408,17 +425,17 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void diff_prefill_kerne
     wait_lds();
   };
 
-  // beta set anew where the sums have moved it by more than a factor of 2.
+  // beta given up where the sums have left it more than a factor of 2 too large.
   auto follow = [&]() __attribute__((always_inline)) {
     const float t1 = add_across_halves(l1), t2 = add_across_halves(l2);
-    const float w1 = fabsf(lam) * t1, w2 = fabsf(beta) * t2;
-    if (__ballot(w2 > 2.f * w1 || w1 > 2.f * w2)) {
-      const float now = lam * t1 / t2, k = beta - now;
+    const bool grown = fabsf(beta) * t2 > 2.f * fabsf(lam) * t1;
+    if (__ballot(grown)) {
+      const float k = grown ? beta : 0.f;
 #pragma unroll
       for (int dt = 0; dt < kDt; ++dt)
 #pragma unroll
         for (int e = 0; e < 16; ++e) oa[dt][e] += k * ob[dt][e];
-      beta = now;
+      beta -= k;
     }
     most2 = fminf(2.f * l2 + 2.f, kSumLimit);
   };
@@ -444,7 +461,7 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void diff_prefill_kerne
         next_k = raw_id(kb + kTileBlocks);
         next_v = raw_id(vb + kTileBlocks);
       }
-      if (j > 0 && u <= last_step) follow();
+      if ((j & 1) && u <= last_step) follow();  // every second tile
     }
     if (u <= last_step) {
       mask(u);

@@ -266,11 +266,12 @@ def test_a_key_that_takes_all_late_and_early(new, half):
 
 @pytest.mark.parametrize("rise", [0.5, 2.0])
 @pytest.mark.parametrize("half", [0, 64])
-def test_scores_that_rise_along_the_keys(half, rise):
+@pytest.mark.parametrize("L,new", [(500, 120), (3000, 120), (500, 1)])
+def test_scores_that_rise_along_the_keys(half, rise, L, new):
     # a map whose every 32 keys outweigh those before them (its weight ratio moves all the time)
-    b = Batch(**wide([500], [120], 8, 1), seed=15)
-    for r, L in enumerate(b.lens):
-        q, k = b.q[120 * r:120 * (r + 1)], b.kd[r]
+    b = Batch(**wide([L], [new], 8, 1)) if new > 1 else Batch([L], [1], 8, 1)
+    for r in range(len(b.lens)):
+        q, k = b.q[new * r:new * (r + 1)], b.kd[r]
         q[..., half] = 4.0
         k[..., half] = (torch.arange(L) * rise / 16)[:, None].to(torch.bfloat16)  # scores rise by that in 32 keys
         for j in range(-(-L // 16)):
