@@ -334,18 +334,19 @@ __global__ __launch_bounds__(64 * group_waves(W), 2) void diff_stream_kernel(
 // O = sum w_k O_k / sum w_k l_k.  Split 0 holds key 0, which every column sees,
 // so M is finite; a split that saw none has m = -inf and weight 0.
 constexpr int kJoinWaves = 4;
+static_assert(kMaxGroups == 16, "the join's sums are over 16 lanes");
 
 template <int D>
 __global__ __launch_bounds__(64 * kJoinWaves) void diff_join_kernel(
     const float* __restrict__ part_o, const float* __restrict__ part_ml, const int32_t* __restrict__ cu_q,
     const int32_t* __restrict__ seq_lens, int n_rows, int max_blocks, int n_req, int max_q_len, int Hq, int Hkv,
-    int n_ct, int n_split, DiffEpilogue ep, uint16_t* __restrict__ out) {
+    int n_ct, int n_split, int cols_cap, DiffEpilogue ep, uint16_t* __restrict__ out) {
   constexpr int kPer = D / 64;  // dimensions of a lane
   typedef float vec_t __attribute__((ext_vector_type(kPer)));
   const int lane = threadIdx.x & 63;
   const int64_t w = int64_t(blockIdx.x) * kJoinWaves + (threadIdx.x >> 6);
-  const int c = int(w % kTileCols);
-  const int64_t unit = w / kTileCols;
+  const int c = int(w % cols_cap);
+  const int64_t unit = w / cols_cap;
   const int ct = int(unit % n_ct), pair = int(unit / n_ct);
   if (pair >= n_req * Hkv) return;
   const int r = pair / Hkv, h = pair % Hkv;
@@ -356,28 +357,39 @@ __global__ __launch_bounds__(64 * kJoinWaves) void diff_join_kernel(
   if (q0 < 0 || q_end > n_rows || q_len <= 0 || q_len > L || col >= n_cols) return;
   const int t = col / G, head = h * G + (col - t * G);
 
-  vec_t y = {};
+  // slots of split 0, and from one split to the next
+  const size_t slot0 = size_t(unit) * n_split * (2 * kTileCols) + c;
+  constexpr size_t kNext = 2 * kTileCols;
+  const float lam = ep.lambda[head];
+  float wgt[2], den[2];
 #pragma unroll
   for (int mp = 0; mp < 2; ++mp) {
-    const size_t slot0 = size_t(unit) * n_split * (2 * kTileCols) + mp * kTileCols + c;
-    constexpr size_t kNext = 2 * kTileCols;  // slots from one split to the next
-    float m = -INFINITY, l = 0.f;
-    if (lane < n_split) {
-      m = part_ml[(slot0 + size_t(lane) * kNext) * 2];
-      l = part_ml[(slot0 + size_t(lane) * kNext) * 2 + 1];
-    }
+    const float* ml = part_ml + (slot0 + mp * kTileCols + size_t(min(lane, n_split - 1)) * kNext) * 2;
+    const float m = lane < n_split ? ml[0] : -INFINITY, l = ml[1];
     float mx = m;
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor(mx, off));
-    const float wgt = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mx);
-    float den = wgt * l;
+    for (int off = kMaxGroups / 2; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor(mx, off));
+    wgt[mp] = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mx);
+    den[mp] = wgt[mp] * l;
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) den += __shfl_xor(den, off);
-    const float* po = part_o + slot0 * D + lane * kPer;
-    vec_t acc = {};
-    for (int k = 0; k < n_split; ++k)
-      acc += __int_as_float(__builtin_amdgcn_readlane(__float_as_int(wgt), k)) * *(const vec_t*)(po + k * kNext * D);
-    y += acc * ((mp ? -ep.lambda[head] : 1.f) / den);
+    for (int off = kMaxGroups / 2; off > 0; off >>= 1) den[mp] += __shfl_xor(den[mp], off);
+  }
+  // (sums over the first 16 lanes, which hold the splits)
+  const float f1 = 1.f / __shfl(den[0], 0), f2 = -lam / __shfl(den[1], 0);
+  const float* po = part_o + slot0 * D + lane * kPer;
+  vec_t y = {};
+  for (int k = 0; k < n_split; k += 4) {
+    vec_t v[4][2];
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int mp = 0; mp < 2; ++mp)
+        v[u][mp] = *(const vec_t*)(po + (size_t(min(k + u, n_split - 1)) * kNext + mp * kTileCols) * D);
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (k + u < n_split)
+        y += v[u][0] * (f1 * __int_as_float(__builtin_amdgcn_readlane(__float_as_int(wgt[0]), k + u))) +
+             v[u][1] * (f2 * __int_as_float(__builtin_amdgcn_readlane(__float_as_int(wgt[1]), k + u)));
   }
   float fac = ep.scale;
   if (ep.norm_w) {
@@ -410,20 +422,21 @@ int64_t column_tiles(int64_t max_q_len, int Hq, int Hkv) {
 // How a launch cuts its units (column tiles of the (request, kv head) pairs).  What a
 // launch waits for is the compute unit with most to do, and a wave's steps follow each
 // other at about 1 us: four waves to a unit, and several workgroups (whose states a
-// second launch joins, 3 to 4 us), while every workgroup has a CU to itself; else two;
+// second launch joins, 3 us), while every workgroup has a CU to itself; else two;
 // and four again, quarters of the load, where twos leave some CUs twice the work of
 // others.  One wave to a unit is never better than two.  8 kv heads, D 128, us:
 //   units, keys       waves x workgroups
-//   8, 1000           4x1 13.8, 4x4 12.0     8, 4000     4x4 18.7, 4x12 15.0
-//   32, 600           4x1 11.0, 4x2 14.0     32, 2100    4x1 27, 4x6 17.1, 4x8 18.2
-//   64, 2100          4x1 26, 4x3 21.7       128, 2100   4x1 26.5, 4x2 29.7
-//   128, 8000         4x1 104, 4x2 94.9      264, 1000   2x1 26.0, 4x1 31.8
+//   8, 1000           4x1 14.0, 4x4 12.2     8, 4000     4x6 15.4, 4x12 13.2
+//   32, 600           4x1 11.1, 4x2 13.0     32, 2100    4x3 18.1, 4x6 15.2, 4x8 15.2
+//   64, 2100          4x2 21.2, 4x3 20.2     88, 3000    4x1 32.5, 4x2 28.2
+//   128, 2100         4x1 25.9, 4x2 29.0     128, 8000   4x1 104, 4x2 95.0
+//   264, 1000         2x1 26.0, 4x1 31.8
 //   576, 1000         1x1 53.6, 2x1 60.3, 4x1 51.2; of 300 21.9, 23.5, 22.4
 //   1024, 1000        2x1 90.0, 4x1 90.8 (60% of the keys shared by all 46.7, 48.5)
 //   1248, 1000        2x1 114, 4x1 107       4096, 2100  1x1 698, 2x1 683, 4x1 683
 // D 64, whose steps and join are shorter: 512 of 2100 2x1 41.8, 4x1 42.2 (shared 32.7,
 // 27.7); 1024 of 1000 40.8, 41.0 (25.9, 30.1); 128 of 2100 4x1 19.7, 8x1 17.3; 16 of
-// 1000 4x1 10.3, 4x4 12.2, of 2100 4x6 13.6.
+// 1000 4x1 10.5, 4x4 12.0, of 2100 4x3 13.0, 4x8 12.0.
 Plan stream_plan(int64_t units, int64_t max_blocks, int D) {
   const int64_t cus = ilpc::device_cus(), steps = (max_blocks * kBlock + kStepKeys - 1) / kStepKeys;
   const bool four = units <= cus || (D == 64 && units <= 3 * cus) ||
@@ -431,7 +444,7 @@ Plan stream_plan(int64_t units, int64_t max_blocks, int D) {
   if (!four) return {2, 1};
   const int64_t room = std::min<int64_t>(cus / units, kMaxGroups);
   if (room >= 3 && steps >= (D == 64 ? 48 : 32)) return {4, int(std::min(room, steps / 8))};
-  if (room == 2 && steps > 128) return {4, 2};
+  if (room == 2 && (steps > 128 || (steps >= 64 && 5 * units <= 2 * cus))) return {4, 2};
   return {D == 64 && units <= cus && steps >= 32 ? 8 : 4, 1};
 }
 
@@ -544,10 +557,11 @@ extern "C" int ilpc_paged_diff_attn(const uint16_t* q, int64_t q_stride, int32_t
   }
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && plan.groups > 1) {
-    const dim3 jgrid{unsigned((units * kTileCols + kJoinWaves - 1) / kJoinWaves)}, jblock{64 * kJoinWaves};
+    const int cols_cap = int(std::min<int64_t>(int64_t(max_q_len) * (Hq / Hkv), kTileCols));
+    const dim3 jgrid{unsigned((units * cols_cap + kJoinWaves - 1) / kJoinWaves)}, jblock{64 * kJoinWaves};
     auto join = [&](auto kernel) {
       hipLaunchKernelGGL(kernel, jgrid, jblock, 0, s, part_o, part_ml, cu_q, seq_lens, n_rows, max_blocks, B, max_q_len,
-                         Hq, Hkv, int(n_ct), plan.groups, ep, out);
+                         Hq, Hkv, int(n_ct), plan.groups, cols_cap, ep, out);
     };
     if (D == 128) join(diff_join_kernel<128>);
     else join(diff_join_kernel<64>);
