@@ -49,9 +49,17 @@ constexpr float kLazyRescale = 8.f;  // log2 growth of a column max tolerated be
 
 template <int D>
 struct StepRegs {
-  u32x4 k[D / 16];      // K operand, one per 16-dimension chunk
+  u32x4 k[D / 16];      // K rows of the step, in the order of memory
   u32x4 v[2][D / 32];   // V^T operand, [pool block of the step][32-dimension tile]
 };
+
+// Orders a wave's LDS stores and reads across its lanes (the hardware keeps a wave's
+// LDS operations in order; the compiler has to as well).
+__device__ __forceinline__ void wave_lds_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
 
 constexpr int group_waves(int W) { return W > 4 ? W : 4; }  // waves of a workgroup, W of them to a pair
 
@@ -63,31 +71,36 @@ __global__ __launch_bounds__(64 * group_waves(W), 2) void diff_stream_kernel(
     float scale_log2, int pairs_layout, DiffEpilogue ep, uint16_t* __restrict__ out, int n_ct, int n_split,
     float* __restrict__ part_o, float* __restrict__ part_ml) {
   constexpr int kDch = D / 16, kDt = D / 32, kWavesPerGroup = group_waves(W);
-  // Q^T of each wave in LDS; for the join the same space holds every wave's O, a row
-  // of kRow floats a column.
+  // Q^T of each wave and the K rows of its step in LDS; for the join the same space
+  // holds every wave's O, a row of kRow floats a column.
   constexpr int kRow = D + 4, kCols = 2 * kTileCols;
   constexpr int kQBytes = kWavesPerGroup * kDch * 64 * 16, kOBytes = kWavesPerGroup * kCols * kRow * 4;
-  static_assert(kOBytes >= kQBytes, "the join's rows are the larger");
+  constexpr int kRowPieces = D / 8 + 1;  // 16-byte pieces of a K row in LDS: one more than it has
+  constexpr int kKBytes = kWavesPerGroup * kStepKeys * kRowPieces * 16;
+  static_assert(kOBytes >= kQBytes + kKBytes, "the join's rows are the larger");
   __shared__ __attribute__((aligned(16))) uint8_t lds[kOBytes];
   __shared__ float s_m[kWavesPerGroup][kCols], s_l[kWavesPerGroup][kCols];
   u32x4(*q_lds)[kDch][64] = reinterpret_cast<u32x4(*)[kDch][64]>(lds);
+  u32x4(*k_lds)[kStepKeys][kRowPieces] = reinterpret_cast<u32x4(*)[kStepKeys][kRowPieces]>(lds + kQBytes);
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 31, hh = lane >> 5;
   const int map = n >> 4, nc = n & 15;  // this lane's map, and its column of the tile
 
   // Workgroup b runs on XCD b % 8; each XCD takes a contiguous range of items,
-  // numbered request-major (all kv heads of a block are adjacent in memory).
+  // numbered head-major: requests of every length fall to each XCD, and the keys that
+  // requests share, of one head or few, stay in its L2 (512 requests, 8 kv heads, 1100
+  // to 2140 keys, 1024 shared: 354 us, numbered by requests 373; none shared 750, 744).
   const unsigned nb = gridDim.x, per = nb >> 3, extra = nb & 7u;
   const unsigned x = blockIdx.x & 7u, i = blockIdx.x >> 3;
   const unsigned group = x * per + min(x, extra) + i;
   const int64_t item = int64_t(group) * (kWavesPerGroup / W) + wave / W;
   const int64_t n_items = int64_t(n_req) * Hkv * n_split * n_ct;
   const bool in_grid = item < n_items;
-  // item = ((request * Hkv + kv head) * n_ct + column tile) * n_split + range of the keys
+  // item = ((kv head * n_req + request) * n_ct + column tile) * n_split + range of the keys
   const int sp = in_grid ? int(item % n_split) : 0, unit = in_grid ? int(item / n_split) : 0;
   const int ct = unit % n_ct, pair = unit / n_ct;
-  const int r = pair / Hkv, h = pair % Hkv;
+  const int h = pair / n_req, r = pair % n_req;
   const int G = Hq / Hkv;
 
   const int q0 = cu_q[r], q_end = cu_q[r + 1], q_len = q_end - q0;
@@ -123,7 +136,6 @@ __global__ __launch_bounds__(64 * group_waves(W), 2) void diff_stream_kernel(
     const int steps_per = (n_steps_all + n_ranges - 1) / n_ranges;
     const int s_begin = min(range * steps_per, n_steps_all);
     const int n_steps = min(s_begin + steps_per, n_steps_all);
-    const int krow = diff_key_of_row(n);
     const size_t head_off = size_t(h) * kBlock * D;
     const size_t slab = size_t(Hkv) * kBlock * D;
 
@@ -152,10 +164,10 @@ __global__ __launch_bounds__(64 * group_waves(W), 2) void diff_stream_kernel(
         ++win;
       }
       const int id0 = block_id(2 * s), id1 = block_id(2 * s + 1);
-      const int idk = krow < kBlock ? id0 : id1;
-      const uint16_t* ks = k_pool + size_t(idk) * slab + head_off + size_t(krow & 15) * D + hh * 8;
 #pragma unroll
-      for (int kc = 0; kc < kDch; ++kc) R.k[kc] = *(const u32x4*)(ks + kc * 16);
+      for (int kc = 0; kc < kDch; ++kc)
+        R.k[kc] = *(const u32x4*)(k_pool + size_t(kc < kDch / 2 ? id0 : id1) * slab + head_off + kc % (kDch / 2) * 512 +
+                                  lane * 8);
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
         const uint16_t* vs = v_pool + size_t(b ? id1 : id0) * slab + head_off + size_t(n) * kBlock + hh * 8;
@@ -166,15 +178,27 @@ __global__ __launch_bounds__(64 * group_waves(W), 2) void diff_stream_kernel(
 
     const int mask_from = L - q_len + col0 / G;  // steps reaching past this key need the causal mask
 
+    // A block's K rows are one contiguous piece of memory and are read as such, 1 KB an
+    // instruction; the operand's layout (a row a lane) comes from LDS, whose rows
+    // are 16 bytes longer, so that neither the stores nor the reads meet in a bank.
+    // Reading rows straight into the operand, 32 bytes of 32 rows an instruction, keeps
+    // the address path busy: 128 requests of 8 kv heads with 812 keys, 512 of them
+    // shared, 48.3 us and 37.6 this way; without shared keys HBM hides most of it.
+    u32x4* k_st = &k_lds[wave][lane / (D / 8)][lane % (D / 8)];
+    const u32x4* k_ld = &k_lds[wave][diff_key_of_row(n)][hh];
+
     auto compute = [&](int s, StepRegs<D>& R) {
       const int j0 = s * kStepKeys;
+#pragma unroll
+      for (int kc = 0; kc < kDch; ++kc) k_st[kc * (512 / D) * kRowPieces] = R.k[kc];
+      wave_lds_fence();
       f32x16 sc;
 #pragma unroll
       for (int e = 0; e < 16; ++e) sc[e] = 0.f;
 #pragma unroll
       for (int kc = 0; kc < kDch; ++kc)
-        sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(R.k[kc]), as_bf16x8(q_lds[wave][kc][lane]), sc, 0, 0,
-                                                    0);
+        sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(k_ld[kc * 2]), as_bf16x8(q_lds[wave][kc][lane]), sc, 0, 0, 0);
+      wave_lds_fence();
       if (j0 + kStepKeys - 1 > mask_from) {
         // causal mask (which also covers keys >= L), and the V rows of keys >=
         // key_end zeroed: unwritten pool slots may hold any bits
@@ -349,7 +373,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void diff_join_kernel(
   const int64_t unit = w / cols_cap;
   const int ct = int(unit % n_ct), pair = int(unit / n_ct);
   if (pair >= n_req * Hkv) return;
-  const int r = pair / Hkv, h = pair % Hkv;
+  const int h = pair / n_req, r = pair % n_req;
   const int G = Hq / Hkv;
   const int q0 = cu_q[r], q_end = cu_q[r + 1], q_len = q_end - q0;
   const int L = min(seq_lens[r], max_blocks * kBlock);
@@ -426,17 +450,17 @@ int64_t column_tiles(int64_t max_q_len, int Hq, int Hkv) {
 // and four again, quarters of the load, where twos leave some CUs twice the work of
 // others.  One wave to a unit is never better than two.  8 kv heads, D 128, us:
 //   units, keys       waves x workgroups
-//   8, 1000           4x1 14.0, 4x4 12.2     8, 4000     4x6 15.4, 4x12 13.2
-//   32, 600           4x1 11.1, 4x2 13.0     32, 2100    4x3 18.1, 4x6 15.2, 4x8 15.2
-//   64, 2100          4x2 21.2, 4x3 20.2     88, 3000    4x1 32.5, 4x2 28.2
-//   128, 2100         4x1 25.9, 4x2 29.0     128, 8000   4x1 104, 4x2 95.0
-//   264, 1000         2x1 26.0, 4x1 31.8
-//   576, 1000         1x1 53.6, 2x1 60.3, 4x1 51.2; of 300 21.9, 23.5, 22.4
-//   1024, 1000        2x1 90.0, 4x1 90.8 (60% of the keys shared by all 46.7, 48.5)
-//   1248, 1000        2x1 114, 4x1 107       4096, 2100  1x1 698, 2x1 683, 4x1 683
-// D 64, whose steps and join are shorter: 512 of 2100 2x1 41.8, 4x1 42.2 (shared 32.7,
-// 27.7); 1024 of 1000 40.8, 41.0 (25.9, 30.1); 128 of 2100 4x1 19.7, 8x1 17.3; 16 of
-// 1000 4x1 10.5, 4x4 12.0, of 2100 4x3 13.0, 4x8 12.0.
+//   8, 1000           4x1 13.0, 4x4 12.1     8, 4000     4x6 14.3, 4x12 12.6
+//   32, 600           4x1 10.4, 4x2 12.3     32, 2100    4x3 16.9, 4x6 14.5, 4x8 14.8
+//   64, 2100          4x2 20.6, 4x3 19.8     88, 3000    4x1 31.5, 4x2 28.2
+//   128, 2100         4x1 25.8, 4x2 29.1     128, 8000   4x1 97.5, 4x2 93.2
+//   264, 1000         2x1 25.3, 4x1 30.9
+//   576, 1000         2x1 58.2, 4x1 50.9; of 300 23.0, 22.8
+//   1024, 1000        2x1 90.3, 4x1 90.8 (60% of the keys shared by all 40.3, 42.6)
+//   1248, 1000        2x1 113, 4x1 108       4096, 2100  2x1 684, 4x1 686 (335, 353)
+// D 64, whose steps and join are shorter: 512 of 2100 2x1 41.5, 4x1 43.5 (shared 32.5,
+// 30.9); 1024 of 1000 40.5, 41.5 (26.7, 29.9); 128 of 2100 4x1 19.3, 8x1 16.8; 16 of
+// 1000 8x1 9.8, 4x1 10.6, 4x4 11.6, of 2100 4x3 12.8, 4x8 12.0.
 Plan stream_plan(int64_t units, int64_t max_blocks, int D) {
   const int64_t cus = ilpc::device_cus(), steps = (max_blocks * kBlock + kStepKeys - 1) / kStepKeys;
   const bool four = units <= cus || (D == 64 && units <= 3 * cus) ||
@@ -449,13 +473,14 @@ Plan stream_plan(int64_t units, int64_t max_blocks, int D) {
 }
 
 // Whether the kernel for many columns takes a batch: of more than one column tile a
-// pair, where there are more than two units to a CU (at D = 64, with its shorter steps,
-// four).  us here, there: D 128, contexts of 2100 keys, 256 units 28, 65; 384 46, 66;
-// 528 67, 68; 640 69, 68; 1056 103, 68; 2176 206, 88; of 100 keys, 320 11, 11; 576 14,
-// 12.  D 64, 2100 keys, 640 40, 55; 1056 59, 54; 2080 106, 69.
+// pair, where there are more than three units to a CU (at D = 64, with its shorter
+// steps, four).  us here, there: D 128, contexts of 2100 keys, 256 units 28, 64; 384 47,
+// 67; 544 57, 69; 640 57, 68; 1056 88, 69; 2176 154, 90; of 600 keys, 640 27, 27; 1056 36,
+// 26; of 100, 640 13, 12; 1056 18, 12.  D 64, 2100 keys, 640 34, 54; 1056 50, 54; 2080 85,
+// 74; of 600, 640 16, 20; 1056 23, 21.
 bool many_columns(int64_t B, int64_t max_q_len, int Hq, int Hkv, int D) {
   const int64_t n_ct = column_tiles(max_q_len, Hq, Hkv);
-  return n_ct > 1 && B * Hkv * n_ct > (D == 64 ? 4 : 2) * int64_t(ilpc::device_cus());
+  return n_ct > 1 && B * Hkv * n_ct > (D == 64 ? 4 : 3) * int64_t(ilpc::device_cus());
 }
 
 size_t part_bytes(int64_t units, int D, int n) {
