@@ -305,10 +305,12 @@ class DeviceTables:
 
     def release(self, ended):
         """Requests with ended[r] (device int32) = 1, not 0, have finished: the blocks that they
-        took by extend are free again, and their context length is 0."""
+        took by extend are free again, and their rows hold nothing, ready for another request's."""
         ilpc.release_tables(self.block_tables, self.first_block, self.seq_lens * ended, self.pc.free_ids,
                             self.pc.free_taken, self.cu_blocks, self.pc.free_taken, self.status)
-        self.seq_lens.mul_(1 - ended)
+        goes_on = 1 - ended
+        self.seq_lens.mul_(goes_on)
+        self.first_block.mul_(goes_on)  # what the row takes from now on is all its own
 
 
 class DecodeGraph:

@@ -433,3 +433,24 @@ def test_decode_loop_on_the_device(captured):
     assert ints(dt.status)[0] & (ilpc.NO_BLOCKS | ilpc.TOO_LONG | ilpc.TOO_MANY_ROWS)
     assert ints(dt.seq_lens) == seq and torch.equal(pc.k_pool.view(torch.int16), pool.view(torch.int16))
     assert (out == 7.0).all()
+
+
+def test_rows_of_ended_requests_are_used_again():
+    """Rows whose request has ended serve another one: all that it takes comes back, the blocks that
+    the first request's prefix held among what it writes over."""
+    pc = pipeline.PagedPrefixCache(2, 64, 16, 6, 2, 8, spare_blocks=9)
+    tables = np.full((2, 6), -1, np.int32)
+    tables[0, :2], tables[1, :3] = [4, 7], [4, 5, 6]
+    dt = pipeline.DeviceTables(pc, tables, [20, 48], max_rows=96)
+    for rounds in range(3):
+        dt.extend(dev([1, 33]), 33)
+        assert ints(dt.status) == [0]
+        held = ints(dt.block_tables[1])
+        dt.release(dev([0, 1]))
+        assert ints(dt.status) == [0] and ints(dt.seq_lens) == [21 + rounds, 0]
+        if rounds:  # (three blocks from the row's first entry on)
+            assert all(x >= pc.num_blocks for x in held[:3])
+        dt.release(dev([0, 1]))  # ended already: nothing to give back
+        assert ints(dt.status) == [0] and ints(pc.free_taken) == [0]
+        assert sorted(ints(pc.free_ids)) == list(range(16, 25))
+    assert ints(dt.block_tables[0])[:2] == [4, 7]
