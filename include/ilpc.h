@@ -489,7 +489,7 @@ int ilpc_release_tables(const int32_t* block_tables, int32_t max_blocks, int32_t
  * k_new, v_new [device] bf16, row i at k_new + i * k_stride (elements; a
  *              multiple of 8, at least Hkv * D): [Hkv, D], contiguous, so that
  *              rows may be parts of a fused projection's
- * slot_map     [device] int32 [n_rows]
+ * slot_map     [device] int32 [n_rows]; n_rows <= 2^28 - 16, Hkv <= 65535 (ILPC_EUNSUP)
  */
 int ilpc_kv_append_slots(const uint16_t* k_new, int64_t k_stride, const uint16_t* v_new, int64_t v_stride,
                          uint16_t* k_pool, uint16_t* v_pool, int32_t num_blocks, const int32_t* slot_map,
@@ -526,7 +526,8 @@ int ilpc_diff_attn_workspace_bytes(int32_t B, int32_t max_q_len, int32_t Hq, int
  * layout       ILPC_DIFF_HALVES or ILPC_DIFF_ROPE
  * lambda       [device] fp32 [Hq]
  * norm_weight  [device] fp32 [D], 16-byte aligned, or NULL
- * out          [device] bf16 [n_rows, Hq, D]; rows of no request stay as they are
+ * out          [device] bf16 [n_rows, Hq, D], not overlapping q; rows of no
+ *              request stay as they are
  * workspace    [device] >= ilpc_diff_attn_workspace_bytes() bytes, 16-byte
  *              aligned, no initial contents needed (NULL with 0 bytes where
  *              that is 0).  Calls that may run concurrently, captured graphs
@@ -536,7 +537,9 @@ int ilpc_diff_attn_workspace_bytes(int32_t B, int32_t max_q_len, int32_t Hq, int
  * enter those products as bf16 numbers whose rounding is made up for (see the
  * kernels), so that the error stays near the rounding of the output also where
  * the maps nearly cancel.  Requests with q_len_r > L_r are not computed;
- * otherwise the bounds rules of ilpc_paged_prefill_attn hold.
+ * otherwise the bounds rules of ilpc_paged_prefill_attn hold.  Up to
+ * 2^18 (request, kv head) pairs of up to 2^22 (query, head of the group)
+ * columns, beyond that up to 2^24 tiles of 16 columns (ILPC_EUNSUP).
  */
 int ilpc_paged_diff_attn(const uint16_t* q, int64_t q_stride, int32_t n_rows, const uint16_t* k_pool,
                          const uint16_t* v_pool, int32_t num_blocks, const int32_t* block_tables, int32_t max_blocks,

@@ -387,7 +387,7 @@ extern "C" int ilpc_kv_append_slots(const uint16_t* k_new, int64_t k_stride, con
   if (n_rows < 0 || num_blocks < 0 || Hkv < 1) return set_error(ILPC_EINVAL, "%s: negative or zero size", fn);
   if (block_size != kBlock) return set_error(ILPC_EUNSUP, "%s: block_size must be 16", fn);
   if (D != 64 && D != 128) return set_error(ILPC_EUNSUP, "%s: head_dim %d unsupported", fn, D);
-  if (Hkv > 65535) return set_error(ILPC_EUNSUP, "%s: grid too large", fn);
+  if (Hkv > 65535 || n_rows > (1 << 28) - kBlock) return set_error(ILPC_EUNSUP, "%s: grid too large", fn);
   if (n_rows == 0) return ILPC_OK;
   if (!k_new || !v_new || !k_pool || !v_pool || !slot_map) return set_error(ILPC_EINVAL, "%s: NULL pointer", fn);
   const int64_t row = int64_t(Hkv) * D;

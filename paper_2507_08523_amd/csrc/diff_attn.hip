@@ -478,8 +478,10 @@ Plan stream_plan(int64_t units, int64_t max_blocks, int D) {
 // 67; 544 57, 69; 640 57, 68; 1056 88, 69; 2176 154, 90; of 600 keys, 640 27, 27; 1056 36,
 // 26; of 100, 640 13, 12; 1056 18, 12.  D 64, 2100 keys, 640 34, 54; 1056 50, 54; 2080 85,
 // 74; of 600, 640 16, 20; 1056 23, 21.
+// (Its grid holds 2^22 columns a request and 2^18 pairs.)
 bool many_columns(int64_t B, int64_t max_q_len, int Hq, int Hkv, int D) {
   const int64_t n_ct = column_tiles(max_q_len, Hq, Hkv);
+  if (max_q_len * (Hq / Hkv) > (int64_t(1) << 22) || B * Hkv > (1 << 18)) return false;
   return n_ct > 1 && B * Hkv * n_ct > (D == 64 ? 4 : 3) * int64_t(ilpc::device_cus());
 }
 
@@ -543,12 +545,10 @@ extern "C" int ilpc_paged_diff_attn(const uint16_t* q, int64_t q_stride, int32_t
     return set_error(ILPC_EINVAL, "%s: Q/K/V/out/norm_weight must be 16-byte aligned", fn);
   if (q_stride < int64_t(Hq) * D || q_stride % 8 != 0)
     return set_error(ILPC_EINVAL, "%s: q_stride must be a multiple of 8 elements, at least Hq * D", fn);
+  const uint16_t *q_end = q + int64_t(n_rows - 1) * q_stride + int64_t(Hq) * D, *out_end = out + int64_t(n_rows) * Hq * D;
+  if (q < out_end && out < q_end) return set_error(ILPC_EINVAL, "%s: q and out overlap", fn);
   if (ilpc::device_cus() <= 0) return set_error(ILPC_EHIP, "%s: cannot query the device", fn);
   if (many_columns(B, max_q_len, Hq, Hkv, D)) {
-    // (grid limits: 65535 column tiles a request, rows / 16 numbers, and pairs / 8)
-    if (int64_t(max_q_len) * (Hq / Hkv) > (int64_t(1) << 22) || int64_t(B) * Hkv > (1 << 18) ||
-        int64_t(n_rows) * (Hq / Hkv) / 128 + B > (1 << 18))
-      return set_error(ILPC_EUNSUP, "%s: batch too large", fn);
     const DiffArgs a{q, q_stride, n_rows, k_pool, v_pool, num_blocks, block_tables, max_blocks, cu_q, seq_lens, B,
                      max_q_len, Hq, Hkv, D, softmax_scale * 1.4426950408889634f, int(layout == ILPC_DIFF_ROPE),
                      DiffEpilogue{lambda, norm_weight, norm_eps, out_scale}, out};
@@ -566,6 +566,7 @@ extern "C" int ilpc_paged_diff_attn(const uint16_t* q, int64_t q_stride, int32_t
   float* part_ml = need ? part_o + size_t(units) * plan.groups * (2 * kTileCols) * D : nullptr;
   const int64_t items = units * plan.groups, per_group = group_waves(plan.waves) / plan.waves;
   const dim3 grid{unsigned((items + per_group - 1) / per_group)}, block{unsigned(64 * group_waves(plan.waves))};
+  if (uint64_t(grid.x) * block.x > UINT32_MAX) return set_error(ILPC_EUNSUP, "%s: batch too large", fn);
   hipStream_t s = static_cast<hipStream_t>(stream);
   auto launch = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, grid, block, 0, s, q, q_stride, n_rows, k_pool, v_pool, num_blocks, block_tables, max_blocks,

@@ -531,7 +531,8 @@ bool launch_diff_prefill(const DiffArgs& a, hipStream_t stream) {
   // the longest request and the sum of all); else by rows.
   const int64_t G = a.Hq / a.Hkv, n_ct = (a.max_q_len * G + kCols - 1) / kCols, pairs = int64_t(a.B) * a.Hkv;
   const int64_t numbers = a.n_rows * G / kCols + a.B;
-  const bool by_pair = (pairs % 8 == 0 || pairs >= 64) && 2 * a.B * n_ct <= 3 * numbers;
+  const bool by_pair = ((pairs % 8 == 0 || pairs >= 64) && 2 * a.B * n_ct <= 3 * numbers) ||
+                       numbers > 8 * 65535 || a.Hkv > 65535;  // (more than the other grid holds)
   const dim3 grid(8, unsigned(by_pair ? n_ct : (numbers + 7) / 8), unsigned(by_pair ? (pairs + 7) / 8 : a.Hkv));
   const dim3 block(64 * kWaves);
   const int recip = 65536 / int(G) + 1, numbering = by_pair ? kByPair : kByRows;

@@ -399,3 +399,19 @@ def test_binding_refusals(native, monkeypatch):
             call(**kw)
     call()
     torch.cuda.synchronize()
+
+
+def test_more_pairs_than_the_many_column_grid_holds():
+    """2^18 + 3 requests of two rows of 9 heads (two column tiles each), all with the same rows and
+    keys: every result is the first one's, and that is right."""
+    one, n = Batch([13], [2], 9, 1, 64, seed=15), (1 << 18) + 3
+    q = one.q.repeat(n, 1, 1)
+    bt, L = one.bt.repeat(n, 1), one.L.repeat(n)
+    cu = torch.arange(n + 1, dtype=torch.int32, device="cuda") * 2
+    out = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device="cuda")
+    ilpc.paged_diff_attn(q, one.kp, one.vp, bt, cu, L, 2, one.scale, one.lam, out, norm_weight=one.w,
+                         out_scale=one.out_scale)
+    torch.cuda.synchronize()
+    first = out[:2].clone()
+    one.check(first)
+    assert (out.view(n, 2, 9, 64) == first).all()

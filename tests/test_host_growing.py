@@ -93,3 +93,14 @@ def test_binding_takes_only_gpu_tensors():
                  lambda: ilpc.paged_diff_attn(h, pool, pool_v, bt, cu, i, 1, 0.1, f[:2], h.clone())):
         with pytest.raises(ilpc.ILPCError, match="must be a CUDA/HIP torch tensor"):
             call()
+
+
+@pytest.mark.parametrize("call,kw,rc", [
+    (append, dict(n=1 << 28), ilpc.EUNSUP),
+    # the output on the queries' first row, on their last one (rows 512 elements apart), around them
+    *[(attn, dict(out=P + x), ilpc.EINVAL) for x in (0, 2 * 2 * 512, -2 * 2 * 512)],
+    (attn, dict(qs=2048, out=P + 2 * 512), ilpc.EINVAL),
+])
+def test_library_refuses_overlaps_and_grids_before_a_launch(call, kw, rc):
+    assert call(**kw) == rc
+    assert (b"overlap" if "out" in kw else b"too large") in ilpc.load().ilpc_last_error()
