@@ -44,7 +44,7 @@ using namespace ilpc;
 constexpr int kBlock = 16;
 constexpr int kStepKeys = 32;        // keys a step (two pool blocks)
 constexpr int kTileCols = 16;        // query columns of a wave (each one twice, once a map)
-constexpr int kMaxGroups = 16;       // most workgroups to a pair
+constexpr int kMaxGroups = 64;       // most workgroups to a pair (a lane of the join each)
 constexpr float kLazyRescale = 8.f;  // log2 growth of a column max tolerated before rescaling O
 
 template <int D>
@@ -358,7 +358,6 @@ __global__ __launch_bounds__(64 * group_waves(W), 2) void diff_stream_kernel(
 // O = sum w_k O_k / sum w_k l_k.  Split 0 holds key 0, which every column sees,
 // so M is finite; a split that saw none has m = -inf and weight 0.
 constexpr int kJoinWaves = 4;
-static_assert(kMaxGroups == 16, "the join's sums are over 16 lanes");
 
 template <int D>
 __global__ __launch_bounds__(64 * kJoinWaves) void diff_join_kernel(
@@ -392,14 +391,13 @@ __global__ __launch_bounds__(64 * kJoinWaves) void diff_join_kernel(
     const float m = lane < n_split ? ml[0] : -INFINITY, l = ml[1];
     float mx = m;
 #pragma unroll
-    for (int off = kMaxGroups / 2; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor(mx, off));
+    for (int off = 32; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor(mx, off));
     wgt[mp] = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mx);
     den[mp] = wgt[mp] * l;
 #pragma unroll
-    for (int off = kMaxGroups / 2; off > 0; off >>= 1) den[mp] += __shfl_xor(den[mp], off);
+    for (int off = 32; off > 0; off >>= 1) den[mp] += __shfl_xor(den[mp], off);
   }
-  // (sums over the first 16 lanes, which hold the splits)
-  const float f1 = 1.f / __shfl(den[0], 0), f2 = -lam / __shfl(den[1], 0);
+  const float f1 = 1.f / den[0], f2 = -lam / den[1];
   const float* po = part_o + slot0 * D + lane * kPer;
   vec_t y = {};
   for (int k = 0; k < n_split; k += 4) {
@@ -461,13 +459,18 @@ int64_t column_tiles(int64_t max_q_len, int Hq, int Hkv) {
 // D 64, whose steps and join are shorter: 512 of 2100 2x1 41.5, 4x1 43.5 (shared 32.5,
 // 30.9); 1024 of 1000 40.5, 41.5 (26.7, 29.9); 128 of 2100 4x1 19.3, 8x1 16.8; 16 of
 // 1000 8x1 9.8, 4x1 10.6, 4x4 11.6, of 2100 4x3 12.8, 4x8 12.0.
+// A workgroup's steps go as 1 / workgroups and the join's reads as their number, so the
+// best number goes as the root of the steps: 16, 32, 64 workgroups to 1 unit of 8000 keys
+// 15.7, 17.0, -; of 16000 19.6, 18.7, 22.8; of 32000 26.7, 22.7, 25.0; of 128000 72.8, 46.7,
+// 39.0.
 Plan stream_plan(int64_t units, int64_t max_blocks, int D) {
   const int64_t cus = ilpc::device_cus(), steps = (max_blocks * kBlock + kStepKeys - 1) / kStepKeys;
   const bool four = units <= cus || (D == 64 && units <= 3 * cus) ||
                     (steps >= 32 && ((units > 2 * cus && units <= 3 * cus) || (units > 4 * cus && units <= 5 * cus)));
   if (!four) return {2, 1};
   const int64_t room = std::min<int64_t>(cus / units, kMaxGroups);
-  if (room >= 3 && steps >= (D == 64 ? 48 : 32)) return {4, int(std::min(room, steps / 8))};
+  if (room >= 3 && steps >= (D == 64 ? 48 : 32))
+    return {4, int(std::min({room, steps / 8, int64_t(std::sqrt(double(steps)))}))};
   if (room == 2 && (steps > 128 || (steps >= 64 && 5 * units <= 2 * cus))) return {4, 2};
   return {D == 64 && units <= cus && steps >= 32 ? 8 : 4, 1};
 }
@@ -496,8 +499,8 @@ int check_sizes(const char* fn, int32_t B, int32_t max_q_len, int32_t Hq, int32_
   if (D != 64 && D != 128) return set_error(ILPC_EUNSUP, "%s: head_dim %d unsupported", fn, D);
   if (Hq % Hkv != 0 || Hq / Hkv > 64) return set_error(ILPC_EUNSUP, "%s: Hq %d / Hkv %d unsupported", fn, Hq, Hkv);
   if (max_blocks > (1 << 24)) return set_error(ILPC_EUNSUP, "%s: max_blocks %d > %d", fn, max_blocks, 1 << 24);
-  if (int64_t(B) * Hkv > INT32_MAX / kMaxGroups || int64_t(max_q_len) * (Hq / Hkv) > (int64_t(1) << 30) ||
-      int64_t(B) * Hkv * column_tiles(max_q_len, Hq, Hkv) > INT32_MAX / kMaxGroups)
+  if (int64_t(B) * Hkv > INT32_MAX / 16 || int64_t(max_q_len) * (Hq / Hkv) > (int64_t(1) << 30) ||
+      int64_t(B) * Hkv * column_tiles(max_q_len, Hq, Hkv) > INT32_MAX / 16)
     return set_error(ILPC_EUNSUP, "%s: batch too large", fn);
   return ILPC_OK;
 }

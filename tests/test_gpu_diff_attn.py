@@ -415,3 +415,11 @@ def test_more_pairs_than_the_many_column_grid_holds():
     first = out[:2].clone()
     one.check(first)
     assert (out.view(n, 2, 9, 64) == first).all()
+
+
+@pytest.mark.parametrize("L,cols,D", [(9001, 700, 128), (33000, 0, 64), (70000, 0, 128), (140000, 0, 64), (40, 9000, 128),
+                                      (2500, 9000, 64)])
+def test_long_contexts_and_wide_tables(L, cols, D):
+    # the keys over up to 64 workgroups, whose ranges need not all hold keys
+    b = Batch([L, 3 + L // 3], [1, 2], 4, 1, D, seed=L, spare_cols=cols)
+    b.check(b.run())
