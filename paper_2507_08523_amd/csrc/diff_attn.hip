@@ -373,42 +373,53 @@ __global__ __launch_bounds__(64 * kJoinWaves) void diff_join_kernel(
   const int ct = int(unit % n_ct), pair = int(unit / n_ct);
   if (pair >= n_req * Hkv) return;
   const int h = pair / n_req, r = pair % n_req;
-  const int G = Hq / Hkv;
-  const int q0 = cu_q[r], q_end = cu_q[r + 1], q_len = q_end - q0;
-  const int L = min(seq_lens[r], max_blocks * kBlock);
-  const int n_cols = min(q_len, max_q_len) * G, col = ct * kTileCols + c;
-  if (q0 < 0 || q_end > n_rows || q_len <= 0 || q_len > L || col >= n_cols) return;
+  const int G = Hq / Hkv, col = ct * kTileCols + c;
   const int t = col / G, head = h * G + (col - t * G);
 
-  // slots of split 0, and from one split to the next
-  const size_t slot0 = size_t(unit) * n_split * (2 * kTileCols) + c;
-  constexpr size_t kNext = 2 * kTileCols;
+  // Everything that the lengths do not decide is asked for with them, in one round trip:
+  // the splits' maxima and sums, the first kAhead of their rows.  (Slots of columns that
+  // the batch does not have hold nothing of use, and nothing comes of it.)
+  const size_t slot0 = size_t(unit) * n_split * (2 * kTileCols) + c;  // of split 0
+  constexpr size_t kNext = 2 * kTileCols;                              // from one split to the next
+  constexpr int kAhead = 8;
+  const float* po = part_o + slot0 * D + lane * kPer;
+  vec_t v[kAhead][2];
+  auto load = [&](int k) {
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+      for (int mp = 0; mp < 2; ++mp)
+        v[u][mp] = *(const vec_t*)(po + (size_t(min(k + u, n_split - 1)) * kNext + mp * kTileCols) * D);
+  };
+  const int q0 = cu_q[r], q_end = cu_q[r + 1], L_in = seq_lens[r];
   const float lam = ep.lambda[head];
+  float2 ml[2];
+#pragma unroll
+  for (int mp = 0; mp < 2; ++mp)
+    ml[mp] = *(const float2*)(part_ml + (slot0 + mp * kTileCols + size_t(min(lane, n_split - 1)) * kNext) * 2);
+  load(0);
+  __builtin_amdgcn_sched_barrier(0);
+  const int q_len = q_end - q0, L = min(L_in, max_blocks * kBlock);
+  if (q0 < 0 || q_end > n_rows || q_len <= 0 || q_len > L || col >= min(q_len, max_q_len) * G) return;
+
   float wgt[2], den[2];
 #pragma unroll
   for (int mp = 0; mp < 2; ++mp) {
-    const float* ml = part_ml + (slot0 + mp * kTileCols + size_t(min(lane, n_split - 1)) * kNext) * 2;
-    const float m = lane < n_split ? ml[0] : -INFINITY, l = ml[1];
+    const float m = lane < n_split ? ml[mp].x : -INFINITY;
     float mx = m;
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor(mx, off));
     wgt[mp] = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mx);
-    den[mp] = wgt[mp] * l;
+    den[mp] = wgt[mp] * ml[mp].y;
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) den[mp] += __shfl_xor(den[mp], off);
   }
   const float f1 = 1.f / den[0], f2 = -lam / den[1];
-  const float* po = part_o + slot0 * D + lane * kPer;
   vec_t y = {};
-  for (int k = 0; k < n_split; k += 4) {
-    vec_t v[4][2];
+  for (int k = 0; k < n_split; k += kAhead) {
+    if (k > 0) load(k);
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
-#pragma unroll
-      for (int mp = 0; mp < 2; ++mp)
-        v[u][mp] = *(const vec_t*)(po + (size_t(min(k + u, n_split - 1)) * kNext + mp * kTileCols) * D);
-#pragma unroll
-    for (int u = 0; u < 4; ++u)
+    for (int u = 0; u < kAhead; ++u)
       if (k + u < n_split)
         y += v[u][0] * (f1 * __int_as_float(__builtin_amdgcn_readlane(__float_as_int(wgt[0]), k + u))) +
              v[u][1] * (f2 * __int_as_float(__builtin_amdgcn_readlane(__float_as_int(wgt[1]), k + u)));
