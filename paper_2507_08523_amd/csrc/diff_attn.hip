@@ -18,7 +18,8 @@
 // Half of those products multiply zeros, which costs nothing here: the kernel is
 // bound by reading K and V from HBM.  Each wave streams its range of a
 // request's keys from the pools into registers, two pool blocks (32 keys) a
-// step, the next step's loads in flight; W waves of a workgroup and n_split
+// step, the next step's loads in flight (K then takes the operand's layout by
+// way of LDS); W waves of a workgroup and n_split
 // workgroups share a (request, kv head, column tile) where there are too few of
 // them to fill the chip, and their states are joined at the end.
 //   Precision: y is a difference, and where the two maps nearly agree (the case
@@ -455,21 +456,21 @@ int64_t column_tiles(int64_t max_q_len, int Hq, int Hkv) {
 // How a launch cuts its units (column tiles of the (request, kv head) pairs).  What a
 // launch waits for is the compute unit with most to do, and a wave's steps follow each
 // other at about 1 us: four waves to a unit, and several workgroups (whose states a
-// second launch joins, 3 us), while every workgroup has a CU to itself; else two;
+// second launch joins, 2 us), while every workgroup has a CU to itself; else two;
 // and four again, quarters of the load, where twos leave some CUs twice the work of
 // others.  One wave to a unit is never better than two.  8 kv heads, D 128, us:
 //   units, keys       waves x workgroups
-//   8, 1000           4x1 13.0, 4x4 12.1     8, 4000     4x6 14.3, 4x12 12.6
-//   32, 600           4x1 10.4, 4x2 12.3     32, 2100    4x3 16.9, 4x6 14.5, 4x8 14.8
-//   64, 2100          4x2 20.6, 4x3 19.8     88, 3000    4x1 31.5, 4x2 28.2
-//   128, 2100         4x1 25.8, 4x2 29.1     128, 8000   4x1 97.5, 4x2 93.2
+//   8, 1000           4x1 13.4, 4x4 11.6     8, 4000     4x6 13.9, 4x12 12.6
+//   32, 600           4x1 10.3, 4x2 12.2     32, 2100    4x3 16.2, 4x6 13.5, 4x8 13.7
+//   64, 2100          4x2 20.8, 4x3 19.6     88, 3000    4x1 31.5, 4x2 28.3
+//   128, 2100         4x1 25.8, 4x2 28.9     128, 8000   4x1 98.1, 4x2 92.9
 //   264, 1000         2x1 25.3, 4x1 30.9
 //   576, 1000         2x1 58.2, 4x1 50.9; of 300 23.0, 22.8
 //   1024, 1000        2x1 90.3, 4x1 90.8 (60% of the keys shared by all 40.3, 42.6)
 //   1248, 1000        2x1 113, 4x1 108       4096, 2100  2x1 684, 4x1 686 (335, 353)
 // D 64, whose steps and join are shorter: 512 of 2100 2x1 41.5, 4x1 43.5 (shared 32.5,
 // 30.9); 1024 of 1000 40.5, 41.5 (26.7, 29.9); 128 of 2100 4x1 19.3, 8x1 16.8; 16 of
-// 1000 8x1 9.8, 4x1 10.6, 4x4 11.6, of 2100 4x3 12.8, 4x8 12.0.
+// 1000 8x1 9.8, 4x1 10.4, 4x4 11.6, of 2100 4x4 11.9, 4x8 11.5.
 // A workgroup's steps go as 1 / workgroups and the join's reads as their number, so the
 // best number goes as the root of the steps: 16, 32, 64 workgroups to 1 unit of 8000 keys
 // 15.7, 17.0, -; of 16000 19.6, 18.7, 22.8; of 32000 26.7, 22.7, 25.0; of 128000 72.8, 46.7,
