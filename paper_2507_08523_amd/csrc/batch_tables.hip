@@ -26,11 +26,11 @@ constexpr int kBlock = 16;
 constexpr int kScanThreads = 1024;
 constexpr int kMaxRequests = 1 << 20;
 // Most rows (of extend; blocks that there can be, of release) that the workgroup of
-// the sums fills in itself.  us in one launch, in two: 512 requests of a row 5.2, 9.3;
-// one request of 4096 rows 5.3, 7.5; 64 requests of 128 rows 10.3, 10.9, of 256 17.2,
-// 10.5.  Released ids (of a table of as many or more): 512 3.7, 5.8; 4096 5.4, 5.9;
-// 8192 8.1, 6.0.
-constexpr int kOneFill = 4096, kOneRelease = 8192;
+// the sums fills in itself.  us in one launch, in two: 512 requests of a row 5.5, 8.6;
+// one request of 4096 rows 5.9, 7.3, of 8192 7.6, 7.7; 64 requests of 96 rows 9.3, 9.9,
+// of 128 11.0, 9.6; 512 of 12 10.9, 12.4, of 16 13.1, 11.4.  Released ids (of a table of
+// as many or more): 512 3.7, 5.8; 4096 5.4, 5.9; 8192 8.1, 6.0.
+constexpr int kOneFill = 6144, kOneRelease = 8192;
 
 // What is refused on the device (bits of *status).
 enum { kNoBlocks = 1, kTooLong = 2, kTooManyRows = 4, kBadValue = 8 };
@@ -83,17 +83,15 @@ struct Growth {
   __device__ __forceinline__ int start(int r) const { return seq_lens[r] - (cu_q[r + 1] - cu_q[r]); }
 };
 
-// Table entry of the e-th block taken (a block of request r).
-__device__ __forceinline__ void put_block(int e, int r, const Growth& g, int32_t* block_tables, int max_blocks,
-                                          const int32_t* free_ids, int first_id) {
-  block_tables[size_t(r) * max_blocks + blocks_of(g.start(r)) + (e - g.cu_blocks[r])] = free_ids[first_id + e];
-}
-
-// Slot of row i (a row of request r).
-__device__ __forceinline__ int slot_of(int i, int r, const Growth& g, const int32_t* block_tables, int max_blocks,
-                                       const int32_t* free_ids, int first_id, int num_blocks) {
+// Slot of row i, a row of request r.  A block that is taken holds a new token at its
+// offset 0 (it starts at or behind the tokens held), so that the rows whose position is
+// a multiple of 16 are the blocks taken, one by one: each writes its table entry.
+__device__ __forceinline__ int place_row(int i, int r, const Growth& g, int32_t* block_tables, int max_blocks,
+                                         const int32_t* free_ids, int first_id, int num_blocks) {
   const int start = g.start(r), pos = start + (i - g.cu_q[r]), lb = pos / kBlock, had = blocks_of(start);
-  const int id = lb < had ? block_tables[size_t(r) * max_blocks + lb] : free_ids[first_id + g.cu_blocks[r] + lb - had];
+  int32_t* entry = block_tables + size_t(r) * max_blocks + lb;
+  const int id = lb < had ? *entry : free_ids[first_id + g.cu_blocks[r] + lb - had];
+  if (pos % kBlock == 0) *entry = id;
   return id >= 0 && id < num_blocks ? id * kBlock + pos % kBlock : -1;
 }
 
@@ -153,19 +151,31 @@ __global__ __launch_bounds__(kScanThreads) void extend_scan_kernel(
   if constexpr (FILL) {
     __syncthreads();
     const Growth g{k_seq, k_cu, k_cb};
-    for (int e = threadIdx.x; e < n_new; e += kScanThreads)
-      put_block(e, owner(k_cb, 0, B, e), g, block_tables, max_blocks, free_ids, int(had));
     for (int i = threadIdx.x; i < max_rows; i += kScanThreads)
-      slot_map[i] = i < n_rows ? slot_of(i, owner(k_cu, 0, B, i), g, block_tables, max_blocks, free_ids, int(had),
-                                         num_blocks)
+      slot_map[i] = i < n_rows ? place_row(i, owner(k_cu, 0, B, i), g, block_tables, max_blocks, free_ids, int(had),
+                                           num_blocks)
                                : -1;
   }
 }
 
 // Table entries and slots from the sums, for many rows: 1024 rows a workgroup, whose
-// requests it looks up once.  What bounds the two launches is their latency (512
-// requests, 1.0 M rows 12 us, 16 K rows 13 us); sums copied to LDS first changed nothing.
+// requests it looks up once, 64 probes a round trip (512 requests, 1.0 M rows: 8.4 us by
+// halves and with the blocks taken looked up on their own, 5.5 to 6.8 so).
 constexpr int kFillThreads = 256, kFillRows = 1024;
+
+// owner() by a wave, sums[0] <= x.
+__device__ __forceinline__ int wave_owner(const int32_t* sums, int n, int x) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int step = (hi - lo + 63) / 64, at = lo + lane * step;
+    // (the lanes that hold are the first ones)
+    const uint64_t holds = __ballot(at < hi && (lane == 0 || sums[at] <= x));
+    lo += (63 - __builtin_clzll(holds)) * step;
+    hi = min(lo + step, hi);
+  }
+  return lo;
+}
 
 __global__ __launch_bounds__(kFillThreads) void extend_fill_kernel(
     int32_t* __restrict__ block_tables, int B, int max_blocks, const int32_t* __restrict__ free_ids,
@@ -173,20 +183,22 @@ __global__ __launch_bounds__(kFillThreads) void extend_fill_kernel(
     const int32_t* __restrict__ cu_q, const int32_t* __restrict__ cu_blocks, int32_t* __restrict__ slot_map,
     int max_rows) {
   __shared__ int s_of[2];
-  const int n_rows = cu_q[B], n_new = cu_blocks[B];
-  const int first_id = *taken_out - n_new;
+  const int n_rows = cu_q[B], first_id = *taken_out - cu_blocks[B];
   const Growth g{seq_lens, cu_q, cu_blocks};
-  for (int64_t e = int64_t(blockIdx.x) * kFillThreads + threadIdx.x; e < n_new; e += int64_t(gridDim.x) * kFillThreads)
-    put_block(int(e), owner(cu_blocks, 0, B, int(e)), g, block_tables, max_blocks, free_ids, first_id);
   const int64_t i0 = int64_t(blockIdx.x) * kFillRows, i1 = min(i0 + kFillRows, int64_t(max_rows));
-  if (threadIdx.x < 2 && i0 < n_rows)
-    s_of[threadIdx.x] = owner(cu_q, 0, B, threadIdx.x ? int(min(i1, int64_t(n_rows))) - 1 : int(i0));
+  const int wave = threadIdx.x >> 6;
+  if (wave < 2 && i0 < n_rows) {
+    const int r = wave_owner(cu_q, B, int(wave ? min(i1, int64_t(n_rows)) - 1 : i0));
+    if ((threadIdx.x & 63) == 0) s_of[wave] = r;
+  }
   __syncthreads();
-  for (int64_t j = i0 + threadIdx.x; j < i1; j += kFillThreads) {
-    const int i = int(j);
-    slot_map[i] = i < n_rows ? slot_of(i, owner(cu_q, s_of[0], s_of[1] + 1, i), g, block_tables, max_blocks, free_ids,
-                                       first_id, num_blocks)
-                             : -1;
+#pragma unroll
+  for (int u = 0; u < kFillRows / kFillThreads; ++u) {
+    const int64_t i = i0 + u * kFillThreads + threadIdx.x;
+    if (i < i1)
+      slot_map[i] = i < n_rows ? place_row(int(i), owner(cu_q, s_of[0], s_of[1] + 1, int(i)), g, block_tables,
+                                           max_blocks, free_ids, first_id, num_blocks)
+                               : -1;
   }
 }
 
@@ -344,7 +356,8 @@ extern "C" int ilpc_extend_tables(int32_t* block_tables, int32_t max_blocks, int
   else launch_scan(extend_scan_kernel<false>);
   const int rc = launch_status(fn);
   if (rc != ILPC_OK || one) return rc;
-  const unsigned grid = unsigned((int64_t(max_rows) + kFillRows - 1) / kFillRows) + (max_rows == 0);
+  if (max_rows == 0) return rc;
+  const unsigned grid = unsigned((int64_t(max_rows) + kFillRows - 1) / kFillRows);
   hipLaunchKernelGGL(extend_fill_kernel, dim3(grid), dim3(kFillThreads), 0, s, block_tables, B, max_blocks, free_ids,
                      taken_out, num_blocks, seq_lens, cu_q, cu_blocks, slot_map, max_rows);
   return launch_status(fn);
