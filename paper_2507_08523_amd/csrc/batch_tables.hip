@@ -251,10 +251,20 @@ __global__ __launch_bounds__(kScanThreads) void release_scan_kernel(
 __global__ __launch_bounds__(kFillThreads) void release_fill_kernel(
     const int32_t* __restrict__ block_tables, int B, int max_blocks, const int32_t* __restrict__ first_block,
     const int32_t* __restrict__ cu_blocks, const int32_t* __restrict__ taken_out, int32_t* __restrict__ free_ids) {
-  const int n = cu_blocks[B], at = *taken_out;
-  for (int64_t e = int64_t(blockIdx.x) * kFillThreads + threadIdx.x; e < n; e += int64_t(gridDim.x) * kFillThreads) {
-    const int r = owner(cu_blocks, 0, B, int(e));
-    free_ids[at + e] = block_tables[size_t(r) * max_blocks + first_block[r] + (e - cu_blocks[r])];
+  __shared__ int s_of[2];
+  const int n = cu_blocks[B], at = *taken_out, wave = threadIdx.x >> 6;
+  for (int64_t e0 = int64_t(blockIdx.x) * kFillThreads; e0 < n; e0 += int64_t(gridDim.x) * kFillThreads) {
+    __syncthreads();
+    if (wave < 2) {
+      const int r = wave_owner(cu_blocks, B, int(wave ? min(e0 + kFillThreads, int64_t(n)) - 1 : e0));
+      if ((threadIdx.x & 63) == 0) s_of[wave] = r;
+    }
+    __syncthreads();
+    const int64_t e = e0 + threadIdx.x;
+    if (e < n) {
+      const int r = owner(cu_blocks, s_of[0], s_of[1] + 1, int(e));
+      free_ids[at + e] = block_tables[size_t(r) * max_blocks + first_block[r] + (e - cu_blocks[r])];
+    }
   }
 }
 
