@@ -458,7 +458,8 @@ int64_t column_tiles(int64_t max_q_len, int Hq, int Hkv) {
 // other at about 1 us: four waves to a unit, and several workgroups (whose states a
 // second launch joins, 2 us), while every workgroup has a CU to itself; else two;
 // and four again, quarters of the load, where twos leave some CUs twice the work of
-// others.  One wave to a unit is never better than two.  8 kv heads, D 128, us:
+// others.  One wave to a unit is better than two only for a few steps of very many units,
+// all starts.  8 kv heads, D 128, us:
 //   units, keys       waves x workgroups
 //   8, 1000           4x1 13.4, 4x4 11.6     8, 4000     4x6 13.9, 4x12 12.6
 //   32, 600           4x1 10.3, 4x2 12.2     32, 2100    4x3 16.2, 4x6 13.5, 4x8 13.7
@@ -471,15 +472,21 @@ int64_t column_tiles(int64_t max_q_len, int Hq, int Hkv) {
 // D 64, whose steps and join are shorter: 512 of 2100 2x1 41.5, 4x1 43.5 (shared 32.5,
 // 30.9); 1024 of 1000 40.5, 41.5 (26.7, 29.9); 128 of 2100 4x1 19.3, 8x1 16.8; 16 of
 // 1000 8x1 9.8, 4x1 10.4, 4x4 11.6, of 2100 4x4 11.9, 4x8 11.5.
+// Short contexts, 1x1 and 2x1: 2048 units of 32 keys 11.4, 15.3, of 96 22.4, 24.0, 4096 22.0,
+// 28.1 and 39.4, 40.5, 1536 9.8, 11.5 and 19.1, 20.8, 1024 9.7, 8.6; D 64, 2048 of 96 13.7,
+// 15.1, 1536 11.9, 10.3.
 // A workgroup's steps go as 1 / workgroups and the join's reads as their number, so the
 // best number goes as the root of the steps: 16, 32, 64 workgroups to 1 unit of 8000 keys
 // 15.7, 17.0, -; of 16000 19.6, 18.7, 22.8; of 32000 26.7, 22.7, 25.0; of 128000 72.8, 46.7,
 // 39.0.
-Plan stream_plan(int64_t units, int64_t max_blocks, int D) {
+// A pair's tiles find each other's keys in L2, and four waves are better up to two units to
+// a CU: 320 units of 2600 keys, 2 tiles a pair 2x1 52.4, 4x1 43.2, 8 tiles 50.5, 38.6; 512
+// of 1300 32.8, 34.6 and 31.8, 28.9; but 576 of 600 24.9, 26.1.
+Plan stream_plan(int64_t units, int64_t n_ct, int64_t max_blocks, int D) {
   const int64_t cus = ilpc::device_cus(), steps = (max_blocks * kBlock + kStepKeys - 1) / kStepKeys;
-  const bool four = units <= cus || (D == 64 && units <= 3 * cus) ||
+  const bool four = units <= cus || (D == 64 && units <= 3 * cus) || (n_ct > 1 && units <= 2 * cus) ||
                     (steps >= 32 && ((units > 2 * cus && units <= 3 * cus) || (units > 4 * cus && units <= 5 * cus)));
-  if (!four) return {2, 1};
+  if (!four) return {steps <= 4 && units > (D == 64 ? 7 : 5) * cus ? 1 : 2, 1};
   const int64_t room = std::min<int64_t>(cus / units, kMaxGroups);
   if (room >= 3 && steps >= (D == 64 ? 48 : 32))
     return {4, int(std::min({room, steps / 8, int64_t(std::sqrt(double(steps)))}))};
@@ -530,7 +537,7 @@ extern "C" int ilpc_diff_attn_workspace_bytes(int32_t B, int32_t max_q_len, int3
   if (ilpc::device_cus() <= 0) return ilpc::set_error(ILPC_EHIP, "%s: cannot query the device", fn);
   if (many_columns(B, max_q_len, Hq, Hkv, D)) return ILPC_OK;
   const int64_t units = int64_t(B) * Hkv * column_tiles(max_q_len, Hq, Hkv);
-  *bytes = part_bytes(units, D, stream_plan(units, max_blocks, D).groups);
+  *bytes = part_bytes(units, D, stream_plan(units, column_tiles(max_q_len, Hq, Hkv), max_blocks, D).groups);
   return ILPC_OK;
 }
 
@@ -572,7 +579,7 @@ extern "C" int ilpc_paged_diff_attn(const uint16_t* q, int64_t q_stride, int32_t
     return ILPC_OK;
   }
   const int64_t n_ct = column_tiles(max_q_len, Hq, Hkv), units = int64_t(B) * Hkv * n_ct;
-  const Plan plan = stream_plan(units, max_blocks, D);
+  const Plan plan = stream_plan(units, n_ct, max_blocks, D);
   const size_t need = part_bytes(units, D, plan.groups);
   if (need && (!workspace || workspace_bytes < need || !aligned16(workspace)))
     return set_error(ILPC_EINVAL, "%s: workspace must be %zu bytes, 16-byte aligned", fn, need);
@@ -589,10 +596,12 @@ extern "C" int ilpc_paged_diff_attn(const uint16_t* q, int64_t q_stride, int32_t
                        int(layout == ILPC_DIFF_ROPE), ep, out, int(n_ct), plan.groups, part_o, part_ml);
   };
   if (D == 128) {
-    if (plan.waves == 2) launch(diff_stream_kernel<128, 2>);
+    if (plan.waves == 1) launch(diff_stream_kernel<128, 1>);
+    else if (plan.waves == 2) launch(diff_stream_kernel<128, 2>);
     else launch(diff_stream_kernel<128, 4>);
   } else {
-    if (plan.waves == 2) launch(diff_stream_kernel<64, 2>);
+    if (plan.waves == 1) launch(diff_stream_kernel<64, 1>);
+    else if (plan.waves == 2) launch(diff_stream_kernel<64, 2>);
     else if (plan.waves == 4) launch(diff_stream_kernel<64, 4>);
     else launch(diff_stream_kernel<64, 8>);
   }

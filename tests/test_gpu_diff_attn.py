@@ -423,3 +423,14 @@ def test_long_contexts_and_wide_tables(L, cols, D):
     # the keys over up to 64 workgroups, whose ranges need not all hold keys
     b = Batch([L, 3 + L // 3], [1, 2], 4, 1, D, seed=L, spare_cols=cols)
     b.check(b.run())
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("longest", [16, 100, 128])
+def test_many_requests_with_short_contexts(longest, D):
+    # more (request, kv head) pairs than seven to a compute unit, each of a few keys; some without rows
+    rng = np.random.default_rng(longest)
+    n = 7 * torch.cuda.get_device_properties(0).multi_processor_count // 8 + 5
+    lens = [longest, *(int(x) for x in rng.integers(1, longest + 1, n - 1))]
+    b = Batch(lens, [1, *(int(x) for x in rng.integers(0, 2, n - 1))], 16, 8, D, seed=D)
+    b.check(b.run())
