@@ -454,3 +454,50 @@ def test_rows_of_ended_requests_are_used_again():
         assert ints(dt.status) == [0] and ints(pc.free_taken) == [0]
         assert sorted(ints(pc.free_ids)) == list(range(16, 25))
     assert ints(dt.block_tables[0])[:2] == [4, 7]
+
+
+@pytest.mark.parametrize("B,grow", [(5000, 5000), (5000, 3), (70000, 900), (4097, 1)])
+def test_thousands_of_requests(B, grow):
+    """Many requests of which few or all grow: which of them a row belongs to is found over long runs of
+    equal sums."""
+    rng = np.random.default_rng(B + grow)
+    tables, start, _, free, taken, nb = make(B, 0, 20, 0, 5, spare=4000)
+    new, which = np.zeros(B, int), rng.permutation(B)[:grow]
+    new[which] = rng.integers(1, 3 if grow > 4000 else 40, grow)
+    new[-1] += 1
+    tables = np.pad(tables, ((0, 0), (0, 3)), constant_values=-1)
+    rows = int(new.sum()) + 7
+    want = extend_ref(tables, start.tolist(), new.tolist(), free.tolist(), taken, nb, rows)
+    assert want[-1] == 0
+    same(State(tables, start, new, free, taken, nb, rows).extend(), want)
+    first, seq = (start // 2 + BLOCK - 1) // BLOCK, (start + new) * (new > 0)
+    gone = int(np.maximum(-(-seq // BLOCK) - first, 0).sum())
+    free = np.arange(gone + 5)
+    want = release_ref(want[0], first.tolist(), seq.tolist(), free.tolist(), gone + 5)
+    assert want[-1] == 0
+    f, cb, k, st = dev(free), dev([9] * (B + 1)), dev([gone + 5]), dev([9])
+    t = State(tables, start, new, make(B, 0, 20, 0, 5, spare=4000)[3], taken, nb, rows)
+    t.extend()
+    ilpc.release_tables(t.t, dev(first), dev(seq), f, k, cb, k, st)
+    torch.cuda.synchronize()
+    assert (ints(f), ints(cb), ints(k)[0], ints(st)[0]) == (list(map(int, want[0])), list(map(int, want[1])),
+                                                           int(want[2]), 0)
+
+
+@pytest.mark.parametrize("kind", ["blocks", "rows", "long"])
+def test_refused_batches_of_many_rows_change_nothing(kind):
+    tables, start, new, free, taken, nb = make(70, 0, 60, 300, 3)
+    rows = int(new.sum())
+    if kind == "blocks":
+        free = free[:-8]
+    elif kind == "rows":
+        rows -= 1
+    else:
+        new[5] = 16 * tables.shape[1] - start[5] + 1
+        rows += 1000
+    want = extend_ref(tables, start.tolist(), new.tolist(), free.tolist(), taken, nb, rows)
+    s = State(tables, start, new, free, taken, nb, rows)
+    got = s.extend()
+    torch.cuda.synchronize()
+    assert rows > 6144 and ints(s.st)[0] & {"blocks": 1, "long": 2, "rows": 4}[kind]
+    same(got[:-1], want[:-1])
