@@ -40,11 +40,12 @@ __device__ __forceinline__ float add_across_halves(float x) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// Map that 16-dimension chunk kc of a head belongs to: its half of D, or in the
-// pair layout its half of each half of D.
+// The i-th 16-dimension chunk of a head that belongs to a map: of its half of D, or in
+// the pair layout of its half of each half of D.
 template <int D>
-__device__ __forceinline__ int diff_map_of_chunk(int kc, int pairs) {
-  return pairs ? (kc / (D / 64)) & 1 : kc / (D / 32);
+__device__ __forceinline__ int diff_chunk_of_map(int map, int i, int pairs) {
+  constexpr int kQuarter = D / 64;  // chunks of a quarter
+  return pairs ? (i / kQuarter * 2 + map) * kQuarter + i % kQuarter : map * (2 * kQuarter) + i;
 }
 
 // Arguments of a launch, already checked.

@@ -95,17 +95,24 @@ __global__ __launch_bounds__(64 * group_waves(W), 2) void diff_stream_kernel(
   const unsigned nb = gridDim.x, per = nb >> 3, extra = nb & 7u;
   const unsigned x = blockIdx.x & 7u, i = blockIdx.x >> 3;
   const unsigned group = x * per + min(x, extra) + i;
-  const int64_t item = int64_t(group) * (kWavesPerGroup / W) + wave / W;
-  const int64_t n_items = int64_t(n_req) * Hkv * n_split * n_ct;
-  const bool in_grid = item < n_items;
+  const unsigned item = group * (kWavesPerGroup / W) + wave / W;  // (fewer than 2^31 of them)
+  const bool in_grid = item < unsigned(n_req) * unsigned(Hkv) * unsigned(n_split) * unsigned(n_ct);
   // item = ((kv head * n_req + request) * n_ct + column tile) * n_split + range of the keys
-  const int sp = in_grid ? int(item % n_split) : 0, unit = in_grid ? int(item / n_split) : 0;
-  const int ct = unit % n_ct, pair = unit / n_ct;
-  const int h = pair / n_req, r = pair % n_req;
+  const unsigned all = in_grid ? item : 0u, unit = all / unsigned(n_split), pair = unit / unsigned(n_ct);
+  const int sp = int(all - unit * unsigned(n_split)), ct = int(unit - pair * unsigned(n_ct));
+  const int h = int(pair / unsigned(n_req)), r = int(pair % unsigned(n_req));
   const int G = Hq / Hkv;
 
-  const int q0 = cu_q[r], q_end = cu_q[r + 1], q_len = q_end - q0;
-  const int L = min(seq_lens[r], max_blocks * kBlock);
+  const int32_t* bt = block_tables + size_t(r) * max_blocks;
+  auto load_ids = [&](int window) { return bt[min(window * 64 + lane, max_blocks - 1)]; };
+  const int q0 = cu_q[r], q_end = cu_q[r + 1], q_len = q_end - q0, L_in = seq_lens[r];
+  // The first 4096 keys' block ids come with the lengths, which say where a range begins.
+  constexpr int kFirst = 5;
+  int first_ids[kFirst];
+#pragma unroll
+  for (int i = 0; i < kFirst; ++i) first_ids[i] = load_ids(i);
+  asm volatile("" : "+v"(first_ids[0]), "+v"(first_ids[1]), "+v"(first_ids[2]), "+v"(first_ids[3]), "+v"(first_ids[4]));
+  const int L = min(L_in, max_blocks * kBlock);
   const int col0 = ct * kTileCols, n_cols = min(min(q_len, max_q_len) * G - col0, kTileCols);
   const bool valid = in_grid && q0 >= 0 && q_end <= n_rows && q_len > 0 && q_len <= L && n_cols > 0;
 
@@ -121,14 +128,11 @@ __global__ __launch_bounds__(64 * group_waves(W), 2) void diff_stream_kernel(
   const int t = colc / G, head = h * G + (colc - t * G);
   if (valid) {
     const int pos = L - q_len + t;  // keys 0 .. pos are visible to this column
+    // (all loads of Q at once: a load under the test of each chunk's map is a round trip each)
     const uint16_t* qr = q + int64_t(q0 + t) * q_stride + size_t(head) * D;
+    u32x4 qc[kDch / 2];
 #pragma unroll
-    for (int kc = 0; kc < kDch; ++kc) {
-      const u32x4 zero = {0, 0, 0, 0};
-      q_lds[wave][kc][lane] =
-          diff_map_of_chunk<D>(kc, pairs_layout) == map ? *(const u32x4*)(qr + kc * 16 + hh * 8) : zero;
-    }
-    const int32_t* bt = block_tables + size_t(r) * max_blocks;
+    for (int i = 0; i < kDch / 2; ++i) qc[i] = *(const u32x4*)(qr + diff_chunk_of_map<D>(map, i, pairs_layout) * 16 + hh * 8);
     const int n_blk = (L + kBlock - 1) / kBlock;
     // keys past the last column's position are not visited (and their V rows zeroed)
     const int key_end = L - q_len + (col0 + n_cols - 1) / G + 1;
@@ -144,15 +148,16 @@ __global__ __launch_bounds__(64 * group_waves(W), 2) void diff_stream_kernel(
     // picks its two with readlane.  Ids past the request's blocks or outside the
     // pool read block 0 (those keys are masked and their V rows zeroed, or the
     // request's output is unspecified).
-    auto load_ids = [&](int window) { return bt[min(window * 64 + lane, max_blocks - 1)]; };
-    int win = (2 * s_begin) >> 6;
-    int ids0, ids1;
-    if (win & 1) {
-      ids1 = load_ids(win);
-      ids0 = load_ids(win + 1);
-    } else {
-      ids0 = load_ids(win);
-      ids1 = load_ids(win + 1);
+    const int s_first = min(s_begin, n_steps_all - 1);  // (an empty range reads a step that is there, and leaves it)
+    int win = (2 * s_first) >> 6;
+    int ids0 = first_ids[0], ids1 = first_ids[1];  // of the even and the odd one of windows win, win + 1
+#pragma unroll
+    for (int i = 1; i < kFirst - 1; ++i)
+      if (win == i) (i & 1 ? ids1 : ids0) = first_ids[i], (i & 1 ? ids0 : ids1) = first_ids[i + 1];
+    if (win >= kFirst - 1) {
+      const int a = load_ids(win), b = load_ids(win + 1);
+      ids0 = win & 1 ? b : a;
+      ids1 = win & 1 ? a : b;
     }
     auto block_id = [&](int lb) {
       const int id = (win & 1) ? __builtin_amdgcn_readlane(ids1, lb & 63) : __builtin_amdgcn_readlane(ids0, lb & 63);
@@ -260,7 +265,13 @@ __global__ __launch_bounds__(64 * group_waves(W), 2) void diff_stream_kernel(
     // computation that frees their registers.
     StepRegs<D> ra, rb;
     int s = s_begin;
-    if (s < n_steps) load(s, ra);
+    load(s_first, ra);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < kDch / 2; ++i) {
+      q_lds[wave][diff_chunk_of_map<D>(map, i, pairs_layout)][lane] = qc[i];
+      q_lds[wave][diff_chunk_of_map<D>(1 - map, i, pairs_layout)][lane] = u32x4{0, 0, 0, 0};
+    }
     for (; s + 1 < n_steps; s += 2) {
       load(s + 1, rb);
       __builtin_amdgcn_sched_barrier(0);
@@ -368,12 +379,11 @@ __global__ __launch_bounds__(64 * kJoinWaves) void diff_join_kernel(
   constexpr int kPer = D / 64;  // dimensions of a lane
   typedef float vec_t __attribute__((ext_vector_type(kPer)));
   const int lane = threadIdx.x & 63;
-  const int64_t w = int64_t(blockIdx.x) * kJoinWaves + (threadIdx.x >> 6);
-  const int c = int(w % cols_cap);
-  const int64_t unit = w / cols_cap;
-  const int ct = int(unit % n_ct), pair = int(unit / n_ct);
-  if (pair >= n_req * Hkv) return;
-  const int h = pair / n_req, r = pair % n_req;
+  const unsigned w = __builtin_amdgcn_readfirstlane(blockIdx.x * kJoinWaves + (threadIdx.x >> 6));
+  const unsigned unit = w / unsigned(cols_cap), pair = unit / unsigned(n_ct);
+  const int c = int(w - unit * unsigned(cols_cap)), ct = int(unit - pair * unsigned(n_ct));
+  if (pair >= unsigned(n_req) * unsigned(Hkv)) return;
+  const int h = int(pair / unsigned(n_req)), r = int(pair % unsigned(n_req));
   const int G = Hq / Hkv, col = ct * kTileCols + c;
   const int t = col / G, head = h * G + (col - t * G);
 
@@ -392,14 +402,27 @@ __global__ __launch_bounds__(64 * kJoinWaves) void diff_join_kernel(
       for (int mp = 0; mp < 2; ++mp)
         v[u][mp] = *(const vec_t*)(po + (size_t(min(k + u, n_split - 1)) * kNext + mp * kTileCols) * D);
   };
-  const int q0 = cu_q[r], q_end = cu_q[r + 1], L_in = seq_lens[r];
-  const float lam = ep.lambda[head];
+  int q0 = cu_q[r], q_end = cu_q[r + 1], L_in = seq_lens[r];
+  float lam = ep.lambda[head];
   float2 ml[2];
 #pragma unroll
   for (int mp = 0; mp < 2; ++mp)
     ml[mp] = *(const float2*)(part_ml + (slot0 + mp * kTileCols + size_t(min(lane, n_split - 1)) * kNext) * 2);
   load(0);
-  __builtin_amdgcn_sched_barrier(0);
+  // (pinned here: they would sink behind the test of the lengths)
+  asm volatile("" : "+s"(q0), "+s"(q_end), "+s"(L_in), "+s"(lam), "+v"(ml[0].x), "+v"(ml[0].y), "+v"(ml[1].x), "+v"(ml[1].y));
+#pragma unroll
+  for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+    for (int mp = 0; mp < 2; ++mp) {
+      if constexpr (kPer == 2) {
+        asm volatile("" : "+v"(v[u][mp]));
+      } else {
+        float x = v[u][mp][0];
+        asm volatile("" : "+v"(x));
+        v[u][mp][0] = x;
+      }
+    }
   const int q_len = q_end - q0, L = min(L_in, max_blocks * kBlock);
   if (q0 < 0 || q_end > n_rows || q_len <= 0 || q_len > L || col >= min(q_len, max_q_len) * G) return;
 
