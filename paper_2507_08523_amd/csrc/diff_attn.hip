@@ -80,7 +80,7 @@ __global__ __launch_bounds__(64 * group_waves(W), 2) void diff_stream_kernel(
   constexpr int kKBytes = kWavesPerGroup * kStepKeys * kRowPieces * 16;
   static_assert(kOBytes >= kQBytes + kKBytes, "the join's rows are the larger");
   __shared__ __attribute__((aligned(16))) uint8_t lds[kOBytes];
-  __shared__ float s_m[kWavesPerGroup][kCols], s_l[kWavesPerGroup][kCols];
+  __shared__ float s_m[kWavesPerGroup][kCols], s_l[kWavesPerGroup][kCols], s_lambda[kWavesPerGroup][kCols];
   u32x4(*q_lds)[kDch][64] = reinterpret_cast<u32x4(*)[kDch][64]>(lds);
   u32x4(*k_lds)[kStepKeys][kRowPieces] = reinterpret_cast<u32x4(*)[kStepKeys][kRowPieces]>(lds + kQBytes);
   const int lane = threadIdx.x & 63;
@@ -126,7 +126,9 @@ __global__ __launch_bounds__(64 * group_waves(W), 2) void diff_stream_kernel(
   const bool col_valid = valid && nc < n_cols;
   const int colc = col0 + (col_valid ? nc : max(n_cols, 1) - 1);
   const int t = colc / G, head = h * G + (colc - t * G);
+  float lambda = 0.f;
   if (valid) {
+    lambda = ep.lambda[head];
     const int pos = L - q_len + t;  // keys 0 .. pos are visible to this column
     // (all loads of Q at once: a load under the test of each chunk's map is a round trip each)
     const uint16_t* qr = q + int64_t(q0 + t) * q_stride + size_t(head) * D;
@@ -272,6 +274,7 @@ __global__ __launch_bounds__(64 * group_waves(W), 2) void diff_stream_kernel(
       q_lds[wave][diff_chunk_of_map<D>(map, i, pairs_layout)][lane] = qc[i];
       q_lds[wave][diff_chunk_of_map<D>(1 - map, i, pairs_layout)][lane] = u32x4{0, 0, 0, 0};
     }
+    asm volatile("" : "+v"(lambda));  // (asked for with Q, and not at the end)
     for (; s + 1 < n_steps; s += 2) {
       load(s + 1, rb);
       __builtin_amdgcn_sched_barrier(0);
@@ -290,6 +293,10 @@ __global__ __launch_bounds__(64 * group_waves(W), 2) void diff_stream_kernel(
   // no wave reads Q from there any more), then a thread sums 4 dimensions of a
   // column over the waves, both maps, with weights 2^(m_k - M).
   float(*so)[kCols][kRow] = reinterpret_cast<float(*)[kCols][kRow]>(lds);
+  constexpr int kPer = D / 4;  // threads to a column
+  const int d = lane % kPer * 4;
+  f32x4 nw = {1.f, 1.f, 1.f, 1.f};
+  if (ep.norm_w && n_split == 1) nw = *(const f32x4*)(ep.norm_w + d);
   __syncthreads();
   if (col_valid) {
 #pragma unroll
@@ -302,14 +309,15 @@ __global__ __launch_bounds__(64 * group_waves(W), 2) void diff_stream_kernel(
     if (hh == 0) {
       s_m[wave][n] = m_run;
       s_l[wave][n] = l_tot;
+      s_lambda[wave][n] = lambda;
     }
   }
+  asm volatile("" : "+v"(nw));  // (on its way since before the barrier)
   __syncthreads();
   if (!valid) return;
   const int w0 = wave / W * W;     // first wave of the pair
-  constexpr int kPer = D / 4;      // threads to a column
   for (int u = (wave - w0) * 64 + lane; u < n_cols * kPer; u += W * 64) {
-    const int c = u / kPer, d = u % kPer * 4;
+    const int c = u / kPer;
     f32x4 acc[2];
     float mx[2], den[2];
 #pragma unroll
@@ -341,7 +349,7 @@ __global__ __launch_bounds__(64 * group_waves(W), 2) void diff_stream_kernel(
     }
     if (n_split > 1) continue;
     const int tt = (col0 + c) / G, hd = h * G + (col0 + c - tt * G);
-    const float w1 = 1.f / den[0], w2 = ep.lambda[hd] / den[1];
+    const float w1 = 1.f / den[0], w2 = s_lambda[w0][c] / den[1];
     f32x4 y;
     float sq = 0.f;
 #pragma unroll
@@ -354,7 +362,6 @@ __global__ __launch_bounds__(64 * group_waves(W), 2) void diff_stream_kernel(
 #pragma unroll
       for (int off = 1; off < kPer; off <<= 1) sq += __shfl_xor(sq, off);
       const float inv = rsqrtf(sq * (1.f / D) + ep.eps);
-      const f32x4 nw = *(const f32x4*)(ep.norm_w + d);
 #pragma unroll
       for (int e = 0; e < 4; ++e) f[e] *= inv * nw[e];
     }
