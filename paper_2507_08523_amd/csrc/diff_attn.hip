@@ -491,17 +491,17 @@ int64_t column_tiles(int64_t max_q_len, int Hq, int Hkv) {
 // others.  One wave to a unit is better than two only for a few steps of very many units,
 // all starts.  8 kv heads, D 128, us:
 //   units, keys       waves x workgroups
-//   8, 1000           4x1 13.4, 4x4 11.6     8, 4000     4x6 13.9, 4x12 12.6
-//   32, 600           4x1 10.3, 4x2 12.2     32, 2100    4x3 16.2, 4x6 13.5, 4x8 13.7
-//   64, 2100          4x2 20.8, 4x3 19.6     88, 3000    4x1 31.5, 4x2 28.3
-//   128, 2100         4x1 25.8, 4x2 28.9     128, 8000   4x1 98.1, 4x2 92.9
-//   264, 1000         2x1 25.3, 4x1 30.9
-//   576, 1000         2x1 58.2, 4x1 50.9; of 300 23.0, 22.8
-//   1024, 1000        2x1 90.3, 4x1 90.8 (60% of the keys shared by all 40.3, 42.6)
-//   1248, 1000        2x1 113, 4x1 108       4096, 2100  2x1 684, 4x1 686 (335, 353)
-// D 64, whose steps and join are shorter: 512 of 2100 2x1 41.5, 4x1 43.5 (shared 32.5,
-// 30.9); 1024 of 1000 40.5, 41.5 (26.7, 29.9); 128 of 2100 4x1 19.3, 8x1 16.8; 16 of
-// 1000 8x1 9.8, 4x1 10.4, 4x4 11.6, of 2100 4x4 11.9, 4x8 11.5.
+//   8, 1000           4x1 12.6, 4x4 11.4     8, 4000     4x6 13.3, 4x12 12.1
+//   32, 600           4x1 9.9, 4x2 11.5      32, 2100    4x3 15.1, 4x6 12.5, 4x8 12.6
+//   64, 2100          4x2 19.0, 4x3 17.8     88, 2100    4x1 22.8, 4x2 21.9
+//   128, 2100         4x1 24.7, 4x2 27.9     128, 8000   4x1 96.3, 4x2 91.5
+//   264, 1000         2x1 24.4, 4x1 29.4
+//   576, 1000         2x1 56.6, 4x1 47.8; of 300 21.3, 20.3
+//   1024, 1000        2x1 88.6, 4x1 87.8 (60% of the keys shared by all 39.0, 41.8)
+//   1248, 1000        2x1 111, 4x1 107       4096, 2100  2x1 684, 4x1 682 (324, 350)
+// D 64, whose steps and join are shorter: 512 of 2100 2x1 41.4, 4x1 41.8 (shared 31.4,
+// 28.1); 1024 of 1000 39.9, 39.1 (25.1, 28.4); 128 of 2100 4x1 18.8, 8x1 16.1; 16 of
+// 1000 8x1 9.3, 4x1 10.1, 4x4 11.2.
 // Short contexts, 1x1 and 2x1: 2048 units of 32 keys 11.4, 15.3, of 96 22.4, 24.0, 4096 22.0,
 // 28.1 and 39.4, 40.5, 1536 9.8, 11.5 and 19.1, 20.8, 1024 9.7, 8.6; D 64, 2048 of 96 13.7,
 // 15.1, 1536 11.9, 10.3.
@@ -526,10 +526,10 @@ Plan stream_plan(int64_t units, int64_t n_ct, int64_t max_blocks, int D) {
 
 // Whether the kernel for many columns takes a batch: of more than one column tile a
 // pair, where there are more than three units to a CU (at D = 64, with its shorter
-// steps, four).  us here, there: D 128, contexts of 2100 keys, 256 units 28, 64; 384 47,
-// 67; 544 57, 69; 640 57, 68; 1056 88, 69; 2176 154, 90; of 600 keys, 640 27, 27; 1056 36,
-// 26; of 100, 640 13, 12; 1056 18, 12.  D 64, 2100 keys, 640 34, 54; 1056 50, 54; 2080 85,
-// 74; of 600, 640 16, 20; 1056 23, 21.
+// steps, four).  us here, there: D 128, contexts of 2100 keys, 384 units 36, 65; 544 54,
+// 67; 768 58, 68; 1056 85, 70; 2176 152, 87; of 600 keys, 768 25, 26; 1056 34, 26; of 100,
+// 640 12, 12; 1056 17, 12.  D 64, 2100 keys, 640 32, 52; 1056 48, 52; 2080 84, 71; of 600,
+// 640 15, 20; 1056 22, 21.
 // (Its grid holds 2^22 columns a request and 2^18 pairs.)
 bool many_columns(int64_t B, int64_t max_q_len, int Hq, int Hkv, int D) {
   const int64_t n_ct = column_tiles(max_q_len, Hq, Hkv);
