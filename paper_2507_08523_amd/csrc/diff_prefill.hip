@@ -161,14 +161,18 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void diff_prefill_kerne
     // it) / 128 + r on, which is room for its tiles whatever the lengths; found eight
     // probes a round trip.
     const unsigned e = blockIdx.y * 8u + blockIdx.x;
-    auto first = [&](int i) { return unsigned(uint64_t(unsigned(max(scalar_load(a.cu_q + i), 0))) * unsigned(G) / kCols) + unsigned(i); };
+    auto first = [&](int row, int i) { return unsigned(uint64_t(unsigned(max(row, 0))) * unsigned(G) / kCols) + unsigned(i); };
     int lo = 0, hi = a.B;  // first(lo) <= e < first(hi)
     unsigned base = 0;
     while (hi - lo > 1) {
       const int st = (hi - lo + 7) >> 3;
+      int row[7];
       unsigned f[7];
 #pragma unroll
-      for (int k = 0; k < 7; ++k) f[k] = first(min(lo + st * (k + 1), a.B));
+      for (int k = 0; k < 7; ++k) row[k] = scalar_load(a.cu_q + min(lo + st * (k + 1), a.B));
+      __builtin_amdgcn_sched_barrier(0);  // (all on their way before the first is looked at)
+#pragma unroll
+      for (int k = 0; k < 7; ++k) f[k] = first(row[k], min(lo + st * (k + 1), a.B));
       int next = lo;
 #pragma unroll
       for (int k = 0; k < 7; ++k)
@@ -184,6 +188,7 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void diff_prefill_kerne
   const int q0 = scalar_load(a.cu_q + r), q_end = scalar_load(a.cu_q + r + 1), L_in = scalar_load(a.seq_lens + r);
   const int first_k = raw_id(max(wave - 2, 0)), k0 = raw_id(2 + wave), v0 = raw_id(wave);
   int next_k = raw_id(kTileBlocks + 2 + wave), next_v = raw_id(kTileBlocks + wave);  // of the next tile, unchecked
+  __builtin_amdgcn_sched_barrier(0);  // (no test of one ahead of the last load)
   asm volatile("" : : "s"(q0), "s"(q_end), "s"(L_in), "s"(first_k), "s"(k0), "s"(v0), "s"(next_k), "s"(next_v));
   const int L = min(L_in, a.max_blocks * kBlock);
   const int q_len = q_end - q0;
