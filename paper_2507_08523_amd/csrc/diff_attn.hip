@@ -200,12 +200,23 @@ __global__ __launch_bounds__(64 * group_waves(W), 2) void diff_stream_kernel(
 #pragma unroll
       for (int kc = 0; kc < kDch; ++kc) k_st[kc * (512 / D) * kRowPieces] = R.k[kc];
       wave_lds_fence();
-      f32x16 sc;
+      // (D = 64: two chains of products that do not wait for each other, 6% where keys come
+      // from L2; at D = 128 there is no register left for a second)
+      constexpr int kChains = D == 64 ? 2 : 1;
+      f32x16 part[kChains];
 #pragma unroll
-      for (int e = 0; e < 16; ++e) sc[e] = 0.f;
+      for (int x = 0; x < kChains; ++x)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) part[x][e] = 0.f;
 #pragma unroll
       for (int kc = 0; kc < kDch; ++kc)
-        sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(k_ld[kc * 2]), as_bf16x8(q_lds[wave][kc][lane]), sc, 0, 0, 0);
+        part[kc % kChains] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(k_ld[kc * 2]), as_bf16x8(q_lds[wave][kc][lane]),
+                                                                     part[kc % kChains], 0, 0, 0);
+      f32x16 sc = part[0];
+      if constexpr (kChains == 2) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sc[e] += part[1][e];
+      }
       wave_lds_fence();
       if (j0 + kStepKeys - 1 > mask_from) {
         // causal mask (which also covers keys >= L), and the V rows of keys >=
@@ -257,10 +268,13 @@ __global__ __launch_bounds__(64 * group_waves(W), 2) void diff_stream_kernel(
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int dt = 0; dt < kDt; ++dt) {
+        for (int dt = 0; dt < kDt; ++dt)
           o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(R.v[b][dt]), ph[b], o[dt], 0, 0, 0);
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int dt = 0; dt < kDt; ++dt)
           o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(R.v[b][dt]), pl[b], o[dt], 0, 0, 0);
-        }
     };
 
     // Two register sets; the scheduling barriers keep a step's loads behind the
