@@ -19,9 +19,9 @@
 // bound by reading K and V from HBM.  Each wave streams its range of a
 // request's keys from the pools into registers, two pool blocks (32 keys) a
 // step, the next step's loads in flight (K then takes the operand's layout by
-// way of LDS); W waves of a workgroup and n_split
-// workgroups share a (request, kv head, column tile) where there are too few of
-// them to fill the chip, and their states are joined at the end.
+// way of LDS); W waves of a workgroup and n_split workgroups share a (request, kv
+// head, column tile) where there are too few of them to fill the chip, and their
+// states are joined at the end.
 //   Precision: y is a difference, and where the two maps nearly agree (the case
 // the method is made for) it is much smaller than its terms, so that a weight
 // rounded to bf16 (2^-9 relative) would leave an error of several bf16 roundings
@@ -134,7 +134,8 @@ __global__ __launch_bounds__(64 * group_waves(W), 2) void diff_stream_kernel(
     const uint16_t* qr = q + int64_t(q0 + t) * q_stride + size_t(head) * D;
     u32x4 qc[kDch / 2];
 #pragma unroll
-    for (int i = 0; i < kDch / 2; ++i) qc[i] = *(const u32x4*)(qr + diff_chunk_of_map<D>(map, i, pairs_layout) * 16 + hh * 8);
+    for (int i = 0; i < kDch / 2; ++i)
+      qc[i] = *(const u32x4*)(qr + diff_chunk_of_map<D>(map, i, pairs_layout) * 16 + hh * 8);
     const int n_blk = (L + kBlock - 1) / kBlock;
     // keys past the last column's position are not visited (and their V rows zeroed)
     const int key_end = L - q_len + (col0 + n_cols - 1) / G + 1;
@@ -200,23 +201,14 @@ __global__ __launch_bounds__(64 * group_waves(W), 2) void diff_stream_kernel(
 #pragma unroll
       for (int kc = 0; kc < kDch; ++kc) k_st[kc * (512 / D) * kRowPieces] = R.k[kc];
       wave_lds_fence();
-      // (D = 64: two chains of products that do not wait for each other, 6% where keys come
-      // from L2; at D = 128 there is no register left for a second)
-      constexpr int kChains = D == 64 ? 2 : 1;
-      f32x16 part[kChains];
+      // (one chain of products: a second one's sums cost the register that a third wave of a
+      // SIMD has at D = 64, and there is none left at D = 128)
+      f32x16 sc;
 #pragma unroll
-      for (int x = 0; x < kChains; ++x)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) part[x][e] = 0.f;
+      for (int e = 0; e < 16; ++e) sc[e] = 0.f;
 #pragma unroll
       for (int kc = 0; kc < kDch; ++kc)
-        part[kc % kChains] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(k_ld[kc * 2]), as_bf16x8(q_lds[wave][kc][lane]),
-                                                                     part[kc % kChains], 0, 0, 0);
-      f32x16 sc = part[0];
-      if constexpr (kChains == 2) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) sc[e] += part[1][e];
-      }
+        sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(k_ld[kc * 2]), as_bf16x8(q_lds[wave][kc][lane]), sc, 0, 0, 0);
       wave_lds_fence();
       if (j0 + kStepKeys - 1 > mask_from) {
         // causal mask (which also covers keys >= L), and the V rows of keys >=
@@ -431,7 +423,8 @@ __global__ __launch_bounds__(64 * kJoinWaves) void diff_join_kernel(
     ml[mp] = *(const float2*)(part_ml + (slot0 + mp * kTileCols + size_t(min(lane, n_split - 1)) * kNext) * 2);
   load(0);
   // (pinned here: they would sink behind the test of the lengths)
-  asm volatile("" : "+s"(q0), "+s"(q_end), "+s"(L_in), "+s"(lam), "+v"(ml[0].x), "+v"(ml[0].y), "+v"(ml[1].x), "+v"(ml[1].y));
+  asm volatile("" : "+s"(q0), "+s"(q_end), "+s"(L_in), "+s"(lam));
+  asm volatile("" : "+v"(ml[0].x), "+v"(ml[0].y), "+v"(ml[1].x), "+v"(ml[1].y));
 #pragma unroll
   for (int u = 0; u < kAhead; ++u)
 #pragma unroll

@@ -161,7 +161,9 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void diff_prefill_kerne
     // it) / 128 + r on, which is room for its tiles whatever the lengths; found eight
     // probes a round trip.
     const unsigned e = blockIdx.y * 8u + blockIdx.x;
-    auto first = [&](int row, int i) { return unsigned(uint64_t(unsigned(max(row, 0))) * unsigned(G) / kCols) + unsigned(i); };
+    auto first = [&](int row, int i) {
+      return unsigned(uint64_t(unsigned(max(row, 0))) * unsigned(G) / kCols) + unsigned(i);
+    };
     int lo = 0, hi = a.B;  // first(lo) <= e < first(hi)
     unsigned base = 0;
     while (hi - lo > 1) {
