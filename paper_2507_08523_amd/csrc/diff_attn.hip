@@ -498,7 +498,8 @@ int64_t column_tiles(int64_t max_q_len, int Hq, int Hkv) {
 // others.  One wave to a unit is better than two only for a few steps of very many units,
 // all starts.  8 kv heads, D 128, us:
 //   units, keys       waves x workgroups
-//   8, 1000           4x1 12.6, 4x4 11.4     8, 4000     4x6 13.3, 4x12 12.1
+//   8, 1000           4x1 12.2, 4x4 9.8      8, 4000     4x6 13.3, 4x12 12.1
+//   8, 800            4x1 10.6, 4x4 9.9      64, 800     4x1 11.5, 4x3 12.0, 4x4 10.9
 //   32, 600           4x1 9.9, 4x2 11.5      32, 2100    4x3 15.1, 4x6 12.5, 4x8 12.6
 //   64, 2100          4x2 19.0, 4x3 17.8     88, 2100    4x1 22.8, 4x2 21.9
 //   128, 2100         4x1 24.7, 4x2 27.9     128, 8000   4x1 96.3, 4x2 91.5
@@ -525,8 +526,8 @@ Plan stream_plan(int64_t units, int64_t n_ct, int64_t max_blocks, int D) {
                     (steps >= 32 && ((units > 2 * cus && units <= 3 * cus) || (units > 4 * cus && units <= 5 * cus)));
   if (!four) return {steps <= 4 && units > (D == 64 ? 7 : 5) * cus ? 1 : 2, 1};
   const int64_t room = std::min<int64_t>(cus / units, kMaxGroups);
-  if (room >= 3 && steps >= (D == 64 ? 48 : 32))
-    return {4, int(std::min({room, steps / 8, int64_t(std::sqrt(double(steps)))}))};
+  if (room >= 3 && steps >= (D == 64 ? 48 : room >= 4 ? 24 : 32))
+    return {4, int(std::min({room, (steps + 7) / 8, int64_t(std::sqrt(double(steps)))}))};
   if (room == 2 && (steps > 128 || (steps >= 64 && 5 * units <= 2 * cus))) return {4, 2};
   return {D == 64 && units <= cus && steps >= 32 ? 8 : 4, 1};
 }
