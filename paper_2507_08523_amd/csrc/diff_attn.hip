@@ -498,18 +498,19 @@ int64_t column_tiles(int64_t max_q_len, int Hq, int Hkv) {
 // others.  One wave to a unit is better than two only for a few steps of very many units,
 // all starts.  8 kv heads, D 128, us:
 //   units, keys       waves x workgroups
-//   8, 1000           4x1 12.2, 4x4 9.8      8, 4000     4x6 13.3, 4x12 12.1
-//   8, 800            4x1 10.6, 4x4 9.9      64, 800     4x1 11.5, 4x3 12.0, 4x4 10.9
-//   32, 600           4x1 9.9, 4x2 11.5      32, 2100    4x3 15.1, 4x6 12.5, 4x8 12.6
-//   64, 2100          4x2 19.0, 4x3 17.8     88, 2100    4x1 22.8, 4x2 21.9
+//   8, 600            4x1 9.4, 4x5 8.6       8, 1000     4x1 12.2, 4x4 9.8, 4x8 8.7
+//   8, 4000           4x6 13.3, 4x16 11.1    32, 500     4x1 8.7, 4x4 9.3
+//   32, 800           4x4 10.5, 4x7 9.6      32, 2100    4x4 14.1, 4x8 12.3
+//   64, 800           4x1 11.6, 4x4 10.9     64, 2100    4x1 22.8, 4x4 18.5
+//   96, 2100          4x1 23.2, 4x2 23.0     96, 4000    4x1 37.8, 4x2 34.1
 //   128, 2100         4x1 24.7, 4x2 27.9     128, 8000   4x1 96.3, 4x2 91.5
 //   264, 1000         2x1 24.4, 4x1 29.4
 //   576, 1000         2x1 56.6, 4x1 47.8; of 300 21.3, 20.3
 //   1024, 1000        2x1 88.6, 4x1 87.8 (60% of the keys shared by all 39.0, 41.8)
 //   1248, 1000        2x1 111, 4x1 107       4096, 2100  2x1 684, 4x1 682 (324, 350)
 // D 64, whose steps and join are shorter: 512 of 2100 2x1 41.4, 4x1 41.8 (shared 31.4,
-// 28.1); 1024 of 1000 39.9, 39.1 (25.1, 28.4); 128 of 2100 4x1 18.8, 8x1 16.1; 16 of
-// 1000 8x1 9.3, 4x1 10.1, 4x4 11.2.
+// 28.1); 1024 of 1000 39.9, 39.1 (25.1, 28.4); 128 of 2100 4x1 18.2, 8x1 15.9; 256 of 2100
+// 23.5, 24.6; 16 of 600 4x1 7.4, 4x6 7.9, of 1000 4x1 9.6, 8x1 9.0, 4x4 8.5, 4x8 8.0.
 // Short contexts, 1x1 and 2x1: 2048 units of 32 keys 11.4, 15.3, of 96 22.4, 24.0, 4096 22.0,
 // 28.1 and 39.4, 40.5, 1536 9.8, 11.5 and 19.1, 20.8, 1024 9.7, 8.6; D 64, 2048 of 96 13.7,
 // 15.1, 1536 11.9, 10.3.
@@ -526,10 +527,12 @@ Plan stream_plan(int64_t units, int64_t n_ct, int64_t max_blocks, int D) {
                     (steps >= 32 && ((units > 2 * cus && units <= 3 * cus) || (units > 4 * cus && units <= 5 * cus)));
   if (!four) return {steps <= 4 && units > (D == 64 ? 7 : 5) * cus ? 1 : 2, 1};
   const int64_t room = std::min<int64_t>(cus / units, kMaxGroups);
-  if (room >= 3 && steps >= (D == 64 ? 48 : room >= 4 ? 24 : 32))
+  const int64_t ones = (steps + 3) / 4;  // workgroups that leave a wave one step
+  if (steps >= (D == 64 ? 24 : 17) && ones <= std::min<int64_t>(room, 10)) return {4, int(ones)};
+  if (room >= 3 && steps >= (room >= 4 ? 24 : D == 64 ? 40 : 32))
     return {4, int(std::min({room, (steps + 7) / 8, int64_t(std::sqrt(double(steps)))}))};
-  if (room == 2 && (steps > 128 || (steps >= 64 && 5 * units <= 2 * cus))) return {4, 2};
-  return {D == 64 && units <= cus && steps >= 32 ? 8 : 4, 1};
+  if (room == 2 && (steps > 128 || (D == 128 && steps >= 64 && 5 * units <= 2 * cus))) return {4, 2};
+  return {D == 64 && 2 * units <= cus && steps >= 32 ? 8 : 4, 1};
 }
 
 // Whether the kernel for many columns takes a batch: of more than one column tile a
