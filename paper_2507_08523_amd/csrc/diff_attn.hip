@@ -24,8 +24,8 @@
 // states are joined at the end.
 //   Precision: y is a difference, and where the two maps nearly agree (the case
 // the method is made for) it is much smaller than its terms, so that a weight
-// rounded to bf16 (2^-9 relative) would leave an error of several bf16 roundings
-// of y.  Each weight p therefore enters as two bf16 numbers, hi = bf16(p) and
+// rounded to bf16 (up to 2^-8 relative) would leave an error of several bf16
+// roundings of y.  Each weight p therefore enters as two bf16 numbers, hi = bf16(p) and
 // lo = bf16(p - hi), 16 bits in all: 8 more products a step, on matrix cores
 // that wait for HBM.
 #include <hip/hip_runtime.h>
@@ -536,16 +536,17 @@ Plan stream_plan(int64_t units, int64_t n_ct, int64_t max_blocks, int D) {
 }
 
 // Whether the kernel for many columns takes a batch: of more than one column tile a
-// pair, where there are more than three units to a CU (at D = 64, with its shorter
-// steps, four).  us here, there: D 128, contexts of 2100 keys, 384 units 36, 65; 544 54,
-// 67; 768 58, 68; 1056 85, 70; 2176 152, 87; of 600 keys, 768 25, 26; 1056 34, 26; of 100,
-// 640 12, 12; 1056 17, 12.  D 64, 2100 keys, 640 32, 52; 1056 48, 52; 2080 84, 71; of 600,
-// 640 15, 20; 1056 22, 21.
+// pair, where there are more than four units to a CU (at D = 64, whose exponentials it
+// takes twice as well, eleven).  us here, there: D 128, contexts of 2100 keys, 768 units 60,
+// 88; 1056 85, 88; 1280 91, 89; 2176 160, 120; of 600 keys, 768 25, 31; 1056 36, 31; 2176 56,
+// 43; of 100, 768 11, 12; 1056 17, 12.  D 64, 2100 keys, 1056 units 52, 74; 1792 76, 74; 2560
+// 95, 103; 3584 129, 106; of 600, 1056 21, 25; 1792 28, 26; 2560 36, 36; 3584 46, 37; of 100,
+// 1056 11, 11; 2176 13, 12.
 // (Its grid holds 2^22 columns a request and 2^18 pairs.)
 bool many_columns(int64_t B, int64_t max_q_len, int Hq, int Hkv, int D) {
   const int64_t n_ct = column_tiles(max_q_len, Hq, Hkv);
   if (max_q_len * (Hq / Hkv) > (int64_t(1) << 22) || B * Hkv > (1 << 18)) return false;
-  return n_ct > 1 && B * Hkv * n_ct > (D == 64 ? 4 : 3) * int64_t(ilpc::device_cus());
+  return n_ct > 1 && B * Hkv * n_ct > (D == 64 ? 11 : 4) * int64_t(ilpc::device_cus());
 }
 
 size_t part_bytes(int64_t units, int D, int n) {

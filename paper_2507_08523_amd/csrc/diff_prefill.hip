@@ -6,39 +6,37 @@
 // 32 columns with both of their maps.  Per 32 keys and wave, on
 // v_mfma_f32_32x32x16_bf16:
 //   S_m^T = K_m Q_m^T            D/32 products a map,
-//   O_m^T += V^T P_m^T           2 * D/32 products a map,
-// six D-wide products a column and key in all: both maps have to meet V in one
-// pass, since their sums are known only at the end.  Both maps in one wave: every
-// V operand read from LDS feeds two products.
+//   O^T += V^T P^T               2 * D/32 products,
+// in two passes over the keys.
 //
-// Precision.  y = O_1 / l_1 - lambda O_2 / l_2 is a difference, and where the maps
-// nearly agree it is much smaller than its terms; weights rounded to bf16 would
-// leave an error of 2^-9 of the terms.  What is accumulated is therefore
-//   A = sum (p_1 - beta p_2) v,   B = sum p_2 v,   beta ~ lambda l_1 / l_2,
-// with the difference of the weights taken in fp32 before it is rounded: beta is
-// lambda l_1 / l_2 as of the last time the running maxima were taken, and in the end
-//   y = (A + (beta - lambda l_1 / l_2) B) / l_1,
-// exact in beta.  A's rounding is relative to the combined weights, B's is scaled
-// by how far beta was off.  When the maxima grow (factors a_1, a_2) and beta is
-// set anew: A <- a_1 A + (a_1 beta - a_2 beta') B, B <- a_2 B.  Where map 2 outgrows
-// beta by more than a factor of 2 the maps do not cancel, and roundings scaled by an
-// old beta would stay in A while the weights they belong to lose their share: beta is
-// given up (0) for that column, whose two maps are then simply summed apart.
-// Error against 64 bits (2-norm; the output's own rounding is 0.0017 of it), q of
-// standard deviation 0.09, 0.3, 1, 2, 4: 0.0024, 0.0024, 0.0023, 0.0021, 0.0018; keys
-// whose scores in map 2 rise by 0.5 every 32 of 8000: 0.0023 (with beta followed and
-// not given up 0.029, never looked at 0.16); second map near the first 0.0024.
+// Precision.  y = (A_1 - lambda A_2) V is a difference, and where the maps nearly
+// agree it is much smaller than its terms; weights of one map rounded to bf16 would
+// leave an error of up to 2^-8 of the terms.  The difference of the weights is therefore
+// taken in fp32 and then rounded, which needs both maps' sums beforehand:
+//   pass 1, K alone:   m_m, l_m = sum 2^(s log2(e) q_m.k_m - m_m),
+//   pass 2, K and V:   y = sum (p_1 - (lambda l_1 / l_2) p_2) v / l_1.
+// The rounding to bf16, half a step of the combined weight, is a choice: the products with V
+// then take half the time that two bf16 numbers a weight would, as the kernel for few
+// columns has.  Error against 64 bits (2-norm; the output's own rounding is 0.0017 of it): q of
+// standard deviation 0.09, 0.3, 1, 2, 4, 30: 0.0023, 0.0023, 0.0023, 0.0021, 0.0020, 0.0018;
+// scores of one map rising by 0.5 every 32 of 3000 keys 0.0023; maps that nearly agree,
+// everywhere or behind some first keys, 0.0017 to 0.0024.
+// One pass with the ratio of the sums so far, sum (p_1 - beta p_2) v and sum p_2 v set
+// right at the end, is as many products (six D-wide ones a column and key: 2 + 4, here
+// 2 + 2 + 2), took 0.72 to 0.87 of the time and was not kept: weights rounded against a ratio that the
+// first keys have and the others do not left 0.006 to 0.026 of nearly agreeing maps.
 //
-// What bounds it: vector instructions and products of the two waves of a SIMD, about
-// 820 and 770 cycles a step and wave, at 2.05 GHz: 64 prompts of 1.9 K tokens (64/8 heads)
-// 6.7 to 7.1 ms (box to box), 0.95 to 1.0 PFLOP/s of products; an item's start and end, 11 K
-// of 114 K cycles there, 14 K of 57 K on prompts of 300 new tokens after 300 cached ones.
-// Tried and slower: one workgroup taking item after item with the next one's loads behind
-// the end of the one before (registers spill across the tile loop: 8.0 ms); 4 or 6 LDS
-// operands in flight instead of 3 (1, 4%); the products' raised priority left out (1%).
+// What bounds it: vector instructions, 242 a step and wave in both passes (64 of them
+// exponentials) or 1320 cycles, and 770 cycles of products, of which two waves a SIMD
+// overlap next to nothing (2030 cycles a step and wave): 64 prompts of 1.9 K tokens (64/8
+// heads) 8.2 to 9.1 ms (box to box), 0.73 to 0.83 PFLOP/s of products.  Tried, within 1% of
+// this: the next step's scores in a second set of registers, their products placed between
+// the exponentials; 3 or 6 LDS operands in flight instead of 4; the products' raised
+// priority left out.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstdint>
 #include <type_traits>
@@ -189,9 +187,9 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void diff_prefill_kerne
   // Lengths and the block ids of the first tiles in one round trip.
   const int q0 = scalar_load(a.cu_q + r), q_end = scalar_load(a.cu_q + r + 1), L_in = scalar_load(a.seq_lens + r);
   const int first_k = raw_id(max(wave - 2, 0)), k0 = raw_id(2 + wave), v0 = raw_id(wave);
-  int next_k = raw_id(kTileBlocks + 2 + wave), next_v = raw_id(kTileBlocks + wave);  // of the next tile, unchecked
+  int next_k = raw_id(kTileBlocks + 2 + wave), next_v = v0;  // of the next tile, unchecked
   __builtin_amdgcn_sched_barrier(0);  // (no test of one ahead of the last load)
-  asm volatile("" : : "s"(q0), "s"(q_end), "s"(L_in), "s"(first_k), "s"(k0), "s"(v0), "s"(next_k), "s"(next_v));
+  asm volatile("" : : "s"(q0), "s"(q_end), "s"(L_in), "s"(first_k), "s"(k0), "s"(v0), "s"(next_k));
   const int L = min(L_in, a.max_blocks * kBlock);
   const int q_len = q_end - q0;
   const int64_t all_cols = int64_t(min(q_len, a.max_q_len)) * G;
@@ -235,11 +233,13 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void diff_prefill_kerne
   const uint64_t vbase = reinterpret_cast<uint64_t>(a.v_pool) + size_t(h) * kSlabBytes;
   // (ids past the last block, or outside the pool, read block 0: masked keys)
   auto usable = [&](int blk, int id) { return (blk < n_blk && id >= 0 && id < a.num_blocks) ? id : 0; };
-  auto k_buf = [&](int j) { return unsigned(j & 1) * kTileBytes; };
-  auto v_buf = [&](int j) { return unsigned(2 + (j & 1)) * kTileBytes; };
-  auto issue_k = [&](int j, int id) {
+  // Tile j of K in the first pass (0) and the second (1), and of V.  The second pass's
+  // first tiles have buffers that the first pass's last tile does not hold.
+  auto k_buf = [&](int pass, int j) { return unsigned(2 * pass + (j & 1)) * kTileBytes; };
+  auto v_buf = [&](int j) { return unsigned((n_tiles + j) & 1) * kTileBytes; };
+  auto issue_k = [&](int pass, int j, int id) {
     const uint64_t base = scalar(kbase + size_t(id) * slab_stride);
-    const uint32_t to = scalar(ring0 + k_buf(j));
+    const uint32_t to = scalar(ring0 + k_buf(pass, j));
     if constexpr (kInsts == 4) load_slab4(koff[0], koff[1], koff[2], koff[3], base, to);
     else load_slab2(koff[0], koff[1], base, to);
   };
@@ -250,9 +250,8 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void diff_prefill_kerne
     else load_slab2(voff, voff, base, to);
   };
 
-  if (wave >= 2) issue_k(-1, usable(wave - 2, first_k));
-  issue_k(0, usable(2 + wave, k0));
-  issue_v(0, usable(wave, v0));
+  if (wave >= 2) issue_k(0, -1, usable(wave - 2, first_k));
+  issue_k(0, 0, usable(2 + wave, k0));
   bf16x8 qf[kDch];  // Q operand, map 1's chunks first
   {
     const uint16_t* qr = a.q + int64_t(q0 + row_a + t_off) * a.q_stride + size_t(head) * D;
@@ -263,15 +262,8 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void diff_prefill_kerne
   const float lam = a.ep.lambda[head];
   if (tid < D) s_norm[tid] = a.ep.norm_w ? a.ep.norm_w[tid] : 1.f;
 
-  f32x16 oa[kDt], ob[kDt];  // A^T and B^T
-#pragma unroll
-  for (int dt = 0; dt < kDt; ++dt)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) oa[dt][e] = 0.f, ob[dt][e] = 0.f;
-  f32x16 s1, s2;                     // scores of the next step
-  bf16x8 pc[2], p2[2];               // p_1 - beta p_2 and p_2 of the step whose products with V are due
-  float m1 = -INFINITY, m2 = -INFINITY, l1 = 0.f, l2 = 0.f;  // l: this lane half's share
-  float beta = 0.f, most2 = 0.f;
+  f32x16 s1, s2;  // scores of the next step
+  float m1 = -FLT_MAX, m2 = -FLT_MAX, l1 = 0.f, l2 = 0.f;  // l: this lane half's share
 
   auto mask = [&](int step) {
     const int j0 = step * 32;
@@ -285,14 +277,9 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void diff_prefill_kerne
     }
   };
 
-  // Weights of a masked step against the running maxima.  The maxima are taken, and
-  // A, B, the sums and beta brought in line, in the first step, where a lane's sum of
-  // weights leaves [0, 2^8] (a maximum that grew), and where map 2's passes most2,
-  // twice what its sum was (and 2: that sum is at least 1 in one lane half) when beta
-  // was last looked at: beta is then too large for them, and scales up their rounding
-  // (error of single rows, q of standard deviation 1, 2, 4, without that test 0.6, 5.5,
-  // 40%, with it 0.5, 0.9, 0.6%).  It costs 4%.
-  auto softmax = [&](bool first) __attribute__((always_inline)) {
+  // Sums of a masked step's exponentials against the running maxima, which are taken
+  // anew where a lane's sum leaves [0, 2^8], the first step among them.
+  auto add_step = [&]() __attribute__((always_inline)) {
     float t1, t2;
     auto exps = [&]() __attribute__((always_inline)) {
       float u1[2], u2[2];
@@ -302,58 +289,31 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void diff_prefill_kerne
         const float a2 = __builtin_amdgcn_exp2f(__builtin_fmaf(s2[e], a.scale_log2, -m2));
         u1[e & 1] = e < 2 ? a1 : u1[e & 1] + a1;
         u2[e & 1] = e < 2 ? a2 : u2[e & 1] + a2;
-        pc[e >> 3][e & 7] = (__bf16)__builtin_fmaf(-beta, a2, a1);
-        p2[e >> 3][e & 7] = (__bf16)a2;
       }
       t1 = u1[0] + u1[1];
       t2 = u2[0] + u2[1];
-      // (formed here, not behind the test below, across which 32 weights would stay live)
-      asm volatile("" : "+v"(pc[0]), "+v"(pc[1]), "+v"(p2[0]), "+v"(p2[1]));
     };
-    bool slow = first;
-    if (!first) {
-      exps();
-      slow = __ballot(!(t1 <= kSumLimit) || !(t2 <= most2)) != 0;
-    }
-    if (slow) {
+    exps();
+    if (__ballot(!(t1 <= kSumLimit) || !(t2 <= kSumLimit))) {
       float x1 = s1[0], x2 = s2[0];
 #pragma unroll
       for (int e = 1; e < 16; ++e) x1 = fmaxf(x1, s1[e]), x2 = fmaxf(x2, s2[e]);
       const float n1 = fmaxf(m1, max_across_halves(x1) * a.scale_log2);
       const float n2 = fmaxf(m2, max_across_halves(x2) * a.scale_log2);
-      const float f1 = __builtin_amdgcn_exp2f(m1 - n1), f2 = __builtin_amdgcn_exp2f(m2 - n2);
+      l1 *= __builtin_amdgcn_exp2f(m1 - n1), l2 *= __builtin_amdgcn_exp2f(m2 - n2);
       m1 = n1, m2 = n2;
-      l1 *= f1, l2 *= f2;
-      const float old = f1 * beta;
-      // the sums of this step, for beta's ratio, before the weights that it enters
-      float y1 = 0.f, y2 = 0.f;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        y1 += __builtin_amdgcn_exp2f(__builtin_fmaf(s1[e], a.scale_log2, -m1));
-        y2 += __builtin_amdgcn_exp2f(__builtin_fmaf(s2[e], a.scale_log2, -m2));
-      }
-      // beta' as long as beta was not more than twice it (nor given up: was = 0 < most)
-      const float now = lam * add_across_halves(l1 + y1) / add_across_halves(l2 + y2);
-      const float was = fabsf(old), most = 2.f * fabsf(f2 * now);
-      beta = bool(int(was <= most) & int(most <= was * 0x1p100f)) ? now : 0.f;
-      most2 = fminf(2.f * (l2 + y2) + 2.f, kSumLimit);
-      const float k = old - f2 * beta;
-#pragma unroll
-      for (int dt = 0; dt < kDt; ++dt)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          oa[dt][e] = f1 * oa[dt][e] + k * ob[dt][e];
-          ob[dt][e] *= f2;
-        }
       exps();
     }
     l1 += t1;
     l2 += t2;
   };
 
-  // Products: A, B += V P of a step (the two V blocks at sV), then the scores of the
+  f32x16 o[kDt];       // sum of (p_1 - beta p_2) v
+  bf16x8 pc[2];        // p_1 - beta p_2 of the step whose products with V are due
+
+  // Products: O += V P of a step (the two V blocks at sV), then the scores of the
   // next (the 32 K rows at sK), the LDS operands read kPrefetch ahead.
-  constexpr int kPv = 2 * kDt, kQk = kDch, kPrefetch = 3;
+  constexpr int kPv = 2 * kDt, kQk = kDch, kPrefetch = 4;
   auto products = [&](auto with_pv, auto with_qk, const uint8_t* sV, const uint8_t* sK)
                       __attribute__((always_inline)) {
     constexpr int first = decltype(with_pv)::value ? 0 : kPv;
@@ -382,29 +342,20 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void diff_prefill_kerne
       const bf16x8 op = buf[st % kPrefetch];
       if (st + kPrefetch < last) buf[st % kPrefetch] = operand(st + kPrefetch);
       if (st < kPv) {
-        const int dt = st % kDt, b = st / kDt;
-        oa[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op, pc[b], oa[dt], 0, 0, 0);
-        ob[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op, p2[b], ob[dt], 0, 0, 0);
+        o[st % kDt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op, pc[st / kDt], o[st % kDt], 0, 0, 0);
       } else {
         const int u = st - kPv;
         if (u & 1) s2 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op, qf[chunk_of(u)], s2, 0, 0, 0);
         else s1 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op, qf[chunk_of(u)], s1, 0, 0, 0);
       }
     }
-    // pin that order: kPrefetch reads, then the product(s) of one operand a read
+    // pin that order: kPrefetch reads, then the product of one operand a read
     constexpr int steps = last - first, lead = steps < kPrefetch ? steps : kPrefetch;
-    constexpr int pv = first < kPv ? kPv : 0, qk = steps - pv;  // operands of each kind
-    constexpr int pv_reads = pv < steps - lead ? pv : steps - lead, qk_reads = steps - lead - pv_reads;
     __builtin_amdgcn_sched_group_barrier(0x100, lead, 0);
 #pragma unroll
-    for (int st = 0; st < pv; ++st) {
-      __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
-      if (st < pv_reads) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-    }
-#pragma unroll
-    for (int st = 0; st < qk; ++st) {
+    for (int st = 0; st < steps; ++st) {
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-      if (st < qk_reads) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      if (st < steps - lead) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
     }
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_setprio(0);
@@ -432,29 +383,50 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void diff_prefill_kerne
     wait_lds();
   };
 
-  // beta given up where the sums have left it more than a factor of 2 too large.
-  auto follow = [&]() __attribute__((always_inline)) {
-    const float t1 = add_across_halves(l1), t2 = add_across_halves(l2);
-    const bool grown = fabsf(beta) * t2 > 2.f * fabsf(lam) * t1;
-    if (__ballot(grown)) {
-      const float k = grown ? beta : 0.f;
-#pragma unroll
-      for (int dt = 0; dt < kDt; ++dt)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) oa[dt][e] += k * ob[dt][e];
-      beta -= k;
-    }
-    most2 = fminf(2.f * l2 + 2.f, kSumLimit);
-  };
-
-  // Two steps a tile.  Before the first of tile j: wait for this wave's loads of
-  // K(j), V(j); barrier; issue K(j+1) and V(j+1) into the buffers of tile j-1, which
-  // every wave has left behind.  The scores of a step past the wave's last one are
-  // computed and ignored.
+  // First pass, the sums of both maps.  Two steps a tile.  Before the first of tile j:
+  // wait for this wave's loads of K(j); barrier; issue K(j+1) into the buffer of tile j-1,
+  // which every wave has left behind, or behind the last tile the second pass's first
+  // ones.  The scores of a step past the wave's last one are computed and ignored.
   wait_loads();
   wait_lds();
   bare_barrier();
-  if (active) products(no(), yes(), ring, ring + k_buf(-1) + 32 * kRowBytes);
+  if (active) products(no(), yes(), ring, ring + k_buf(0, -1) + 32 * kRowBytes);
+  for (int u = 0; u < 2 * n_tiles; ++u) {
+    const int j = u >> 1;
+    if (!(u & 1)) {
+      if (j > 0) wait_loads();
+      bare_barrier();
+      if (j + 1 < n_tiles) {
+        const int kb = (j + 1) * kTileBlocks + 2 + wave;
+        issue_k(0, j + 1, usable(kb, next_k));
+        next_k = raw_id(kb + kTileBlocks);
+      } else {
+        if (wave >= 2) issue_k(1, -1, usable(wave - 2, first_k));
+        issue_k(1, 0, usable(2 + wave, k0));
+        issue_v(0, usable(wave, v0));
+        next_k = raw_id(kTileBlocks + 2 + wave);
+        next_v = raw_id(kTileBlocks + wave);
+      }
+    }
+    if (u <= last_step) {
+      mask(u);
+      add_step();
+      // (the ids' scalar loads are waited for here, and not with the first LDS operands of the products)
+      asm volatile("" : "+s"(next_k), "+s"(next_v));
+      products(no(), yes(), ring, ring + k_buf(0, j) + (u & 1) * 32 * kRowBytes);
+    }
+  }
+  const float sum1 = add_across_halves(l1), sum2 = add_across_halves(l2);
+  const float beta = lam * sum1 / sum2, inv = 1.f / sum1;
+
+  // Second pass, the products with V: the same over K and V.
+#pragma unroll
+  for (int dt = 0; dt < kDt; ++dt)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[dt][e] = 0.f;
+  wait_loads();
+  bare_barrier();
+  if (active) products(no(), yes(), ring, ring + k_buf(1, -1) + 32 * kRowBytes);
   for (int u = 0; u < 2 * n_tiles; ++u) {
     const int j = u >> 1;
     if (!(u & 1)) {
@@ -463,35 +435,33 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void diff_prefill_kerne
       bare_barrier();
       if (j + 1 < n_tiles) {
         const int kb = (j + 1) * kTileBlocks + 2 + wave, vb = kb - 2;
-        issue_k(j + 1, usable(kb, next_k));
+        issue_k(1, j + 1, usable(kb, next_k));
         issue_v(j + 1, usable(vb, next_v));
         next_k = raw_id(kb + kTileBlocks);
         next_v = raw_id(vb + kTileBlocks);
       }
-      if ((j & 1) && u <= last_step) follow();  // every second tile
     }
     if (u <= last_step) {
       mask(u);
-      int uu = u;
-      asm volatile("" : "+s"(uu));  // (one body for the first step and the others)
-      softmax(uu == 0);
-      // (the ids' scalar loads are waited for here, and not with the first LDS operands of the products)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float a1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s1[e], a.scale_log2, -m1));
+        const float a2 = __builtin_amdgcn_exp2f(__builtin_fmaf(s2[e], a.scale_log2, -m2));
+        pc[e >> 3][e & 7] = (__bf16)__builtin_fmaf(-beta, a2, a1);
+      }
       asm volatile("" : "+s"(next_k), "+s"(next_v));
-      products(yes(), yes(), ring + v_buf(j) + (u & 1) * 2 * kSlabBytes, ring + k_buf(j) + (u & 1) * 32 * kRowBytes);
+      products(yes(), yes(), ring + v_buf(j) + (u & 1) * 2 * kSlabBytes, ring + k_buf(1, j) + (u & 1) * 32 * kRowBytes);
     }
   }
   if (!active) return;
 
-  const float t1 = add_across_halves(l1), t2 = add_across_halves(l2);
-  const float k = beta - lam * t1 / t2, inv = 1.f / t1;
   float sq = 0.f;
 #pragma unroll
   for (int dt = 0; dt < kDt; ++dt)
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      const float y = (oa[dt][e] + k * ob[dt][e]) * inv;
-      oa[dt][e] = y;
-      sq += y * y;
+      o[dt][e] *= inv;
+      sq += o[dt][e] * o[dt][e];
     }
   float fac = a.ep.scale;
   if (a.ep.norm_w) fac *= rsqrtf(add_across_halves(sq) * (1.f / D) + a.ep.eps);
@@ -499,7 +469,7 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void diff_prefill_kerne
   // holds 8-byte pieces of one row).  4 KiB a wave, in the buffers of the tile
   // before the last, which every wave has left behind: 32 rows of 64 dimensions a
   // pass, 16-byte chunks XOR-swizzled by row.
-  uint8_t* tb = ring + (wave < 2 ? k_buf(n_tiles) : v_buf(n_tiles)) + (wave & 1) * 4096;
+  uint8_t* tb = ring + (wave < 2 ? k_buf(1, n_tiles) : v_buf(n_tiles)) + (wave & 1) * 4096;
   size_t orow[4];
   bool ok[4];
 #pragma unroll
@@ -517,7 +487,7 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void diff_prefill_kerne
         const f32x4 w = *(const f32x4*)&s_norm[(2 * p + dl) * 32 + g4 * 8 + hh * 4];
         bf16x4 v;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = (__bf16)(oa[2 * p + dl][g4 * 4 + e] * (fac * w[e]));
+        for (int e = 0; e < 4; ++e) v[e] = (__bf16)(o[2 * p + dl][g4 * 4 + e] * (fac * w[e]));
         *(bf16x4*)(tb + n * 128 + (((dl * 4 + g4) ^ (n & 7)) << 4) + hh * 8) = v;
       }
 #pragma unroll

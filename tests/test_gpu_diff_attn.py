@@ -434,3 +434,89 @@ def test_many_requests_with_short_contexts(longest, D):
     lens = [longest, *(int(x) for x in rng.integers(1, longest + 1, n - 1))]
     b = Batch(lens, [1, *(int(x) for x in rng.integers(0, 2, n - 1))], 16, 8, D, seed=D)
     b.check(b.run())
+
+
+def set_map2_scores(b, scores):
+    """Adds scores[j] to every query's score of key j in map 2, by a dimension of each half that holds
+    nothing else (a sink, an instruction that the maps see apart)."""
+    half = b.D // 2
+    b.q[..., 0] = b.q[..., half] = 4.0
+    for r, k in enumerate(b.kd):
+        k[..., 0] = 0.0
+        k[..., half] = (torch.as_tensor(scores[:len(k)]) / (4.0 * b.scale))[:, None].to(torch.bfloat16)
+        for j in range(-(-len(k) // 16)):
+            n = min(16, len(k) - 16 * j)
+            b.kp[b.bt[r, j], :, :n] = k[16 * j:16 * j + n].permute(1, 0, 2).cuda()
+
+
+@pytest.mark.parametrize("first,shift", [(32, -0.8), (64, -1.0), (32, -1.5), (32, -2.8), (32, 1.0), (16, 1.0), (1, 8.0),
+                                         (1000, -1.0)])
+@pytest.mark.parametrize("lam", [0.8, 0.95, 1.0])
+@pytest.mark.parametrize("new", [1, 0])
+def test_maps_that_differ_in_the_first_keys_and_nearly_cancel_after(first, shift, lam, new):
+    # the weight ratio of the first keys is not the one at the end
+    L = 2048
+    kw = dict(lens=[L], new=[1], Hq=8, Hkv=1) if new else wide([L], [130], 8, 1)
+    b = Batch(**kw, near=0.02, lam=lam, seed=first)
+    set_map2_scores(b, np.where(np.arange(L) < first, shift, 0.0))
+    b.check(b.run(), rows_of=range(min(3, len(b.lens))))
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("L", [300, 8192])
+def test_ratios_that_move_and_come_back(L, D):
+    # apart in stretches of the keys, both ways, equal in the rest
+    b = Batch(**wide([L], [130], 8, 1, D), near=0.02, lam=0.95, seed=D)
+    j = np.arange(L)
+    set_map2_scores(b, np.where(j < 40, -1.5, np.where((j >= L // 3) & (j < L // 3 + 50), 2.0, 0.0)))
+    b.check(b.run(), rows_of=range(2))
+
+
+def wider(lens, new, Hq, Hkv, D=64):
+    """As wide(), with more than 11 column tiles to a compute unit: the kernel for many columns at D = 64."""
+    cus = torch.cuda.get_device_properties(0).multi_processor_count
+    tiles = -(-max(new) * (Hq // Hkv) // 16)
+    assert tiles > 1
+    k = -(-(11 * cus + 1) // (len(lens) * Hkv * tiles))
+    return dict(lens=list(lens) * k, new=list(new) * k, Hq=Hq, Hkv=Hkv, D=D)
+
+
+@pytest.mark.parametrize("Hq,Hkv,lens,new", [
+    *[(Hq, Hkv, [1, 40, 100, 129, 60, 64], [1, 40, 36, 33, 17, 0]) for Hq, Hkv in ((4, 1), (6, 2), (20, 1), (12, 4))],
+    *[(8, 4, [S + 48, S, S + 200], [S, S, S]) for S in (17, 31, 32, 33, 64, 65, 127, 128, 129, 257)],
+    *[(16, 2, [L], [40]) for L in (40, 63, 64, 65, 96, 127, 128, 129, 191, 193, 1500)]])
+def test_many_columns_of_64_dimensions(Hq, Hkv, lens, new):
+    b = Batch(**wider(lens, new, Hq, Hkv), spare_cols=5, seed=len(lens) + Hq)
+    out = b.run()
+    n = len(b.lens)
+    b.check(out, rows_of={*range(min(n, 12)), *range(max(n - 6, 0), n)})
+    assert out.isfinite().all()
+
+
+@pytest.mark.parametrize("layout", ["halves", "rope"])
+@pytest.mark.parametrize("norm,fused", [(False, True), (True, False)])
+def test_many_columns_of_64_dimensions_layouts(layout, norm, fused):
+    b = Batch(**wider([150, 77], [90, 65], 16, 2), norm=norm, layout=layout, fused=fused, extra=5, seed=16)
+    out = b.run()
+    b.check(out, rows_of=range(6))
+    assert (out[sum(b.new):] == 7.0).all()
+
+
+@pytest.mark.parametrize("first,shift,lam,std", [(32, -1.5, 0.95, 1.0), (64, -1.0, 1.0, 1.0), (16, 1.0, 0.95, 1.0),
+                                                 (1, 8.0, 0.8, 1.0), (700, -1.0, 0.95, 1.0), (300, 6.0, 0.8, 4.0)])
+def test_many_columns_of_64_dimensions_nearly_cancelling(first, shift, lam, std):
+    b = Batch(**wider([1500], [130], 8, 1), near=0.02, lam=lam, std=std, seed=first)
+    set_map2_scores(b, np.where(np.arange(1500) < first, shift, 0.0))
+    b.check(b.run(), rows_of=range(2))
+
+
+def test_many_columns_of_64_dimensions_rows_that_stay_and_bad_ids():
+    b = Batch(**wider([80, 40, 50, 110], [30, 20, 40, 60], 16, 4), seed=17)
+    n, ends = len(b.lens), np.cumsum([0, *b.new])
+    b.L[1] = 1            # more rows than keys
+    b.cu[n] += 1          # a row past q
+    b.bt[3, 2], b.bt[3, 3], b.bt[3, 4] = -1, 1 << 30, -(1 << 31)
+    b.L[7] = (1 << 31) - 1  # far past its row of the table
+    out = b.run()
+    b.check(out, rows_of=[r for r in range(12) if r not in (1, 3, 7)])
+    assert (out[ends[1]:ends[2]] == 7.0).all() and (out[ends[n - 1]:] == 7.0).all()
