@@ -280,8 +280,9 @@ class DeviceTables:
         def empty(n):
             return torch.zeros(n, dtype=torch.int32, device=pc.device)
 
-        self.block_tables, self.seq_lens = dev(tables), dev(L)
-        self.start_pos, self.first_block = dev(L), dev(-(-L // BLOCK))
+        self.block_tables, self.start_pos = dev(tables), dev(L)
+        self._rows = dev(np.stack([L, -(-L // BLOCK)]))
+        self.seq_lens, self.first_block = self._rows[0], self._rows[1]
         self.cu_q, self.cu_blocks = empty(self.B + 1), empty(self.B + 1)
         self.slot_map, self.status = empty(self.max_rows).fill_(-1), empty(1)
 
@@ -289,7 +290,7 @@ class DeviceTables:
         """Every request r gets new_lens[r] (device int32, at most max_new) tokens.
 
         The rows of the returned batch are the new tokens', in request order,
-        ``max_rows`` at most; its views hold until the next extend."""
+        ``max_rows`` at most; its views hold until the next extend or release."""
         import torch
 
         torch.add(self.seq_lens, 0, out=self.start_pos)
@@ -304,13 +305,23 @@ class DeviceTables:
         self.pc.append_slots(self.slot_map, k_new, v_new)
 
     def release(self, ended):
-        """Requests with ended[r] (device int32) = 1, not 0, have finished: the blocks that they
-        took by extend are free again, and their rows hold nothing, ready for another request's."""
+        """Requests with ended[r] (device bool or integer) not 0 have finished: the blocks that they
+        took by extend are free again, and their rows hold nothing, ready for another request's.
+
+        Where the device refuses it (``status``), nothing is given back and the rows stay as they
+        were, so that it can be called again."""
+        import torch
+
+        if not isinstance(ended, torch.Tensor) or ended.device != self.seq_lens.device:
+            raise ilpc.ILPCError(ilpc.EINVAL, f"release: ended must be a tensor on {self.seq_lens.device}")
+        if ended.shape != (self.B,) or ended.is_floating_point() or ended.is_complex():
+            raise ilpc.ILPCError(ilpc.EINVAL, f"release: ended must be bool or integers [{self.B}]")
+        ended = ended if ended.dtype == torch.bool else ended != 0
         ilpc.release_tables(self.block_tables, self.first_block, self.seq_lens * ended, self.pc.free_ids,
                             self.pc.free_taken, self.cu_blocks, self.pc.free_taken, self.status)
-        goes_on = 1 - ended
-        self.seq_lens.mul_(goes_on)
-        self.first_block.mul_(goes_on)  # what the row takes from now on is all its own
+        # a row stays unless it has ended and was not refused: ended <= status (0, or bits).  What an
+        # emptied row takes from now on is all its own, so that its first_block is 0 as well.
+        self._rows.mul_(ended <= self.status)
 
 
 class DecodeGraph:

@@ -501,3 +501,66 @@ def test_refused_batches_of_many_rows_change_nothing(kind):
     torch.cuda.synchronize()
     assert rows > 6144 and ints(s.st)[0] & {"blocks": 1, "long": 2, "rows": 4}[kind]
     same(got[:-1], want[:-1])
+
+
+def two_rows():
+    """Two requests of 21 and 33 tokens, whose rows took one block each from nine spare ones."""
+    pc = pipeline.PagedPrefixCache(2, 64, 16, 6, 2, 8, spare_blocks=9)
+    tables = np.full((2, 6), -1, np.int32)
+    tables[0, :2], tables[1, :2] = [4, 7], [4, 5]
+    dt = pipeline.DeviceTables(pc, tables, [32, 32], max_rows=4)
+    dt.extend(dev([1, 1]), 1)
+    assert ints(dt.status) == [0] and ints(pc.free_taken) == [2]
+    return pc, dt
+
+
+@pytest.mark.parametrize("dtype", [torch.bool, torch.int32, torch.int64, torch.uint8, torch.int8])
+@pytest.mark.parametrize("value", [1, 7, -1])
+def test_release_takes_any_mask(dtype, value):
+    # what is not 0 has ended
+    if value < 0 and dtype == torch.uint8:
+        value = 255
+    pc, dt = two_rows()
+    dt.release(torch.tensor([0, value], device="cuda").to(dtype))
+    torch.cuda.synchronize()
+    assert (ints(dt.status), ints(pc.free_taken), ints(dt.seq_lens), ints(dt.first_block)) == ([0], [1], [33, 0], [2, 0])
+    assert ints(pc.free_ids)[1:] == [17, *range(18, 25)]
+    dt.extend(dev([0, 3]), 3)
+    assert ints(dt.status) == [0] and ints(dt.seq_lens) == [33, 3] and ints(dt.block_tables)[1][0] == 17
+
+
+def test_release_refuses_other_masks_before_anything_changes():
+    pc, dt = two_rows()
+    for bad in (torch.tensor([0.0, 1.0]).cuda(), dev([1]), dev([0, 1, 0]), dev([[0, 1]]), torch.tensor([0, 1]), [0, 1],
+                None, 1):
+        with pytest.raises(ilpc.ILPCError):
+            dt.release(bad)
+    torch.cuda.synchronize()
+    assert (ints(pc.free_taken), ints(dt.seq_lens), ints(dt.first_block)) == ([2], [33, 33], [2, 2])
+    assert ints(pc.free_ids) == list(range(16, 25))
+
+
+@pytest.mark.parametrize("captured", [False, True])
+def test_a_refused_release_changes_nothing_and_can_be_made_again(captured):
+    pc, dt = two_rows()
+    ended = dev([1, 1])
+    call = lambda: dt.release(ended)  # noqa: E731
+    if captured:
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            call()
+        call = graph.replay
+    pc.free_taken.fill_(1)  # (fewer than the rows hold)
+    for _ in range(2):
+        call()
+        torch.cuda.synchronize()
+        assert ints(dt.status) == [ilpc.NO_BLOCKS]
+        assert (ints(pc.free_taken), ints(dt.seq_lens), ints(dt.first_block)) == ([1], [33, 33], [2, 2])
+        assert ints(pc.free_ids) == list(range(16, 25))
+    pc.free_taken.fill_(2)
+    for _ in range(2):  # (the second one finds nothing to give back)
+        call()
+        torch.cuda.synchronize()
+        assert (ints(dt.status), ints(pc.free_taken), ints(dt.seq_lens), ints(dt.first_block)) == ([0], [0], [0, 0], [0, 0])
+        assert sorted(ints(pc.free_ids)) == list(range(16, 25))
