@@ -539,7 +539,10 @@ int ilpc_diff_attn_workspace_bytes(int32_t B, int32_t max_q_len, int32_t Hq, int
  * the maps nearly cancel.  Requests with q_len_r > L_r are not computed;
  * otherwise the bounds rules of ilpc_paged_prefill_attn hold.  Up to
  * 2^18 (request, kv head) pairs of up to 2^22 (query, head of the group)
- * columns, beyond that up to 2^24 tiles of 16 columns (ILPC_EUNSUP).
+ * columns, beyond that up to 2^24 tiles of 16 columns (ILPC_EUNSUP).  A batch
+ * of more than 2^25 columns in all (n_rows * Hq / Hkv) needs requests that are
+ * two thirds as long as max_q_len on average, or max_q_len for which all pairs
+ * have up to 2^24 tiles of 128 columns (ILPC_EUNSUP).
  */
 int ilpc_paged_diff_attn(const uint16_t* q, int64_t q_stride, int32_t n_rows, const uint16_t* k_pool,
                          const uint16_t* v_pool, int32_t num_blocks, const int32_t* block_tables, int32_t max_blocks,

@@ -65,7 +65,8 @@ struct DiffArgs {
   uint16_t* out;
 };
 
-// The kernel for many columns (diff_prefill.hip); false: the launch failed.
-bool launch_diff_prefill(const DiffArgs& a, hipStream_t stream);
+// The kernel for many columns (diff_prefill.hip); ILPC_EUNSUP: its grid does not hold the
+// batch, ILPC_EHIP: no device, or the launch failed.
+int launch_diff_prefill(const DiffArgs& a, hipStream_t stream);
 
 }  // namespace ilpc

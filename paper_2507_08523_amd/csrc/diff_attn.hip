@@ -545,8 +545,14 @@ Plan stream_plan(int64_t units, int64_t n_ct, int64_t max_blocks, int D) {
 // (Its grid holds 2^22 columns a request and 2^18 pairs.)
 bool many_columns(int64_t B, int64_t max_q_len, int Hq, int Hkv, int D) {
   const int64_t n_ct = column_tiles(max_q_len, Hq, Hkv);
-  if (max_q_len * (Hq / Hkv) > (int64_t(1) << 22) || B * Hkv > (1 << 18)) return false;
+  if (max_q_len * (Hq / Hkv) > (1 << 22) || B * Hkv > (1 << 18)) return false;
   return n_ct > 1 && B * Hkv * n_ct > (D == 64 ? 11 : 4) * int64_t(ilpc::device_cus());
+}
+
+// Workgroups of a launch.
+int64_t stream_grid(int64_t units, const Plan& plan) {
+  const int64_t per_group = group_waves(plan.waves) / plan.waves;
+  return (units * plan.groups + per_group - 1) / per_group;
 }
 
 size_t part_bytes(int64_t units, int D, int n) {
@@ -560,8 +566,13 @@ int check_sizes(const char* fn, int32_t B, int32_t max_q_len, int32_t Hq, int32_
   if (D != 64 && D != 128) return set_error(ILPC_EUNSUP, "%s: head_dim %d unsupported", fn, D);
   if (Hq % Hkv != 0 || Hq / Hkv > 64) return set_error(ILPC_EUNSUP, "%s: Hq %d / Hkv %d unsupported", fn, Hq, Hkv);
   if (max_blocks > (1 << 24)) return set_error(ILPC_EUNSUP, "%s: max_blocks %d > %d", fn, max_blocks, 1 << 24);
-  if (int64_t(B) * Hkv > INT32_MAX / 16 || int64_t(max_q_len) * (Hq / Hkv) > (int64_t(1) << 30) ||
-      int64_t(B) * Hkv * column_tiles(max_q_len, Hq, Hkv) > INT32_MAX / 16)
+  if (int64_t(B) * Hkv > INT32_MAX / 16 || int64_t(max_q_len) * (Hq / Hkv) > (1 << 30))
+    return set_error(ILPC_EUNSUP, "%s: batch too large", fn);
+  // The kernel for few columns: fewer than 2^32 threads (and 2^31 items).  So many units
+  // are one or two waves each whatever the device.
+  const int64_t n_ct = column_tiles(max_q_len, Hq, Hkv), units = int64_t(B) * Hkv * n_ct;
+  if (units > (1 << 24) && !many_columns(B, max_q_len, Hq, Hkv, D) &&
+      stream_grid(units, stream_plan(units, n_ct, max_blocks, D)) * (64 * 4) > UINT32_MAX)
     return set_error(ILPC_EUNSUP, "%s: batch too large", fn);
   return ILPC_OK;
 }
@@ -611,15 +622,16 @@ extern "C" int ilpc_paged_diff_attn(const uint16_t* q, int64_t q_stride, int32_t
     return set_error(ILPC_EINVAL, "%s: q_stride must be a multiple of 8 elements, at least Hq * D", fn);
   const uint16_t *q_end = q + int64_t(n_rows - 1) * q_stride + int64_t(Hq) * D, *out_end = out + int64_t(n_rows) * Hq * D;
   if (q < out_end && out < q_end) return set_error(ILPC_EINVAL, "%s: q and out overlap", fn);
-  if (ilpc::device_cus() <= 0) return set_error(ILPC_EHIP, "%s: cannot query the device", fn);
   if (many_columns(B, max_q_len, Hq, Hkv, D)) {
     const DiffArgs a{q, q_stride, n_rows, k_pool, v_pool, num_blocks, block_tables, max_blocks, cu_q, seq_lens, B,
                      max_q_len, Hq, Hkv, D, softmax_scale * 1.4426950408889634f, int(layout == ILPC_DIFF_ROPE),
                      DiffEpilogue{lambda, norm_weight, norm_eps, out_scale}, out};
-    if (!launch_diff_prefill(a, static_cast<hipStream_t>(stream)))
-      return set_error(ILPC_EHIP, "%s: launch failed", fn);
+    const int rc = launch_diff_prefill(a, static_cast<hipStream_t>(stream));
+    if (rc == ILPC_EUNSUP) return set_error(rc, "%s: batch too large", fn);
+    if (rc != ILPC_OK) return set_error(rc, "%s: no device, or the launch failed", fn);
     return ILPC_OK;
   }
+  if (ilpc::device_cus() <= 0) return set_error(ILPC_EHIP, "%s: cannot query the device", fn);
   const int64_t n_ct = column_tiles(max_q_len, Hq, Hkv), units = int64_t(B) * Hkv * n_ct;
   const Plan plan = stream_plan(units, n_ct, max_blocks, D);
   const size_t need = part_bytes(units, D, plan.groups);
@@ -628,9 +640,7 @@ extern "C" int ilpc_paged_diff_attn(const uint16_t* q, int64_t q_stride, int32_t
   const DiffEpilogue ep{lambda, norm_weight, norm_eps, out_scale};
   float* part_o = need ? static_cast<float*>(workspace) : nullptr;
   float* part_ml = need ? part_o + size_t(units) * plan.groups * (2 * kTileCols) * D : nullptr;
-  const int64_t items = units * plan.groups, per_group = group_waves(plan.waves) / plan.waves;
-  const dim3 grid{unsigned((items + per_group - 1) / per_group)}, block{unsigned(64 * group_waves(plan.waves))};
-  if (uint64_t(grid.x) * block.x > UINT32_MAX) return set_error(ILPC_EUNSUP, "%s: batch too large", fn);
+  const dim3 grid{unsigned(stream_grid(units, plan))}, block{unsigned(64 * group_waves(plan.waves))};
   hipStream_t s = static_cast<hipStream_t>(stream);
   auto launch = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, grid, block, 0, s, q, q_stride, n_rows, k_pool, v_pool, num_blocks, block_tables, max_blocks,

@@ -41,6 +41,7 @@
 #include <cstdint>
 #include <type_traits>
 
+#include "../../include/ilpc.h"
 #include "diff_attn.h"
 #include "ilpc_internal.h"
 
@@ -503,19 +504,22 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void diff_prefill_kerne
 
 namespace ilpc {
 
-bool launch_diff_prefill(const DiffArgs& a, hipStream_t stream) {
+int launch_diff_prefill(const DiffArgs& a, hipStream_t stream) {
   // By pair where that fills all XCDs evenly and most numbers hold rows (the host knows
-  // the longest request and the sum of all); else by rows.
+  // the longest request and the sum of all); else by rows, as far as that grid goes; past
+  // that by pair again, up to 2^25 workgroups, most of which may be idle.
   const int64_t G = a.Hq / a.Hkv, n_ct = (a.max_q_len * G + kCols - 1) / kCols, pairs = int64_t(a.B) * a.Hkv;
   const int64_t numbers = a.n_rows * G / kCols + a.B;
-  const bool by_pair = ((pairs % 8 == 0 || pairs >= 64) && 2 * a.B * n_ct <= 3 * numbers) ||
-                       numbers > 8 * 65535 || a.Hkv > 65535;  // (more than the other grid holds)
+  const bool even = (pairs % 8 == 0 || pairs >= 64) && 2 * a.B * n_ct <= 3 * numbers;
+  const bool by_pair = even || numbers > 8 * 65535 || a.Hkv > 65535;
+  if (by_pair && !even && pairs * n_ct > (1 << 25)) return ILPC_EUNSUP;
+  if (device_cus() <= 0) return ILPC_EHIP;
   const dim3 grid(8, unsigned(by_pair ? n_ct : (numbers + 7) / 8), unsigned(by_pair ? (pairs + 7) / 8 : a.Hkv));
   const dim3 block(64 * kWaves);
   const int recip = 65536 / int(G) + 1, numbering = by_pair ? kByPair : kByRows;
   if (a.D == 128) hipLaunchKernelGGL(diff_prefill_kernel<128>, grid, block, 0, stream, a, recip, numbering);
   else hipLaunchKernelGGL(diff_prefill_kernel<64>, grid, block, 0, stream, a, recip, numbering);
-  return hipGetLastError() == hipSuccess;
+  return hipGetLastError() == hipSuccess ? ILPC_OK : ILPC_EHIP;
 }
 
 }  // namespace ilpc

@@ -520,3 +520,17 @@ def test_many_columns_of_64_dimensions_rows_that_stay_and_bad_ids():
     out = b.run()
     b.check(out, rows_of=[r for r in range(12) if r not in (1, 3, 7)])
     assert (out[ends[1]:ends[2]] == 7.0).all() and (out[ends[n - 1]:] == 7.0).all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_a_long_bound_over_many_requests(D):
+    """4096 requests of 8 kv heads, the longest bounded by 2^17 rows (more than 2^27 tiles of 16
+    columns, few of them with rows)."""
+    rng = np.random.default_rng(D)
+    lens = [int(x) for x in rng.integers(1, 40, 4096)]
+    new = [int(rng.integers(0, 2)) for _ in lens]
+    lens[2900], new[2900] = 500, 300
+    b = Batch(lens, new, 8, 8, D, seed=18)
+    b.max_q = 1 << 17
+    assert ilpc.diff_attn_workspace_bytes(4096, b.max_q, 8, 8, D, b.bt.shape[1]) == 0
+    b.check(b.run(), rows_of=[*range(0, 2890, 97), *range(2895, 2905), *range(4080, 4096)])

@@ -104,3 +104,33 @@ def test_binding_takes_only_gpu_tensors():
 def test_library_refuses_overlaps_and_grids_before_a_launch(call, kw, rc):
     assert call(**kw) == rc
     assert (b"overlap" if "out" in kw else b"too large") in ilpc.load().ilpc_last_error()
+
+
+# (B, max_q_len, Hq, Hkv, D, max_blocks): what the documented limits allow, and not
+ALLOWED = [(512, 131072, 64, 8, 128, 8192), (1 << 15, 1 << 19, 64, 8, 64, 9), (1 << 18, 1 << 16, 64, 1, 128, 4),
+           (1 << 24, 1, 16, 1, 128, 4), (1 << 21, 1, 128, 8, 64, 9000), ((1 << 18) + 1, 63, 16, 1, 128, 4),
+           (9, (1 << 16) + 1, 512, 8, 128, 4)]
+TOO_LARGE = [(1 << 25, 1, 16, 1, 128, 9), (1 << 22, 1, 64, 8, 64, 9000), ((1 << 18) + 1, 128, 16, 1, 128, 9),
+             (1 << 26, 1, 16, 1, 128, 4), (1 << 27, 1, 8, 1, 128, 4)]
+
+
+def test_sizes_within_the_documented_limits_are_taken():
+    n = ctypes.c_size_t()
+    for sizes in ALLOWED:  # (EHIP: no device to ask)
+        rc = code("ilpc_diff_attn_workspace_bytes", *sizes, ctypes.byref(n))
+        assert rc in (ilpc.OK, ilpc.EHIP), (sizes, ilpc.load().ilpc_last_error())
+
+
+@pytest.mark.parametrize("sizes", TOO_LARGE)
+def test_query_and_launch_refuse_the_same_sizes(sizes):
+    n = ctypes.c_size_t()
+    B, mq, Hq, Hkv, D, mb = sizes
+    assert code("ilpc_diff_attn_workspace_bytes", *sizes, ctypes.byref(n)) == ilpc.EUNSUP
+    assert attn(B=B, mq=mq, Hq=Hq, Hkv=Hkv, D=D, mb=mb, qs=Hq * D, out=1 << 50) == ilpc.EUNSUP
+
+
+def test_batches_past_both_grids_are_refused_before_a_launch():
+    # more than 2^25 columns in all, most of the requests much shorter than the longest
+    big = dict(B=1 << 15, mq=1 << 19, Hq=64, Hkv=8, D=64, mb=9, qs=4096, out=1 << 50)
+    assert attn(rows=1 << 24, **big) == ilpc.EUNSUP
+    assert b"too large" in ilpc.load().ilpc_last_error()
