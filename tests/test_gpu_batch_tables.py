@@ -564,3 +564,90 @@ def test_a_refused_release_changes_nothing_and_can_be_made_again(captured):
         torch.cuda.synchronize()
         assert (ints(dt.status), ints(pc.free_taken), ints(dt.seq_lens), ints(dt.first_block)) == ([0], [0], [0, 0], [0, 0])
         assert sorted(ints(pc.free_ids)) == list(range(16, 25))
+
+
+@pytest.mark.parametrize("captured", [False, True])
+def test_steps_until_the_free_list_is_drained(captured):
+    """One-token steps of two requests take every spare block; the next one is refused for that alone
+    and changes nothing, and steps go on once the other request has ended."""
+    pc = pipeline.PagedPrefixCache(2, 64, 16, 8, 2, 8, spare_blocks=4)
+    tables = np.full((2, 8), -1, np.int32)
+    tables[0, 0], tables[1, 0] = 3, 9
+    dt = pipeline.DeviceTables(pc, tables, [16, 16], max_rows=2)
+    new, k = dev([1, 1]), torch.zeros(2, 2, 64, dtype=torch.bfloat16, device="cuda")
+
+    def step():
+        dt.extend(new, 1)
+        dt.append(k, k)
+
+    if captured:
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step()
+        step = graph.replay
+    for s in range(32):  # two blocks each
+        k.fill_(float(s + 1))
+        step()
+        assert ints(dt.status) == [0] and ints(dt.seq_lens) == [17 + s] * 2
+    assert ints(pc.free_taken) == [4]
+    pool, held = pc.k_pool.clone(), ints(dt.block_tables)
+    k.fill_(99.0)
+    for _ in range(2):
+        step()
+        assert ints(dt.status) == [ilpc.NO_BLOCKS]
+        assert (ints(dt.seq_lens), ints(dt.cu_q), ints(dt.slot_map)) == ([48, 48], [0, 0, 0], [-1, -1])
+        assert ints(pc.free_taken) == [4] and ints(dt.block_tables) == held and torch.equal(pc.k_pool, pool)
+    dt.release(torch.tensor([False, True], device="cuda"))
+    assert ints(dt.status) == [0] and ints(pc.free_taken) == [2]
+    new.copy_(dev([1, 0]))
+    for s in range(32):
+        step()
+        assert ints(dt.status) == [0] and ints(dt.seq_lens) == [49 + s, 0] and ints(dt.slot_map)[1] == -1
+    assert ints(pc.free_taken) == [4] and len(set(ints(dt.block_tables)[0][:5])) == 5
+    step()
+    assert ints(dt.status) == [ilpc.NO_BLOCKS]
+
+
+def test_prefill_and_decode_against_the_stored_keys():
+    """As the decode loop above, the oracle fed with the rows that the pools and the rotated queries
+    hold, so that only the kernels' own error is left: the output's rounding and as much of the
+    weights' (0.0045 in the 2-norm, as for single calls)."""
+    Hq, Hkv, D, B = 8, 2, 128, 3
+    L0 = np.array([50, 16, 77])
+    freq = np.concatenate([pipeline.rope_inv_freq(D // 2, 10000.0)] * 2)
+    fr = torch.from_numpy(freq).cuda()
+    rng = np.random.default_rng(5)
+    pc = pipeline.PagedPrefixCache(Hkv, D, 16, 10, B, 8, spare_blocks=12)
+    rnd = lambda *s: torch.randn(*s, device="cuda").to(torch.bfloat16)  # noqa: E731
+    lam, w, scale = torch.rand(Hq, device="cuda"), 1 + 0.1 * torch.randn(D, device="cuda"), (D // 2) ** -0.5
+    cached, tables = pc.match([rng.integers(0, 1000, n).astype(np.int32) for n in L0])
+    dt = pipeline.DeviceTables(pc, tables, L0, max_rows=B + 1)
+
+    def check(q, out, table, L):
+        table = np.array(ints(table)[:-(-L // BLOCK)])
+        k = pc.k_pool[table].float().permute(0, 2, 1, 3).reshape(-1, Hkv, D)[:L].cpu().numpy()
+        v = pc.v_pool[table].float().permute(0, 3, 1, 2).reshape(-1, Hkv, D)[:L].cpu().numpy()
+        ref = diff_attention_ref(q.float().cpu().numpy(), k, v, scale, lam.double().cpu().numpy(),
+                                 w.double().cpu().numpy(), out_scale=0.2, layout="rope")
+        err = np.linalg.norm(out.float().cpu().numpy() - ref) / np.linalg.norm(ref)
+        assert err <= 0.0045, err
+
+    def forward(batch, n):
+        q, k, v = rnd(n, Hq, D), rnd(n, Hkv, D), rnd(n, Hkv, D)
+        qr, out = torch.zeros_like(q), torch.empty_like(q)
+        pc.append_rope(batch, k, v, fr, q, qr)  # (by the tables; rows behind the last stay)
+        pc.attend_diff(batch, qr, out, scale, lam, w, out_scale=0.2, layout=ilpc.DIFF_ROPE)
+        return qr, out
+
+    batch = pc.upload_prefill(cached, tables, L0)
+    qr, out = forward(batch, int(L0.sum()))
+    cu = np.concatenate([[0], np.cumsum(L0)])
+    for r in range(B):
+        check(qr[cu[r]:cu[r + 1]], out[cu[r]:cu[r + 1]], batch.block_tables[r], int(L0[r]))
+    for s in range(35):
+        qr, out = forward(dt.extend(dev([1] * B), 1), B + 1)
+        assert ints(dt.status) == [0]
+        for r in range(B):
+            if s % 6 == 0 or s > 32:
+                check(qr[r:r + 1], out[r:r + 1], dt.block_tables[r], int(L0[r]) + s + 1)
