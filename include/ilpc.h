@@ -534,9 +534,9 @@ int ilpc_diff_attn_workspace_bytes(int32_t B, int32_t max_q_len, int32_t Hq, int
  *              among them, need separate ones.
  *
  * Scores, softmax sums and the products with V are held in fp32; the weights
- * enter those products as bf16 numbers whose rounding is made up for (see the
- * kernels), so that the error stays near the rounding of the output also where
- * the maps nearly cancel.  Requests with q_len_r > L_r are not computed;
+ * enter those products as bf16 numbers, two to a weight or one to the difference
+ * of both maps' weights (see the kernels), so that the error stays near the
+ * rounding of the output also where the maps nearly cancel.  Requests with q_len_r > L_r are not computed;
  * otherwise the bounds rules of ilpc_paged_prefill_attn hold.  Up to
  * 2^18 (request, kv head) pairs of up to 2^22 (query, head of the group)
  * columns, beyond that up to 2^24 tiles of 16 columns (ILPC_EUNSUP).  A batch

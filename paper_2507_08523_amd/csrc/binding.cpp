@@ -8,9 +8,10 @@
 //
 // A function returns the library's code, or None with nothing called for
 // whatever it does not take as it stands (another type of argument or tensor, a
-// failed check, a workspace still to be allocated): ilpc.py then takes its own
-// path, which allocates, converts, or raises the error with its text.  Nothing
-// is kept from one call to the next but the library's entry points.
+// failed check; for ordinary attention a workspace still to be allocated):
+// ilpc.py then takes its own path, which allocates, converts, or raises the error
+// with its text.  Differential attention's workspace, which needs no initial
+// contents, is allocated here on the current stream.  Nothing is kept from one call to the next but the library's entry points.
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/ops/empty.h>

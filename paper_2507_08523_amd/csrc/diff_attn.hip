@@ -499,13 +499,14 @@ int64_t column_tiles(int64_t max_q_len, int Hq, int Hkv) {
 // all starts.  8 kv heads, D 128, us:
 //   units, keys       waves x workgroups
 //   8, 600            4x1 9.4, 4x5 8.6       8, 1000     4x1 12.2, 4x4 9.8, 4x8 8.7
-//   8, 4000           4x6 13.3, 4x16 11.1    32, 500     4x1 8.7, 4x4 9.3
+//   8, 4000           4x6 13.3, 4x11 12.0 (taken), 4x16 11.1
+//   32, 500           4x1 8.7, 4x4 9.3
 //   32, 800           4x4 10.5, 4x7 9.6      32, 2100    4x4 14.1, 4x8 12.3
 //   64, 800           4x1 11.6, 4x4 10.9     64, 2100    4x1 22.8, 4x4 18.5
 //   96, 2100          4x1 23.2, 4x2 23.0     96, 4000    4x1 37.8, 4x2 34.1
 //   128, 2100         4x1 24.7, 4x2 27.9     128, 8000   4x1 96.3, 4x2 91.5
 //   264, 1000         2x1 24.4, 4x1 29.4
-//   576, 1000         2x1 56.6, 4x1 47.8; of 300 21.3, 20.3
+//   576, 1000         2x1 56.6, 4x1 47.8; of 300 21.3 (taken), 20.3
 //   1024, 1000        2x1 88.6, 4x1 87.8 (60% of the keys shared by all 39.0, 41.8)
 //   1248, 1000        2x1 111, 4x1 107       4096, 2100  2x1 684, 4x1 682 (324, 350)
 // D 64, whose steps and join are shorter: 512 of 2100 2x1 41.4, 4x1 41.8 (shared 31.4,

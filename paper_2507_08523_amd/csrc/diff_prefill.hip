@@ -26,13 +26,13 @@
 // 2 + 2 + 2), took 0.72 to 0.87 of the time and was not kept: weights rounded against a ratio that the
 // first keys have and the others do not left 0.006 to 0.026 of nearly agreeing maps.
 //
-// What bounds it: vector instructions, 242 a step and wave in both passes (64 of them
-// exponentials) or 1320 cycles, and 770 cycles of products, of which two waves a SIMD
-// overlap next to nothing (2030 cycles a step and wave): 64 prompts of 1.9 K tokens (64/8
-// heads) 8.2 to 9.1 ms (box to box), 0.73 to 0.83 PFLOP/s of products.  Tried, within 1% of
-// this: the next step's scores in a second set of registers, their products placed between
-// the exponentials; 3 or 6 LDS operands in flight instead of 4; the products' raised
-// priority left out.
+// What bounds it: vector instructions.  242 a step and wave in both passes, 64 of them
+// exponentials of 8 cycles, keep a SIMD busy 66% of the time, the products 38%, 16% both at
+// once (a product also holds up the vector instructions beside it, 12 to 25 cycles each): 64
+// prompts of 1.9 K tokens (64/8 heads) 8.2 to 9.1 ms (box to box), 0.73 to 0.83 PFLOP/s of
+// products.  Tried, within 1% of this: the next step's scores in a second set of registers,
+// their products placed between the exponentials; 3 or 6 LDS operands in flight instead of 4;
+// the products' raised priority left out.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

@@ -134,3 +134,17 @@ def test_batches_past_both_grids_are_refused_before_a_launch():
     big = dict(B=1 << 15, mq=1 << 19, Hq=64, Hkv=8, D=64, mb=9, qs=4096, out=1 << 50)
     assert attn(rows=1 << 24, **big) == ilpc.EUNSUP
     assert b"too large" in ilpc.load().ilpc_last_error()
+
+
+def test_the_committed_profile_names_the_current_kernel_code(monkeypatch):
+    import os
+    import re
+
+    import bench
+
+    text = open(os.path.join(bench.ROOT, "profiles", "diff_attn_kernel_trace.txt"), encoding="utf-8").read()
+    found = dict(re.findall(r"^# code of (\w+\.hip): ([0-9a-f]{16})$", text, re.M))
+    assert set(found) == {"diff_attn.hip", "diff_prefill.hip", "batch_tables.hip"}
+    for name, sha in found.items():
+        monkeypatch.setattr(bench, "KERNEL_SRC", os.path.join(bench.ROOT, "paper_2507_08523_amd", "csrc", name))
+        assert bench.kernel_source_sha() == sha, name
