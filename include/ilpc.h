@@ -552,6 +552,190 @@ int ilpc_paged_diff_attn(const uint16_t* q, int64_t q_stride, int32_t n_rows, co
                          uint16_t* out, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Trees of drafted tokens (speculative decoding over the paged cache, section
+ * 2.1.2: the newest tokens attend to the cached KV of their context).  A request
+ * of P tokens gets n drafted ones at the positions P .. P+n-1 of its cache
+ * (ilpc_extend_tables, ilpc_kv_append_slots); its node i continues node
+ * parents[i] < i, or the context (-1).  ilpc_tree_masks says which nodes a node
+ * sees, ilpc_paged_tree_attn attends, ilpc_tree_accept finds the nodes that the
+ * target model's picks confirm, ilpc_kv_compact moves their K/V rows to the front;
+ * blocks behind them go back by ilpc_release_tables (first_block = kept_blocks,
+ * seq_lens = the lengths with all nodes).  Rows of request r are cu_q[r] ..
+ * cu_q[r+1]-1 in all of them; requests with rows outside [0, n_rows) are taken as
+ * having none.  B <= 2^20 (ILPC_EUNSUP).
+ */
+
+/*
+ * Ancestor masks of the trees: bit j % 64 of word j / 64 of row i is set where
+ * node j of the request is node i or an ancestor of it.
+ *
+ * parents    [device] int32 [n_rows]  within the request; a value outside [-1, i)
+ *                                     (padding) is a node that sees itself alone
+ * cu_q       [device] int32 [B+1]
+ * start_pos  [device] int32 [B] or NULL (0)  position of the request's roots
+ * masks      [device] uint64 [n_rows, mask_words], 8-byte aligned, out;
+ *            1 <= mask_words <= 16 (ILPC_EUNSUP); nodes at or past 64 * mask_words
+ *            see no node
+ * positions  [device] int32 [n_rows] or NULL  out: start_pos + the node's depth
+ *
+ * Rows of no request stay as they are.
+ */
+int ilpc_tree_masks(const int32_t* parents, const int32_t* cu_q, const int32_t* start_pos, int32_t B,
+                    int32_t n_rows, int32_t mask_words, uint64_t* masks, int32_t* positions, void* stream);
+
+/* Bytes of device workspace ilpc_paged_tree_attn needs for these sizes on the
+ * current device (0 where one workgroup works a request's keys). */
+int ilpc_tree_attn_workspace_bytes(int32_t B, int32_t max_q_len, int32_t Hq, int32_t Hkv, int32_t D,
+                                   int32_t max_blocks, size_t* bytes);
+
+/*
+ * Attention of each request's newest q_len_r tokens, its nodes, whose keys are
+ * the last q_len_r of its L_r: node i sees the keys 0 .. L_r - q_len_r - 1 and, of
+ * the nodes, those of its mask (any mask, not only a tree's; its own bit counts
+ * like the others).  A row that sees no key gives zeros.  Pools, tables, head groups
+ * and scale are those of ilpc_paged_prefill_attn, with these arguments:
+ *
+ * q            [device] bf16, row i at q + i * q_stride (elements; a multiple
+ *              of 8, at least Hq * D): [Hq, D], contiguous
+ * n_rows       [host]   rows of q, masks and out
+ * max_q_len    [host]   >= every q_len_r, at most 1024 (ILPC_EUNSUP); rows beyond it
+ *              are not computed
+ * softmax_scale > 0
+ * masks        [device] uint64 [n_rows, mask_words], 8-byte aligned;
+ *              max_q_len <= 64 * mask_words <= 1024; bits of nodes that are not there
+ *              are ignored
+ * out          [device] bf16 [n_rows, Hq, D], not overlapping q; rows of no
+ *              request stay as they are
+ * workspace    [device] >= ilpc_tree_attn_workspace_bytes() bytes, 16-byte
+ *              aligned, no initial contents needed (NULL with 0 bytes where
+ *              that is 0).  Calls that may run concurrently, captured graphs
+ *              among them, need separate ones.
+ *
+ * K and V of a node that none of its request's rows sees may be anything (slots
+ * that hold no token); V of the others is finite.  Requests with q_len_r > L_r are
+ * not computed; otherwise the bounds rules of ilpc_paged_prefill_attn hold.  At
+ * most 2^23 tiles of 32 columns (B * Hkv * ceil(max_q_len * Hq / Hkv / 32);
+ * ILPC_EUNSUP).
+ */
+int ilpc_paged_tree_attn(const uint16_t* q, int64_t q_stride, int32_t n_rows, const uint16_t* k_pool,
+                         const uint16_t* v_pool, int32_t num_blocks, const int32_t* block_tables, int32_t max_blocks,
+                         const int32_t* cu_q, const int32_t* seq_lens, int32_t B, int32_t max_q_len, int32_t Hq,
+                         int32_t Hkv, int32_t D, int32_t block_size, float softmax_scale, const uint64_t* masks,
+                         int32_t mask_words, uint16_t* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The path of nodes that the target model confirms: from the root on, always the
+ * first node (lowest index) that continues the last accepted one and whose token
+ * is the target's pick behind it.
+ *
+ * parents, tokens, targets [device] int32 [n_rows]  targets[i]: the target's pick
+ *              behind node i (greedy or sampled; a pick is an input)
+ * root_targets [device] int32 [B] or NULL  the pick behind the context, which a
+ *              node of parent -1 has to be.  NULL: node 0 (parent -1) is the root,
+ *              a token already decided, accepted whatever it is; other nodes of
+ *              parent -1 are not.
+ * start_pos    [device] int32 [B]  tokens before the nodes
+ * path         [device] int32 [n_rows]  out: the accepted nodes of request r at
+ *              cu_q[r] .., ascending, then -1; rows of no request stay as they are
+ * n_accepted   [device] int32 [B]  out
+ * next_tokens  [device] int32 [B]  out: the pick behind the last accepted node; with
+ *              none accepted root_targets[r], or -1
+ * kept_lens    [device] int32 [B]  out: start_pos + n_accepted
+ * kept_blocks  [device] int32 [B]  out: blocks that these tokens fill or begin
+ *
+ * A node whose parent is outside [-1, i) is not accepted.  Outputs must not
+ * overlap inputs.
+ */
+int ilpc_tree_accept(const int32_t* parents, const int32_t* tokens, const int32_t* targets,
+                     const int32_t* root_targets, const int32_t* cu_q, const int32_t* start_pos, int32_t B,
+                     int32_t n_rows, int32_t* path, int32_t* n_accepted, int32_t* next_tokens, int32_t* kept_lens,
+                     int32_t* kept_blocks, void* stream);
+
+/*
+ * K/V rows of accepted nodes to the front of the draft: of request r, the row at
+ * position start_pos[r] + path[cu_q[r] + i] goes to position start_pos[r] + i, for
+ * i < n_accepted[r] (n_accepted and path as ilpc_tree_accept writes them: ascending,
+ * so that path[cu_q[r] + i] >= i).  In place, every row as it was before the call;
+ * rows that no accepted one goes to stay as they are.  The blocks written are held by
+ * this request alone.  Entries of path outside [i, q_len_r), blocks outside
+ * [0, num_blocks) and positions past 16 * max_blocks are left out.  Hkv <= 65535,
+ * max_blocks <= 2^24 (ILPC_EUNSUP).
+ */
+int ilpc_kv_compact(uint16_t* k_pool, uint16_t* v_pool, int32_t num_blocks, const int32_t* block_tables,
+                    int32_t max_blocks, const int32_t* cu_q, const int32_t* start_pos, int32_t B, int32_t n_rows,
+                    const int32_t* path, const int32_t* n_accepted, int32_t Hkv, int32_t D, int32_t block_size,
+                    void* stream);
+
+/* int32 words of the hold counts of n_blocks blocks: a count a block, and a bit a
+ * block that ilpc_release_shared uses and leaves zero. */
+int ilpc_holds_words(int32_t n_blocks, int32_t* words);
+
+/*
+ * Rows of a batch become forks of other rows (several answers sampled from one
+ * prompt, beams; section 2.1.2: requests share the blocks of a common prefix).
+ * Row r with sources[r] = s != r then holds row s's tokens: the entries of its full
+ * blocks with s, each counted as held once more, and a block of its own, taken
+ * from the free list, for a partly filled last one, which ilpc_copy_blocks
+ * fills in (copy_src, copy_dst: once for every layer's pools).  Rows with
+ * sources[r] = r stay; a source has to be one of them.  What row r held before is
+ * not given back (ilpc_release_shared).
+ *
+ * block_tables [device] int32 [B, max_blocks]  in/out: forks' rows are written
+ *              whole, -1 behind their blocks
+ * seq_lens     [device] int32 [B]  in/out: tokens held; a fork gets its source's
+ * sources      [device] int32 [B]
+ * holds        [device] int32 [ilpc_holds_words(num_blocks - first_id)]  in/out:
+ *              holders of block first_id + b beyond the first; zero-filled when all
+ *              these blocks are free or held once.  Blocks below first_id (the prefix
+ *              cache's) are shared without being counted.
+ * free_ids, n_free, taken, taken_out  as for ilpc_extend_tables; forks take their
+ *              blocks in row order
+ * copy_src, copy_dst [device] int32 [B]  out: block to copy from and to, or -1
+ * status       [device] int32 [1]  out: 0, or bits: 1 free_ids does not hold enough, 2 a
+ *              source longer than 16 * max_blocks, 8 a source that is no row or
+ *              does not stay, a negative length or taken outside [0, n_free]; then
+ *              nothing is changed, and the copies are -1
+ *
+ * A shared block is full and stays so: no row may be cut back below the length it
+ * was forked at.  Limits as for ilpc_extend_tables.  Outputs must not overlap other
+ * arguments (taken_out may be taken).
+ */
+int ilpc_fork_tables(int32_t* block_tables, int32_t max_blocks, int32_t B, int32_t* seq_lens, const int32_t* sources,
+                     int32_t* holds, int32_t first_id, const int32_t* free_ids, int32_t n_free, const int32_t* taken,
+                     int32_t num_blocks, int32_t* copy_src, int32_t* copy_dst, int32_t* taken_out, int32_t* status,
+                     void* stream);
+
+/*
+ * Blocks of ended rows given back where rows share them: of row r, the first
+ * ceil(seq_lens[r] / 16) entries each drop one hold (those of blocks below first_id,
+ * or past num_blocks, none); a block without a holder left goes back to the free
+ * list, in front of the ids still free, in ascending order of the ids:
+ *   free_ids[taken - n + k] = the k-th of the n blocks.
+ * A row that goes on has seq_lens[r] = 0 here.  The tables are not changed.
+ *
+ * holds      [device] int32, as for ilpc_fork_tables, in/out
+ * free_ids   [device] int32 [n_free]  in/out
+ * taken_out  [device] int32 [1]  out: taken - n; may be taken
+ * status     [device] int32 [1]  out: 0, or bits: 1 more blocks than were taken, 2 a row
+ *            longer than its table, 8 a negative length or taken outside [0, n_free], 16 a
+ *            block given back more often than it is held; then nothing is changed
+ */
+int ilpc_release_shared(const int32_t* block_tables, int32_t max_blocks, int32_t B, const int32_t* seq_lens,
+                        int32_t* holds, int32_t first_id, int32_t* free_ids, int32_t n_free, const int32_t* taken,
+                        int32_t num_blocks, int32_t* taken_out, int32_t* status, void* stream);
+
+/*
+ * Whole blocks copied within the pools, K and V: block src[i] to block dst[i], for
+ * the pairs with both in [0, num_blocks).  A block that is copied to is in no other
+ * pair (else it holds unspecified ones of the values).
+ *
+ * src, dst [device] int32 [n]
+ * 2 * n * ceil(Hkv * D / 512) < 2^24, Hkv <= 65535 (ILPC_EUNSUP)
+ */
+int ilpc_copy_blocks(uint16_t* k_pool, uint16_t* v_pool, int32_t num_blocks, const int32_t* src, const int32_t* dst,
+                     int32_t n, int32_t Hkv, int32_t D, int32_t block_size, void* stream);
+
+/*
  * Scheduler steps of a chunked prefill (the per-step token bound that section
  * 3.3 tunes, vLLM's max-num-batched-tokens; section 4.1's PC-Chunk baseline).
  * Host only.

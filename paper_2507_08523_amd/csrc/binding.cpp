@@ -10,8 +10,8 @@
 // whatever it does not take as it stands (another type of argument or tensor, a
 // failed check; for ordinary attention a workspace still to be allocated):
 // ilpc.py then takes its own path, which allocates, converts, or raises the error
-// with its text.  Differential attention's workspace, which needs no initial
-// contents, is allocated here on the current stream.  Nothing is kept from one call to the next but the library's entry points.
+// with its text.  The workspaces of differential and of tree attention, which need no
+// initial contents, are allocated here on the current stream.  Nothing is kept from one call to the next but the library's entry points.
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/ops/empty.h>
@@ -37,6 +37,14 @@ decltype(&ilpc_release_tables) release_tables = nullptr;
 decltype(&ilpc_kv_append_slots) kv_append_slots = nullptr;
 decltype(&ilpc_diff_attn_workspace_bytes) diff_attn_workspace_bytes = nullptr;
 decltype(&ilpc_paged_diff_attn) paged_diff_attn = nullptr;
+decltype(&ilpc_tree_masks) tree_masks = nullptr;
+decltype(&ilpc_tree_attn_workspace_bytes) tree_attn_workspace_bytes = nullptr;
+decltype(&ilpc_paged_tree_attn) paged_tree_attn = nullptr;
+decltype(&ilpc_tree_accept) tree_accept = nullptr;
+decltype(&ilpc_kv_compact) kv_compact = nullptr;
+decltype(&ilpc_fork_tables) fork_tables = nullptr;
+decltype(&ilpc_release_shared) release_shared = nullptr;
+decltype(&ilpc_copy_blocks) copy_blocks = nullptr;
 
 constexpr int kNotHere = INT_MIN;  // what a body returns for a call it does not take
 
@@ -151,7 +159,7 @@ int call(int (*fn)(P...), A... args) {
 
 // bind(addresses of the entry points above, in their order)
 PyObject* py_bind(PyObject*, PyObject* const* argv, Py_ssize_t n) {
-  constexpr int kEntries = 10;
+  constexpr int kEntries = 18;
   void* p[kEntries];
   if (n != kEntries) {
     PyErr_Format(PyExc_TypeError, "bind() takes %d addresses", kEntries);
@@ -163,6 +171,8 @@ PyObject* py_bind(PyObject*, PyObject* const* argv, Py_ssize_t n) {
   auto set = [&](auto& fn) { fn = reinterpret_cast<std::decay_t<decltype(fn)>>(p[i++]); };
   set(kv_append), set(rope_kv_append), set(attn_workspace_bytes), set(prefill_attn), set(prefill_attn_cascade);
   set(extend_tables), set(release_tables), set(kv_append_slots), set(diff_attn_workspace_bytes), set(paged_diff_attn);
+  set(tree_masks), set(tree_attn_workspace_bytes), set(paged_tree_attn), set(tree_accept), set(kv_compact);
+  set(fork_tables), set(release_shared), set(copy_blocks);
   Py_RETURN_NONE;
 }
 
@@ -440,6 +450,176 @@ PyObject* py_paged_diff_attn(PyObject*, PyObject* const* argv, Py_ssize_t n) {
   });
 }
 
+uint64_t* u64(const at::Tensor* t) { return static_cast<uint64_t*>(t->data_ptr()); }
+
+// tree_masks(parents, cu_q, masks, positions, start_pos, stream)
+PyObject* py_tree_masks(PyObject*, PyObject* const* argv, Py_ssize_t n) {
+  return guarded([&]() -> int {
+    Args a{argv, n};
+    const at::Tensor *par = a.tensor(at::kInt, 1), *cu = a.tensor(at::kInt, 1), *m = a.tensor(at::kLong, 2),
+                     *pos = a.tensor_or_none(at::kInt, 1), *start = a.tensor_or_none(at::kInt, 1);
+    PyObject* so = a.next();
+    if (!a.ok) return kNotHere;
+    const int64_t rows = par->size(0), B = cu->size(0) - 1;
+    if (m->size(0) != rows || (pos && pos->size(0) != rows) || (start && start->size(0) != B)) return kNotHere;
+    if (pos ? !apart({m, pos}, {par, cu, start}) : !apart({m}, {par, cu, start})) return kNotHere;
+    void* s;
+    if (!placed({par, cu, m, pos, start}, so, &s)) return kNotHere;
+    return call(tree_masks, i32(par), i32(cu), start ? i32(start) : nullptr, int32_t(B), int32_t(rows),
+                int32_t(m->size(1)), u64(m), pos ? i32(pos) : nullptr, s);
+  });
+}
+
+// paged_tree_attn(q, k_pool, v_pool, block_tables, cu_q, seq_lens, max_q_len, scale, masks, out, workspace, stream)
+PyObject* py_paged_tree_attn(PyObject*, PyObject* const* argv, Py_ssize_t n) {
+  return guarded([&]() -> int {
+    Args a{argv, n};
+    int64_t qs = 0;
+    const at::Tensor *q = rows(a, &qs), *kp = a.tensor(at::kBFloat16, 4), *vp = a.tensor(at::kBFloat16, 4),
+                     *bt = a.tensor(at::kInt, 2), *cu = a.tensor(at::kInt, 1), *L = a.tensor(at::kInt, 1);
+    const int32_t max_q = a.integer();
+    const float scale = a.real();
+    const at::Tensor *m = a.tensor(at::kLong, 2), *out = a.tensor(at::kBFloat16, 3),
+                     *ws = a.tensor_or_none(at::kByte, 1);
+    PyObject* so = a.next();
+    if (!a.ok) return kNotHere;
+    const int64_t B = cu->size(0) - 1, Hq = q->size(1), Hkv = kp->size(1), D = kp->size(3);
+    if (!pools_fit(*kp, *vp) || q->size(2) != D || out->sizes() != q->sizes() || bt->size(0) != B ||
+        L->size(0) != B || m->size(0) != q->size(0))
+      return kNotHere;
+    void* s;
+    if (!placed({q, kp, vp, bt, cu, L, m, out, ws}, so, &s)) return kNotHere;
+    at::Tensor own;  // the call's scratch, from the current stream's memory
+    if (!ws) {
+      size_t need = 0;
+      if (tree_attn_workspace_bytes(int32_t(B), max_q, int32_t(Hq), int32_t(Hkv), int32_t(D), int32_t(bt->size(1)),
+                                    &need) != ILPC_OK ||
+          (need && so != Py_None))
+        return kNotHere;
+      if (need) own = at::empty({int64_t(need)}, q->options().dtype(at::kByte));
+    }
+    const at::Tensor* scratch = ws ? ws : own.defined() ? &own : nullptr;
+    return call(paged_tree_attn, bf16(q), qs, int32_t(q->size(0)), bf16(kp), bf16(vp), int32_t(kp->size(0)), i32(bt),
+                int32_t(bt->size(1)), i32(cu), i32(L), int32_t(B), max_q, int32_t(Hq), int32_t(Hkv), int32_t(D),
+                int32_t(kp->size(2)), scale, u64(m), int32_t(m->size(1)), bf16(out),
+                scratch ? scratch->data_ptr() : nullptr, scratch ? size_t(scratch->numel()) : size_t(0), s);
+  });
+}
+
+// tree_accept(parents, tokens, targets, cu_q, start_pos, path, n_accepted, next_tokens, kept_lens, kept_blocks,
+//             root_targets, stream)
+PyObject* py_tree_accept(PyObject*, PyObject* const* argv, Py_ssize_t n) {
+  return guarded([&]() -> int {
+    Args a{argv, n};
+    auto ints = [&]() { return a.tensor(at::kInt, 1); };
+    const at::Tensor *par = ints(), *tok = ints(), *pick = ints(), *cu = ints(), *start = ints(), *path = ints(),
+                     *count = ints(), *next = ints(), *lens = ints(), *blocks = ints(),
+                     *root = a.tensor_or_none(at::kInt, 1);
+    PyObject* so = a.next();
+    if (!a.ok) return kNotHere;
+    const int64_t N = par->size(0), B = start->size(0);
+    if (tok->size(0) != N || pick->size(0) != N || path->size(0) != N || cu->size(0) != B + 1 || count->size(0) != B ||
+        next->size(0) != B || lens->size(0) != B || blocks->size(0) != B || (root && root->size(0) != B))
+      return kNotHere;
+    if (!apart({path, count, next, lens, blocks}, {par, tok, pick, cu, start, root})) return kNotHere;
+    void* s;
+    if (!placed({par, tok, pick, cu, start, path, count, next, lens, blocks, root}, so, &s)) return kNotHere;
+    return call(tree_accept, i32(par), i32(tok), i32(pick), root ? i32(root) : nullptr, i32(cu), i32(start),
+                int32_t(B), int32_t(N), i32(path), i32(count), i32(next), i32(lens), i32(blocks), s);
+  });
+}
+
+// kv_compact(k_pool, v_pool, block_tables, cu_q, start_pos, path, n_accepted, stream)
+PyObject* py_kv_compact(PyObject*, PyObject* const* argv, Py_ssize_t n) {
+  return guarded([&]() -> int {
+    Args a{argv, n};
+    const at::Tensor *kp = a.tensor(at::kBFloat16, 4), *vp = a.tensor(at::kBFloat16, 4), *bt = a.tensor(at::kInt, 2),
+                     *cu = a.tensor(at::kInt, 1), *start = a.tensor(at::kInt, 1), *path = a.tensor(at::kInt, 1),
+                     *count = a.tensor(at::kInt, 1);
+    PyObject* so = a.next();
+    if (!a.ok) return kNotHere;
+    const int64_t B = start->size(0);
+    if (!pools_fit(*kp, *vp) || bt->size(0) != B || cu->size(0) != B + 1 || count->size(0) != B) return kNotHere;
+    void* s;
+    if (!placed({kp, vp, bt, cu, start, path, count}, so, &s)) return kNotHere;
+    return call(kv_compact, bf16(kp), bf16(vp), int32_t(kp->size(0)), i32(bt), int32_t(bt->size(1)), i32(cu),
+                i32(start), int32_t(B), int32_t(path->size(0)), i32(path), i32(count), int32_t(kp->size(1)),
+                int32_t(kp->size(3)), int32_t(kp->size(2)), s);
+  });
+}
+
+// Whether these are the hold counts of blocks first .. num_blocks - 1.
+bool holds_fit(const at::Tensor& holds, int64_t num_blocks, int64_t first) {
+  const int64_t held = num_blocks - first;
+  return first >= 0 && held >= 0 && holds.size(0) == held + (held + 31) / 32;
+}
+
+// fork_tables(block_tables, seq_lens, sources, holds, first_id, free_ids, taken, copy_src, copy_dst, taken_out, status,
+//             num_blocks, stream)
+PyObject* py_fork_tables(PyObject*, PyObject* const* argv, Py_ssize_t n) {
+  return guarded([&]() -> int {
+    Args a{argv, n};
+    auto ints = [&](int64_t dim) { return a.tensor(at::kInt, dim); };
+    const at::Tensor *bt = ints(2), *seq = ints(1), *src = ints(1), *holds = ints(1);
+    const int32_t first = a.integer();
+    const at::Tensor *free = ints(1), *taken = ints(1), *from = ints(1), *to = ints(1), *out = ints(1),
+                     *status = ints(1);
+    const int32_t nb = a.integer();
+    PyObject* so = a.next();
+    if (!a.ok) return kNotHere;
+    const int64_t B = src->size(0);
+    if (bt->size(0) != B || seq->size(0) != B || from->size(0) != B || to->size(0) != B || taken->size(0) != 1 ||
+        out->size(0) != 1 || status->size(0) != 1 || !holds_fit(*holds, nb, first))
+      return kNotHere;
+    if (!apart({bt, seq, holds, from, to, status, out},
+               {src, free, out->data_ptr() == taken->data_ptr() ? nullptr : taken}))
+      return kNotHere;
+    void* s;
+    if (!placed({bt, seq, src, holds, free, taken, from, to, out, status}, so, &s)) return kNotHere;
+    return call(fork_tables, i32(bt), int32_t(bt->size(1)), int32_t(B), i32(seq), i32(src), i32(holds), first,
+                i32(free), int32_t(free->size(0)), i32(taken), nb, i32(from), i32(to), i32(out), i32(status), s);
+  });
+}
+
+// release_shared(block_tables, seq_lens, holds, first_id, free_ids, taken, taken_out, status, num_blocks, stream)
+PyObject* py_release_shared(PyObject*, PyObject* const* argv, Py_ssize_t n) {
+  return guarded([&]() -> int {
+    Args a{argv, n};
+    auto ints = [&](int64_t dim) { return a.tensor(at::kInt, dim); };
+    const at::Tensor *bt = ints(2), *seq = ints(1), *holds = ints(1);
+    const int32_t first = a.integer();
+    const at::Tensor *free = ints(1), *taken = ints(1), *out = ints(1), *status = ints(1);
+    const int32_t nb = a.integer();
+    PyObject* so = a.next();
+    if (!a.ok) return kNotHere;
+    const int64_t B = seq->size(0);
+    if (bt->size(0) != B || taken->size(0) != 1 || out->size(0) != 1 || status->size(0) != 1 ||
+        !holds_fit(*holds, nb, first))
+      return kNotHere;
+    if (!apart({holds, free, status, out}, {bt, seq, out->data_ptr() == taken->data_ptr() ? nullptr : taken}))
+      return kNotHere;
+    void* s;
+    if (!placed({bt, seq, holds, free, taken, out, status}, so, &s)) return kNotHere;
+    return call(release_shared, i32(bt), int32_t(bt->size(1)), int32_t(B), i32(seq), i32(holds), first, i32(free),
+                int32_t(free->size(0)), i32(taken), nb, i32(out), i32(status), s);
+  });
+}
+
+// copy_blocks(k_pool, v_pool, src, dst, stream)
+PyObject* py_copy_blocks(PyObject*, PyObject* const* argv, Py_ssize_t n) {
+  return guarded([&]() -> int {
+    Args a{argv, n};
+    const at::Tensor *kp = a.tensor(at::kBFloat16, 4), *vp = a.tensor(at::kBFloat16, 4), *src = a.tensor(at::kInt, 1),
+                     *dst = a.tensor(at::kInt, 1);
+    PyObject* so = a.next();
+    if (!a.ok || !pools_fit(*kp, *vp) || dst->size(0) != src->size(0)) return kNotHere;
+    void* s;
+    if (!placed({kp, vp, src, dst}, so, &s)) return kNotHere;
+    return call(copy_blocks, bf16(kp), bf16(vp), int32_t(kp->size(0)), i32(src), i32(dst), int32_t(src->size(0)),
+                int32_t(kp->size(1)), int32_t(kp->size(3)), int32_t(kp->size(2)), s);
+  });
+}
+
 #define FAST(name, fn) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(fn)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST("bind", py_bind),
                          FAST("kv_append", py_kv_append), FAST("rope_kv_append", py_rope_kv_append),
@@ -447,6 +627,10 @@ PyMethodDef methods[] = {FAST("bind", py_bind),
                          FAST("paged_prefill_attn_cascade", py_prefill_attn_cascade),
                          FAST("extend_tables", py_extend_tables), FAST("release_tables", py_release_tables),
                          FAST("kv_append_slots", py_kv_append_slots), FAST("paged_diff_attn", py_paged_diff_attn),
+                         FAST("tree_masks", py_tree_masks), FAST("paged_tree_attn", py_paged_tree_attn),
+                         FAST("tree_accept", py_tree_accept), FAST("kv_compact", py_kv_compact),
+                         FAST("fork_tables", py_fork_tables), FAST("release_shared", py_release_shared),
+                         FAST("copy_blocks", py_copy_blocks),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -24,8 +24,8 @@ LIB_PATH = os.path.join(_HERE, "libilpc.so")
 OK, EINVAL, ENOSPC, ETABLE, EUNSUP, EHIP = 0, -1, -2, -3, -4, -5
 NO_LOOKUP, NO_REGISTER = 1, 2
 DIFF_HALVES, DIFF_ROPE = 0, 1  # dimensions of the two maps of a differential head (see the C header)
-# bits of the status that extend_tables and release_tables write
-NO_BLOCKS, TOO_LONG, TOO_MANY_ROWS, BAD_VALUE = 1, 2, 4, 8
+# bits of the status that the calls on tables and free lists write
+NO_BLOCKS, TOO_LONG, TOO_MANY_ROWS, BAD_VALUE, NOT_HELD = 1, 2, 4, 8, 16
 BLOCK = 16
 _NAMES = {EINVAL: "EINVAL", ENOSPC: "ENOSPC", ETABLE: "ETABLE", EUNSUP: "EUNSUP", EHIP: "EHIP"}
 
@@ -67,6 +67,17 @@ _SIGS = [
                                               ctypes.POINTER(ctypes.c_size_t)]),
     ("ilpc_paged_diff_attn", _i32, [_vp, _i64, _i32, _vp, _vp, _i32, _vp, _i32, _vp, _vp, _i32, _i32, _i32, _i32,
                                     _i32, _i32, _f32, _i32, _vp, _vp, _f32, _f32, _vp, _vp, ctypes.c_size_t, _vp]),
+    ("ilpc_tree_masks", _i32, [_vp, _vp, _vp, _i32, _i32, _i32, _vp, _vp, _vp]),
+    ("ilpc_tree_attn_workspace_bytes", _i32, [_i32, _i32, _i32, _i32, _i32, _i32,
+                                              ctypes.POINTER(ctypes.c_size_t)]),
+    ("ilpc_paged_tree_attn", _i32, [_vp, _i64, _i32, _vp, _vp, _i32, _vp, _i32, _vp, _vp, _i32, _i32, _i32, _i32,
+                                    _i32, _i32, _f32, _vp, _i32, _vp, _vp, ctypes.c_size_t, _vp]),
+    ("ilpc_tree_accept", _i32, [_vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp]),
+    ("ilpc_kv_compact", _i32, [_vp, _vp, _i32, _vp, _i32, _vp, _vp, _i32, _i32, _vp, _vp, _i32, _i32, _i32, _vp]),
+    ("ilpc_holds_words", _i32, [_i32, ctypes.POINTER(_i32)]),
+    ("ilpc_fork_tables", _i32, [_vp, _i32, _i32, _vp, _vp, _vp, _i32, _vp, _i32, _vp, _i32, _vp, _vp, _vp, _vp, _vp]),
+    ("ilpc_release_shared", _i32, [_vp, _i32, _i32, _vp, _vp, _i32, _vp, _i32, _vp, _i32, _vp, _vp, _vp]),
+    ("ilpc_copy_blocks", _i32, [_vp, _vp, _i32, _vp, _vp, _i32, _i32, _i32, _i32, _vp]),
     ("ilpc_chunk_schedule", _i32, [_vp, _i32, _i32, _i32, _vp, _vp, _vp, _vp, ctypes.POINTER(_i32),
                                    ctypes.POINTER(_i32)]),
     ("ilpc_shared_prefix_len", _i32, [_vp, _vp, _i32, _i32, ctypes.POINTER(_i32)]),
@@ -138,7 +149,9 @@ def _native():
         mod.bind(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in (
             "ilpc_kv_append", "ilpc_rope_kv_append", "ilpc_attn_workspace_bytes", "ilpc_paged_prefill_attn",
             "ilpc_paged_prefill_attn_cascade", "ilpc_extend_tables", "ilpc_release_tables", "ilpc_kv_append_slots",
-            "ilpc_diff_attn_workspace_bytes", "ilpc_paged_diff_attn")))
+            "ilpc_diff_attn_workspace_bytes", "ilpc_paged_diff_attn", "ilpc_tree_masks",
+            "ilpc_tree_attn_workspace_bytes", "ilpc_paged_tree_attn", "ilpc_tree_accept", "ilpc_kv_compact",
+            "ilpc_fork_tables", "ilpc_release_shared", "ilpc_copy_blocks")))
         _binding = mod
     return _binding
 
@@ -678,9 +691,12 @@ def _ints(fn, **tensors):
 
 def _apart(fn, outputs, inputs):
     """Refuses outputs that share memory with an input or with each other."""
-    spans = [(t.data_ptr(), t.data_ptr() + 4 * t.numel(), name) for name, t in outputs + inputs if t.numel()]
-    for i, (a0, a1, an) in enumerate(spans[:len(outputs)]):
-        for b0, b1, bn in spans[i + 1:]:
+    def spans(named):
+        return [(t.data_ptr(), t.data_ptr() + t.element_size() * t.numel(), name) for name, t in named if t.numel()]
+
+    outs, ins = spans(outputs), spans(inputs)
+    for i, (a0, a1, an) in enumerate(outs):
+        for b0, b1, bn in outs[i + 1:] + ins:
             if a0 < b1 and b0 < a1:
                 raise ILPCError(EINVAL, f"{fn}: {an} and {bn} overlap")
 
@@ -828,3 +844,238 @@ def paged_diff_attn(q, k_pool, v_pool, block_tables, cu_q, seq_lens, max_q_len: 
                                            int(max_q_len), Hq, Hkv, D, bs, float(scale), int(layout), lp, wp,
                                            float(norm_eps), float(out_scale), op, ws, nbytes,
                                            ctypes.c_void_p(s.cuda_stream)))
+
+
+# -- trees of drafted tokens, forked requests -----------------------------------
+
+def _taken(outs, ins, taken_out, taken):
+    """Adds a free list's counts, which may be one tensor, to the spans that have to be apart."""
+    outs.append(("taken_out", taken_out))
+    if taken_out.data_ptr() != taken.data_ptr():
+        ins.append(("taken", taken))
+
+
+def tree_masks(parents, cu_q, masks, positions=None, start_pos=None, stream=None):
+    """Ancestor bits of the trees of drafted tokens (see the C header).
+
+    parents: int32 [rows], a node's parent within its request (-1: the context);
+    cu_q: int32 [B+1].  Out: masks int64 [rows, words] (64 nodes a word), positions
+    int32 [rows] = start_pos (int32 [B], or 0) + depth.
+    """
+    import torch
+
+    rc = (_binding or _native()).tree_masks(parents, cu_q, masks, positions, start_pos, stream)
+    if rc is not None:
+        return _check(rc)
+
+    fn = "tree_masks"
+    n = parents.shape[0] if getattr(parents, "ndim", 0) == 1 else -1
+    pp, cu = _ints(fn, parents=(parents, (n,)), cu_q=(cu_q, (-1,)))
+    B = cu_q.shape[0] - 1
+    mp = _dev(masks, torch.int64, "masks", 2)
+    if masks.shape[0] != n:
+        raise ILPCError(EINVAL, f"{fn}: masks must be [{n}, words], got {list(masks.shape)}")
+    ps = _ints(fn, positions=(positions, (n,)))[0] if positions is not None else None
+    sp = _ints(fn, start_pos=(start_pos, (B,)))[0] if start_pos is not None else None
+    outs = [("masks", masks)] + ([("positions", positions)] if positions is not None else [])
+    _apart(fn, outs, [("parents", parents), ("cu_q", cu_q)] + ([("start_pos", start_pos)] if sp else []))
+    ctx, s = _at((parents, cu_q, masks, positions, start_pos), stream)
+    with ctx:
+        _check(load().ilpc_tree_masks(pp, cu, sp, B, n, masks.shape[1], mp, ps, ctypes.c_void_p(s.cuda_stream)))
+
+
+def tree_attn_workspace_bytes(B, max_q_len, Hq, Hkv, D, max_blocks) -> int:
+    n = ctypes.c_size_t()
+    _check(load().ilpc_tree_attn_workspace_bytes(B, max_q_len, Hq, Hkv, D, max_blocks, ctypes.byref(n)))
+    return int(n.value)
+
+
+def paged_tree_attn(q, k_pool, v_pool, block_tables, cu_q, seq_lens, max_q_len: int, scale: float, masks, out,
+                    workspace=None, stream=None):
+    """Attention of packed queries [total, Hq, D], each request's newest tokens, over all
+    keys before them and those of their own that a row's mask names; see the C header.
+
+    masks: int64 [total, words], bit j of a row: it sees its request's j-th newest token
+    (tree_masks).  q may be a view of a wider row.  `workspace` (uint8,
+    tree_attn_workspace_bytes() bytes) is allocated for the call when omitted, on its
+    stream, so that calls and captured graphs do not share one.
+    """
+    import torch
+
+    rc = (_binding or _native()).paged_tree_attn(q, k_pool, v_pool, block_tables, cu_q, seq_lens, max_q_len, scale,
+                                                 masks, out, workspace, stream)
+    if rc is not None:
+        return _check(rc)
+
+    fn = "paged_tree_attn"
+    kp, vp, NB, Hkv, bs, D = _pools(k_pool, v_pool, fn)
+    if not isinstance(q, torch.Tensor) or q.dim() != 3 or out.shape != q.shape:
+        raise ILPCError(EINVAL, f"{fn}: q and out must both be [total, Hq, {D}]")
+    total, Hq, _ = q.shape
+    qp, q_stride = _rows(q, "q", (Hq, D))
+    B = cu_q.shape[0] - 1 if getattr(cu_q, "ndim", 0) == 1 else -1
+    bt, cu, L = _ints(fn, block_tables=(block_tables, (B, -1)), cu_q=(cu_q, (B + 1,)), seq_lens=(seq_lens, (B,)))
+    mp = _dev(masks, torch.int64, "masks", 2)
+    if masks.shape[0] != total:
+        raise ILPCError(EINVAL, f"{fn}: masks must be [{total}, words], got {list(masks.shape)}")
+    op = _dev(out, torch.bfloat16, "out", 3)
+    ctx, s = _at((k_pool, v_pool, q, out, block_tables, cu_q, seq_lens, masks, workspace), stream)
+    with ctx:
+        if workspace is None:
+            need = tree_attn_workspace_bytes(B, int(max_q_len), Hq, Hkv, D, block_tables.shape[1])
+            if need:
+                with torch.cuda.stream(s):
+                    workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        ws, nbytes = (None, 0) if workspace is None else (_dev(workspace, torch.uint8, "workspace", 1),
+                                                         workspace.numel())
+        _check(load().ilpc_paged_tree_attn(qp, q_stride, total, kp, vp, NB, bt, block_tables.shape[1], cu, L, B,
+                                           int(max_q_len), Hq, Hkv, D, bs, float(scale), mp, masks.shape[1], op, ws,
+                                           nbytes, ctypes.c_void_p(s.cuda_stream)))
+
+
+def tree_accept(parents, tokens, targets, cu_q, start_pos, path, n_accepted, next_tokens, kept_lens, kept_blocks,
+                root_targets=None, stream=None):
+    """The path of drafted nodes that the target's picks confirm (see the C header).
+
+    int32 device tensors: parents, tokens, targets (the pick behind each node) [rows],
+    cu_q [B+1], start_pos [B], root_targets [B] (the pick behind the context) or
+    None (node 0 is the root, accepted as it is).  Out: path [rows], n_accepted,
+    next_tokens, kept_lens, kept_blocks [B].
+    """
+    rc = (_binding or _native()).tree_accept(parents, tokens, targets, cu_q, start_pos, path, n_accepted, next_tokens,
+                                             kept_lens, kept_blocks, root_targets, stream)
+    if rc is not None:
+        return _check(rc)
+
+    fn = "tree_accept"
+    n = parents.shape[0] if getattr(parents, "ndim", 0) == 1 else -1
+    B = start_pos.shape[0] if getattr(start_pos, "ndim", 0) == 1 else -1
+    ins = dict(parents=(parents, (n,)), tokens=(tokens, (n,)), targets=(targets, (n,)), cu_q=(cu_q, (B + 1,)),
+               start_pos=(start_pos, (B,)))
+    outs = dict(path=(path, (n,)), n_accepted=(n_accepted, (B,)), next_tokens=(next_tokens, (B,)),
+                kept_lens=(kept_lens, (B,)), kept_blocks=(kept_blocks, (B,)))
+    if root_targets is not None:
+        ins["root_targets"] = (root_targets, (B,))
+    p, o = _ints(fn, **ins), _ints(fn, **outs)
+    _apart(fn, [(k, t) for k, (t, _) in outs.items()], [(k, t) for k, (t, _) in ins.items()])
+    ctx, s = _at((parents, tokens, targets, cu_q, start_pos, path, n_accepted, next_tokens, kept_lens, kept_blocks,
+                  root_targets), stream)
+    with ctx:
+        _check(load().ilpc_tree_accept(p[0], p[1], p[2], p[5] if root_targets is not None else None, p[3], p[4], B, n,
+                                       *o, ctypes.c_void_p(s.cuda_stream)))
+
+
+def kv_compact(k_pool, v_pool, block_tables, cu_q, start_pos, path, n_accepted, stream=None):
+    """K/V rows of accepted nodes to the front of the draft, in place: of each request, position
+    start_pos + path[cu_q + i] to start_pos + i for i < n_accepted (see the C header).
+
+    int32 device tensors: block_tables [B, max_blocks], cu_q [B+1], start_pos and
+    n_accepted [B], path [rows] (tree_accept's).
+    """
+    rc = (_binding or _native()).kv_compact(k_pool, v_pool, block_tables, cu_q, start_pos, path, n_accepted, stream)
+    if rc is not None:
+        return _check(rc)
+
+    fn = "kv_compact"
+    kp, vp, NB, Hkv, bs, D = _pools(k_pool, v_pool, fn)
+    B = start_pos.shape[0] if getattr(start_pos, "ndim", 0) == 1 else -1
+    p = _ints(fn, block_tables=(block_tables, (B, -1)), cu_q=(cu_q, (B + 1,)), start_pos=(start_pos, (B,)),
+              path=(path, (-1,)), n_accepted=(n_accepted, (B,)))
+    ctx, s = _at((k_pool, v_pool, block_tables, cu_q, start_pos, path, n_accepted), stream)
+    with ctx:
+        _check(load().ilpc_kv_compact(kp, vp, NB, p[0], block_tables.shape[1], p[1], p[2], B, path.shape[0], p[3],
+                                      p[4], Hkv, D, bs, ctypes.c_void_p(s.cuda_stream)))
+
+
+def holds_words(n_blocks: int) -> int:
+    """int32 words of the hold counts of n_blocks blocks (fork_tables, release_shared)."""
+    n = _i32()
+    _check(load().ilpc_holds_words(n_blocks, ctypes.byref(n)))
+    return int(n.value)
+
+
+def _holds(fn, holds, num_blocks, first_id):
+    """Pointer of the hold counts of blocks first_id .. num_blocks - 1."""
+    want = holds_words(num_blocks - first_id) if 0 <= first_id <= num_blocks else -1
+    return _ints(fn, holds=(holds, (want,)))[0]
+
+
+def fork_tables(block_tables, seq_lens, sources, holds, first_id: int, free_ids, taken, copy_src, copy_dst, taken_out,
+                status, num_blocks: int, stream=None):
+    """Rows of a batch become forks of others: r of sources[r] where that is another row
+    (see the C header).
+
+    All int32 device tensors: block_tables [B, max_blocks] and seq_lens [B] (in/out),
+    sources [B], holds [holds_words(num_blocks - first_id)] (in/out), free_ids [n],
+    taken [1]; out: copy_src and copy_dst [B] (copy_blocks'), taken_out [1] (may be
+    taken), status [1].
+    """
+    rc = (_binding or _native()).fork_tables(block_tables, seq_lens, sources, holds, first_id, free_ids, taken,
+                                             copy_src, copy_dst, taken_out, status, num_blocks, stream)
+    if rc is not None:
+        return _check(rc)
+
+    fn = "fork_tables"
+    B = sources.shape[0] if getattr(sources, "ndim", 0) == 1 else -1
+    p = _ints(fn, block_tables=(block_tables, (B, -1)), seq_lens=(seq_lens, (B,)), sources=(sources, (B,)),
+              free_ids=(free_ids, (-1,)), taken=(taken, (1,)), copy_src=(copy_src, (B,)), copy_dst=(copy_dst, (B,)),
+              taken_out=(taken_out, (1,)), status=(status, (1,)))
+    hp = _holds(fn, holds, int(num_blocks), int(first_id))
+    outs = [("block_tables", block_tables), ("seq_lens", seq_lens), ("holds", holds), ("copy_src", copy_src),
+            ("copy_dst", copy_dst), ("status", status)]
+    ins = [("sources", sources), ("free_ids", free_ids)]
+    _taken(outs, ins, taken_out, taken)
+    _apart(fn, outs, ins)
+    ctx, s = _at((sources, block_tables, seq_lens, holds, free_ids, taken, copy_src, copy_dst, taken_out, status),
+                 stream)
+    with ctx:
+        _check(load().ilpc_fork_tables(p[0], block_tables.shape[1], B, p[1], p[2], hp, int(first_id), p[3],
+                                       free_ids.shape[0], p[4], int(num_blocks), p[5], p[6], p[7], p[8],
+                                       ctypes.c_void_p(s.cuda_stream)))
+
+
+def release_shared(block_tables, seq_lens, holds, first_id: int, free_ids, taken, taken_out, status, num_blocks: int,
+                   stream=None):
+    """Give blocks of ended rows back where rows share them (see the C header): each of a row's
+    first ceil(seq_lens[r] / 16) entries drops a hold, and blocks that none holds any more
+    go back to the free list in ascending order.
+
+    All int32 device tensors: block_tables [B, max_blocks], seq_lens [B], holds
+    [holds_words(num_blocks - first_id)] and free_ids [n] (in/out), taken [1]; out: taken_out [1]
+    (may be taken), status [1] (0, or bits, NOT_HELD among them, with nothing changed).
+    """
+    rc = (_binding or _native()).release_shared(block_tables, seq_lens, holds, first_id, free_ids, taken, taken_out,
+                                                status, num_blocks, stream)
+    if rc is not None:
+        return _check(rc)
+
+    fn = "release_shared"
+    B = seq_lens.shape[0] if getattr(seq_lens, "ndim", 0) == 1 else -1
+    p = _ints(fn, block_tables=(block_tables, (B, -1)), seq_lens=(seq_lens, (B,)), free_ids=(free_ids, (-1,)),
+              taken=(taken, (1,)), taken_out=(taken_out, (1,)), status=(status, (1,)))
+    hp = _holds(fn, holds, int(num_blocks), int(first_id))
+    outs = [("holds", holds), ("free_ids", free_ids), ("status", status)]
+    ins = [("block_tables", block_tables), ("seq_lens", seq_lens)]
+    _taken(outs, ins, taken_out, taken)
+    _apart(fn, outs, ins)
+    ctx, s = _at((seq_lens, block_tables, holds, free_ids, taken, taken_out, status), stream)
+    with ctx:
+        _check(load().ilpc_release_shared(p[0], block_tables.shape[1], B, p[1], hp, int(first_id), p[2],
+                                          free_ids.shape[0], p[3], int(num_blocks), p[4], p[5],
+                                          ctypes.c_void_p(s.cuda_stream)))
+
+
+def copy_blocks(k_pool, v_pool, src, dst, stream=None):
+    """Copy whole blocks within the pools: src[i] to dst[i] (int32 device tensors [n]; pairs with an
+    id outside the pools, -1 among them, are left out).  A block copied to is in no other pair."""
+    rc = (_binding or _native()).copy_blocks(k_pool, v_pool, src, dst, stream)
+    if rc is not None:
+        return _check(rc)
+
+    fn = "copy_blocks"
+    kp, vp, NB, Hkv, bs, D = _pools(k_pool, v_pool, fn)
+    n = src.shape[0] if getattr(src, "ndim", 0) == 1 else -1
+    sp, dp = _ints(fn, src=(src, (n,)), dst=(dst, (n,)))
+    ctx, s = _at((k_pool, v_pool, src, dst), stream)
+    with ctx:
+        _check(load().ilpc_copy_blocks(kp, vp, NB, sp, dp, n, Hkv, D, bs, ctypes.c_void_p(s.cuda_stream)))

@@ -50,6 +50,8 @@ class PagedPrefixCache:
         # the free list on the device: ids, and how many at its front are taken
         self.free_ids = torch.arange(num_blocks, num_blocks + spare_blocks, dtype=torch.int32, device=self.device)
         self.free_taken = torch.zeros(1, dtype=torch.int32, device=self.device)
+        # holders of each spare block beyond the first (DeviceTables with shared rows)
+        self.holds = torch.zeros(ilpc.holds_words(spare_blocks), dtype=torch.int32, device=self.device)
         n = max_batch * max_blocks + 3 * max_batch + 1
         self._host = [torch.empty(n, dtype=torch.int32, pin_memory=True) for _ in range(2)]
         self._host_np = [h.numpy() for h in self._host]
@@ -238,6 +240,22 @@ class PagedPrefixCache:
                              batch.max_q_len, scale, lam, out, norm_weight, norm_eps, out_scale, layout, workspace,
                              stream)
 
+    def attend_tree(self, batch: DeviceBatch, q, out, scale: float, masks, workspace=None, stream=None):
+        """Attention of each request's newest tokens as a tree: all keys before them, and of
+        themselves those that a row's mask names (DeviceTables.tree, ilpc.paged_tree_attn)."""
+        ilpc.paged_tree_attn(q, self.k_pool, self.v_pool, batch.block_tables, batch.cu_q, batch.seq_lens,
+                             batch.max_q_len, scale, masks, out, workspace, stream)
+
+    def compact(self, batch: DeviceBatch, path, n_accepted, stream=None):
+        """K/V rows of a draft's accepted nodes to its front, before the next extend on this cache
+        (DeviceTables.accept's path; in every layer's pools)."""
+        ilpc.kv_compact(self.k_pool, self.v_pool, batch.block_tables, batch.cu_q, batch.start_pos, path, n_accepted,
+                        stream)
+
+    def copy_blocks(self, src, dst, stream=None):
+        """Whole blocks copied within the pools (DeviceTables.fork's pairs; in every layer's pools)."""
+        ilpc.copy_blocks(self.k_pool, self.v_pool, src, dst, stream)
+
     def cascade_workspace(self, batch: DeviceBatch, n_q_heads: int):
         """A workspace for attend_cascade on this batch shape (first 128 bytes zeroed)."""
         import torch
@@ -260,12 +278,19 @@ class DeviceTables:
     blocks of ended requests back.  Calls are ordered on one stream; batches
     that share ``pc`` share its free list and that order.
 
-    ``status`` (device, 1 value) holds what the last extend or release refused
-    (0: nothing): a refused extend changes nothing, and the append and attention
-    queued behind it do nothing.
+    ``status`` (device, 1 value) holds what the last extend, accept, fork or release
+    refused (0: nothing): a refused extend changes nothing, and the append and
+    attention queued behind it do nothing.
+
+    A step of speculative decoding (``max_nodes`` > 0) extends by drafted tokens, a tree
+    a request: ``tree`` makes the masks that ``pc.attend_tree`` reads, ``accept`` keeps
+    the path that the target's picks confirm and gives the blocks behind it back, and
+    ``pc.compact`` moves its K/V rows.  With ``shared`` rows can be forks of others
+    (``fork``, then ``pc.copy_blocks``), and blocks go back once no row holds them.  A
+    batch's forks end before the host gives its prompts back (``pc.release``).
     """
 
-    def __init__(self, pc: PagedPrefixCache, tables, seq_lens, max_rows: int):
+    def __init__(self, pc: PagedPrefixCache, tables, seq_lens, max_rows: int, max_nodes: int = 0, shared: bool = False):
         import torch
 
         tables = np.ascontiguousarray(tables, dtype=np.int32)
@@ -285,6 +310,15 @@ class DeviceTables:
         self.seq_lens, self.first_block = self._rows[0], self._rows[1]
         self.cu_q, self.cu_blocks = empty(self.B + 1), empty(self.B + 1)
         self.slot_map, self.status = empty(self.max_rows).fill_(-1), empty(1)
+        self.shared, self.max_nodes = bool(shared), int(max_nodes)
+        if self.max_nodes > 0:
+            words = -(-self.max_nodes // 64)
+            self.masks = torch.zeros(self.max_rows, words, dtype=torch.int64, device=pc.device)
+            self.positions, self.path = empty(self.max_rows), empty(self.max_rows).fill_(-1)
+            self.n_accepted, self.next_tokens = empty(self.B), empty(self.B)
+            self.kept_lens, self.kept_blocks = empty(self.B), empty(self.B)
+        if self.shared:
+            self.copy_src, self.copy_dst = empty(self.B).fill_(-1), empty(self.B).fill_(-1)
 
     def extend(self, new_lens, max_new: int) -> DeviceBatch:
         """Every request r gets new_lens[r] (device int32, at most max_new) tokens.
@@ -304,9 +338,48 @@ class DeviceTables:
         """K/V of the last extend's tokens [max_rows, Hkv, D] into the pools."""
         self.pc.append_slots(self.slot_map, k_new, v_new)
 
+    def _draft(self, call):
+        if self.max_nodes <= 0:
+            raise ilpc.ILPCError(ilpc.EINVAL, f"{call}: DeviceTables was made without max_nodes")
+
+    def tree(self, parents):
+        """Masks and positions of the last extend's tokens as trees: parents (device int32 [max_rows])
+        are indexes within a request, -1 for its roots.  The views hold until the next call."""
+        self._draft("tree")
+        ilpc.tree_masks(parents, self.cu_q, self.masks, self.positions, self.start_pos)
+        return self.masks, self.positions
+
+    def accept(self, parents, tokens, targets, root_targets=None):
+        """Of the last extend's drafted tokens the path that the target's picks confirm stays
+        (ilpc.tree_accept; all device int32 [max_rows], root_targets [B]): ``path``, ``n_accepted`` and
+        ``next_tokens`` say which and what follows, the lengths end behind it, and blocks that it does
+        not reach are free again.  ``pc.compact`` then moves the K/V rows."""
+        import torch
+
+        self._draft("accept")
+        ilpc.tree_accept(parents, tokens, targets, self.cu_q, self.start_pos, self.path, self.n_accepted,
+                         self.next_tokens, self.kept_lens, self.kept_blocks, root_targets)
+        ilpc.release_tables(self.block_tables, self.kept_blocks, self.seq_lens, self.pc.free_ids, self.pc.free_taken,
+                            self.cu_blocks, self.pc.free_taken, self.status)
+        # (refused, which no state of this class is, would leave the lengths with their blocks)
+        self.seq_lens.copy_(torch.where(self.status == 0, self.kept_lens, self.seq_lens))
+        return self.path, self.n_accepted, self.next_tokens
+
+    def fork(self, sources):
+        """Row r holds row sources[r]'s tokens from now on, where that is another row (device int32
+        [B]; rows forked from name themselves, as do those that stay; what a fork's row held has
+        been released).  Returns the block pairs that ``pc.copy_blocks`` copies, in every layer."""
+        if not self.shared:
+            raise ilpc.ILPCError(ilpc.EINVAL, "fork: DeviceTables was made without shared")
+        pc = self.pc
+        ilpc.fork_tables(self.block_tables, self.seq_lens, sources, pc.holds, pc.num_blocks, pc.free_ids,
+                         pc.free_taken, self.copy_src, self.copy_dst, pc.free_taken, self.status, pc.k_pool.shape[0])
+        return self.copy_src, self.copy_dst
+
     def release(self, ended):
         """Requests with ended[r] (device bool or integer) not 0 have finished: the blocks that they
-        took by extend are free again, and their rows hold nothing, ready for another request's.
+        took by extend (or fork, where no other row holds them) are free again, and their rows hold
+        nothing, ready for another request's.
 
         Where the device refuses it (``status``), nothing is given back and the rows stay as they
         were, so that it can be called again."""
@@ -317,8 +390,13 @@ class DeviceTables:
         if ended.shape != (self.B,) or ended.is_floating_point() or ended.is_complex():
             raise ilpc.ILPCError(ilpc.EINVAL, f"release: ended must be bool or integers [{self.B}]")
         ended = ended if ended.dtype == torch.bool else ended != 0
-        ilpc.release_tables(self.block_tables, self.first_block, self.seq_lens * ended, self.pc.free_ids,
-                            self.pc.free_taken, self.cu_blocks, self.pc.free_taken, self.status)
+        if self.shared:
+            pc = self.pc
+            ilpc.release_shared(self.block_tables, self.seq_lens * ended, pc.holds, pc.num_blocks, pc.free_ids,
+                                pc.free_taken, pc.free_taken, self.status, pc.k_pool.shape[0])
+        else:
+            ilpc.release_tables(self.block_tables, self.first_block, self.seq_lens * ended, self.pc.free_ids,
+                                self.pc.free_taken, self.cu_blocks, self.pc.free_taken, self.status)
         # a row stays unless it has ended and was not refused: ended <= status (0, or bits).  What an
         # emptied row takes from now on is all its own, so that its first_block is 0 as well.
         self._rows.mul_(ended <= self.status)

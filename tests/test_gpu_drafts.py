@@ -1,0 +1,677 @@
+"""GPU: ancestor masks, accepted paths, moved rows, forked rows, block copies and shared
+releases against plain lists; and whole decoding loops of them.  Integers have to be
+equal, stored rows the same bits."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import tree_ref
+from oracle.tables_ref import release_ref
+from paper_2507_08523_amd import ilpc, pipeline
+
+pytestmark = pytest.mark.gpu
+
+BLOCK = 16
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a ROCm GPU (run with -m 'not gpu' on the CPU)")
+    ilpc.load()
+    yield
+    torch.cuda.synchronize()
+
+
+def dev(a, dtype=np.int32):
+    return torch.from_numpy(np.array(a, dtype=dtype, order="C")).cuda()
+
+
+def ints(t):
+    return t.cpu().numpy().tolist()
+
+
+def random_tree(n, rng, branch=2, pad=0.0):
+    out = [-1] + [int(rng.integers(max(0, (i - 1) // branch - 2), (i - 1) // branch + 1)) for i in range(1, n)]
+    for i in range(1, n):
+        if rng.random() < pad:
+            out[i] = int(rng.choice([-2, -1, i, i + 3, -(1 << 31), (1 << 31) - 1]))
+    return out[:n]
+
+
+def signed(words):
+    return [w - (1 << 64) if w >> 63 else w for w in words]
+
+
+# -- masks ------------------------------------------------------------------------
+
+@pytest.mark.parametrize("sizes", [[1], [0], [64], [65], [5, 0, 64, 1, 63], [100, 128, 2], [200, 129, 256, 1], [1000, 30],
+                                   [1024, 1023]])
+@pytest.mark.parametrize("branch,pad", [(1, 0.0), (3, 0.0), (2, 0.2)])
+def test_masks(sizes, branch, pad):
+    rng = np.random.default_rng(sum(sizes) + branch)
+    par = [random_tree(n, rng, branch, pad) for n in sizes]
+    start = rng.integers(0, 5000, len(sizes))
+    for extra_words in (0, 1):
+        words = min(16, max(1, -(-max(sizes) // 64)) + extra_words)
+        n = sum(sizes)
+        masks, pos = dev(np.full((n + 3, words), 5), np.int64), dev([9] * (n + 3))
+        cu = dev(np.concatenate([[0], np.cumsum(sizes)]))
+        flat = dev(sum(par, []) + [0] * 3)
+        ilpc.tree_masks(flat, cu, masks, pos, dev(start))
+        only = dev(np.full((n + 3, words), 5), np.int64)
+        ilpc.tree_masks(flat, cu, only)
+        torch.cuda.synchronize()
+        want_m, want_p = [], []
+        for p, s in zip(par, start):
+            m, q = tree_ref.masks_ref(p, int(s), words)
+            want_m += [signed(x) for x in m]
+            want_p += q
+        assert ints(masks) == want_m + [[5] * words] * 3 and ints(pos) == want_p + [9] * 3
+        assert torch.equal(only, masks)
+
+
+def test_masks_of_a_chain_and_of_too_many_nodes():
+    chain = list(range(-1, 149))
+    for words in (1, 2, 3):
+        m, p = dev(np.zeros((150, words)), np.int64), dev([0] * 150)
+        ilpc.tree_masks(dev(chain), dev([0, 150]), m, p, dev([7]))
+        torch.cuda.synchronize()
+        wm, wp = tree_ref.masks_ref(chain, 7, words)
+        assert ints(m) == [signed(x) for x in wm] and ints(p) == wp
+
+
+def test_requests_with_rows_outside_the_buffers_are_taken_as_having_none():
+    m, p = dev([[3]] * 6, np.int64), dev([9] * 6)
+    ilpc.tree_masks(dev([-1, 0, 0, -1, 0, 1]), dev([0, 3, 7, 2, -1]), m, p)
+    torch.cuda.synchronize()
+    assert ints(m) == [[1], [3], [5], [3], [3], [3]] and ints(p) == [0, 1, 1, 9, 9, 9]
+
+
+# -- accepted paths ------------------------------------------------------------------
+
+def picks_for(par, tok, rng, hit=0.8, vocab=50):
+    out = [int(x) for x in rng.integers(0, vocab, len(par))]
+    for i in rng.permutation(len(par)):
+        if 0 <= par[i] < i and rng.random() < hit:
+            out[par[i]] = tok[i]
+    return out
+
+
+def run_accept(par, tok, pick, cu, start, root=None):
+    n, B = len(par), len(start)
+    outs = [dev([9] * n)] + [dev([9] * B) for _ in range(4)]
+    ilpc.tree_accept(dev(par), dev(tok), dev(pick), dev(cu), dev(start), *outs,
+                     root_targets=None if root is None else dev(root))
+    torch.cuda.synchronize()
+    return [ints(o) for o in outs]
+
+
+@pytest.mark.parametrize("sizes", [[1], [0, 3], [64], [65, 1], [20] * 40, [300, 7, 256, 257], [1000]])
+@pytest.mark.parametrize("branch,vocab,pad", [(1, 1000, 0.0), (3, 1000, 0.0), (2, 3, 0.0), (2, 20, 0.15)])
+@pytest.mark.parametrize("rooted", [False, True])
+def test_accept(sizes, branch, vocab, pad, rooted):
+    rng = np.random.default_rng(sum(sizes) + vocab)
+    par, tok, pick, path, rest = [], [], [], [], [[], [], [], []]
+    start, root = rng.integers(0, 999, len(sizes)).tolist(), rng.integers(0, vocab, len(sizes)).tolist()
+    for r, n in enumerate(sizes):
+        p = random_tree(n, rng, branch, pad)
+        t = rng.integers(0, vocab, n).tolist()
+        k = picks_for(p, t, rng, vocab=vocab)
+        if n and rng.random() < 0.7:
+            root[r] = t[0]
+        got, want = tree_ref.accept_ref(p, t, k, root[r] if rooted else None)
+        par, tok, pick = par + p, tok + t, pick + k
+        path += got + [-1] * (n - len(got))
+        kept = start[r] + len(got)
+        for o, x in zip(rest, (len(got), want, kept, -(-kept // 16))):
+            o.append(x)
+    cu = np.concatenate([[0], np.cumsum(sizes)])
+    got = run_accept(par + [0, 0], tok + [0, 0], pick + [0, 0], cu, start, root if rooted else None)
+    assert got == [path + [9, 9]] + rest
+
+
+def test_a_long_chain_is_accepted_whole():
+    n = 700
+    tok = list(range(n))
+    got = run_accept(list(range(-1, n - 1)), tok, tok[1:] + [5], [0, n], [16])
+    assert got == [list(range(n)), [n], [5], [16 + n], [-(-(16 + n) // 16)]]
+
+
+# -- moved rows -------------------------------------------------------------------
+
+def pools(nb, Hkv, D, seed=0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    rnd = lambda *s: torch.randn(*s, generator=g, device="cuda").to(torch.bfloat16)  # noqa: E731
+    return rnd(nb, Hkv, 16, D), rnd(nb, Hkv, D, 16)
+
+
+def same_bits(a, b):
+    return torch.equal(a.view(torch.int16), b.view(torch.int16))
+
+
+@pytest.mark.parametrize("Hkv,D", [(1, 64), (8, 128), (3, 64), (2, 128)])
+@pytest.mark.parametrize("sizes,counts", [([5], [5]), ([64], [7]), ([1, 0, 40, 20], [1, 0, 6, 0]), ([300, 33], [70, 33]),
+                                          ([20] * 30, [4] * 30), ([1000], [400])])
+def test_compact(Hkv, D, sizes, counts):
+    rng = np.random.default_rng(sum(sizes) + D)
+    start = rng.integers(0, 70, len(sizes))
+    lens = start + sizes
+    nb = int(sum(-(-lens // 16))) + 4
+    ids = rng.permutation(nb)
+    mb = int((-(-lens // 16)).max()) + 1
+    bt, at = np.full((len(sizes), mb), -1), 0
+    path = []
+    for r, (n, k) in enumerate(zip(sizes, counts)):
+        m = -(-int(lens[r]) // 16)
+        bt[r, :m] = ids[at:at + m]
+        at += m
+        path += sorted(rng.choice(n, k, replace=False).tolist()) + [-1] * (n - k) if n else []
+    kp, vp = pools(nb, Hkv, D)
+    kp[0, 0, 0, 0], vp[1, 0, 0, 0] = float("nan"), float("inf")
+    wk, wv = kp.clone(), vp.clone()
+    cu = np.concatenate([[0], np.cumsum(sizes)])
+    for r, k in enumerate(counts):
+        s = start[r] + np.array(path[cu[r]:cu[r] + k], int)
+        d = start[r] + np.arange(k)
+        wk[bt[r, d // 16], :, d % 16] = kp[bt[r, s // 16], :, s % 16]
+        wv[bt[r, d // 16], :, :, d % 16] = vp[bt[r, s // 16], :, :, s % 16]
+    ilpc.kv_compact(kp, vp, dev(bt), dev(cu), dev(start), dev(path + [3]), dev(counts))
+    torch.cuda.synchronize()
+    assert same_bits(kp, wk) and same_bits(vp, wv)
+
+
+def test_compact_leaves_out_what_is_not_there():
+    kp, vp = pools(4, 2, 64)
+    wk, wv = kp.clone(), vp.clone()
+    # rows outside the path's range, blocks outside the pools, positions past the table, counts past the nodes
+    bt, cu, start = dev([[0, 9, -1], [1, 2, -5], [3, 1 << 30, 3]]), dev([0, 20, 26, 29]), dev([14, 30, -4])
+    path = np.full(29, -1)
+    path[:3], path[20:26], path[26:29] = [1, 2, 99], [0, 1, 2, 3, 40, 5], [1, 2, 3]
+    wk[0, :, 14], wv[0, :, :, 14] = kp[0, :, 15], vp[0, :, :, 15]  # the one move that is whole
+    ilpc.kv_compact(kp, vp, bt, cu, start, dev(path), dev([3, 99, 3]))
+    torch.cuda.synchronize()
+    assert same_bits(kp, wk) and same_bits(vp, wv)
+
+
+# -- copies, forks, releases ----------------------------------------------------------
+
+@pytest.mark.parametrize("Hkv,D", [(1, 64), (8, 128), (3, 64), (32, 128)])
+@pytest.mark.parametrize("n", [1, 2, 50])
+def test_copy_blocks(Hkv, D, n):
+    nb = 2 * n + 3
+    kp, vp = pools(nb, Hkv, D)
+    rng = np.random.default_rng(n)
+    ids = rng.permutation(nb)
+    src, dst = ids[:n].copy(), ids[n:2 * n].copy()
+    src[n // 2:] = src[0]  # one block to several places
+    bad = n > 2
+    if bad:
+        src[1], dst[3], src[5], dst[6] = -1, -1, nb, 1 << 30
+    wk, wv = kp.clone(), vp.clone()
+    for s, d in zip(src, dst):
+        if 0 <= s < nb and 0 <= d < nb:
+            wk[d], wv[d] = kp[s], vp[s]
+    ilpc.copy_blocks(kp, vp, dev(src), dev(dst))
+    torch.cuda.synchronize()
+    assert same_bits(kp, wk) and same_bits(vp, wv)
+
+
+class Rows:
+    """A batch of rows, some of which hold requests, over `first` blocks of the cache and a free list."""
+
+    def __init__(self, B, live, hi, first, spare, seed, width=None):
+        rng = np.random.default_rng(seed)
+        self.B, self.first, self.taken = B, first, 0
+        self.lens = [int(rng.integers(0, hi + 1)) if r < live else 0 for r in range(B)]
+        mb = width or -(-hi // 16) + 1
+        own = sum(-(-n // 16) for n in self.lens)
+        self.nb = first + own + spare
+        self.free = list(range(first, self.nb))
+        rng.shuffle(self.free)
+        self.tables = [[-1] * mb for _ in range(B)]
+        for r in range(live):
+            for j in range(-(-self.lens[r] // 16)):
+                if first and j < 2:
+                    self.tables[r][j] = int(rng.integers(0, first))
+                else:
+                    self.tables[r][j] = self.free[self.taken]
+                    self.taken += 1
+        self.holds = [0] * (self.nb - first)
+        words = -(-len(self.holds) // 32)
+        self.d = dict(bt=dev(np.array(self.tables).reshape(B, mb)), lens=dev(self.lens), holds=dev(self.holds + [0] * words),
+                      free=dev(self.free), taken=dev([self.taken]), src=dev([9] * B), dst=dev([9] * B), status=dev([9]),
+                      out=dev([9]))
+
+    def state(self, want_copies=None):
+        torch.cuda.synchronize()
+        d = self.d
+        assert ints(d["bt"]) == self.tables and ints(d["lens"]) == self.lens
+        assert ints(d["holds"]) == self.holds + [0] * -(-len(self.holds) // 32)
+        assert ints(d["free"]) == self.free and ints(d["taken"]) == [self.taken]
+        if want_copies:
+            assert (ints(d["src"]), ints(d["dst"])) == want_copies
+
+    def fork(self, sources, in_place=True):
+        d = self.d
+        out = d["taken"] if in_place else d["out"]
+        ilpc.fork_tables(d["bt"], d["lens"], dev(sources), d["holds"], self.first, d["free"], d["taken"], d["src"],
+                         d["dst"], out, d["status"], self.nb)
+        *rest, self.taken_after, st = tree_ref.fork_ref(self.tables, self.lens, sources, self.holds, self.first,
+                                                        self.free, self.taken, self.nb)
+        self.tables, self.lens, self.holds, src, dst = rest
+        torch.cuda.synchronize()
+        assert ints(d["status"]) == [st] and ints(out) == [self.taken_after]
+        self.taken = self.taken_after
+        d["taken"] = out if in_place else out.clone()
+        self.state((src, dst))
+        return st
+
+    def release(self, lens, in_place=True):
+        d = self.d
+        out = d["taken"] if in_place else d["out"]
+        ilpc.release_shared(d["bt"], dev(lens), d["holds"], self.first, d["free"], d["taken"], out, d["status"], self.nb)
+        self.holds, self.free, self.taken, st = tree_ref.release_shared_ref(self.tables, lens, self.holds, self.first,
+                                                                            self.free, self.taken, self.nb)
+        torch.cuda.synchronize()
+        assert ints(d["status"]) == [st] and ints(out) == [self.taken]
+        d["taken"] = out if in_place else out.clone()
+        self.state()
+        return st
+
+
+@pytest.mark.parametrize("B,live,hi,first", [(2, 1, 40, 0), (4, 1, 16, 0), (16, 4, 350, 5), (64, 64, 100, 3), (300, 20, 90, 0),
+                                             (1100, 100, 60, 7), (512, 64, 2000, 9), (7, 2, 30000, 0), (3000, 5, 33, 1)])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_forks_and_releases(B, live, hi, first, in_place):
+    rng = np.random.default_rng(B + hi)
+    s = Rows(B, live, hi, first, B + 8, B)
+    sources = [r if r < live or rng.random() < 0.1 else int(rng.integers(0, live)) for r in range(B)]
+    assert s.fork(sources, in_place) == 0
+    ended = [r for r in range(B) if rng.random() < 0.5]
+    assert s.release([n if r in set(ended) else 0 for r, n in enumerate(s.lens)], in_place) == 0
+    left = [0 if r in set(ended) else n for r, n in enumerate(s.lens)]
+    assert s.release(left, in_place) == 0
+    assert s.taken == 0 and sorted(s.free) == list(range(first, s.nb))
+
+
+def test_forks_of_forks_and_of_lengths_at_block_ends():
+    s = Rows(9, 1, 0, 2, 60, 0, width=8)
+    for n, row in ((0, 0), (1, 0), (15, 0), (16, 0), (17, 0), (64, 0), (128, 0)):
+        s.lens[0] = n
+        s.tables[0] = [1] + [s.free[i] for i in range(s.taken, s.taken + 7)]
+        s.tables[0] = s.tables[0][:-(-n // 16)] + [-1] * (8 - -(-n // 16))
+        s.taken += max(-(-n // 16) - 1, 0)
+        s.d["bt"].copy_(dev(s.tables)), s.d["lens"].copy_(dev(s.lens)), s.d["taken"].copy_(dev([s.taken]))
+        assert s.fork([0, 0, 0, 3, 4, 5, 6, 7, 8]) == 0
+        assert s.fork([0, 1, 2, 1, 2, 2, 0, 7, 8]) == 0
+        assert s.release([x if r in (0, 2, 5) else 0 for r, x in enumerate(s.lens)]) == 0
+        assert s.release([0 if r in (0, 2, 5) else x for r, x in enumerate(s.lens)]) == 0
+        assert s.taken == 0
+        s.lens = [0] * 9
+        s.d["lens"].zero_()
+
+
+@pytest.mark.parametrize("kind", ["blocks", "source", "low source", "source moves", "long", "negative", "taken",
+                                  "taken low"])
+@pytest.mark.parametrize("B", [12, 700])
+def test_refused_forks_change_nothing(kind, B):
+    s = Rows(B, 4, 100, 2, 40, 1)
+    s.lens[:4] = [33, 20, 47, 5] if kind != "blocks" else [33] * 4
+    need = max(-(-n // 16) for n in s.lens)
+    s.tables = [row[:8] + [-1] * (8 - len(row)) for row in s.tables]
+    s.d["bt"], s.d["lens"] = dev(s.tables), dev(s.lens)
+    assert need <= 8
+    src = list(range(B))
+    src[5], src[B - 1] = 1, 2
+    bit = ilpc.BAD_VALUE
+    if kind == "blocks":
+        src, bit = [0] + [0] * (B - 1), ilpc.NO_BLOCKS
+        src[1:4] = [1, 2, 3]
+        s.free = s.free[:s.taken + 3]
+        s.d["free"] = dev(s.free)
+    elif kind == "source":
+        src[7] = B
+    elif kind == "low source":
+        src[7] = -1
+    elif kind == "source moves":
+        src[6] = 5
+    elif kind == "long":
+        s.lens[2], bit = 129, ilpc.TOO_LONG
+    elif kind == "negative":
+        s.lens[1] = -3
+    elif kind == "taken":
+        s.taken = len(s.free) + 1
+    else:
+        s.taken = -1
+    s.d["lens"], s.d["taken"] = dev(s.lens), dev([s.taken])
+    assert s.fork(src) & bit
+
+
+@pytest.mark.parametrize("kind", ["twice", "too many", "long", "negative", "taken"])
+@pytest.mark.parametrize("B", [12, 1500])
+def test_refused_releases_change_nothing(kind, B):
+    s = Rows(B, B // 2, 100, 2, B, 2)
+    assert s.fork([r if r < B // 2 else r % (B // 2) for r in range(B)]) == 0
+    lens, bit = list(s.lens), {"twice": ilpc.NOT_HELD, "too many": ilpc.NO_BLOCKS, "long": ilpc.TOO_LONG}.get(kind, 8)
+    if kind == "twice":
+        row = next(r for r in range(B // 2) if s.lens[r] > 48)
+        s.tables[row] = list(s.tables[row])
+        s.tables[row][-(-s.lens[row] // 16) - 1] = s.tables[row][2]
+        s.d["bt"].copy_(dev(s.tables))
+    elif kind == "too many":
+        s.taken = 1
+        s.d["taken"].fill_(1)
+    elif kind == "long":
+        lens[3] = 16 * len(s.tables[0]) + 1
+    elif kind == "negative":
+        lens[3] = -1
+    else:
+        s.taken = len(s.free) + 5
+        s.d["taken"].fill_(s.taken)
+    assert s.release(lens) & bit
+
+
+def test_ids_outside_the_counted_blocks_are_shared_uncounted():
+    s = Rows(3, 1, 0, 4, 20, 3, width=6)
+    s.lens[0], s.tables[0] = 80, [1, 3, 4, 23, 1 << 30, -1]
+    s.taken = 2
+    s.nb = 24
+    s.d["bt"].copy_(dev(s.tables)), s.d["lens"].copy_(dev(s.lens)), s.d["taken"].fill_(2)
+    assert s.fork([0, 0, 0]) == 0 and s.holds[0] == 2 and s.holds[19] == 2
+    assert s.release(s.lens) == 0 and s.taken == 0
+
+
+def test_the_binding_refuses_overlaps_and_shapes():
+    s = Rows(4, 2, 40, 2, 20, 4)
+    d, src = s.d, dev([0, 1, 0, 1])
+    fork = lambda **k: ilpc.fork_tables(**dict(dict(  # noqa: E731
+        block_tables=d["bt"], seq_lens=d["lens"], sources=src, holds=d["holds"], first_id=2, free_ids=d["free"],
+        taken=d["taken"], copy_src=d["src"], copy_dst=d["dst"], taken_out=d["out"], status=d["status"],
+        num_blocks=s.nb), **k))
+    for bad in (dict(copy_src=d["lens"]), dict(copy_dst=src), dict(status=d["taken"]), dict(taken_out=d["lens"][:1]),
+                dict(holds=d["holds"][:-1]), dict(first_id=3), dict(first_id=-1), dict(num_blocks=s.nb + 1),
+                dict(sources=src[:3]), dict(sources=src.long()), dict(first_id=s.nb + 1), dict(copy_src=d["free"][:4])):
+        with pytest.raises(ilpc.ILPCError):
+            fork(**bad)
+    with pytest.raises(ilpc.ILPCError):
+        ilpc.release_shared(d["bt"], d["lens"], d["holds"], 2, d["holds"][:3], d["taken"], d["out"], d["status"], s.nb)
+    n = dev([-1, 0, 0, 1])
+    cu, st = dev([0, 4]), dev([3])
+    o = [dev([0] * 4)] + [dev([0]) for _ in range(4)]
+    with pytest.raises(ilpc.ILPCError, match="overlap"):
+        ilpc.tree_accept(n, n, n, cu, st, n, *o[1:])
+    with pytest.raises(ilpc.ILPCError, match="overlap"):
+        ilpc.tree_accept(n, n, n, cu, st, o[0], o[1], o[1], *o[3:])
+    with pytest.raises(ilpc.ILPCError):
+        ilpc.tree_accept(n, n[:3], n, cu, st, *o)
+    with pytest.raises(ilpc.ILPCError):
+        ilpc.tree_masks(n, cu, dev([[0]] * 3, np.int64))
+    with pytest.raises(ilpc.ILPCError):
+        ilpc.tree_masks(n, cu, dev([[0]] * 4, np.int64), n)
+    with pytest.raises(ilpc.ILPCError):
+        ilpc.tree_masks(n, cu, dev([[0] * 17] * 4, np.int64))
+    s.state()
+
+
+def test_no_request_at_all():
+    e, one = dev([]), dev([0])
+    bt, m = torch.zeros(0, 4, dtype=torch.int32, device="cuda"), torch.zeros(0, 1, dtype=torch.int64, device="cuda")
+    kp, vp = pools(4, 2, 64)
+    out, st, holds = dev([9]), dev([9]), dev([0, 0, 0])
+    ilpc.tree_masks(e, one, m)
+    ilpc.tree_accept(e, e, e, one, e, *[e.clone() for _ in range(5)])
+    ilpc.kv_compact(kp, vp, bt, one, e, e, e)
+    ilpc.copy_blocks(kp, vp, e, e)
+    ilpc.fork_tables(bt, e, e.clone(), holds, 2, dev([2, 3]), dev([1]), e.clone(), e.clone(), out, st, 4)
+    torch.cuda.synchronize()
+    assert (ints(out), ints(st)) == ([1], [0])
+    ilpc.release_shared(bt, e, holds, 2, dev([2, 3]), dev([1]), out, st, 4)
+    torch.cuda.synchronize()
+    assert (ints(out), ints(st)) == ([1], [0])
+    # requests without nodes
+    z, path = dev([0, 0]), [dev([9, 9]) for _ in range(4)]
+    ilpc.tree_accept(e, e, e, dev([0, 0, 0]), dev([5, 16]), e.clone(), *path, root_targets=dev([7, 8]))
+    torch.cuda.synchronize()
+    assert [ints(p) for p in path] == [[0, 0], [7, 8], [5, 16], [1, 1]]
+    del z
+
+
+# -- together: decoding by trees, and sampling several answers -----------------------
+
+class Model:
+    """A fixed next token, and K/V that depend on (token, position) alone."""
+
+    def __init__(self, Hkv, D, vocab=40, seed=0):
+        g = torch.Generator().manual_seed(seed)
+        self.next = np.random.default_rng(seed).permutation(vocab)
+        rnd = lambda: torch.randn(vocab, Hkv, D, generator=g)  # noqa: E731
+        self.k, self.v, self.vocab = rnd(), rnd(), vocab
+
+    def kv(self, tokens, positions):
+        t, p = np.asarray(tokens, int), torch.as_tensor(np.asarray(positions), dtype=torch.float32)[:, None, None]
+        return ((self.k[t] * torch.cos(p * 0.1)).to(torch.bfloat16), (self.v[t] * torch.cos(p * 0.07)).to(torch.bfloat16))
+
+
+@pytest.mark.parametrize("captured", [False, True])
+@pytest.mark.parametrize("shared", [False, True])
+def test_speculative_decoding_leaves_the_cache_of_plain_decoding(captured, shared):
+    Hq, Hkv, D, B, N = 8, 2, 64, 3, 21
+    rng = np.random.default_rng(5)
+    m = Model(Hkv, D)
+    lens = [37, 5, 64]
+    pc = pipeline.PagedPrefixCache(Hkv, D, 16, 20, B, 10, spare_blocks=40)
+    prompts = [rng.integers(0, m.vocab, n).astype(np.int32) for n in lens]
+    c, t = pc.match(prompts)
+    b0 = pc.upload_prefill(c, t, lens)
+    k, v = m.kv(np.concatenate(prompts), np.concatenate([np.arange(n) for n in lens]))
+    pc.append(b0, k.cuda(), v.cuda())
+    tab = pipeline.DeviceTables(pc, t, lens, B * N + 4, max_nodes=N, shared=shared)
+    seqs = [list(p) for p in prompts]
+    roots = [int(m.next[s[-1]]) for s in seqs]
+    R = tab.max_rows
+    d = dict(new=dev([0] * B), par=dev([0] * R), tok=dev([0] * R), pick=dev([0] * R))
+    kv = [torch.zeros(R, Hkv, D, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    q, out = torch.randn(R, Hq, D, device="cuda").to(torch.bfloat16), torch.zeros(R, Hq, D, dtype=torch.bfloat16, device="cuda")
+
+    def step():
+        batch = tab.extend(d["new"], N)
+        masks, _ = tab.tree(d["par"])
+        pc.append_slots(tab.slot_map, *kv)
+        pc.attend_tree(batch, q, out, D ** -0.5, masks)
+        tab.accept(d["par"], d["tok"], d["pick"])
+        pc.compact(batch, tab.path, tab.n_accepted)
+
+    graph = None
+    if captured:
+        # (warmed up without new tokens, which changes nothing)
+        step()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step()
+    for it in range(12):
+        new, par, tok, pick, pos = [], [], [], [], []
+        drafts = []
+        for r in range(B):
+            n = int(rng.integers(1, N + 1)) if it % 4 else (0 if r == 1 else 1)
+            p = random_tree(n, rng, 2)
+            tk = [0] * n
+            for i in range(n):
+                right = m.next[tk[p[i]]] if i else roots[r]
+                tk[i] = int(right) if i == 0 or rng.random() < 0.6 else int(rng.integers(0, m.vocab))
+            new.append(n)
+            drafts.append((p, tk))
+            par += p
+            tok += tk
+            pick += [int(m.next[x]) for x in tk]
+            pos += [len(seqs[r]) + len(a) - 1 for a in tree_ref.ancestors(p)]
+        n = len(par)
+        d["new"].copy_(dev(new))
+        for key, x in (("par", par), ("tok", tok), ("pick", pick)):
+            d[key][:n] = dev(x)
+        for dst, src in zip(kv, m.kv(tok, pos)):
+            dst[:n] = src.cuda()
+            dst[n:] = float("nan")
+        if graph is None:
+            step()
+        else:
+            graph.replay()
+        torch.cuda.synchronize()
+        assert ints(tab.status) == [0]
+        assert ints(tab.positions)[:n] == pos
+        at = 0
+        for r, (p, tk) in enumerate(drafts):
+            path, nxt = tree_ref.accept_ref(p, tk, [int(m.next[x]) for x in tk])
+            # attention of the nodes, over what plain decoding would have stored
+            if p:
+                keys = seqs[r]
+                ck, cv = m.kv(keys + tk, list(range(len(keys))) + pos[at:at + len(p)])
+                seen = np.zeros((len(p), len(p)), bool)
+                for i, line in enumerate(tree_ref.ancestors(p)):
+                    seen[i, line] = True
+                ref, mag = tree_ref.tree_attention_ref(q[at:at + len(p)].float().cpu().numpy(), ck.float().numpy(),
+                                                       cv.float().numpy(), D ** -0.5, seen)
+                err = np.abs(out[at:at + len(p)].float().cpu().numpy() - ref)
+                assert (err <= 2.0 ** -8 * np.abs(ref) + (2.0 ** -8 * (1 + 2.0 ** -8) + 2.0 ** -13) * mag).all(), (it, r)
+            seqs[r] += [tk[i] for i in path]
+            if p:
+                roots[r] = nxt
+            assert ints(tab.next_tokens)[r] == nxt
+            at += len(p)
+        assert ints(tab.seq_lens) == [len(s) for s in seqs]
+        # every block once: held by the rows, or free
+        rows, taken = ints(tab.block_tables), ints(pc.free_taken)[0]
+        used = [b for r in range(B) for b in rows[r][:-(-len(seqs[r]) // 16)]]
+        assert len(set(used)) == len(used)
+        assert sorted([b for b in used if b >= 16] + ints(pc.free_ids)[taken:]) == list(range(16, 56))
+    # the cache holds the accepted sequences, as plain decoding would have stored them
+    for r, s in enumerate(seqs):
+        k, v = m.kv(s, np.arange(len(s)))
+        row, at = rows[r], np.arange(len(s))
+        blk = torch.tensor(row, device="cuda")[torch.tensor(at // 16, device="cuda")]
+        off = torch.tensor(at % 16, device="cuda")
+        assert same_bits(pc.k_pool[blk, :, off], k.cuda()) and same_bits(pc.v_pool[blk, :, :, off], v.cuda())
+        assert s[-1] == (m.next[s[-2]] if len(s) > lens[r] + 1 else s[-1])
+    tab.release(dev([1] * B))
+    torch.cuda.synchronize()
+    assert ints(pc.free_taken) == [0] and ints(tab.seq_lens) == [0] * B
+
+
+@pytest.mark.parametrize("lens", [[37, 5], [64, 16], [30, 0]])
+def test_sampling_several_answers_of_each_prompt(lens):
+    Hq, Hkv, D, B = 8, 2, 64, 8
+    rng = np.random.default_rng(6)
+    m = Model(Hkv, D)
+    pc = pipeline.PagedPrefixCache(Hkv, D, 16, 20, B, 10, spare_blocks=60)
+    prompts = [rng.integers(0, m.vocab, n).astype(np.int32) for n in lens]
+    live = [p for p in prompts if len(p)]
+    c, t = pc.match(live)
+    k, v = m.kv(np.concatenate(live), np.concatenate([np.arange(len(p)) for p in live]))
+    pc.append(pc.upload_prefill(c, t, [len(p) for p in live]), k.cuda(), v.cuda())
+    tables = np.full((B, 20), -1, np.int32)
+    tables[:len(live)] = t
+    tab = pipeline.DeviceTables(pc, tables, [len(p) for p in live] + [0] * (B - len(live)), B, shared=True)
+    src, dst = tab.fork(dev([0, 1, 0, 0, 1, 1, 0, 7]))
+    pc.copy_blocks(src, dst)
+    of = [0, 1, 0, 0, 1, 1, 0]
+    seqs = [list(prompts[p]) for p in of] + [[]]
+    q, out = torch.randn(B, Hq, D, device="cuda").to(torch.bfloat16), torch.zeros(B, Hq, D, dtype=torch.bfloat16, device="cuda")
+    alive = [True] * 7 + [False]
+    for it in range(40):
+        tok = rng.integers(0, m.vocab, B).tolist()
+        new = [int(a) for a in alive]
+        batch = tab.extend(dev(new), 1)
+        rows = [r for r in range(B) if alive[r]]
+        k, v = m.kv([tok[r] for r in rows], [len(seqs[r]) for r in rows])
+        pad = torch.full((B - len(rows), Hkv, D), float("nan"), dtype=torch.bfloat16)
+        tab.append(torch.cat([k, pad]).cuda(), torch.cat([v, pad]).cuda())
+        pc.attend(batch, q, out, D ** -0.5)
+        for r in rows:
+            seqs[r].append(tok[r])
+        torch.cuda.synchronize()
+        assert ints(tab.status) == [0]
+        if it in (5, 20):  # two answers end; at 20 their rows become forks of a living one
+            end = [r for r in (1, 3) if alive[r]] if it == 5 else [r for r in (0, 6) if alive[r]]
+            tab.release(dev([int(r in end) for r in range(B)]))
+            for r in end:
+                alive[r], seqs[r] = False, []
+        if it == 25:
+            s, d = tab.fork(dev([2 if r in (0, 3) else r for r in range(B)]))
+            pc.copy_blocks(s, d)
+            for r in (0, 3):
+                alive[r], seqs[r] = True, list(seqs[2])
+        torch.cuda.synchronize()
+        assert ints(tab.seq_lens) == [len(s) for s in seqs]
+    tables = ints(tab.block_tables)
+    count = {}
+    for r in range(B):
+        s = seqs[r]
+        if not s:
+            continue
+        k, v = m.kv(s, np.arange(len(s)))
+        at = np.arange(len(s))
+        blk = torch.tensor(tables[r], device="cuda")[torch.tensor(at // 16, device="cuda")]
+        off = torch.tensor(at % 16, device="cuda")
+        assert same_bits(pc.k_pool[blk, :, off], k.cuda()) and same_bits(pc.v_pool[blk, :, :, off], v.cuda())
+        for b in tables[r][:-(-len(s) // 16)]:
+            count[b] = count.get(b, 0) + 1
+    holds, taken = ints(pc.holds), ints(pc.free_taken)[0]
+    assert all(holds[b - 16] == max(count.get(b, 0) - 1, 0) for b in range(16, 76)) and not any(holds[60:])
+    assert sorted([b for b in count if b >= 16] + ints(pc.free_ids)[taken:]) == list(range(16, 76))
+    tab.release(dev([1] * B))
+    torch.cuda.synchronize()
+    assert ints(pc.free_taken) == [0] and not any(ints(pc.holds))
+
+
+def test_device_tables_say_what_they_were_made_without():
+    pc = pipeline.PagedPrefixCache(1, 64, 4, 4, 2, 6, spare_blocks=4)
+    tab = pipeline.DeviceTables(pc, np.full((2, 4), -1, np.int32), [0, 0], 2)
+    z = dev([0, 0])
+    for call in (lambda: tab.tree(z), lambda: tab.accept(z, z, z), lambda: tab.fork(z)):
+        with pytest.raises(ilpc.ILPCError, match="was made without"):
+            call()
+    assert release_ref([[1]], [0], [0], [], 0)[-1] == 0
+
+
+@pytest.mark.parametrize("case", ["plan", "forks"])
+def test_captured_calls_follow_their_inputs(case):
+    if case == "plan":
+        rng = np.random.default_rng(0)
+        par, tok = dev([-1] * 20), dev(range(20))
+        cu, start, masks, pos = dev([0, 12, 20]), dev([3, 40]), dev(np.zeros((20, 1)), np.int64), dev([0] * 20)
+        pick, outs = dev([0] * 20), [dev([0] * 20)] + [dev([0, 0]) for _ in range(4)]
+
+        def calls():
+            ilpc.tree_masks(par, cu, masks, pos, start)
+            ilpc.tree_accept(par, tok, pick, cu, start, *outs)
+            return [masks, pos] + outs
+    else:
+        s = Rows(40, 5, 300, 2, 300, 5)
+        d = s.d
+        src, ended = dev(range(40)), dev([0] * 40)
+
+        def calls():
+            ilpc.fork_tables(d["bt"], d["lens"], src, d["holds"], 2, d["free"], d["taken"], d["src"], d["dst"], d["taken"],
+                             d["status"], s.nb)
+            ilpc.release_shared(d["bt"], ended, d["holds"], 2, d["free"], d["taken"], d["taken"], d["status"], s.nb)
+            return list(d.values())
+    calls()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        calls()
+    for k in range(4):
+        if case == "plan":
+            p = random_tree(12, rng, 2) + random_tree(8, rng, 1)
+            par.copy_(dev(p))
+            pick.copy_(dev(picks_for(p, list(range(20)), rng)))
+        else:
+            src.copy_(dev([r if r < 5 or r % 7 == k else r % 5 for r in range(40)]))
+            ended.copy_(dev([0 if r < 5 or r % 7 == k else int(d["lens"][r % 5]) for r in range(40)]))
+        g.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in calls()]
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, calls()))
