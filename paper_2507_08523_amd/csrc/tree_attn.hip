@@ -311,7 +311,8 @@ __global__ __launch_bounds__(64 * group_waves(W), 2) void tree_stream_kernel(Tre
 constexpr int kJoinWaves = 4;
 
 template <int D>
-__global__ __launch_bounds__(64 * kJoinWaves) void tree_join_kernel(TreeArgs a, int n_ct, int n_split, int cols_cap) {
+__global__ __launch_bounds__(64 * kJoinWaves) void tree_join_kernel(TreeArgs a, int n_ct, int n_split, int tile_cols,
+                                                                 int cols_cap) {
   constexpr int kPer = D / 64;  // dimensions of a lane
   typedef float vec_t __attribute__((ext_vector_type(kPer)));
   const int lane = threadIdx.x & 63;
@@ -320,28 +321,53 @@ __global__ __launch_bounds__(64 * kJoinWaves) void tree_join_kernel(TreeArgs a, 
   const int c = int(w - unit * unsigned(cols_cap)), ct = int(unit - pair * unsigned(n_ct));
   if (pair >= unsigned(a.B) * unsigned(a.Hkv)) return;
   const int h = int(pair / unsigned(a.B)), r = int(pair % unsigned(a.B));
-  const int G = a.Hq / a.Hkv, col = ct * kTileCols + c;
+  const int G = a.Hq / a.Hkv, col = ct * tile_cols + c;
   const int t = col / G, head = h * G + (col - t * G);
-  const int q0 = a.cu_q[r], q_end = a.cu_q[r + 1], q_len = q_end - q0, L = min(a.seq_lens[r], a.max_blocks * kBlock);
-  if (q0 < 0 || q_end > a.n_rows || q_len <= 0 || q_len > L || col >= min(q_len, a.max_q_len) * G) return;
-  const size_t slot0 = size_t(unit) * n_split * kTileCols + c;  // of split 0
+  // Everything that the lengths do not decide is asked for with them, in one round trip:
+  // the splits' maxima and sums, the first kAhead of their rows.  (Slots of columns that
+  // the batch does not have hold nothing of use, and nothing comes of it.)
+  const size_t slot0 = size_t(unit) * n_split * tile_cols + c;  // of split 0
+  constexpr int kAhead = 8;
   const float* po = a.part_o + slot0 * D + lane * kPer;
-  float m = -INFINITY, l = 0.f;
-  if (lane < n_split) {
-    const float* ml = a.part_ml + (slot0 + size_t(lane) * kTileCols) * 2;
-    m = ml[0], l = ml[1];
+  vec_t v[kAhead];
+  auto load = [&](int k) {
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) v[u] = *(const vec_t*)(po + size_t(min(k + u, n_split - 1)) * tile_cols * D);
+  };
+  int q0 = a.cu_q[r], q_end = a.cu_q[r + 1], L_in = a.seq_lens[r];
+  float2 ml = *(const float2*)(a.part_ml + (slot0 + size_t(min(lane, n_split - 1)) * tile_cols) * 2);
+  load(0);
+  // (pinned here: they would sink behind the test of the lengths)
+  asm volatile("" : "+s"(q0), "+s"(q_end), "+s"(L_in));
+  asm volatile("" : "+v"(ml.x), "+v"(ml.y));
+#pragma unroll
+  for (int u = 0; u < kAhead; ++u) {
+    if constexpr (kPer == 2) {
+      asm volatile("" : "+v"(v[u]));
+    } else {
+      float x = v[u][0];
+      asm volatile("" : "+v"(x));
+      v[u][0] = x;
+    }
   }
+  const int q_len = q_end - q0, L = min(L_in, a.max_blocks * kBlock);
+  if (q0 < 0 || q_end > a.n_rows || q_len <= 0 || q_len > L || col >= min(q_len, a.max_q_len) * G) return;
+  const float m = lane < n_split ? ml.x : -INFINITY;
   float mx = m;
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor(mx, off));
   const float wgt = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mx);
-  float den = wgt * l;
+  float den = wgt * ml.y;
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) den += __shfl_xor(den, off);
   const float inv = den > 0.f ? 1.f / den : 0.f;
   vec_t y = {};
-  for (int k = 0; k < n_split; ++k)
-    y += *(const vec_t*)(po + size_t(k) * kTileCols * D) * __int_as_float(__builtin_amdgcn_readlane(__float_as_int(wgt), k));
+  for (int k = 0; k < n_split; k += kAhead) {
+    if (k > 0) load(k);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      if (k + u < n_split) y += v[u] * __int_as_float(__builtin_amdgcn_readlane(__float_as_int(wgt), k + u));
+  }
   uint16_t* orow = a.out + (size_t(q0 + t) * a.Hq + head) * D + lane * kPer;
 #pragma unroll
   for (int e = 0; e < kPer; ++e) orow[e] = __builtin_bit_cast(uint16_t, (__bf16)(y[e] * inv));
@@ -349,31 +375,40 @@ __global__ __launch_bounds__(64 * kJoinWaves) void tree_join_kernel(TreeArgs a, 
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
-// Waves of a workgroup, and workgroups, to a column tile.
+// How a launch cuts its work: columns of a tile (32: the kernel above, `waves` of a workgroup to
+// a tile; kTreeTileCols: tree_tiles.hip), and workgroups to a tile's keys.
 struct Plan {
-  int waves, groups;
+  int cols, waves, groups;
+  int64_t n_ct, units;  // column tiles of a (request, kv head), of the batch
 };
+
+Plan make_plan(int64_t B, int64_t max_q_len, int Hq, int Hkv, int D, int64_t max_blocks) {
+  const int64_t cus = ilpc::device_cus(), cols = max_q_len * (Hq / Hkv), pairs = B * Hkv;
+  const int64_t tiles64 = (max_blocks * kBlock + 63) / 64, steps = 2 * tiles64;
+  Plan p{kTileCols, 4, 1, 0, 0};
+  auto cut = [&](int c) { p.cols = c, p.n_ct = (cols + c - 1) / c, p.units = pairs * p.n_ct; };
+  if (cols > 64) {
+    cut(kTreeTileCols);
+    const int64_t room = std::min<int64_t>(2 * cus / p.units, kMaxGroups);
+    if (room >= 2) p.groups = int(std::max<int64_t>(1, std::min(room, tiles64 / 4)));
+    return p;
+  }
+  cut(kTileCols);
+  if (p.units > 2 * cus) {
+    p.waves = steps <= 4 ? 1 : 2;
+    return p;
+  }
+  const int64_t room = std::min<int64_t>(cus / p.units, kMaxGroups);
+  if (room >= 2 && steps >= 16) p.groups = int(std::min(room, (steps + 7) / 8));
+  return p;
+}
+
+size_t part_bytes(const Plan& p, int D) {
+  return p.groups > 1 ? size_t(p.units) * p.groups * p.cols * (D + 2) * sizeof(float) : 0;
+}
 
 int64_t column_tiles(int64_t max_q_len, int Hq, int Hkv) {
   return (max_q_len * (Hq / Hkv) + kTileCols - 1) / kTileCols;
-}
-
-Plan stream_plan(int64_t units, int64_t max_blocks) {
-  const int64_t cus = ilpc::device_cus(), steps = (max_blocks * kBlock + kStepKeys - 1) / kStepKeys;
-  if (units > 2 * cus) return {steps <= 4 ? 1 : 2, 1};
-  const int64_t room = std::min<int64_t>(cus / units, kMaxGroups);
-  if (room >= 2 && steps >= 16) return {4, int(std::min(room, (steps + 7) / 8))};
-  return {4, 1};
-}
-
-// Workgroups of a launch.
-int64_t stream_grid(int64_t units, const Plan& plan) {
-  const int64_t per_group = group_waves(plan.waves) / plan.waves;
-  return (units * plan.groups + per_group - 1) / per_group;
-}
-
-size_t part_bytes(int64_t units, int D, int n) {
-  return n > 1 ? size_t(units) * n * kTileCols * (D + 2) * sizeof(float) : 0;
 }
 
 int check_sizes(const char* fn, int32_t B, int32_t max_q_len, int32_t Hq, int32_t Hkv, int32_t D, int32_t max_blocks) {
@@ -400,8 +435,7 @@ extern "C" int ilpc_tree_attn_workspace_bytes(int32_t B, int32_t max_q_len, int3
   *bytes = 0;
   if (B == 0 || max_q_len == 0) return ILPC_OK;
   if (ilpc::device_cus() <= 0) return ilpc::set_error(ILPC_EHIP, "%s: cannot query the device", fn);
-  const int64_t units = int64_t(B) * Hkv * column_tiles(max_q_len, Hq, Hkv);
-  *bytes = part_bytes(units, D, stream_plan(units, max_blocks).groups);
+  *bytes = part_bytes(make_plan(B, max_q_len, Hq, Hkv, D, max_blocks), D);
   return ILPC_OK;
 }
 
@@ -432,33 +466,41 @@ extern "C" int ilpc_paged_tree_attn(const uint16_t* q, int64_t q_stride, int32_t
   const uint16_t *q_end = q + int64_t(n_rows - 1) * q_stride + int64_t(Hq) * D, *out_end = out + int64_t(n_rows) * Hq * D;
   if (q < out_end && out < q_end) return set_error(ILPC_EINVAL, "%s: q and out overlap", fn);
   if (ilpc::device_cus() <= 0) return set_error(ILPC_EHIP, "%s: cannot query the device", fn);
-  const int64_t n_ct = column_tiles(max_q_len, Hq, Hkv), units = int64_t(B) * Hkv * n_ct;
-  const Plan plan = stream_plan(units, max_blocks);
-  const size_t need = part_bytes(units, D, plan.groups);
+  const Plan plan = make_plan(B, max_q_len, Hq, Hkv, D, max_blocks);
+  const size_t need = part_bytes(plan, D);
   if (need && (!workspace || workspace_bytes < need || !aligned16(workspace)))
     return set_error(ILPC_EINVAL, "%s: workspace must be %zu bytes, 16-byte aligned", fn, need);
   float* part_o = need ? static_cast<float*>(workspace) : nullptr;
-  float* part_ml = need ? part_o + size_t(units) * plan.groups * kTileCols * D : nullptr;
+  float* part_ml = need ? part_o + size_t(plan.units) * plan.groups * plan.cols * D : nullptr;
   const TreeArgs a{q, q_stride, n_rows, k_pool, v_pool, num_blocks, block_tables, max_blocks, cu_q, seq_lens, B,
                    max_q_len, Hq, Hkv, D, softmax_scale * 1.4426950408889634f,
                    reinterpret_cast<const uint32_t*>(masks), mask_words * 2, out, part_o, part_ml};
-  const dim3 grid{unsigned(stream_grid(units, plan))}, block{unsigned(64 * group_waves(plan.waves))};
+  const int n_ct = int(plan.n_ct);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, a, int(n_ct), plan.groups); };
-  if (D == 128) {
-    if (plan.waves == 1) launch(tree_stream_kernel<128, 1>);
-    else if (plan.waves == 2) launch(tree_stream_kernel<128, 2>);
-    else launch(tree_stream_kernel<128, 4>);
+  hipError_t e;
+  if (plan.cols > kTileCols) {
+    e = launch_tree_tiles(a, n_ct, plan.groups, s);
   } else {
-    if (plan.waves == 1) launch(tree_stream_kernel<64, 1>);
-    else if (plan.waves == 2) launch(tree_stream_kernel<64, 2>);
-    else launch(tree_stream_kernel<64, 4>);
+    const int waves = group_waves(plan.waves), per_group = waves / plan.waves;
+    const dim3 grid{unsigned((plan.units * plan.groups + per_group - 1) / per_group)}, block{unsigned(64 * waves)};
+    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, a, n_ct, plan.groups); };
+    if (D == 128) {
+      if (plan.waves == 1) launch(tree_stream_kernel<128, 1>);
+      else if (plan.waves == 2) launch(tree_stream_kernel<128, 2>);
+      else if (plan.waves == 4) launch(tree_stream_kernel<128, 4>);
+      else launch(tree_stream_kernel<128, 8>);
+    } else {
+      if (plan.waves == 1) launch(tree_stream_kernel<64, 1>);
+      else if (plan.waves == 2) launch(tree_stream_kernel<64, 2>);
+      else if (plan.waves == 4) launch(tree_stream_kernel<64, 4>);
+      else launch(tree_stream_kernel<64, 8>);
+    }
+    e = hipGetLastError();
   }
-  hipError_t e = hipGetLastError();
   if (e == hipSuccess && plan.groups > 1) {
-    const int cols_cap = int(std::min<int64_t>(int64_t(max_q_len) * (Hq / Hkv), kTileCols));
-    const dim3 jgrid{unsigned((units * cols_cap + kJoinWaves - 1) / kJoinWaves)}, jblock{64 * kJoinWaves};
-    auto join = [&](auto kernel) { hipLaunchKernelGGL(kernel, jgrid, jblock, 0, s, a, int(n_ct), plan.groups, cols_cap); };
+    const int cols_cap = int(std::min<int64_t>(int64_t(max_q_len) * (Hq / Hkv), plan.cols));
+    const dim3 grid{unsigned((plan.units * cols_cap + kJoinWaves - 1) / kJoinWaves)}, block{64 * kJoinWaves};
+    auto join = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, a, n_ct, plan.groups, plan.cols, cols_cap); };
     if (D == 128) join(tree_join_kernel<128>);
     else join(tree_join_kernel<64>);
     e = hipGetLastError();
