@@ -47,8 +47,8 @@ __device__ __forceinline__ void tree_words(const uint32_t* row, int half_words, 
 }
 
 // The kernel for many columns (tree_tiles.hip), kTreeTileCols to a workgroup: a (request, kv
-// head)'s columns in n_ct tiles, each one's keys over n_split workgroups.
+// head)'s columns in n_ct tiles.
 constexpr int kTreeTileCols = 128;
-hipError_t launch_tree_tiles(const TreeArgs& a, int n_ct, int n_split, hipStream_t stream);
+hipError_t launch_tree_tiles(const TreeArgs& a, int n_ct, hipStream_t stream);
 
 }  // namespace ilpc

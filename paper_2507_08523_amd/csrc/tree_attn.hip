@@ -311,8 +311,7 @@ __global__ __launch_bounds__(64 * group_waves(W), 2) void tree_stream_kernel(Tre
 constexpr int kJoinWaves = 4;
 
 template <int D>
-__global__ __launch_bounds__(64 * kJoinWaves) void tree_join_kernel(TreeArgs a, int n_ct, int n_split, int tile_cols,
-                                                                 int cols_cap) {
+__global__ __launch_bounds__(64 * kJoinWaves) void tree_join_kernel(TreeArgs a, int n_ct, int n_split, int cols_cap) {
   constexpr int kPer = D / 64;  // dimensions of a lane
   typedef float vec_t __attribute__((ext_vector_type(kPer)));
   const int lane = threadIdx.x & 63;
@@ -321,21 +320,21 @@ __global__ __launch_bounds__(64 * kJoinWaves) void tree_join_kernel(TreeArgs a, 
   const int c = int(w - unit * unsigned(cols_cap)), ct = int(unit - pair * unsigned(n_ct));
   if (pair >= unsigned(a.B) * unsigned(a.Hkv)) return;
   const int h = int(pair / unsigned(a.B)), r = int(pair % unsigned(a.B));
-  const int G = a.Hq / a.Hkv, col = ct * tile_cols + c;
+  const int G = a.Hq / a.Hkv, col = ct * kTileCols + c;
   const int t = col / G, head = h * G + (col - t * G);
   // Everything that the lengths do not decide is asked for with them, in one round trip:
   // the splits' maxima and sums, the first kAhead of their rows.  (Slots of columns that
   // the batch does not have hold nothing of use, and nothing comes of it.)
-  const size_t slot0 = size_t(unit) * n_split * tile_cols + c;  // of split 0
+  const size_t slot0 = size_t(unit) * n_split * kTileCols + c;  // of split 0
   constexpr int kAhead = 8;
   const float* po = a.part_o + slot0 * D + lane * kPer;
   vec_t v[kAhead];
   auto load = [&](int k) {
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) v[u] = *(const vec_t*)(po + size_t(min(k + u, n_split - 1)) * tile_cols * D);
+    for (int u = 0; u < kAhead; ++u) v[u] = *(const vec_t*)(po + size_t(min(k + u, n_split - 1)) * kTileCols * D);
   };
   int q0 = a.cu_q[r], q_end = a.cu_q[r + 1], L_in = a.seq_lens[r];
-  float2 ml = *(const float2*)(a.part_ml + (slot0 + size_t(min(lane, n_split - 1)) * tile_cols) * 2);
+  float2 ml = *(const float2*)(a.part_ml + (slot0 + size_t(min(lane, n_split - 1)) * kTileCols) * 2);
   load(0);
   // (pinned here: they would sink behind the test of the lengths)
   asm volatile("" : "+s"(q0), "+s"(q_end), "+s"(L_in));
@@ -376,35 +375,53 @@ __global__ __launch_bounds__(64 * kJoinWaves) void tree_join_kernel(TreeArgs a, 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // How a launch cuts its work: columns of a tile (32: the kernel above, `waves` of a workgroup to
-// a tile; kTreeTileCols: tree_tiles.hip), and workgroups to a tile's keys.
+// a tile and `groups` workgroups to its keys; kTreeTileCols: tree_tiles.hip), and how many tiles.
 struct Plan {
   int cols, waves, groups;
   int64_t n_ct, units;  // column tiles of a (request, kv head), of the batch
 };
 
+// What few tiles wait for is a wave's steps, about 1 us each one after the other: four waves to a tile,
+// and more workgroups while there are compute units without one; but their states' join is
+// a launch more (3 us, and more for many columns), so that contexts up to about 1.2 K
+// keys are not cut, and a tile's range count goes as the root of its steps: the steps fall as 1 / ranges
+// and the join's reads grow with them.  us (waves x groups; 8 kv heads, D 128 where not said):
+//   tiles, keys       8, 300    4x1 8.6, 4x4 10.4             8, 1000    4x8 10.6, 4x4 11.7, 8x1 12.3
+//   8, 4000           4x8 13.0, 4x16 13.3, 4x4 16.1           8, 16000   4x16 21.4, 4x24 23.9, 4x8 24.7
+//   32, 500           4x1 10.2, 4x4 10.8                      32, 1500   4x6 13.1, 4x4 13.3, 4x1 15.9
+//   64, 1000          4x1 13.8, 4x3 14.6                      64, 2000   4x4 16.9, 4x2 18.0, 4x1 20.5
+//   64, 4096          4x4 20.3, 8x3 19.6, 4x8 21.4            128, 1000  4x1 13.8, 8x1 14.0, 4x2 16.7
+//   128, 3000         8x2 22.3, 4x2 23.5, 4x1 27.5            128, 6000  8x2 30.2, 4x2 33.3, 4x1 47.7
+//   256, 2000         4x1 22.9, 4x2 27.9                      D 64: 32, 1000  8x1 9.0, 4x8 9.8, 4x1 10.0
+//   D 64: 128, 2500   8x1 14.5, 4x4 16.1, 4x1 18.2            D 64: 32, 3000  4x8 10.8, 8x1 14.9
+// Many tiles are taken 128 columns at a time on LDS tiles, where a pair has more than one of 32 (here, there):
+//   320, 1200   22.0, 26.9      512, 2000   33.5, 40.4       768, 800    28.4, 22.3     1024, 2000  57.2, 49.7
+//   1024, 300   18.0, 14.8      2048, 2000  124, 76.5        1536, 800   45.8, 40.1     16384, 2050 873, 600
+//   D 64: 768, 1000  18.5, 19.7    800, 700  18.6, 19.3      2048, 1500  51.6, 37.6     3072, 1000  55.5, 47.4
+// of one tile a pair 1024 of 500 keys 48.2, 51.7, of 1000 95.4, 95.9; 2400 of 100 34.0, 39.2.
+// Waves for those: 800 (D 64, 700 keys) 2x1 18.6, 4x1 20.3; 1024, 500 4x1 48.2, 2x1 49.1, 1x1 51.2; 2400, 100
+// 1x1 34.0, 2x1 34.5, 4x1 38.5.
 Plan make_plan(int64_t B, int64_t max_q_len, int Hq, int Hkv, int D, int64_t max_blocks) {
   const int64_t cus = ilpc::device_cus(), cols = max_q_len * (Hq / Hkv), pairs = B * Hkv;
-  const int64_t tiles64 = (max_blocks * kBlock + 63) / 64, steps = 2 * tiles64;
-  Plan p{kTileCols, 4, 1, 0, 0};
-  auto cut = [&](int c) { p.cols = c, p.n_ct = (cols + c - 1) / c, p.units = pairs * p.n_ct; };
-  if (cols > 64) {
-    cut(kTreeTileCols);
-    const int64_t room = std::min<int64_t>(2 * cus / p.units, kMaxGroups);
-    if (room >= 2) p.groups = int(std::max<int64_t>(1, std::min(room, tiles64 / 4)));
-    return p;
+  const int64_t steps = (max_blocks * kBlock + kStepKeys - 1) / kStepKeys;
+  auto cut = [&](int c) -> Plan { return {c, 4, 1, (cols + c - 1) / c, pairs * ((cols + c - 1) / c)}; };
+  Plan p = cut(kTileCols);
+  const int64_t u = p.units;
+  if (2 * u > (D == 64 ? 7 : 5) * cus && p.n_ct > 1) return cut(kTreeTileCols);
+  if (u > 3 * cus) {
+    p.waves = steps <= 8 ? 1 : 2;
+  } else if (2 * u <= cus) {
+    const int64_t room = std::min<int64_t>(cus / u, kMaxGroups);
+    if (room >= 3 && (steps >= 40 || (room >= 16 && steps >= 28)))
+      p.groups = int(std::min<int64_t>(room, int64_t(std::sqrt(double(steps)))));
+    else if (D == 64 ? steps >= 20 : room == 2 && steps >= 64)
+      p.waves = 8, p.groups = D == 64 ? 1 : 2;
   }
-  cut(kTileCols);
-  if (p.units > 2 * cus) {
-    p.waves = steps <= 4 ? 1 : 2;
-    return p;
-  }
-  const int64_t room = std::min<int64_t>(cus / p.units, kMaxGroups);
-  if (room >= 2 && steps >= 16) p.groups = int(std::min(room, (steps + 7) / 8));
   return p;
 }
 
 size_t part_bytes(const Plan& p, int D) {
-  return p.groups > 1 ? size_t(p.units) * p.groups * p.cols * (D + 2) * sizeof(float) : 0;
+  return p.groups > 1 ? size_t(p.units) * p.groups * kTileCols * (D + 2) * sizeof(float) : 0;
 }
 
 int64_t column_tiles(int64_t max_q_len, int Hq, int Hkv) {
@@ -471,7 +488,7 @@ extern "C" int ilpc_paged_tree_attn(const uint16_t* q, int64_t q_stride, int32_t
   if (need && (!workspace || workspace_bytes < need || !aligned16(workspace)))
     return set_error(ILPC_EINVAL, "%s: workspace must be %zu bytes, 16-byte aligned", fn, need);
   float* part_o = need ? static_cast<float*>(workspace) : nullptr;
-  float* part_ml = need ? part_o + size_t(plan.units) * plan.groups * plan.cols * D : nullptr;
+  float* part_ml = need ? part_o + size_t(plan.units) * plan.groups * kTileCols * D : nullptr;
   const TreeArgs a{q, q_stride, n_rows, k_pool, v_pool, num_blocks, block_tables, max_blocks, cu_q, seq_lens, B,
                    max_q_len, Hq, Hkv, D, softmax_scale * 1.4426950408889634f,
                    reinterpret_cast<const uint32_t*>(masks), mask_words * 2, out, part_o, part_ml};
@@ -479,7 +496,7 @@ extern "C" int ilpc_paged_tree_attn(const uint16_t* q, int64_t q_stride, int32_t
   hipStream_t s = static_cast<hipStream_t>(stream);
   hipError_t e;
   if (plan.cols > kTileCols) {
-    e = launch_tree_tiles(a, n_ct, plan.groups, s);
+    e = launch_tree_tiles(a, n_ct, s);
   } else {
     const int waves = group_waves(plan.waves), per_group = waves / plan.waves;
     const dim3 grid{unsigned((plan.units * plan.groups + per_group - 1) / per_group)}, block{unsigned(64 * waves)};
@@ -498,9 +515,9 @@ extern "C" int ilpc_paged_tree_attn(const uint16_t* q, int64_t q_stride, int32_t
     e = hipGetLastError();
   }
   if (e == hipSuccess && plan.groups > 1) {
-    const int cols_cap = int(std::min<int64_t>(int64_t(max_q_len) * (Hq / Hkv), plan.cols));
+    const int cols_cap = int(std::min<int64_t>(int64_t(max_q_len) * (Hq / Hkv), kTileCols));
     const dim3 grid{unsigned((plan.units * cols_cap + kJoinWaves - 1) / kJoinWaves)}, block{64 * kJoinWaves};
-    auto join = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, a, n_ct, plan.groups, plan.cols, cols_cap); };
+    auto join = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, a, n_ct, plan.groups, cols_cap); };
     if (D == 128) join(tree_join_kernel<128>);
     else join(tree_join_kernel<64>);
     e = hipGetLastError();

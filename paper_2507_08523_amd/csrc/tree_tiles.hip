@@ -97,7 +97,7 @@ __device__ __forceinline__ void bare_barrier() {
 constexpr int wgs_per_cu(int D) { return D == 64 ? 3 : 2; }
 
 template <int D>
-__global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void tree_tile_kernel(TreeArgs a, int n_ct, int n_split, int recip) {
+__global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void tree_tile_kernel(TreeArgs a, int n_ct, int recip) {
   constexpr int kDch = D / 16, kDt = D / 32;  // 16-dimension chunks of a row, 32-row tiles of O^T
   constexpr int kRowBytes = D * 2, kKch = D / 8;
   constexpr int kSlabBytes = kBlock * D * 2, kTileBytes = kTileBlocks * kSlabBytes;
@@ -110,12 +110,12 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void tree_tile_kernel(T
   const int n = lane & 31, hh = lane >> 5;
   const int G = a.Hq / a.Hkv;
 
-  // Workgroup b runs on XCD b % 8; each XCD takes a contiguous range of items:
-  // item = ((kv head * B + request) * n_ct + column tile) * n_split + range of the keys
+  // Workgroup b runs on XCD b % 8; each XCD takes a contiguous range of items, so that a pair's
+  // column tiles read its keys through one L2: item = (kv head * B + request) * n_ct + column tile
   const unsigned nb = gridDim.x, per_x = nb >> 3, extra = nb & 7u, x = blockIdx.x & 7u;
   const unsigned item = x * per_x + min(x, extra) + (blockIdx.x >> 3);
-  const unsigned unit = item / unsigned(n_split), pair = unit / unsigned(n_ct);
-  const int sp = int(item - unit * unsigned(n_split)), ct = int(unit - pair * unsigned(n_ct));
+  const unsigned pair = item / unsigned(n_ct);
+  const int ct = int(item - pair * unsigned(n_ct));
   const int h = int(pair / unsigned(a.B)), r = int(pair % unsigned(a.B));
   const int32_t* bt = a.block_tables + size_t(r) * a.max_blocks;
   auto raw_id = [&](int blk) { return scalar_load(bt + min(blk, a.max_blocks - 1)); };
@@ -125,9 +125,7 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void tree_tile_kernel(T
   if (q0 < 0 || q_end > a.n_rows || q_len <= 0 || q_len > L || n_valid <= 0) return;
   const int start = L - q_len;  // the nodes' first key
   const int n_blk = (L + kBlock - 1) / kBlock;
-  const int all_tiles = (L + kKeys - 1) / kKeys, per = (all_tiles + n_split - 1) / n_split;
-  const int j0 = min(sp * per, all_tiles), n_tiles = min(j0 + per, all_tiles) - j0;  // tiles j0 .. j0 + n_tiles - 1
-  const int blk0 = j0 * kTileBlocks;
+  const int n_tiles = (L + kKeys - 1) / kKeys;
 
   // Columns are split into (node, head of the group) by a 16-bit reciprocal of G, exact for the
   // offsets met here, below G + kCols <= 192.
@@ -141,7 +139,7 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void tree_tile_kernel(T
 
   // A wave loads one pool block of every K tile and of every V tile.  In step u the
   // scores of step u + 1 and the products with V of step u - 1 are taken, so K runs half a
-  // tile ahead and V half a tile behind: K tile j holds the range's blocks 4j+2 .. 4j+5, V tile j
+  // tile ahead and V half a tile behind: K tile j holds the blocks 4j+2 .. 4j+5, V tile j
   // its blocks 4j-2 .. 4j+1, and both are free at the same barrier; K tile -1 holds the
   // first two blocks.
   uint32_t koff[kInsts];
@@ -172,8 +170,8 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void tree_tile_kernel(T
     else load_slab2(voff, voff, base, to);
   };
 
-  const int first_k = raw_id(blk0 + max(wave - 2, 0)), id_k0 = raw_id(blk0 + 2 + wave);
-  int next_k = raw_id(blk0 + kTileBlocks + 2 + wave), next_v = raw_id(blk0 + 2 + wave);  // of tile 1, unchecked
+  const int first_k = raw_id(max(wave - 2, 0)), id_k0 = raw_id(2 + wave);
+  int next_k = raw_id(kTileBlocks + 2 + wave), next_v = raw_id(2 + wave);  // of tile 1, unchecked
   __builtin_amdgcn_sched_barrier(0);  // (all on their way before the first is looked at)
   bf16x8 qf[kDch];  // Q operand
   {
@@ -182,21 +180,18 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void tree_tile_kernel(T
     for (int kc = 0; kc < kDch; ++kc) qf[kc] = as_bf16x8(*(const u32x4*)(qr + kc * 16 + hh * 8));
   }
   // Which nodes some row sees, for V (below).
-  const bool tail = (j0 + n_tiles) * kKeys > start;
-  if (tail) {
-    if (tid < kMaxHalfWords) s_any[tid] = 0;
-    __syncthreads();
+  if (tid < kMaxHalfWords) s_any[tid] = 0;
+  __syncthreads();
+  if (wave >= 2) {
+    issue_k(-1, usable(wave - 2, first_k));
+    issue_v(0, usable(wave - 2, first_k));
+  } else {
+#pragma unroll
+    for (int i = 0; i < kInsts; ++i) *(u32x4*)(ring + v_buf(0) + wave * kSlabBytes + i * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
   }
-  if (n_tiles > 0) {
-    if (wave >= 2) issue_k(-1, usable(blk0 + wave - 2, first_k));
-    issue_k(0, usable(blk0 + 2 + wave, id_k0));
-    if (wave >= 2) issue_v(0, usable(blk0 + wave - 2, first_k));
-    else
-      for (int i = 0; i < kInsts; ++i) *(u32x4*)(ring + v_buf(0) + wave * kSlabBytes + i * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
-  }
-  if (tail)
-    for (int e = tid; e < n_rows * a.half_words; e += 64 * kWaves)
-      atomicOr(&s_any[e % a.half_words], a.masks[size_t(q0) * a.half_words + e]);
+  issue_k(0, usable(2 + wave, id_k0));
+  for (int e = tid; e < n_rows * a.half_words; e += 64 * kWaves)
+    atomicOr(&s_any[e % a.half_words], a.masks[size_t(q0) * a.half_words + e]);
 
   f32x16 sA, sB;          // scores of this step and of the next, in turn
   bf16x8 pA[2], pB[2];    // weights of this step and of the one before, in turn
@@ -288,7 +283,7 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void tree_tile_kernel(T
   // landed; others read it behind the next barrier): slots that hold no token may have any bits, and
   // a weight of 0 does not hide a NaN.
   auto zero_hidden_v = [&](int j) {
-    const int k0 = (j0 + j) * kKeys + (wave - 2) * kBlock;
+    const int k0 = j * kKeys + (wave - 2) * kBlock;
     if (k0 + kBlock <= start) return;
     uint32_t lo, hi;
     tree_words(s_any, a.half_words, k0, start, &lo, &hi);
@@ -310,7 +305,7 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void tree_tile_kernel(T
 
   // One step (the first one multiplies weights of 0 with zeros).
   auto body = [&](int u, f32x16& sc, f32x16& sn, bf16x8(&pp)[2], bf16x8(&pc)[2]) __attribute__((always_inline)) {
-    const int j = u >> 1, k0 = j0 * kKeys + u * 32;
+    const int j = u >> 1, k0 = u * 32;
     if (k0 + 32 > start) {
       uint32_t lo, hi;
       tree_words(mask_row, a.half_words, k0, start, &lo, &hi);
@@ -331,50 +326,29 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void tree_tile_kernel(T
     zero_hidden_v(j);
     bare_barrier();
   };
-  if (n_tiles > 0) {
-    wait_loads();
-    wait_lds();
-    bare_barrier();
-    if (active) products(no(), no(), yes(), ring, ring + k_buf(-1) + 32 * kRowBytes, sB, sA, pB, pA);
-    for (int j = 0; j < n_tiles; ++j) {
-      turn(j);
-      const int kb = blk0 + (j + 1) * kTileBlocks + 2 + wave, vb = kb - 4;
-      if (j + 1 < n_tiles) issue_k(j + 1, usable(kb, next_k));
-      issue_v(j + 1, usable(vb, next_v));
-      next_k = raw_id(kb + kTileBlocks);
-      next_v = raw_id(vb + kTileBlocks);
-      if (active) {
-        // (the ids' scalar loads are waited for here, and not with the first LDS operands of the products)
-        asm volatile("" : "+s"(next_k), "+s"(next_v));
-        body(2 * j, sA, sB, pB, pA);
-        body(2 * j + 1, sB, sA, pA, pB);
-      }
+  wait_loads();
+  wait_lds();
+  bare_barrier();
+  if (active) products(no(), no(), yes(), ring, ring + k_buf(-1) + 32 * kRowBytes, sB, sA, pB, pA);
+  for (int j = 0; j < n_tiles; ++j) {
+    turn(j);
+    const int kb = (j + 1) * kTileBlocks + 2 + wave, vb = kb - 4;
+    if (j + 1 < n_tiles) issue_k(j + 1, usable(kb, next_k));
+    issue_v(j + 1, usable(vb, next_v));
+    next_k = raw_id(kb + kTileBlocks);
+    next_v = raw_id(vb + kTileBlocks);
+    if (active) {
+      // (the ids' scalar loads are waited for here, and not with the first LDS operands of the products)
+      asm volatile("" : "+s"(next_k), "+s"(next_v));
+      body(2 * j, sA, sB, pB, pA);
+      body(2 * j + 1, sB, sA, pA, pB);
     }
-    turn(n_tiles);
-    if (active) products(yes(), no(), no(), ring + v_buf(n_tiles), ring, sA, sB, pB, pA);
   }
+  turn(n_tiles);
+  if (active) products(yes(), no(), no(), ring + v_buf(n_tiles), ring, sA, sB, pB, pA);
   if (!active) return;
 
   const float total = add_across_halves(l);
-  if (n_split > 1) {
-    // partial state: O (not normalised), max and sum of this wave's columns
-    if (wave_first + n < n_valid) {
-      const size_t slot = (size_t(unit) * n_split + sp) * kCols + wave_first + n;
-      float* po = a.part_o + slot * D;
-#pragma unroll
-      for (int dt = 0; dt < kDt; ++dt)
-#pragma unroll
-        for (int g4 = 0; g4 < 4; ++g4) {
-          const f32x4 v = {o[dt][g4 * 4], o[dt][g4 * 4 + 1], o[dt][g4 * 4 + 2], o[dt][g4 * 4 + 3]};
-          *(f32x4*)(po + dt * 32 + g4 * 8 + hh * 4) = v;
-        }
-      if (hh == 0) {
-        a.part_ml[slot * 2] = m;
-        a.part_ml[slot * 2 + 1] = total;
-      }
-    }
-    return;
-  }
   const float inv = total > 0.f ? 1.f / total : 0.f;
   // The rows leave through LDS, so that whole 128-byte half rows are stored (a lane
   // holds 8-byte pieces of one row).  4 KiB a wave, where K was, which every wave has left
@@ -412,10 +386,10 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void tree_tile_kernel(T
 
 namespace ilpc {
 
-hipError_t launch_tree_tiles(const TreeArgs& a, int n_ct, int n_split, hipStream_t stream) {
-  const dim3 grid{unsigned(int64_t(a.B) * a.Hkv * n_ct * n_split)}, block{64 * kWaves};
+hipError_t launch_tree_tiles(const TreeArgs& a, int n_ct, hipStream_t stream) {
+  const dim3 grid{unsigned(int64_t(a.B) * a.Hkv * n_ct)}, block{64 * kWaves};
   auto launch = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, grid, block, 0, stream, a, n_ct, n_split, 65536 / (a.Hq / a.Hkv) + 1);
+    hipLaunchKernelGGL(kernel, grid, block, 0, stream, a, n_ct, 65536 / (a.Hq / a.Hkv) + 1);
   };
   if (a.D == 128) launch(tree_tile_kernel<128>);
   else launch(tree_tile_kernel<64>);
