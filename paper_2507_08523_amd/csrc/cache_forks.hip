@@ -147,9 +147,9 @@ __global__ __launch_bounds__(kFillThreads) void fork_fill_kernel(
 
 // -- release ------------------------------------------------------------------
 // First every entry's hold is dropped; the one that drops a block's last hold marks the
-// block.  Then the marked blocks go back in the order of their ids, which does not
-// depend on the order of the drops.  Marks are the bits of the words behind the counts,
-// zero between calls.
+// block (one dropped below that shows that it was given back too often).  Then the marked
+// blocks go back in the order of their ids, which does not depend on the order of the drops.
+// Marks are the bits of the words behind the counts, zero between calls.
 
 struct Release {
   const int32_t* block_tables;
@@ -163,8 +163,7 @@ struct Release {
     const int b = block_tables[size_t(r) * max_blocks + j] - first_id;
     return b >= 0 && b < n_held ? b : -1;
   }
-  __device__ __forceinline__ void drop(int r, int j) const {
-    const int b = block(r, j);
+  __device__ __forceinline__ void drop(int b) const {
     if (b >= 0 && atomicSub(holds + b, 1) == 0) atomicOr(marks() + (b >> 5), 1u << (b & 31));
   }
   __device__ __forceinline__ int bad_len(int r) const {
@@ -180,70 +179,117 @@ __device__ __forceinline__ int check_lens(const Release& a, int64_t had, int n_f
   return bad;
 }
 
-// (every workgroup checks all lengths: nothing is dropped unless all are right)
+// (every workgroup checks all lengths: nothing is dropped unless all are right; a row's first
+// entries are on their way meanwhile)
 __global__ __launch_bounds__(kFillThreads) void drop_kernel(Release a, const int32_t* __restrict__ taken, int n_free) {
   __shared__ int s_bad;
-  if (threadIdx.x == 0) s_bad = 0;
+  const int tid = threadIdx.x;
+  if (tid == 0) s_bad = 0;
+  int r = blockIdx.x, b = a.block(r, min(tid, a.max_blocks - 1)), len = a.seq_lens[r];
   __syncthreads();
   const int bad = check_lens(a, *taken, n_free);
   if (bad) atomicOr(&s_bad, bad);
   __syncthreads();
   if (s_bad) return;
-  for (int r = blockIdx.x; r < a.B; r += gridDim.x) {
-    const int n = blocks_of(a.seq_lens[r]);
-    for (int j = threadIdx.x; j < n; j += kFillThreads) a.drop(r, j);
+  while (true) {
+    const int n = blocks_of(len);
+    if (tid < n) a.drop(b);
+    for (int j = tid + kFillThreads; j < n; j += kFillThreads) a.drop(a.block(r, j));
+    if ((r += gridDim.x) >= a.B) return;
+    len = a.seq_lens[r];
+    b = a.block(r, min(tid, a.max_blocks - 1));
   }
 }
+
+// The marked blocks in ascending order, by one workgroup: kChunk words of marks at a time in LDS with the
+// marks before each, so that every thread places one bit.  DROP: the same workgroup has dropped
+// the holds, and marked the blocks in LDS alone (so they fit one chunk).
+constexpr int kChunk = 4096;
 
 template <bool DROP>
 __global__ __launch_bounds__(kThreads) void collect_kernel(Release a, const int32_t* taken, int32_t* __restrict__ free_ids,
                                                            int n_free, int32_t* taken_out,
                                                            int32_t* __restrict__ status) {
+  __shared__ uint32_t s_marks[kChunk];
+  __shared__ int s_before[kChunk];
+  const int tid = threadIdx.x, words = (a.n_held + 31) / 32, chunks = (words + kChunk - 1) / kChunk;
   const int64_t had = *taken;
+  int over = 0;
+  if (DROP)
+    for (int w = tid; w < words; w += kThreads) s_marks[w] = 0;
   const int bad = scan(0, check_lens(a, had, n_free)).flags;
   if (DROP && !bad) {
-    for (int e = threadIdx.x; e < a.B * a.max_blocks; e += kThreads) {
-      const int r = e / a.max_blocks, j = e - r * a.max_blocks;
-      if (j < blocks_of(a.seq_lens[r])) a.drop(r, j);
+    for (int e = tid; e < a.B * a.max_blocks; e += kThreads) {
+      const int r = e / a.max_blocks, j = e - r * a.max_blocks, b = a.block(r, j);
+      if (j >= blocks_of(a.seq_lens[r]) || b < 0) continue;
+      const int left = atomicSub(a.holds + b, 1);
+      if (left == 0) atomicOr(&s_marks[b >> 5], 1u << (b & 31));
+      if (left < 0) over = kNotHeld;
     }
-    __threadfence();
     __syncthreads();
   }
-  const int words = (a.n_held + 31) / 32, per = (words + kThreads - 1) / kThreads;
-  const int w0 = min(int(threadIdx.x) * per, words), w1 = min(w0 + per, words);
-  auto word = [&](int w) { return __hip_atomic_load(a.marks() + w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
-  auto held = [&](int b) { return __hip_atomic_load(a.holds + b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
-  int count = 0, over = 0;
-  if (!bad)
-    for (int w = w0; w < w1; ++w)
-      for (uint32_t m = word(w); m; m &= m - 1) {
-        ++count;
-        if (held(w * 32 + __builtin_ctz(m)) < -1) over = kNotHeld;
-      }
-  const Sum t = scan(count, over);
-  int refused = bad | t.flags;
-  if (!bad && t.total > had) refused |= kNoBlocks;
-  int64_t at = had - t.total + t.before;
-  if (!bad)
-    for (int w = w0; w < w1; ++w) {
-      const uint32_t all = word(w);
-      if (!all) continue;
-      if (!refused)
-        for (uint32_t m = all; m; m &= m - 1) {
-          const int b = w * 32 + __builtin_ctz(m);
-          a.holds[b] = 0;
-          free_ids[at++] = a.first_id + b;
-        }
-      a.marks()[w] = 0;
+  // Marks of chunk c in LDS, with the number before each word; their number.
+  auto take = [&](int c) -> int {
+    const int n = min(words - c * kChunk, kChunk), per = (n + kThreads - 1) / kThreads;
+    if (!DROP) {
+      for (int w = tid; w < n; w += kThreads) s_marks[w] = a.marks()[c * kChunk + w];
+      __syncthreads();
     }
-  if (threadIdx.x == 0) {
-    *taken_out = int32_t(refused ? had : had - t.total);
+    const int w0 = min(tid * per, n), w1 = min(w0 + per, n);
+    int count = 0;
+    for (int w = w0; w < w1; ++w) count += __popc(s_marks[w]);
+    const Sum t = scan(count, 0);
+    int at = t.before;
+    for (int w = w0; w < w1; ++w) s_before[w] = at, at += __popc(s_marks[w]);
+    __syncthreads();
+    return t.total;
+  };
+  // Every mark of the chunk: f(block, its place).
+  auto each = [&](int c, auto f) {
+    const int n = min(words - c * kChunk, kChunk);
+#pragma unroll 4
+    for (int e = tid; e < n * 32; e += kThreads) {
+      const int w = e >> 5, bit = e & 31;
+      const uint32_t m = s_marks[w];
+      if (m >> bit & 1u) f((c * kChunk + w) * 32 + bit, s_before[w] + __popc(m & ((1u << bit) - 1)));
+    }
+  };
+  int total = 0;
+  if (!bad)
+    for (int c = 0; c < chunks; ++c) {
+      total += take(c);
+      if (!DROP) {
+        each(c, [&](int b, int) { over |= a.holds[b] < -1 ? int(kNotHeld) : 0; });
+        __syncthreads();
+      }
+    }
+  int refused = bad | scan(0, over).flags;
+  if (!bad && total > had) refused |= kNoBlocks;
+  if (!bad) {
+    int64_t at = had - total;
+    for (int c = 0; c < chunks; ++c) {
+      const int n = chunks > 1 ? take(c) : total;
+      if (!refused)
+        each(c, [&](int b, int k) {
+          a.holds[b] = 0;
+          free_ids[at + k] = a.first_id + b;
+        });
+      at += n;
+      if (!DROP) {
+        for (int w = tid; w < min(words - c * kChunk, kChunk); w += kThreads)
+          if (s_marks[w]) a.marks()[c * kChunk + w] = 0;
+        __syncthreads();
+      }
+    }
+  }
+  if (tid == 0) {
+    *taken_out = int32_t(refused ? had : had - total);
     *status = refused;
   }
   if (refused && !bad)  // every hold as it was
     for (int r = 0; r < a.B; ++r) {
       const int n = blocks_of(a.seq_lens[r]);
-      for (int j = threadIdx.x; j < n; j += kThreads) {
+      for (int j = tid; j < n; j += kThreads) {
         const int b = a.block(r, j);
         if (b >= 0) atomicAdd(a.holds + b, 1);
       }
@@ -333,7 +379,7 @@ extern "C" int ilpc_release_shared(const int32_t* block_tables, int32_t max_bloc
     return set_error(ILPC_EINVAL, "%s: NULL pointer", fn);
   hipStream_t s = static_cast<hipStream_t>(stream);
   const Release a{block_tables, max_blocks, B, seq_lens, holds, first_id, num_blocks - first_id};
-  if (int64_t(B) * max_blocks <= kOneRelease) {
+  if (B == 0 || (int64_t(B) * max_blocks <= kOneRelease && a.n_held <= kChunk * 32)) {
     hipLaunchKernelGGL(collect_kernel<true>, dim3(1), dim3(kThreads), 0, s, a, taken, free_ids, n_free, taken_out,
                        status);
     return launch_status(fn);

@@ -138,60 +138,82 @@ __global__ __launch_bounds__(64) void tree_accept_kernel(
   }
 }
 
-// One workgroup a (request, kv head), 32 rows of the path at a time: read, then written,
-// the K row in 16-byte pieces, the V row one dimension a thread (V blocks are
-// dimension-major).
+// One wave a (request, kv head), so that all of a batch's are resident at once; 64 rows of the path
+// at a time, one a lane, with the block table's entries behind the start, one a lane as well; and of
+// the rows that move kMoved at a time read into registers, then written: the K row in 16-byte
+// pieces, the V row one dimension a lane (V blocks are dimension-major).
+constexpr int kMoved = 8;
+
 template <int D>
-__global__ __launch_bounds__(256) void compact_kernel(uint16_t* __restrict__ k_pool, uint16_t* __restrict__ v_pool,
-                                                      int num_blocks, const int32_t* __restrict__ block_tables,
-                                                      int max_blocks, const int32_t* __restrict__ cu_q,
-                                                      const int32_t* __restrict__ start_pos, int n_rows,
-                                                      const int32_t* __restrict__ path,
-                                                      const int32_t* __restrict__ n_accepted, int Hkv) {
-  constexpr int kRows = 32, kPieces = D / 8;
-  __shared__ __attribute__((aligned(16))) uint16_t s_k[kRows][D], s_v[kRows][D];
-  __shared__ int64_t s_src[kRows], s_dst[kRows];  // token's place: block * 16 + offset, or -1
-  const int r = blockIdx.x, h = blockIdx.y, tid = threadIdx.x;
+__global__ __launch_bounds__(64) void compact_kernel(uint16_t* k_pool, uint16_t* v_pool, int num_blocks,
+                                                     const int32_t* __restrict__ block_tables, int max_blocks,
+                                                     const int32_t* __restrict__ cu_q,
+                                                     const int32_t* __restrict__ start_pos, int n_rows,
+                                                     const int32_t* __restrict__ path,
+                                                     const int32_t* __restrict__ n_accepted, int Hkv) {
+  constexpr int kPieces = D / 8, kAtOnce = 64 / kPieces;  // pieces of a K row, rows of K that the lanes take at once
+  const int r = blockIdx.x, h = blockIdx.y, lane = threadIdx.x;
   int q0;
   const int n = rows_of(cu_q, r, n_rows, &q0), start = start_pos[r], count = min(n_accepted[r], n);
   if (start < 0) return;
   const int32_t* bt = block_tables + size_t(r) * max_blocks;
-  auto place = [&](int64_t pos) -> int64_t {
-    const int64_t lb = pos / kBlock;
-    const int id = lb < max_blocks ? bt[lb] : -1;
+  const int lb0 = start / kBlock;
+  const int window = bt[min(lb0 + lane, max_blocks - 1)];
+  auto place = [&](int64_t pos) -> int64_t {  // block * 16 + offset, or -1
+    const int64_t lb = pos / kBlock, w = lb - lb0;
+    const int near = __shfl(window, int(w & 63));
+    const int id = lb >= max_blocks ? -1 : w < 64 ? near : bt[lb];
     return id >= 0 && id < num_blocks ? int64_t(id) * kBlock + pos % kBlock : -1;
   };
-  for (int i0 = 0; i0 < count; i0 += kRows) {
-    const int rows = min(count - i0, kRows);
-    if (tid < kRows) {
-      const int i = i0 + tid, p = tid < rows ? path[q0 + i] : -1;
-      const bool moves = p > i && p < n;
-      s_src[tid] = moves ? place(int64_t(start) + p) : -1;
-      s_dst[tid] = moves ? place(int64_t(start) + i) : -1;
+  for (int i0 = 0; i0 < count; i0 += 64) {
+    const int i = i0 + lane, p = i < count ? path[q0 + i] : -1;
+    const int64_t src = place(int64_t(start) + max(p, 0)), dst = place(int64_t(start) + i);
+    uint64_t moves = __ballot(p > i && p < n && src >= 0 && dst >= 0);
+    while (moves) {
+      const int rows = min(__popcll(moves), kMoved);
+      int row[kMoved];  // lanes of the rows that move now
+#pragma unroll
+      for (int k = 0; k < kMoved; ++k) {
+        row[k] = moves ? __builtin_ctzll(moves) : 0;
+        moves &= moves - 1;
+      }
+      u32x4 kv[kMoved / kAtOnce];
+      int64_t to[kMoved / kAtOnce];
+#pragma unroll
+      for (int k = 0; k < kMoved / kAtOnce; ++k) {
+        int l = row[k * kAtOnce];
+#pragma unroll
+        for (int e = 1; e < kAtOnce; ++e) l = lane / kPieces == e ? row[k * kAtOnce + e] : l;
+        const int64_t s = __shfl(src, l);
+        to[k] = __shfl(dst, l);
+        if (k * kAtOnce + lane / kPieces < rows)
+          kv[k] = *(const u32x4*)(k_pool + ((s / kBlock * Hkv + h) * kBlock + s % kBlock) * D + lane % kPieces * 8);
+      }
+      uint16_t v[kMoved][D / 64];
+#pragma unroll
+      for (int k = 0; k < kMoved; ++k)
+        if (k < rows) {
+          const int64_t s = __shfl(src, row[k]);
+#pragma unroll
+          for (int e = 0; e < D / 64; ++e)
+            v[k][e] = v_pool[((s / kBlock * Hkv + h) * D + e * 64 + lane) * kBlock + s % kBlock];
+        }
+      // all rows have arrived before the first one is written (by other lanes than read it)
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+      for (int k = 0; k < kMoved / kAtOnce; ++k)
+        if (k * kAtOnce + lane / kPieces < rows)
+          *(u32x4*)(k_pool + ((to[k] / kBlock * Hkv + h) * kBlock + to[k] % kBlock) * D + lane % kPieces * 8) = kv[k];
+#pragma unroll
+      for (int k = 0; k < kMoved; ++k)
+        if (k < rows) {
+          const int64_t t = __shfl(dst, row[k]);
+#pragma unroll
+          for (int e = 0; e < D / 64; ++e)
+            v_pool[((t / kBlock * Hkv + h) * D + e * 64 + lane) * kBlock + t % kBlock] = v[k][e];
+        }
+      asm volatile("" ::: "memory");
     }
-    __syncthreads();
-    for (int u = tid; u < rows * kPieces; u += 256) {
-      const int64_t s = s_src[u / kPieces];
-      if (s >= 0)
-        *(u32x4*)&s_k[u / kPieces][u % kPieces * 8] =
-            *(const u32x4*)(k_pool + ((s / kBlock * Hkv + h) * kBlock + s % kBlock) * D + u % kPieces * 8);
-    }
-    for (int u = tid; u < rows * D; u += 256) {
-      const int64_t s = s_src[u / D];
-      if (s >= 0) s_v[u / D][u % D] = v_pool[((s / kBlock * Hkv + h) * D + u % D) * kBlock + s % kBlock];
-    }
-    __syncthreads();
-    for (int u = tid; u < rows * kPieces; u += 256) {
-      const int64_t s = s_src[u / kPieces], t = s_dst[u / kPieces];
-      if (s >= 0 && t >= 0)
-        *(u32x4*)(k_pool + ((t / kBlock * Hkv + h) * kBlock + t % kBlock) * D + u % kPieces * 8) =
-            *(const u32x4*)&s_k[u / kPieces][u % kPieces * 8];
-    }
-    for (int u = tid; u < rows * D; u += 256) {
-      const int64_t s = s_src[u / D], t = s_dst[u / D];
-      if (s >= 0 && t >= 0) v_pool[((t / kBlock * Hkv + h) * D + u % D) * kBlock + t % kBlock] = s_v[u / D][u % D];
-    }
-    __syncthreads();
   }
 }
 
@@ -257,7 +279,7 @@ extern "C" int ilpc_kv_compact(uint16_t* k_pool, uint16_t* v_pool, int32_t num_b
   const dim3 grid{unsigned(B), unsigned(Hkv)};
   hipStream_t s = static_cast<hipStream_t>(stream);
   auto launch = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, k_pool, v_pool, num_blocks, block_tables, max_blocks, cu_q,
+    hipLaunchKernelGGL(kernel, grid, dim3(64), 0, s, k_pool, v_pool, num_blocks, block_tables, max_blocks, cu_q,
                        start_pos, n_rows, path, n_accepted, Hkv);
   };
   if (D == 128) launch(compact_kernel<128>);
