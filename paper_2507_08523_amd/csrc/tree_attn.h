@@ -46,9 +46,9 @@ __device__ __forceinline__ void tree_words(const uint32_t* row, int half_words, 
   *hi = w + 1 < half_words ? row[w + 1] : 0u;
 }
 
-// The kernel for many columns (tree_tiles.hip), kTreeTileCols to a workgroup: a (request, kv
-// head)'s columns in n_ct tiles.
+// The kernel for many columns (tree_tiles.hip): kTreeTileCols to a workgroup, a (request, kv
+// head)'s in n_ct tiles; one or two groups of four waves share a tile's keys.
 constexpr int kTreeTileCols = 128;
-hipError_t launch_tree_tiles(const TreeArgs& a, int n_ct, hipStream_t stream);
+hipError_t launch_tree_tiles(const TreeArgs& a, int groups, int n_ct, hipStream_t stream);
 
 }  // namespace ilpc

@@ -375,7 +375,8 @@ __global__ __launch_bounds__(64 * kJoinWaves) void tree_join_kernel(TreeArgs a, 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // How a launch cuts its work: columns of a tile (32: the kernel above, `waves` of a workgroup to
-// a tile and `groups` workgroups to its keys; kTreeTileCols: tree_tiles.hip), and how many tiles.
+// a tile and `groups` workgroups to its keys; kTreeTileCols: tree_tiles.hip, four waves or eight), and how
+// many tiles.
 struct Plan {
   int cols, waves, groups;
   int64_t n_ct, units;  // column tiles of a (request, kv head), of the batch
@@ -398,7 +399,9 @@ struct Plan {
 //   320, 1200   22.0, 26.9      512, 2000   33.5, 40.4       768, 800    28.4, 22.3     1024, 2000  57.2, 49.7
 //   1024, 300   18.0, 14.8      2048, 2000  124, 76.5        1536, 800   45.8, 40.1     16384, 2050 873, 600
 //   D 64: 768, 1000  18.5, 19.7    800, 700  18.6, 19.3      2048, 1500  51.6, 37.6     3072, 1000  55.5, 47.4
-// of one tile a pair 1024 of 500 keys 48.2, 51.7, of 1000 95.4, 95.9; 2400 of 100 34.0, 39.2.
+// and by two groups of waves where no compute unit has two of those (one group, two): 192 tiles of 128, 1200 keys
+// 29.5, 27.1; 256, 2000 46.2, 42.2; 256, 800 23.3, 23.8; 384, 2000 62.5, 75.7; D 64: 256, 1500 26.7, 22.5.
+// Of one tile a pair 1024 of 500 keys 48.2, 51.7, of 1000 95.4, 95.9; 2400 of 100 34.0, 39.2.
 // Waves for those: 800 (D 64, 700 keys) 2x1 18.6, 4x1 20.3; 1024, 500 4x1 48.2, 2x1 49.1, 1x1 51.2; 2400, 100
 // 1x1 34.0, 2x1 34.5, 4x1 38.5.
 Plan make_plan(int64_t B, int64_t max_q_len, int Hq, int Hkv, int D, int64_t max_blocks) {
@@ -407,7 +410,11 @@ Plan make_plan(int64_t B, int64_t max_q_len, int Hq, int Hkv, int D, int64_t max
   auto cut = [&](int c) -> Plan { return {c, 4, 1, (cols + c - 1) / c, pairs * ((cols + c - 1) / c)}; };
   Plan p = cut(kTileCols);
   const int64_t u = p.units;
-  if (2 * u > (D == 64 ? 7 : 5) * cus && p.n_ct > 1) return cut(kTreeTileCols);
+  if (2 * u > (D == 64 ? 7 : 5) * cus && p.n_ct > 1) {
+    p = cut(kTreeTileCols);
+    if (p.units <= cus && steps >= 32) p.waves = 8;
+    return p;
+  }
   if (u > 3 * cus) {
     p.waves = steps <= 8 ? 1 : 2;
   } else if (2 * u <= cus) {
@@ -496,7 +503,7 @@ extern "C" int ilpc_paged_tree_attn(const uint16_t* q, int64_t q_stride, int32_t
   hipStream_t s = static_cast<hipStream_t>(stream);
   hipError_t e;
   if (plan.cols > kTileCols) {
-    e = launch_tree_tiles(a, n_ct, s);
+    e = launch_tree_tiles(a, plan.waves / 4, n_ct, s);
   } else {
     const int waves = group_waves(plan.waves), per_group = waves / plan.waves;
     const dim3 grid{unsigned((plan.units * plan.groups + per_group - 1) / per_group)}, block{unsigned(64 * waves)};

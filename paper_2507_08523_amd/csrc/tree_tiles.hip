@@ -96,17 +96,22 @@ __device__ __forceinline__ void bare_barrier() {
 
 constexpr int wgs_per_cu(int D) { return D == 64 ? 3 : 2; }
 
-template <int D>
-__global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void tree_tile_kernel(TreeArgs a, int n_ct, int recip) {
+// R groups of four waves work the same columns, each its range of the tiles in buffers of
+// its own, and the first joins their states.
+template <int D, int R>
+__global__ __launch_bounds__(64 * kWaves * R, R == 1 ? wgs_per_cu(D) : 1) void tree_tile_kernel(TreeArgs a, int n_ct,
+                                                                                              int recip) {
   constexpr int kDch = D / 16, kDt = D / 32;  // 16-dimension chunks of a row, 32-row tiles of O^T
   constexpr int kRowBytes = D * 2, kKch = D / 8;
   constexpr int kSlabBytes = kBlock * D * 2, kTileBytes = kTileBlocks * kSlabBytes;
   constexpr int kInsts = kSlabBytes / 1024;
-  __shared__ __attribute__((aligned(16))) uint8_t ring[4 * kTileBytes];  // two K tiles, two V tiles
+  __shared__ __attribute__((aligned(16))) uint8_t rings[R][4 * kTileBytes];  // two K tiles, two V tiles
   __shared__ uint32_t s_any[kMaxHalfWords];  // nodes that some row of the request sees
+  __shared__ float s_ml[kWaves][2][32];      // maxima and sums of the second group
 
   const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int group = __builtin_amdgcn_readfirstlane(tid >> 8), wave = __builtin_amdgcn_readfirstlane(tid >> 6) & (kWaves - 1);
+  uint8_t* ring = rings[group];
   const int n = lane & 31, hh = lane >> 5;
   const int G = a.Hq / a.Hkv;
 
@@ -125,7 +130,9 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void tree_tile_kernel(T
   if (q0 < 0 || q_end > a.n_rows || q_len <= 0 || q_len > L || n_valid <= 0) return;
   const int start = L - q_len;  // the nodes' first key
   const int n_blk = (L + kBlock - 1) / kBlock;
-  const int n_tiles = (L + kKeys - 1) / kKeys;
+  const int all_tiles = (L + kKeys - 1) / kKeys, turns = (all_tiles + R - 1) / R;
+  const int j0 = min(group * turns, all_tiles), n_tiles = min(j0 + turns, all_tiles) - j0;  // tiles j0 .. j0 + n_tiles - 1
+  const int blk0 = j0 * kTileBlocks;
 
   // Columns are split into (node, head of the group) by a 16-bit reciprocal of G, exact for the
   // offsets met here, below G + kCols <= 192.
@@ -139,7 +146,7 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void tree_tile_kernel(T
 
   // A wave loads one pool block of every K tile and of every V tile.  In step u the
   // scores of step u + 1 and the products with V of step u - 1 are taken, so K runs half a
-  // tile ahead and V half a tile behind: K tile j holds the blocks 4j+2 .. 4j+5, V tile j
+  // tile ahead and V half a tile behind: K K tile j holds the range's blocks 4j+2 .. 4j+5, V tile j
   // its blocks 4j-2 .. 4j+1, and both are free at the same barrier; K tile -1 holds the
   // first two blocks.
   uint32_t koff[kInsts];
@@ -170,8 +177,8 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void tree_tile_kernel(T
     else load_slab2(voff, voff, base, to);
   };
 
-  const int first_k = raw_id(max(wave - 2, 0)), id_k0 = raw_id(2 + wave);
-  int next_k = raw_id(kTileBlocks + 2 + wave), next_v = raw_id(2 + wave);  // of tile 1, unchecked
+  const int first_k = raw_id(blk0 + max(wave - 2, 0)), id_k0 = raw_id(blk0 + 2 + wave);
+  int next_k = raw_id(blk0 + kTileBlocks + 2 + wave), next_v = raw_id(blk0 + 2 + wave);  // of tile 1, unchecked
   __builtin_amdgcn_sched_barrier(0);  // (all on their way before the first is looked at)
   bf16x8 qf[kDch];  // Q operand
   {
@@ -183,14 +190,14 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void tree_tile_kernel(T
   if (tid < kMaxHalfWords) s_any[tid] = 0;
   __syncthreads();
   if (wave >= 2) {
-    issue_k(-1, usable(wave - 2, first_k));
-    issue_v(0, usable(wave - 2, first_k));
+    issue_k(-1, usable(blk0 + wave - 2, first_k));
+    issue_v(0, usable(blk0 + wave - 2, first_k));
   } else {
 #pragma unroll
     for (int i = 0; i < kInsts; ++i) *(u32x4*)(ring + v_buf(0) + wave * kSlabBytes + i * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
   }
-  issue_k(0, usable(2 + wave, id_k0));
-  for (int e = tid; e < n_rows * a.half_words; e += 64 * kWaves)
+  issue_k(0, usable(blk0 + 2 + wave, id_k0));
+  for (int e = tid; e < n_rows * a.half_words; e += 64 * kWaves * R)
     atomicOr(&s_any[e % a.half_words], a.masks[size_t(q0) * a.half_words + e]);
 
   f32x16 sA, sB;          // scores of this step and of the next, in turn
@@ -283,8 +290,8 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void tree_tile_kernel(T
   // landed; others read it behind the next barrier): slots that hold no token may have any bits, and
   // a weight of 0 does not hide a NaN.
   auto zero_hidden_v = [&](int j) {
-    const int k0 = j * kKeys + (wave - 2) * kBlock;
-    if (k0 + kBlock <= start) return;
+    const int k0 = (j0 + j) * kKeys + (wave - 2) * kBlock;
+    if (k0 + kBlock <= start || (j == 0 && wave < 2)) return;
     uint32_t lo, hi;
     tree_words(s_any, a.half_words, k0, start, &lo, &hi);
     const uint32_t seen = tree_window(k0, start, L, lo, hi) & 0xFFFFu;
@@ -305,7 +312,7 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void tree_tile_kernel(T
 
   // One step (the first one multiplies weights of 0 with zeros).
   auto body = [&](int u, f32x16& sc, f32x16& sn, bf16x8(&pp)[2], bf16x8(&pc)[2]) __attribute__((always_inline)) {
-    const int j = u >> 1, k0 = u * 32;
+    const int j = u >> 1, k0 = j0 * kKeys + u * 32;
     if (k0 + 32 > start) {
       uint32_t lo, hi;
       tree_words(mask_row, a.half_words, k0, start, &lo, &hi);
@@ -330,9 +337,10 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void tree_tile_kernel(T
   wait_lds();
   bare_barrier();
   if (active) products(no(), no(), yes(), ring, ring + k_buf(-1) + 32 * kRowBytes, sB, sA, pB, pA);
-  for (int j = 0; j < n_tiles; ++j) {
+  for (int j = 0; j < turns; ++j) {
     turn(j);
-    const int kb = (j + 1) * kTileBlocks + 2 + wave, vb = kb - 4;
+    if (j == n_tiles) break;  // (the second range may have a tile fewer)
+    const int kb = blk0 + (j + 1) * kTileBlocks + 2 + wave, vb = kb - 4;
     if (j + 1 < n_tiles) issue_k(j + 1, usable(kb, next_k));
     issue_v(j + 1, usable(vb, next_v));
     next_k = raw_id(kb + kTileBlocks);
@@ -345,10 +353,34 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void tree_tile_kernel(T
     }
   }
   turn(n_tiles);
-  if (active) products(yes(), no(), no(), ring + v_buf(n_tiles), ring, sA, sB, pB, pA);
+  if (active && n_tiles > 0) products(yes(), no(), no(), ring + v_buf(n_tiles), ring, sA, sB, pB, pA);
+  float total = add_across_halves(l);
+  if constexpr (R == 2) {
+    // O as it lies in the lanes, by way of the second group's buffers (behind a barrier: its waves have all left them)
+    __syncthreads();
+    f32x4* so = reinterpret_cast<f32x4*>(rings[1]) + wave * (kDt * 4 * 64) + lane;
+    if (group == 1 && active) {
+#pragma unroll
+      for (int i = 0; i < kDt * 4; ++i) {
+        const f32x16& x = o[i >> 2];
+        so[i * 64] = f32x4{x[(i & 3) * 4], x[(i & 3) * 4 + 1], x[(i & 3) * 4 + 2], x[(i & 3) * 4 + 3]};
+      }
+      if (hh == 0) s_ml[wave][0][n] = m, s_ml[wave][1][n] = total;
+    }
+    __syncthreads();
+    if (group == 1 || !active) return;
+    const float m1 = s_ml[wave][0][n], top = fmaxf(m, m1);
+    const float w0 = __builtin_amdgcn_exp2f(m - top), w1 = __builtin_amdgcn_exp2f(m1 - top);
+    total = total * w0 + s_ml[wave][1][n] * w1;
+#pragma unroll
+    for (int i = 0; i < kDt * 4; ++i) {
+      const f32x4 v = so[i * 64];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[i >> 2][(i & 3) * 4 + e] = o[i >> 2][(i & 3) * 4 + e] * w0 + v[e] * w1;
+    }
+  }
   if (!active) return;
 
-  const float total = add_across_halves(l);
   const float inv = total > 0.f ? 1.f / total : 0.f;
   // The rows leave through LDS, so that whole 128-byte half rows are stored (a lane
   // holds 8-byte pieces of one row).  4 KiB a wave, where K was, which every wave has left
@@ -386,13 +418,18 @@ __global__ __launch_bounds__(64 * kWaves, wgs_per_cu(D)) void tree_tile_kernel(T
 
 namespace ilpc {
 
-hipError_t launch_tree_tiles(const TreeArgs& a, int n_ct, hipStream_t stream) {
-  const dim3 grid{unsigned(int64_t(a.B) * a.Hkv * n_ct)}, block{64 * kWaves};
+hipError_t launch_tree_tiles(const TreeArgs& a, int groups, int n_ct, hipStream_t stream) {
+  const dim3 grid{unsigned(int64_t(a.B) * a.Hkv * n_ct)}, block{unsigned(64 * kWaves * groups)};
   auto launch = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, grid, block, 0, stream, a, n_ct, 65536 / (a.Hq / a.Hkv) + 1);
   };
-  if (a.D == 128) launch(tree_tile_kernel<128>);
-  else launch(tree_tile_kernel<64>);
+  if (a.D == 128) {
+    if (groups == 1) launch(tree_tile_kernel<128, 1>);
+    else launch(tree_tile_kernel<128, 2>);
+  } else {
+    if (groups == 1) launch(tree_tile_kernel<64, 1>);
+    else launch(tree_tile_kernel<64, 2>);
+  }
   return hipGetLastError();
 }
 

@@ -168,6 +168,54 @@ def test_batch_sizes(B):
     b.check(b.run())
 
 
+def wide(before, nodes, Hq, Hkv, D, two_groups):
+    """The requests again and again, until the kernel for many columns takes the batch: more than 2.5 (D 64:
+    3.5) tiles of 32 columns to a compute unit; with one group of waves, or (contexts of more than 1 K keys,
+    at most one tile of 128 columns to a unit) two."""
+    cus = torch.cuda.get_device_properties(0).multi_processor_count
+    cols = max(nodes) * (Hq // Hkv)
+    t32, t128 = -(-cols // 32), -(-cols // 128)
+    assert t32 > 1
+    need = (7 if D == 64 else 5) * cus // 2 + 1
+    k = -(-need // (len(before) * Hkv * t32))
+    if two_groups:
+        assert k * len(before) * Hkv * t128 <= cus and max(before) >= 1000
+    return dict(before=list(before) * k, nodes=list(nodes) * k, Hq=Hq, Hkv=Hkv, D=D)
+
+
+@pytest.mark.parametrize("heads", [h for h in HEADS if h[0] // h[1] > 1])
+def test_many_columns_head_shapes(heads):
+    Hq, Hkv, D = heads
+    b = trees(**wide([0, 3, 16, 31, 63, 64, 130], [33, 40, 1, 0, 64, 17, 50], Hq, Hkv, D, False), seed=Hq)
+    b.check(b.run())
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n", [17, 32, 33, 63, 64, 65, 130])
+def test_many_columns_node_counts(n, D):
+    b = trees(**wide([48, 0, 200, 61], [n, n, n, n], 8, 2, D, False), seed=n, fused=True)
+    b.check(b.run())
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("P", [0, 1, 15, 16, 31, 33, 47, 48, 49, 63, 64, 65, 95, 96, 127, 128, 129, 1500])
+def test_many_columns_context_lengths(P, D):
+    b = trees(**wide([P], [33], 16, 4, D, False), seed=P, spare_cols=5)
+    b.check(b.run())
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("longest", [1000, 1063, 1064, 1130])
+def test_two_groups_of_waves(D, longest):
+    # contexts of one tile of keys to many, so that the second group has none, as many, or one tile fewer
+    before = [longest, 0, 1, 40, 63, 64, 65, 100, 127, 128, 129, 191, 192, 193, 700]
+    nodes = [64, 64, 63, 24, 1, 64, 63, 28, 64, 64, 0, 64, 5, 63, 64]
+    b = trees(**wide(before, nodes, 32, 4, D, True), seed=longest, fused=True, extra=3)
+    out = b.run()
+    b.check(out)
+    assert (out[-3:] == 7).all()
+
+
 def test_many_long_trees():
     b = trees([700] * 12 + [100] * 4, [64] * 12 + [60, 1, 0, 64], seed=1, Hq=32, Hkv=4)
     b.check(b.run())
@@ -182,7 +230,7 @@ def test_the_largest_trees(n):
 
 
 @pytest.mark.parametrize("D", [64, 128])
-@pytest.mark.parametrize("heads", [(4, 1), (16, 2), (40, 8)])
+@pytest.mark.parametrize("heads", [(4, 1), (16, 2), (40, 8), (256, 8)])
 def test_any_mask_rows_without_a_key_among_them(D, heads):
     rng = np.random.default_rng(D)
     seen = [rng.random((n, n)) < p for n, p in ((40, 0.1), (70, 0.5), (9, 0.0), (33, 1.0), (128, 0.02))]
@@ -196,7 +244,7 @@ def test_any_mask_rows_without_a_key_among_them(D, heads):
             assert (out[cu[0] + 5] == 0).all() and (out[cu[2]:cu[3]] == 0).all() and (out[cu[4] + 100] == 0).all()
 
 
-@pytest.mark.parametrize("heads", [(4, 1, 64), (32, 2, 128)])
+@pytest.mark.parametrize("heads", [(4, 1, 64), (32, 2, 128), (512, 8, 64), (256, 8, 128)])
 def test_nodes_that_no_row_sees_may_hold_anything(heads):
     rng = np.random.default_rng(3)
     seen = [seen_of(random_tree(n, rng)) for n in (20, 70, 140)]
@@ -208,12 +256,14 @@ def test_nodes_that_no_row_sees_may_hold_anything(heads):
 
 
 @pytest.mark.parametrize("std", [128 ** -0.5, 1.0, 4.0, 30.0])
-def test_small_and_large_scores(std):
-    b = trees([700, 40, 5], [40, 40, 40], seed=4, Hq=16, Hkv=2, std=std)
+@pytest.mark.parametrize("Hq", [16, 512])
+def test_small_and_large_scores(std, Hq):
+    b = trees([700, 40, 5], [40, 40, 40], seed=4, Hq=Hq, Hkv=8, std=std)
     b.check(b.run())
 
 
-def test_a_maximum_that_keeps_rising():
+@pytest.mark.parametrize("copies", [1, 330])
+def test_a_maximum_that_keeps_rising(copies):
     # every 32 keys the scores rise by much more than the growth that is let pass
     b = trees([600], [20], seed=5, Hq=4, Hkv=1)
     b.kd[0][:] = (b.kd[0].float() * 0.01).to(torch.bfloat16)
@@ -225,6 +275,12 @@ def test_a_maximum_that_keeps_rising():
         if blk >= 0:
             a, e = 16 * j, min(16 * j + 16, 620)
             b.kp[blk, :, :e - a] = b.kd[0][a:e].permute(1, 0, 2).cuda()
+    if copies > 1:  # (requests that share all their blocks)
+        n = b.q.shape[0]
+        for name in ("kd", "vd", "seen", "new", "before"):
+            setattr(b, name, getattr(b, name) * copies)
+        b.q, b.masks, b.bt, b.L = b.q.repeat(copies, 1, 1), b.masks.repeat(copies, 1), b.bt.repeat(copies, 1), b.L.repeat(copies)
+        b.cu = torch.arange(copies + 1, dtype=torch.int32, device="cuda") * n
     b.check(b.run())
 
 
