@@ -89,6 +89,12 @@ __global__ __launch_bounds__(64 * group_waves(W), 2) void tree_stream_kernel(Tre
   const int32_t* bt = a.block_tables + size_t(r) * a.max_blocks;
   auto load_ids = [&](int window) { return bt[min(window * 64 + lane, a.max_blocks - 1)]; };
   const int q0 = a.cu_q[r], q_end = a.cu_q[r + 1], q_len = q_end - q0, L_in = a.seq_lens[r];
+  // The first 4096 keys' block ids come with the lengths, which say where a range begins.
+  constexpr int kFirst = 5;
+  int first_ids[kFirst];
+#pragma unroll
+  for (int i = 0; i < kFirst; ++i) first_ids[i] = load_ids(i);
+  asm volatile("" : "+v"(first_ids[0]), "+v"(first_ids[1]), "+v"(first_ids[2]), "+v"(first_ids[3]), "+v"(first_ids[4]));
   const int L = min(L_in, a.max_blocks * kBlock);
   const int col0 = ct * kTileCols, n_cols = min(min(q_len, a.max_q_len) * G - col0, kTileCols);
   const bool valid = in_grid && q0 >= 0 && q_end <= a.n_rows && q_len > 0 && q_len <= L && n_cols > 0;
@@ -125,7 +131,15 @@ __global__ __launch_bounds__(64 * group_waves(W), 2) void tree_stream_kernel(Tre
     // request's output is unspecified).
     const int s_first = min(s_begin, n_steps_all - 1);  // (an empty range reads a step that is there, and leaves it)
     int win = (2 * s_first) >> 6;
-    int ids0 = load_ids(win & 1 ? win + 1 : win), ids1 = load_ids(win & 1 ? win : win + 1);
+    int ids0 = first_ids[0], ids1 = first_ids[1];  // of the even and the odd one of windows win, win + 1
+#pragma unroll
+    for (int i = 1; i < kFirst - 1; ++i)
+      if (win == i) (i & 1 ? ids1 : ids0) = first_ids[i], (i & 1 ? ids0 : ids1) = first_ids[i + 1];
+    if (win >= kFirst - 1) {
+      const int x0 = load_ids(win), x1 = load_ids(win + 1);
+      ids0 = win & 1 ? x1 : x0;
+      ids1 = win & 1 ? x0 : x1;
+    }
     auto block_id = [&](int lb) {
       const int id = (win & 1) ? __builtin_amdgcn_readlane(ids1, lb & 63) : __builtin_amdgcn_readlane(ids0, lb & 63);
       return (lb < n_blk && id >= 0 && id < a.num_blocks) ? id : 0;

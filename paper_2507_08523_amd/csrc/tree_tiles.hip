@@ -124,7 +124,16 @@ __global__ __launch_bounds__(64 * kWaves * R, R == 1 ? wgs_per_cu(D) : 1) void t
   const int h = int(pair / unsigned(a.B)), r = int(pair % unsigned(a.B));
   const int32_t* bt = a.block_tables + size_t(r) * a.max_blocks;
   auto raw_id = [&](int blk) { return scalar_load(bt + min(blk, a.max_blocks - 1)); };
-  const int q0 = scalar_load(a.cu_q + r), q_end = scalar_load(a.cu_q + r + 1), L_in = scalar_load(a.seq_lens + r);
+  // Lengths, and where the range is the whole context the block ids of its first tiles, in one round trip.
+  int q0 = scalar_load(a.cu_q + r), q_end = scalar_load(a.cu_q + r + 1), L_in = scalar_load(a.seq_lens + r);
+  int first_k, id_k0, next_k, next_v;  // unchecked; the last two of tile 1
+  auto ask_ids = [&](int blk0) {
+    first_k = raw_id(blk0 + max(wave - 2, 0)), id_k0 = raw_id(blk0 + 2 + wave);
+    next_k = raw_id(blk0 + kTileBlocks + 2 + wave), next_v = id_k0;
+    __builtin_amdgcn_sched_barrier(0);  // (all on their way before the first is looked at)
+  };
+  if constexpr (R == 1) ask_ids(0);
+  asm volatile("" : "+s"(q0), "+s"(q_end), "+s"(L_in));
   const int L = min(L_in, a.max_blocks * kBlock), q_len = q_end - q0, n_rows = min(q_len, a.max_q_len);
   const int first_col = ct * kCols, n_valid = min(n_rows * G - first_col, kCols);
   if (q0 < 0 || q_end > a.n_rows || q_len <= 0 || q_len > L || n_valid <= 0) return;
@@ -177,9 +186,7 @@ __global__ __launch_bounds__(64 * kWaves * R, R == 1 ? wgs_per_cu(D) : 1) void t
     else load_slab2(voff, voff, base, to);
   };
 
-  const int first_k = raw_id(blk0 + max(wave - 2, 0)), id_k0 = raw_id(blk0 + 2 + wave);
-  int next_k = raw_id(blk0 + kTileBlocks + 2 + wave), next_v = raw_id(blk0 + 2 + wave);  // of tile 1, unchecked
-  __builtin_amdgcn_sched_barrier(0);  // (all on their way before the first is looked at)
+  if constexpr (R > 1) ask_ids(blk0);
   bf16x8 qf[kDch];  // Q operand
   {
     const uint16_t* qr = a.q + int64_t(q0 + t) * a.q_stride + size_t(head) * D;
