@@ -378,7 +378,8 @@ extern "C" int ilpc_release_shared(const int32_t* block_tables, int32_t max_bloc
       !taken_out || !status)
     return set_error(ILPC_EINVAL, "%s: NULL pointer", fn);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const Release a{block_tables, max_blocks, B, seq_lens, holds, first_id, num_blocks - first_id};
+  // (without rows there is no block to look at, however many there are)
+  const Release a{block_tables, max_blocks, B, seq_lens, holds, first_id, B ? num_blocks - first_id : 0};
   if (B == 0 || (int64_t(B) * max_blocks <= kOneRelease && a.n_held <= kChunk * 32)) {
     hipLaunchKernelGGL(collect_kernel<true>, dim3(1), dim3(kThreads), 0, s, a, taken, free_ids, n_free, taken_out,
                        status);

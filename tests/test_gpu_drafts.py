@@ -437,6 +437,21 @@ def test_no_request_at_all():
     del z
 
 
+@pytest.mark.parametrize("n", [131072, 131073, 300001])
+def test_no_row_to_release_over_many_blocks(n):
+    bt, e = torch.zeros(0, 4, dtype=torch.int32, device="cuda"), dev([])
+    holds = torch.zeros(ilpc.holds_words(n), dtype=torch.int32, device="cuda")
+    holds[:n] = torch.arange(n, dtype=torch.int32, device="cuda") % 3
+    want = holds.clone()
+    free, out, st = dev([5, 6, 7]), dev([9]), dev([9])
+    ilpc.release_shared(bt, e, holds, 2, free, dev([1]), out, st, n + 2)
+    torch.cuda.synchronize()
+    assert (ints(out), ints(st), ints(free)) == ([1], [0], [5, 6, 7]) and torch.equal(holds, want)
+    ilpc.release_shared(bt, e, holds, 2, free, dev([4]), out, st, n + 2)
+    torch.cuda.synchronize()
+    assert (ints(out), ints(st)) == ([4], [ilpc.BAD_VALUE]) and torch.equal(holds, want)
+
+
 # -- together: decoding by trees, and sampling several answers -----------------------
 
 class Model:
