@@ -361,8 +361,9 @@ class DeviceTables:
                          self.next_tokens, self.kept_lens, self.kept_blocks, root_targets)
         ilpc.release_tables(self.block_tables, self.kept_blocks, self.seq_lens, self.pc.free_ids, self.pc.free_taken,
                             self.cu_blocks, self.pc.free_taken, self.status)
-        # (refused, which no state of this class is, would leave the lengths with their blocks)
-        self.seq_lens.copy_(torch.where(self.status == 0, self.kept_lens, self.seq_lens))
+        # (refused, which no state of this class is, would leave the lengths with their blocks; a row
+        # that was released meanwhile, or accepted shorter, does not get its tokens back)
+        self.seq_lens.copy_(torch.where(self.status == 0, torch.minimum(self.kept_lens, self.seq_lens), self.seq_lens))
         return self.path, self.n_accepted, self.next_tokens
 
     def fork(self, sources):

@@ -573,6 +573,32 @@ def test_speculative_decoding_leaves_the_cache_of_plain_decoding(captured, share
     assert ints(pc.free_taken) == [0] and ints(tab.seq_lens) == [0] * B
 
 
+@pytest.mark.parametrize("shared", [False, True])
+def test_accept_gives_no_row_tokens_that_it_has_not(shared):
+    pc = pipeline.PagedPrefixCache(1, 64, 4, 8, 3, 8, spare_blocks=30)
+    tab = pipeline.DeviceTables(pc, np.full((3, 8), -1, np.int32), [0, 0, 0], 60, max_nodes=20, shared=shared)
+    chain = list(range(-1, 19)) * 3
+    par, tok, all_of, none = dev(chain), dev([3] * 60), dev([3] * 60), dev([4] * 60)
+    tab.extend(dev([20, 20, 20]), 20)
+    tab.release(dev([0, 1, 0]))
+    # a request released before the draft is decided stays released
+    tab.accept(par, tok, all_of)
+    torch.cuda.synchronize()
+    assert ints(tab.n_accepted) == [20] * 3 and ints(tab.seq_lens) == [20, 0, 20] and ints(pc.free_taken) == [4]
+    # decided again: fewer, and then more than are left
+    for picks in (none, all_of):
+        tab.accept(par, tok, picks)
+        torch.cuda.synchronize()
+        assert ints(tab.status) == [0] and ints(tab.seq_lens) == [1, 0, 1] and ints(pc.free_taken) == [2]
+    # an extend that is refused is no draft
+    tab.extend(dev([20, 200, 20]), 200)
+    tab.accept(par, tok, all_of)
+    torch.cuda.synchronize()
+    assert ints(tab.n_accepted) == [0] * 3 and ints(tab.seq_lens) == [1, 0, 1] and ints(pc.free_taken) == [2]
+    rows, taken = ints(tab.block_tables), ints(pc.free_taken)[0]
+    assert sorted([rows[0][0], rows[2][0]] + ints(pc.free_ids)[taken:]) == list(range(4, 34))
+
+
 @pytest.mark.parametrize("lens", [[37, 5], [64, 16], [30, 0]])
 def test_sampling_several_answers_of_each_prompt(lens):
     Hq, Hkv, D, B = 8, 2, 64, 8
