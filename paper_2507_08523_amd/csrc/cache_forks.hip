@@ -334,8 +334,10 @@ int check_sizes(const char* fn, int32_t B, int32_t max_blocks, int32_t n_free, i
   return ILPC_OK;
 }
 
-// Most table entries that one workgroup fills, or drops, by itself.
-constexpr int kOneFork = 8192, kOneRelease = 8192;
+// Most table entries that one workgroup fills, or drops, by itself.  us in one launch, in two (a call
+// alone; forks, releases): 368 entries 8, 11 and 7, 11; 2048 8, 11 and 8, 12; 4096 9 to 10, 11 and 9 to 10,
+// 12; 8192 15, 11 and 13, 12 to 13; 16384 22 to 26, 11 and 20, 14; 70656 82, 11 and 69, 25.
+constexpr int kOneFork = 4096, kOneRelease = 4096;
 
 }  // namespace
 

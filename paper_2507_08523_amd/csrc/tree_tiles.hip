@@ -58,9 +58,9 @@ __device__ __forceinline__ void load_slab4(uint32_t o0, uint32_t o1, uint32_t o2
                "global_load_lds_dwordx4 %0, %4\n\t"
                "global_load_lds_dwordx4 %1, %4 offset:1024\n\t"
                "global_load_lds_dwordx4 %2, %4 offset:2048\n\t"
-               "global_load_lds_dwordx4 %3, %4 offset:3072"
+               "global_load_lds_dwordx4 %3, %4 offset:%6"
                :
-               : "v"(o0), "v"(o1), "v"(o2), "v"(o3), "s"(base), "s"(lds)
+               : "v"(o0), "v"(o1), "v"(o2), "v"(o3), "s"(base), "s"(lds), "n"(3 * 1024)
                : "memory", "m0");
 }
 __device__ __forceinline__ void load_slab2(uint32_t o0, uint32_t o1, uint64_t base, uint32_t lds) {

@@ -196,6 +196,34 @@ def test_compact_leaves_out_what_is_not_there():
 
 # -- copies, forks, releases ----------------------------------------------------------
 
+def test_blocks_whose_offsets_pass_32_bits():
+    nb, Hkv, D, n = 264000, 8, 128, 12  # 2^32 elements lie in the first 2^18 blocks
+    big = [torch.empty(nb, Hkv, 16, D, dtype=torch.bfloat16, device="cuda"),
+           torch.empty(nb, Hkv, D, 16, dtype=torch.bfloat16, device="cuda")]
+    small = pools(2 * n, Hkv, D)
+    ids = [nb - 1 - 37 * i for i in range(n)] + [131072 + i for i in range(n)]
+    rows, at = dev([list(range(2 * n))]), torch.tensor(ids, device="cuda")
+    for b, s in zip(big, small):
+        b[at] = s
+    P, nodes = 2 * n * 16 - 100, 60
+    cu, start, path = dev([0, nodes]), dev([P]), dev([2 * i for i in range(30)] + [-1] * 30)
+    masks = torch.zeros(nodes, 1, dtype=torch.int64, device="cuda")
+    ilpc.tree_masks(dev(range(-1, nodes - 1)), cu, masks)
+    for Hq in (8, 256, 512):  # of every kernel
+        q = torch.randn(nodes, Hq, D, device="cuda").to(torch.bfloat16)
+        outs = [torch.zeros_like(q) for _ in range(2)]
+        for o, (kp, vp), table in zip(outs, (big, small), (dev([ids]), rows)):
+            ilpc.paged_tree_attn(q, kp, vp, table, cu, dev([P + nodes]), nodes, D ** -0.5, masks, o)
+        torch.cuda.synchronize()
+        assert same_bits(*outs)
+    for (kp, vp), table in ((big, dev([ids])), (small, rows)):
+        ilpc.kv_compact(kp, vp, table, cu, start, path, dev([30]))
+    ilpc.copy_blocks(*big, dev(ids[:3]), dev(ids[n + 3:n + 6]))
+    ilpc.copy_blocks(*small, dev([0, 1, 2]), dev([n + 3, n + 4, n + 5]))
+    torch.cuda.synchronize()
+    assert all(same_bits(b[at], s) for b, s in zip(big, small))
+
+
 @pytest.mark.parametrize("Hkv,D", [(1, 64), (8, 128), (3, 64), (32, 128)])
 @pytest.mark.parametrize("n", [1, 2, 50])
 def test_copy_blocks(Hkv, D, n):
@@ -293,6 +321,23 @@ def test_forks_and_releases(B, live, hi, first, in_place):
     left = [0 if r in set(ended) else n for r, n in enumerate(s.lens)]
     assert s.release(left, in_place) == 0
     assert s.taken == 0 and sorted(s.free) == list(range(first, s.nb))
+
+
+@pytest.mark.parametrize("B,live,spare", [(20, 6, 300000), (700, 30, 140000)])
+def test_many_counted_blocks(B, live, spare):
+    s = Rows(B, live, 400, 3, spare, B)
+    sources = [r if r < live else r % live for r in range(B)]
+    assert s.fork(sources) == 0
+    assert s.release([n if r % 3 else 0 for r, n in enumerate(s.lens)]) == 0
+    rest = [0 if r % 3 else n for r, n in enumerate(s.lens)]
+    last = s.tables[0][-(-s.lens[0] // 16) - 1]
+    s.tables[0] = list(s.tables[0])
+    s.tables[0][2] = last  # once too often
+    s.d["bt"].copy_(dev(s.tables))
+    assert s.release(rest) == ilpc.NOT_HELD
+    s.tables[0][2] = 1  # (not counted; what stood there stays held)
+    s.d["bt"].copy_(dev(s.tables))
+    assert s.release(rest) == 0 and s.taken <= 1
 
 
 def test_forks_of_forks_and_of_lengths_at_block_ends():
