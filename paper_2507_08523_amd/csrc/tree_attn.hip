@@ -412,7 +412,7 @@ struct Plan {
 // Many tiles are taken 128 columns at a time on LDS tiles, where a pair has more than one of 32 (here, there):
 //   320, 1200   22.0, 26.9      512, 2000   33.5, 40.4       768, 800    28.4, 22.3     1024, 2000  57.2, 49.7
 //   1024, 300   18.0, 14.8      2048, 2000  124, 76.5        1536, 800   45.8, 40.1     16384, 2050 873, 600
-//   D 64: 768, 1000  18.5, 19.7    800, 700  18.6, 19.3      2048, 1500  51.6, 37.6     3072, 1000  55.5, 47.4
+//   D 64: 768, 1000  18.5, 19.7    800, 700  18.6, 19.3      2048, 1500  51.6, 37.6     2816, 1000  50.6, 36.7
 // and by two groups of waves where no compute unit has two of those (one group, two): 192 tiles of 128, 1200 keys
 // 29.5, 27.1; 256, 2000 46.2, 42.2; 256, 800 23.3, 23.8; 384, 2000 62.5, 75.7; D 64: 256, 1500 26.7, 22.5.
 // Of one tile a pair 1024 of 500 keys 48.2, 51.7, of 1000 95.4, 95.9; 2400 of 100 34.0, 39.2.
