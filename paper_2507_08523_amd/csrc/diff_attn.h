@@ -1,5 +1,5 @@
-// What the differential attention kernels share (not part of the ABI; the
-// mathematics is in diff_attn.hip).
+// What the kernels of differential attention share, and those of tree attention with them
+// (not part of the ABI; the mathematics is in diff_attn.hip and tree_attn.hip).
 #pragma once
 
 #include <hip/hip_runtime.h>

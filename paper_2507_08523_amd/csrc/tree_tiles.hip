@@ -9,7 +9,18 @@
 // the exponentials; what overlaps a wave's exponentials with products is the other
 // wave of its SIMD.  Exponentials are taken against the running maximum; where a
 // lane's sum of 16 of them leaves [0, 2^8] the step's maximum is taken and they are
-// taken again (the first step always).
+// taken again (the first step always).  Weights enter the products with V rounded to
+// bf16 (half a step, 2^-8 of each), the sums add the fp32 values.
+//
+// Why 128 columns and LDS: a wave that streams K and V into its registers reads them once for
+// every 32 columns, and the largest batches then wait for the path from L2 (128 requests of
+// 64 nodes behind 2050 keys, 64 heads on 8 of D 128: 873 us; here 590 to 610, 0.91 PFLOP/s).
+// What bounds it there: of the SIMDs' cycles 54% have matrix products and 45% other vector
+// instructions, 23% both, and under that load the clock is at 1.7 GHz, where a large
+// library product reaches 1.23 PFLOP/s.  The order of the operands' reads, how far ahead
+// they are taken (3, 4, 6) and priorities of waves change nothing (606 to 613); 64
+// columns a wave, which halve the reads from LDS, do not fit the registers beside O (740 to
+// 890), nor with O in accumulation registers (657).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -97,7 +108,10 @@ __device__ __forceinline__ void bare_barrier() {
 constexpr int wgs_per_cu(int D) { return D == 64 ? 3 : 2; }
 
 // R groups of four waves work the same columns, each its range of the tiles in buffers of
-// its own, and the first joins their states.
+// its own, and the first joins their states: where a compute unit has one workgroup, a group's
+// barriers and loads are waited for while the other works (32 requests of 12 to 32 nodes behind
+// 570 to 1050 keys, 32 heads on 8: 23.8 us, with 48% of the wave-cycles still waiting; one group
+// 24.5; ranges over workgroups, joined by a kernel of their own, 36).
 template <int D, int R>
 __global__ __launch_bounds__(64 * kWaves * R, R == 1 ? wgs_per_cu(D) : 1) void tree_tile_kernel(TreeArgs a, int n_ct,
                                                                                               int recip) {

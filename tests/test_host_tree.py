@@ -1,6 +1,8 @@
 """What the calls for drafted trees and forked rows refuse (CPU): every argument is checked
 before anything is launched, in the library and in the binding."""
 import ctypes
+import os
+import re
 
 import pytest
 import torch
@@ -111,3 +113,14 @@ def test_binding_takes_only_gpu_tensors():
                  lambda: ilpc.copy_blocks(pool, pool_v, i, i)):
         with pytest.raises(ilpc.ILPCError, match="must be a CUDA/HIP torch tensor"):
             call()
+
+
+def test_the_committed_profile_names_the_current_kernel_code(monkeypatch):
+    import bench
+
+    with open(os.path.join(bench.ROOT, "profiles", "tree_attn_kernel_trace.txt"), encoding="utf-8") as f:
+        named = dict(re.findall(r"^# code of (\w+\.hip): ([0-9a-f]{16})$", f.read(), re.M))
+    assert sorted(named) == ["cache_forks.hip", "tree_attn.hip", "tree_draft.hip", "tree_tiles.hip"]
+    for name, sha in named.items():
+        monkeypatch.setattr(bench, "KERNEL_SRC", os.path.join(bench.ROOT, "paper_2507_08523_amd", "csrc", name))
+        assert bench.kernel_source_sha() == sha, name
