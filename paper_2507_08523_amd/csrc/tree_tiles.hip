@@ -14,7 +14,7 @@
 //
 // Why 128 columns and LDS: a wave that streams K and V into its registers reads them once for
 // every 32 columns, and the largest batches then wait for the path from L2 (128 requests of
-// 64 nodes behind 2050 keys, 64 heads on 8 of D 128: 873 us; here 590 to 610, 0.91 PFLOP/s).
+// 64 nodes behind 2050 keys, 64 heads on 8 of D 128: 873 us; here 584 to 610, 0.91 PFLOP/s).
 // What bounds it there: of the SIMDs' cycles 54% have matrix products and 45% other vector
 // instructions, 23% both, and under that load the clock is at 1.7 GHz, where a large
 // library product reaches 1.23 PFLOP/s.  The order of the operands' reads, how far ahead
@@ -120,7 +120,7 @@ __global__ __launch_bounds__(64 * kWaves * R, R == 1 ? wgs_per_cu(D) : 1) void t
   constexpr int kSlabBytes = kBlock * D * 2, kTileBytes = kTileBlocks * kSlabBytes;
   constexpr int kInsts = kSlabBytes / 1024;
   __shared__ __attribute__((aligned(16))) uint8_t rings[R][4 * kTileBytes];  // two K tiles, two V tiles
-  __shared__ uint32_t s_any[kMaxHalfWords];  // nodes that some row of the request sees
+  __shared__ uint32_t s_any[kMaxHalfWords];  // nodes that some row of the tile sees
   __shared__ float s_ml[kWaves][2][32];      // maxima and sums of the second group
 
   const int tid = threadIdx.x, lane = tid & 63;
@@ -148,13 +148,13 @@ __global__ __launch_bounds__(64 * kWaves * R, R == 1 ? wgs_per_cu(D) : 1) void t
   };
   if constexpr (R == 1) ask_ids(0);
   asm volatile("" : "+s"(q0), "+s"(q_end), "+s"(L_in));
-  const int L = min(L_in, a.max_blocks * kBlock), q_len = q_end - q0, n_rows = min(q_len, a.max_q_len);
-  const int first_col = ct * kCols, n_valid = min(n_rows * G - first_col, kCols);
+  const int L = min(L_in, a.max_blocks * kBlock), q_len = q_end - q0;
+  const int first_col = ct * kCols, n_valid = min(min(q_len, a.max_q_len) * G - first_col, kCols);
   if (q0 < 0 || q_end > a.n_rows || q_len <= 0 || q_len > L || n_valid <= 0) return;
   const int start = L - q_len;  // the nodes' first key
   const int n_blk = (L + kBlock - 1) / kBlock;
-  const int all_tiles = (L + kKeys - 1) / kKeys, turns = (all_tiles + R - 1) / R;
-  const int j0 = min(group * turns, all_tiles), n_tiles = min(j0 + turns, all_tiles) - j0;  // tiles j0 .. j0 + n_tiles - 1
+  const int all_tiles = (L + kKeys - 1) / kKeys, range = (all_tiles + R - 1) / R;
+  const int j0 = min(group * range, all_tiles);  // the range's first tile
   const int blk0 = j0 * kTileBlocks;
 
   // Columns are split into (node, head of the group) by a 16-bit reciprocal of G, exact for the
@@ -169,7 +169,7 @@ __global__ __launch_bounds__(64 * kWaves * R, R == 1 ? wgs_per_cu(D) : 1) void t
 
   // A wave loads one pool block of every K tile and of every V tile.  In step u the
   // scores of step u + 1 and the products with V of step u - 1 are taken, so K runs half a
-  // tile ahead and V half a tile behind: K K tile j holds the range's blocks 4j+2 .. 4j+5, V tile j
+  // tile ahead and V half a tile behind: K tile j holds the range's blocks 4j+2 .. 4j+5, V tile j
   // its blocks 4j-2 .. 4j+1, and both are free at the same barrier; K tile -1 holds the
   // first two blocks.
   uint32_t koff[kInsts];
@@ -207,9 +207,8 @@ __global__ __launch_bounds__(64 * kWaves * R, R == 1 ? wgs_per_cu(D) : 1) void t
 #pragma unroll
     for (int kc = 0; kc < kDch; ++kc) qf[kc] = as_bf16x8(*(const u32x4*)(qr + kc * 16 + hh * 8));
   }
-  // Which nodes some row sees, for V (below).
+  // Which nodes some row of the tile sees: V of the others is zeroed, and keys behind the last are left out (below).
   if (tid < kMaxHalfWords) s_any[tid] = 0;
-  __syncthreads();
   if (wave >= 2) {
     issue_k(-1, usable(blk0 + wave - 2, first_k));
     issue_v(0, usable(blk0 + wave - 2, first_k));
@@ -218,8 +217,16 @@ __global__ __launch_bounds__(64 * kWaves * R, R == 1 ? wgs_per_cu(D) : 1) void t
     for (int i = 0; i < kInsts; ++i) *(u32x4*)(ring + v_buf(0) + wave * kSlabBytes + i * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
   }
   issue_k(0, usable(blk0 + 2 + wave, id_k0));
-  for (int e = tid; e < n_rows * a.half_words; e += 64 * kWaves * R)
-    atomicOr(&s_any[e % a.half_words], a.masks[size_t(q0) * a.half_words + e]);
+  // (a thread takes words of one column of the masks, and adds them to LDS once)
+  const int n_words = (div_g(rem0 + n_valid - 1) + 1) * a.half_words;
+  const int word_step = 64 * kWaves * R / a.half_words * a.half_words;
+  const uint32_t* tile_masks = a.masks + size_t(q0 + t0) * a.half_words;
+  uint32_t any = tid < min(n_words, word_step) ? tile_masks[tid] : 0u;
+  wait_lds();
+  bare_barrier();
+  if (tid < word_step)
+    for (int e = tid + word_step; e < n_words; e += word_step) any |= tile_masks[e];
+  if (any) atomicOr(&s_any[tid % a.half_words], any);
 
   f32x16 sA, sB;          // scores of this step and of the next, in turn
   bf16x8 pA[2], pB[2];    // weights of this step and of the one before, in turn
@@ -357,10 +364,19 @@ __global__ __launch_bounds__(64 * kWaves * R, R == 1 ? wgs_per_cu(D) : 1) void t
   wait_loads();
   wait_lds();
   bare_barrier();
+  // The range's tiles are those up to the last node that these columns' rows see, and a tree's rows see none behind
+  // their own (4 requests of 1000 nodes, 500 keys before them, 32 heads on 8: 180 us with all keys, 115 so; 32 of 198
+  // to 238 behind 370 to 500: 120, 110; the 128 of above: 591, 584).
+  const uint32_t seen = lane < a.half_words ? s_any[lane] : 0u;
+  const uint64_t some = __ballot(seen != 0);
+  const int top = some ? 63 - __builtin_clzll(some) : 0;
+  const uint32_t top_bits = __builtin_amdgcn_readlane(seen, top);
+  const int n_seen = top_bits ? min(top * 32 + 32 - __builtin_clz(top_bits), q_len) : 0;
+  const int seen_tiles = (start + n_seen + kKeys - 1) / kKeys, turns = min(range, seen_tiles);
+  const int n_tiles = max(min(j0 + range, seen_tiles) - j0, 0);
   if (active) products(no(), no(), yes(), ring, ring + k_buf(-1) + 32 * kRowBytes, sB, sA, pB, pA);
-  for (int j = 0; j < turns; ++j) {
+  for (int j = 0; j < n_tiles; ++j) {
     turn(j);
-    if (j == n_tiles) break;  // (the second range may have a tile fewer)
     const int kb = blk0 + (j + 1) * kTileBlocks + 2 + wave, vb = kb - 4;
     if (j + 1 < n_tiles) issue_k(j + 1, usable(kb, next_k));
     issue_v(j + 1, usable(vb, next_v));
@@ -373,6 +389,8 @@ __global__ __launch_bounds__(64 * kWaves * R, R == 1 ? wgs_per_cu(D) : 1) void t
       body(2 * j + 1, sB, sA, pA, pB);
     }
   }
+  if constexpr (R > 1)  // (the second range may have fewer tiles than the first)
+    for (int j = n_tiles; j < turns; ++j) bare_barrier();
   turn(n_tiles);
   if (active && n_tiles > 0) products(yes(), no(), no(), ring + v_buf(n_tiles), ring, sA, sB, pB, pA);
   float total = add_across_halves(l);

@@ -244,6 +244,22 @@ def test_any_mask_rows_without_a_key_among_them(D, heads):
             assert (out[cu[0] + 5] == 0).all() and (out[cu[2]:cu[3]] == 0).all() and (out[cu[4] + 100] == 0).all()
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("two_groups", [False, True])
+def test_tiles_of_columns_whose_rows_see_few_nodes_or_none(D, two_groups):
+    # 128 columns are 16 rows here: of a request's tiles some see nothing, some the first nodes, some late ones alone
+    n = 160
+    seen = np.zeros((n, n), bool)
+    seen[40:70, :3] = seen[70:71, 64] = seen[71:100, 130:] = True
+    seen[100:130] = np.tril(np.ones((n, n), bool))[100:130]
+    seen[150:] = True
+    shape = wide([0, 64, 1000 if two_groups else 700, 1], [n] * 4, 16, 2, D, two_groups)
+    b = Batch(seen=[seen] * len(shape.pop("nodes")), seed=D, **shape)
+    out = b.run()
+    b.check(out)
+    assert (out[:40] == 0).all() and (out[130:150] == 0).all()
+
+
 @pytest.mark.parametrize("heads", [(4, 1, 64), (32, 2, 128), (512, 8, 64), (256, 8, 128)])
 def test_nodes_that_no_row_sees_may_hold_anything(heads):
     rng = np.random.default_rng(3)
