@@ -417,28 +417,39 @@ struct Plan {
 //   128, 3000         8x2 22.3, 4x2 23.5, 4x1 27.5            128, 6000  8x2 30.2, 4x2 33.3, 4x1 47.7
 //   256, 2000         4x1 22.9, 4x2 27.9                      D 64: 32, 1000  8x1 9.0, 4x8 9.8, 4x1 10.0
 //   D 64: 128, 2500   8x1 14.5, 4x4 16.1, 4x1 18.2            D 64: 32, 3000  4x8 10.8, 8x1 14.9
-// Many tiles are taken 128 columns at a time on LDS tiles, where a pair has more than one of 32 (here, there):
-//   320, 1200   22.0, 26.9      512, 2000   33.5, 40.4       768, 800    28.4, 22.3     1024, 2000  57.2, 49.7
-//   1024, 300   18.0, 14.8      2048, 2000  124, 76.5        1536, 800   45.8, 40.1     16384, 2050 873, 600
-//   D 64: 768, 1000  18.5, 19.7    800, 700  18.6, 19.3      2048, 1500  51.6, 37.6     2816, 1000  50.6, 36.7
+// From two tiles of 32 to a compute unit on, and from one on in contexts up to 320 keys, columns are taken 128 at a
+// time on LDS tiles, where a pair has more than one of 32 (here, there; up to two tiles to a unit are resident at once):
+//   280, 150    10.1, 9.8       384, 110    8.9, 7.6         400, 290    11.9, 11.8     400, 490    14.6, 14.5
+//   512, 230    11.9, 10.7      512, 320    12.6, 13.2       512, 2000   32.6, 36.2     400, 2000   30.5, 34.0
+//   520, 70     13.2, 8.8       520, 290    18.4, 12.1       520, 1000   29.7, 23.1     520, 4000   81.5, 59.2
+//   640, 2000   67.6, 61.0      1024, 300   18.0, 14.8       2048, 2000  124, 76.5      16384, 2050 873, 584
+//   D 64: 384, 110  6.2, 6.3     500, 290   8.3, 9.4         768, 110    7.4, 6.5       768, 490    12.1, 11.4
+//   D 64: 520, 740  14.1, 14.8   768, 2000  26.7, 24.8       2048, 1500  51.6, 37.6     2816, 1000  50.6, 36.7
 // and by two groups of waves where no compute unit has two of those (one group, two): 192 tiles of 128, 1200 keys
 // 29.5, 27.1; 256, 2000 46.2, 42.2; 256, 800 23.3, 23.8; 384, 2000 62.5, 75.7; D 64: 256, 1500 26.7, 22.5.
-// Of one tile a pair 1024 of 500 keys 48.2, 51.7, of 1000 95.4, 95.9; 2400 of 100 34.0, 39.2.
-// Waves for those: 800 (D 64, 700 keys) 2x1 18.6, 4x1 20.3; 1024, 500 4x1 48.2, 2x1 49.1, 1x1 51.2; 2400, 100
-// 1x1 34.0, 2x1 34.5, 4x1 38.5.
+// One tile a pair stays here (1024 of 500 keys 48.2, 51.7, of 1000 95.4, 95.9; 2400 of 100 34.0, 39.2), and its waves go by
+// the tiles that a compute unit has at once (waves 1, 2, 4): 280 of 150 keys 12.4, 9.1, 9.6, of 1000 37.3, 26.9, 31.3; 512 of
+// 30 10.6, 7.9, 9.2, of 1000 44.4, 44.6, 43.7; 520 of 300 20.0, 23.1, 21.3, of 2000 107, 127, 112; 768 of 30 11.1, 10.7,
+// 13.7, of 1000 76.4, 78.8, 75.0; 904 of 150 19.1, 18.0, 19.5, of 2000 165, 167, 171; 1024 of 500 51.2, 49.1, 48.2; 2400 of
+// 100 34.0, 34.5, 38.5; D 64: 400 of 150 8.7, 6.4, 6.8; 520 of 1000 28.9, 29.6, 27.5; 900 of 150 9.9, 9.3, 10.4.  Where a pair
+// has more, they share its keys from L2: 384 of 500 23.3, 15.4, 14.0.
 Plan make_plan(int64_t B, int64_t max_q_len, int Hq, int Hkv, int D, int64_t max_blocks) {
   const int64_t cus = ilpc::device_cus(), cols = max_q_len * (Hq / Hkv), pairs = B * Hkv;
   const int64_t steps = (max_blocks * kBlock + kStepKeys - 1) / kStepKeys;
   auto cut = [&](int c) -> Plan { return {c, 4, 1, (cols + c - 1) / c, pairs * ((cols + c - 1) / c)}; };
   Plan p = cut(kTileCols);
   const int64_t u = p.units;
-  if (2 * u > (D == 64 ? 7 : 5) * cus && p.n_ct > 1) {
+  if (p.n_ct > 1 && (u > 2 * cus || (D == 128 && u > cus && steps <= 10))) {
     p = cut(kTreeTileCols);
     if (p.units <= cus && steps >= 32) p.waves = 8;
     return p;
   }
   if (u > 3 * cus) {
-    p.waves = steps <= 8 ? 1 : 2;
+    p.waves = 2;
+  } else if (u > 2 * cus) {
+    p.waves = D == 64 ? 4 : 1;
+  } else if (u > cus) {
+    p.waves = p.n_ct == 1 ? 2 : 4;
   } else if (2 * u <= cus) {
     const int64_t room = std::min<int64_t>(cus / u, kMaxGroups);
     if (room >= 3 && (steps >= 40 || (room >= 16 && steps >= 28)))
@@ -536,8 +547,7 @@ extern "C" int ilpc_paged_tree_attn(const uint16_t* q, int64_t q_stride, int32_t
       else if (plan.waves == 4) launch(tree_stream_kernel<128, 4>);
       else launch(tree_stream_kernel<128, 8>);
     } else {
-      if (plan.waves == 1) launch(tree_stream_kernel<64, 1>);
-      else if (plan.waves == 2) launch(tree_stream_kernel<64, 2>);
+      if (plan.waves == 2) launch(tree_stream_kernel<64, 2>);
       else if (plan.waves == 4) launch(tree_stream_kernel<64, 4>);
       else launch(tree_stream_kernel<64, 8>);
     }

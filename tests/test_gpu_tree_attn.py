@@ -168,9 +168,22 @@ def test_batch_sizes(B):
     b.check(b.run())
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("tiles", [0.6, 1.2, 2.2, 3.2])
+@pytest.mark.parametrize("longest", [40, 700])
+def test_one_tile_of_columns_a_pair(D, tiles, longest):
+    # by tiles of 32 columns to a compute unit
+    cus = torch.cuda.get_device_properties(0).multi_processor_count
+    B = -(-int(tiles * cus) // 8)
+    rng = np.random.default_rng(B)
+    before = [longest] + [int(x) for x in rng.integers(0, longest + 1, B - 1)]
+    b = trees(before, [8] + [int(x) for x in rng.integers(0, 9, B - 1)], seed=B, Hq=32, Hkv=8, D=D, fused=D == 64)
+    b.check(b.run())
+
+
 def wide(before, nodes, Hq, Hkv, D, two_groups):
-    """The requests again and again, until the kernel for many columns takes the batch: more than 2.5 (D 64:
-    3.5) tiles of 32 columns to a compute unit; with one group of waves, or (contexts of more than 1 K keys,
+    """The requests again and again, until the kernel for many columns takes the batch: more than two tiles of 32
+    columns to a compute unit (and well more: 2.5, D 64 3.5); with one group of waves, or (contexts of more than 1 K keys,
     at most one tile of 128 columns to a unit) two."""
     cus = torch.cuda.get_device_properties(0).multi_processor_count
     cols = max(nodes) * (Hq // Hkv)
