@@ -153,7 +153,7 @@ __global__ __launch_bounds__(kFillThreads) void fork_fill_kernel(
 // block (one dropped below that shows that it was given back too often).  Then the marked
 // blocks go back in the order of their ids, which does not depend on the order of the drops.
 // Marks are the bits of the words behind the counts, zero between calls.  448 rows of 64 to
-// 138 blocks that end together: 6.3 us to drop, by atomics on the same blocks' counts, and 5.2 to
+// 138 blocks that end together: 5.2 to 5.8 us to drop, by atomics on the same blocks' counts, and 5.2 to
 // collect; 12 rows of up to 38 blocks in one launch 4.7.
 
 struct Release {
@@ -171,6 +171,8 @@ struct Release {
   __device__ __forceinline__ void drop(int b) const {
     if (b >= 0 && atomicSub(holds + b, 1) == 0) atomicOr(marks() + (b >> 5), 1u << (b & 31));
   }
+  // entries of row r that drop a hold
+  __device__ __forceinline__ int entries(int r) const { return min(blocks_of(max(seq_lens[r], 0)), max_blocks); }
   __device__ __forceinline__ int bad_len(int r) const {
     const int len = seq_lens[r];
     return len < 0 ? kBadValue : len > int64_t(max_blocks) * kBlock ? kTooLong : 0;
@@ -184,25 +186,13 @@ __device__ __forceinline__ int check_lens(const Release& a, int64_t had, int n_f
   return bad;
 }
 
-// (every workgroup checks all lengths: nothing is dropped unless all are right; a row's first
-// entries are on their way meanwhile)
-__global__ __launch_bounds__(kFillThreads) void drop_kernel(Release a, const int32_t* __restrict__ taken, int n_free) {
-  __shared__ int s_bad;
-  const int tid = threadIdx.x;
-  if (tid == 0) s_bad = 0;
-  int r = blockIdx.x, b = a.block(r, min(tid, a.max_blocks - 1)), len = a.seq_lens[r];
-  __syncthreads();
-  const int bad = check_lens(a, *taken, n_free);
-  if (bad) atomicOr(&s_bad, bad);
-  __syncthreads();
-  if (s_bad) return;
-  while (true) {
-    const int n = blocks_of(len);
-    if (tid < n) a.drop(b);
-    for (int j = tid + kFillThreads; j < n; j += kFillThreads) a.drop(a.block(r, j));
-    if ((r += gridDim.x) >= a.B) return;
-    len = a.seq_lens[r];
-    b = a.block(r, min(tid, a.max_blocks - 1));
+// Lengths and taken are checked behind it, by the workgroup that collects (which gives the holds back where they are
+// refused), so that a row's length and its first entries are asked for at once.
+__global__ __launch_bounds__(kFillThreads) void drop_kernel(Release a) {
+  for (int r = blockIdx.x; r < a.B; r += gridDim.x) {
+    const int first = a.block(r, min(int(threadIdx.x), a.max_blocks - 1)), n = a.entries(r);
+    if (threadIdx.x < n) a.drop(first);
+    for (int j = threadIdx.x + kFillThreads; j < n; j += kFillThreads) a.drop(a.block(r, j));
   }
 }
 
@@ -260,40 +250,38 @@ __global__ __launch_bounds__(kThreads) void collect_kernel(Release a, const int3
     }
   };
   int total = 0;
-  if (!bad)
-    for (int c = 0; c < chunks; ++c) {
-      total += take(c);
-      if (!DROP) {
-        each(c, [&](int b, int) { over |= a.holds[b] < -1 ? int(kNotHeld) : 0; });
-        __syncthreads();
-      }
+  for (int c = 0; c < chunks; ++c) {
+    total += take(c);
+    if (!DROP) {
+      each(c, [&](int b, int) { over |= a.holds[b] < -1 ? int(kNotHeld) : 0; });
+      __syncthreads();
     }
-  int refused = bad | scan(0, over).flags;
-  if (!bad && total > had) refused |= kNoBlocks;
-  if (!bad) {
-    int64_t at = had - total;
-    for (int c = 0; c < chunks; ++c) {
-      const int n = chunks > 1 ? take(c) : total;
-      if (!refused)
-        each(c, [&](int b, int k) {
-          a.holds[b] = 0;
-          free_ids[at + k] = a.first_id + b;
-        });
-      at += n;
-      if (!DROP) {
-        for (int w = tid; w < min(words - c * kChunk, kChunk); w += kThreads)
-          if (s_marks[w]) a.marks()[c * kChunk + w] = 0;
-        __syncthreads();
-      }
+  }
+  int refused = scan(0, over).flags;
+  if (total > had) refused |= kNoBlocks;
+  if (bad) refused = bad;  // (what was dropped by such lengths says nothing)
+  int64_t at = had - total;
+  for (int c = 0; c < chunks; ++c) {
+    const int n = chunks > 1 ? take(c) : total;
+    if (!refused)
+      each(c, [&](int b, int k) {
+        a.holds[b] = 0;
+        free_ids[at + k] = a.first_id + b;
+      });
+    at += n;
+    if (!DROP) {
+      for (int w = tid; w < min(words - c * kChunk, kChunk); w += kThreads)
+        if (s_marks[w]) a.marks()[c * kChunk + w] = 0;
+      __syncthreads();
     }
   }
   if (tid == 0) {
     *taken_out = int32_t(refused ? had : had - total);
     *status = refused;
   }
-  if (refused && !bad)  // every hold as it was
+  if (refused && !(DROP && bad))  // every hold as it was
     for (int r = 0; r < a.B; ++r) {
-      const int n = blocks_of(a.seq_lens[r]);
+      const int n = a.entries(r);
       for (int j = tid; j < n; j += kThreads) {
         const int b = a.block(r, j);
         if (b >= 0) atomicAdd(a.holds + b, 1);
@@ -394,7 +382,7 @@ extern "C" int ilpc_release_shared(const int32_t* block_tables, int32_t max_bloc
                        status);
     return launch_status(fn);
   }
-  hipLaunchKernelGGL(drop_kernel, dim3(unsigned(std::min(B, 1024))), dim3(kFillThreads), 0, s, a, taken, n_free);
+  hipLaunchKernelGGL(drop_kernel, dim3(unsigned(std::min(B, 1024))), dim3(kFillThreads), 0, s, a);
   const int rc1 = launch_status(fn);
   if (rc1 != ILPC_OK) return rc1;
   hipLaunchKernelGGL(collect_kernel<false>, dim3(1), dim3(kThreads), 0, s, a, taken, free_ids, n_free, taken_out,
