@@ -417,8 +417,9 @@ struct Plan {
 //   128, 3000         8x2 22.3, 4x2 23.5, 4x1 27.5            128, 6000  8x2 30.2, 4x2 33.3, 4x1 47.7
 //   256, 2000         4x1 22.9, 4x2 27.9                      D 64: 32, 1000  8x1 9.0, 4x8 9.8, 4x1 10.0
 //   D 64: 128, 2500   8x1 14.5, 4x4 16.1, 4x1 18.2            D 64: 32, 3000  4x8 10.8, 8x1 14.9
-// From two tiles of 32 to a compute unit on, and from one on in contexts up to 320 keys, columns are taken 128 at a
-// time on LDS tiles, where a pair has more than one of 32 (here, there; up to two tiles to a unit are resident at once):
+// A compute unit holds two workgroups of the kernel above.  From more than two tiles of 32 to a unit on, and in
+// contexts up to 320 keys from more than one (D 128), columns are taken 128 at a time on LDS tiles, where a pair has
+// more than one tile of 32 (here, there):
 //   280, 150    10.1, 9.8       384, 110    8.9, 7.6         400, 290    11.9, 11.8     400, 490    14.6, 14.5
 //   512, 230    11.9, 10.7      512, 320    12.6, 13.2       512, 2000   32.6, 36.2     400, 2000   30.5, 34.0
 //   520, 70     13.2, 8.8       520, 290    18.4, 12.1       520, 1000   29.7, 23.1     520, 4000   81.5, 59.2
@@ -427,12 +428,13 @@ struct Plan {
 //   D 64: 520, 740  14.1, 14.8   768, 2000  26.7, 24.8       2048, 1500  51.6, 37.6     2816, 1000  50.6, 36.7
 // and by two groups of waves where no compute unit has two of those (one group, two): 192 tiles of 128, 1200 keys
 // 29.5, 27.1; 256, 2000 46.2, 42.2; 256, 800 23.3, 23.8; 384, 2000 62.5, 75.7; D 64: 256, 1500 26.7, 22.5.
-// One tile a pair stays here (1024 of 500 keys 48.2, 51.7, of 1000 95.4, 95.9; 2400 of 100 34.0, 39.2), and its waves go by
-// the tiles that a compute unit has at once (waves 1, 2, 4): 280 of 150 keys 12.4, 9.1, 9.6, of 1000 37.3, 26.9, 31.3; 512 of
-// 30 10.6, 7.9, 9.2, of 1000 44.4, 44.6, 43.7; 520 of 300 20.0, 23.1, 21.3, of 2000 107, 127, 112; 768 of 30 11.1, 10.7,
-// 13.7, of 1000 76.4, 78.8, 75.0; 904 of 150 19.1, 18.0, 19.5, of 2000 165, 167, 171; 1024 of 500 51.2, 49.1, 48.2; 2400 of
-// 100 34.0, 34.5, 38.5; D 64: 400 of 150 8.7, 6.4, 6.8; 520 of 1000 28.9, 29.6, 27.5; 900 of 150 9.9, 9.3, 10.4.  Where a pair
-// has more, they share its keys from L2: 384 of 500 23.3, 15.4, 14.0.
+// One tile a pair stays here: 1024 of 500 keys 48.2, 51.7, of 1000 95.4, 95.9; 2400 of 100 34.0, 39.2.  Its waves go by
+// how many of its workgroups a unit gets (1, 2, 4 waves):
+//   280, 150    12.4, 9.1, 9.6    280, 1000  37.3, 26.9, 31.3    512, 30    10.6, 7.9, 9.2     512, 1000  44.4, 44.6, 43.7
+//   520, 300    20.0, 23.1, 21.3  520, 2000  107, 127, 112       768, 30    11.1, 10.7, 13.7   768, 1000  76.4, 78.8, 75.0
+//   904, 150    19.1, 18.0, 19.5  904, 2000  165, 167, 171       1024, 500  51.2, 49.1, 48.2   2400, 100  34.0, 34.5, 38.5
+//   D 64: 400, 150  8.7, 6.4, 6.8     520, 1000  28.9, 29.6, 27.5     900, 150  9.9, 9.3, 10.4
+// Where a pair has more tiles, they share its keys from L2: 384 of 500 keys 23.3, 15.4, 14.0.
 Plan make_plan(int64_t B, int64_t max_q_len, int Hq, int Hkv, int D, int64_t max_blocks) {
   const int64_t cus = ilpc::device_cus(), cols = max_q_len * (Hq / Hkv), pairs = B * Hkv;
   const int64_t steps = (max_blocks * kBlock + kStepKeys - 1) / kStepKeys;
