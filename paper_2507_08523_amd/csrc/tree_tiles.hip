@@ -16,11 +16,12 @@
 // every 32 columns, and the largest batches then wait for the path from L2 (128 requests of
 // 64 nodes behind 2050 keys, 64 heads on 8 of D 128: 873 us; here 584 to 610, 0.91 PFLOP/s).
 // What bounds it there: of the SIMDs' cycles 54% have matrix products and 45% other vector
-// instructions, 23% both, and under that load the clock is at 1.7 GHz, where a large
-// library product reaches 1.23 PFLOP/s.  The order of the operands' reads, how far ahead
-// they are taken (3, 4, 6) and priorities of waves change nothing (606 to 613); 64
-// columns a wave, which halve the reads from LDS, do not fit the registers beside O (740 to
-// 890), nor with O in accumulation registers (657).
+// instructions, 23% both, and under that load the clock falls to 1.5 to 1.7 GHz, so that the
+// products alone, without exponentials and with operands that stay in registers, still take
+// 530 us (a large library product reaches 1.23 PFLOP/s).  The order of the operands' reads,
+// how far ahead they are taken (3, 4, 6) and priorities of waves change nothing (606 to
+// 613); 64 columns a wave, which halve the reads from LDS, do not fit the registers beside O
+// (740 to 890), nor with O in accumulation registers (657).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
