@@ -111,7 +111,7 @@ constexpr int wgs_per_cu(int D) { return D == 64 ? 3 : 2; }
 // R groups of four waves work the same columns, each its range of the tiles in buffers of
 // its own, and the first joins their states: where a compute unit has one workgroup, a group's
 // barriers and loads are waited for while the other works (32 requests of 12 to 32 nodes behind
-// 570 to 1050 keys, 32 heads on 8: 23.8 us, with 48% of the wave-cycles still waiting; one group
+// 570 to 1050 keys, 32 heads on 8: 23.3 us, with 48% of the wave-cycles still waiting; one group
 // 24.5; ranges over workgroups, joined by a kernel of their own, 36).
 template <int D, int R>
 __global__ __launch_bounds__(64 * kWaves * R, R == 1 ? wgs_per_cu(D) : 1) void tree_tile_kernel(TreeArgs a, int n_ct,
