@@ -278,9 +278,9 @@ class DeviceTables:
     blocks of ended requests back.  Calls are ordered on one stream; batches
     that share ``pc`` share its free list and that order.
 
-    ``status`` (device, 1 value) holds what the last extend, accept, fork or release
-    refused (0: nothing): a refused extend changes nothing, and the append and
-    attention queued behind it do nothing.
+    ``status`` (device, 1 value) holds what the last extend, fork or release refused
+    (0: nothing), and what accepts behind it did: a refused extend changes nothing, and
+    the append, attention and accept queued behind it do nothing.
 
     A step of speculative decoding (``max_nodes`` > 0) extends by drafted tokens, a tree
     a request: ``tree`` makes the masks that ``pc.attend_tree`` reads, ``accept`` keeps
@@ -317,6 +317,7 @@ class DeviceTables:
             self.positions, self.path = empty(self.max_rows), empty(self.max_rows).fill_(-1)
             self.n_accepted, self.next_tokens = empty(self.B), empty(self.B)
             self.kept_lens, self.kept_blocks = empty(self.B), empty(self.B)
+            self._accept_status = empty(1)
         if self.shared:
             self.copy_src, self.copy_dst = empty(self.B).fill_(-1), empty(self.B).fill_(-1)
 
@@ -353,17 +354,21 @@ class DeviceTables:
         """Of the last extend's drafted tokens the path that the target's picks confirm stays
         (ilpc.tree_accept; all device int32 [max_rows], root_targets [B]): ``path``, ``n_accepted`` and
         ``next_tokens`` say which and what follows, the lengths end behind it, and blocks that it does
-        not reach are free again.  ``pc.compact`` then moves the K/V rows."""
+        not reach are free again.  ``pc.compact`` then moves the K/V rows.  ``status`` keeps the bits of
+        a refused extend, whose batch has no draft (``n_accepted`` 0)."""
         import torch
 
         self._draft("accept")
         ilpc.tree_accept(parents, tokens, targets, self.cu_q, self.start_pos, self.path, self.n_accepted,
                          self.next_tokens, self.kept_lens, self.kept_blocks, root_targets)
+        own = self._accept_status
         ilpc.release_tables(self.block_tables, self.kept_blocks, self.seq_lens, self.pc.free_ids, self.pc.free_taken,
-                            self.cu_blocks, self.pc.free_taken, self.status)
+                            self.cu_blocks, self.pc.free_taken, own)
         # (refused, which no state of this class is, would leave the lengths with their blocks; a row
         # that was released meanwhile, or accepted shorter, does not get its tokens back)
-        self.seq_lens.copy_(torch.where(self.status == 0, torch.minimum(self.kept_lens, self.seq_lens), self.seq_lens))
+        torch.where(own == 0, torch.minimum(self.kept_lens, self.seq_lens), self.seq_lens, out=self.seq_lens)
+        # (beside the extend's bits, which one read a step has to show)
+        self.status.bitwise_or_(own)
         return self.path, self.n_accepted, self.next_tokens
 
     def fork(self, sources):

@@ -761,3 +761,59 @@ def test_captured_calls_follow_their_inputs(case):
         g.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, calls()))
+
+
+@pytest.mark.parametrize("captured", [False, True])
+@pytest.mark.parametrize("shared", [False, True])
+@pytest.mark.parametrize("rooted", [False, True])
+def test_accept_leaves_a_refused_extend_to_be_read(captured, shared, rooted):
+    # one read a step has to tell a refused extend from a draft of which nothing was accepted
+    pc = pipeline.PagedPrefixCache(1, 64, 4, 8, 2, 8, spare_blocks=12)
+    tab = pipeline.DeviceTables(pc, np.full((2, 8), -1, np.int32), [0, 0], 60, max_nodes=20, shared=shared)
+    new, par, tok, pick = dev([0, 0]), dev(list(range(-1, 29)) * 2), dev([3] * 60), dev([3] * 60)
+    root = dev([3, 3]) if rooted else None
+
+    def step():
+        tab.extend(new, 20)
+        tab.accept(par, tok, pick, root)
+
+    step()
+    torch.cuda.synchronize()
+    if captured:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step()
+    # refused: a request past its table, more rows than there are, no block left
+    for lens, bit, after in (([9, 12], 0, [9, 12]),
+                             ([200, 1], ilpc.NO_BLOCKS | ilpc.TOO_LONG | ilpc.TOO_MANY_ROWS, [9, 12]),
+                             ([1, 9], 0, [10, 21]), ([31, 30], ilpc.TOO_MANY_ROWS, [10, 21]), ([0, 0], 0, [10, 21]),
+                             ([-1, 3], ilpc.BAD_VALUE, [10, 21]), ([4, 0], 0, [14, 21])):
+        new.copy_(dev(lens))
+        p = sum((list(range(-1, max(n, 0) - 1)) for n in lens), [])[:60]
+        par[:len(p)] = dev(p)
+        graph.replay() if captured else step()
+        torch.cuda.synchronize()
+        assert ints(tab.status) == [bit] and ints(tab.seq_lens) == after, lens
+        if bit:
+            assert ints(tab.n_accepted) == [0, 0]
+    pc.free_ids = pc.free_ids[:3]
+    if not captured:
+        new.copy_(dev([20, 20]))
+        step()
+        torch.cuda.synchronize()
+        assert ints(tab.status) == [ilpc.NO_BLOCKS] and ints(tab.seq_lens) == [14, 21]
+
+
+def test_what_accept_itself_refuses_is_added():
+    pc = pipeline.PagedPrefixCache(1, 64, 4, 8, 1, 8, spare_blocks=12)
+    tab = pipeline.DeviceTables(pc, np.full((1, 8), -1, np.int32), [0], 60, max_nodes=20)
+    tab.extend(dev([20]), 20)
+    pc.free_taken.fill_(0)  # (not by any call of the class)
+    par, tok, none = dev(list(range(-1, 59))), dev([3] * 60), dev([4] * 60)
+    tab.accept(par, tok, none)
+    torch.cuda.synchronize()
+    assert ints(tab.status) == [ilpc.NO_BLOCKS] and ints(tab.seq_lens) == [20] and ints(pc.free_taken) == [0]
+    pc.free_taken.fill_(2)
+    tab.extend(dev([0]), 20)
+    torch.cuda.synchronize()
+    assert ints(tab.status) == [0] and ints(tab.seq_lens) == [20]
