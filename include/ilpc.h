@@ -634,7 +634,9 @@ int ilpc_paged_tree_attn(const uint16_t* q, int64_t q_stride, int32_t n_rows, co
  *              node of parent -1 has to be.  NULL: node 0 (parent -1) is the root,
  *              a token already decided, accepted whatever it is; other nodes of
  *              parent -1 are not.
- * start_pos    [device] int32 [B]  tokens before the nodes
+ * start_pos    [device] int32 [B]  tokens before the nodes.  Negative: the request has no
+ *              draft (any more): nothing is accepted, and kept_lens and kept_blocks are
+ *              INT32_MAX, which cuts nothing
  * path         [device] int32 [n_rows]  out: the accepted nodes of request r at
  *              cu_q[r] .., ascending, then -1; rows of no request stay as they are
  * n_accepted   [device] int32 [B]  out
@@ -658,8 +660,8 @@ int ilpc_tree_accept(const int32_t* parents, const int32_t* tokens, const int32_
  * so that path[cu_q[r] + i] >= i).  In place, every row as it was before the call;
  * rows that no accepted one goes to stay as they are.  The blocks written are held by
  * this request alone.  Entries of path outside [i, q_len_r), blocks outside
- * [0, num_blocks) and positions past 16 * max_blocks are left out.  Hkv <= 65535,
- * max_blocks <= 2^24 (ILPC_EUNSUP).
+ * [0, num_blocks), positions past 16 * max_blocks and requests with start_pos[r] < 0 (no draft) are left
+ * out.  Hkv <= 65535, max_blocks <= 2^24 (ILPC_EUNSUP).
  */
 int ilpc_kv_compact(uint16_t* k_pool, uint16_t* v_pool, int32_t num_blocks, const int32_t* block_tables,
                     int32_t max_blocks, const int32_t* cu_q, const int32_t* start_pos, int32_t B, int32_t n_rows,
@@ -697,7 +699,9 @@ int ilpc_holds_words(int32_t n_blocks, int32_t* words);
  *              nothing is changed, and the copies are -1
  *
  * A shared block is full and stays so: no row may be cut back below the length it
- * was forked at.  Limits as for ilpc_extend_tables.  Outputs must not overlap other
+ * was forked at, nor its rows below that moved: a draft that was open when its row was
+ * forked from or over is none any more (start_pos < 0 in ilpc_tree_accept and
+ * ilpc_kv_compact).  Limits as for ilpc_extend_tables.  Outputs must not overlap other
  * arguments (taken_out may be taken).
  */
 int ilpc_fork_tables(int32_t* block_tables, int32_t max_blocks, int32_t B, int32_t* seq_lens, const int32_t* sources,

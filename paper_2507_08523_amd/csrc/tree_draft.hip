@@ -99,7 +99,8 @@ __global__ __launch_bounds__(64) void tree_accept_kernel(
     int32_t* __restrict__ kept_lens, int32_t* __restrict__ kept_blocks) {
   const int r = blockIdx.x, lane = threadIdx.x;
   int q0;
-  const int n = rows_of(cu_q, r, n_rows, &q0), start = start_pos[r];
+  const int rows = rows_of(cu_q, r, n_rows, &q0), start = start_pos[r];
+  const int n = start < 0 ? 0 : rows;  // (no draft: nothing is accepted, and nothing cut)
   int want = root_targets ? root_targets[r] : -1, cur = -1, count = 0;
   bool any_token = !root_targets;  // of the root: node 0, whatever its token
   for (int b0 = 0; b0 < n; b0 += 64 * kAhead) {
@@ -131,12 +132,12 @@ __global__ __launch_bounds__(64) void tree_accept_kernel(
     }
     if (any_token) break;
   }
-  for (int i = count + lane; i < n; i += 64) path[q0 + i] = -1;
+  for (int i = count + lane; i < rows; i += 64) path[q0 + i] = -1;
   if (lane == 0) {
     n_accepted[r] = count;
     next_tokens[r] = want;
-    kept_lens[r] = start + count;
-    kept_blocks[r] = (start + count + kBlock - 1) / kBlock;
+    kept_lens[r] = start < 0 ? INT32_MAX : start + count;
+    kept_blocks[r] = start < 0 ? INT32_MAX : (start + count + kBlock - 1) / kBlock;
   }
 }
 

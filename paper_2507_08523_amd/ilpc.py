@@ -938,8 +938,8 @@ def tree_accept(parents, tokens, targets, cu_q, start_pos, path, n_accepted, nex
     """The path of drafted nodes that the target's picks confirm (see the C header).
 
     int32 device tensors: parents, tokens, targets (the pick behind each node) [rows],
-    cu_q [B+1], start_pos [B], root_targets [B] (the pick behind the context) or
-    None (node 0 is the root, accepted as it is).  Out: path [rows], n_accepted,
+    cu_q [B+1], start_pos [B] (negative: no draft), root_targets [B] (the pick behind the
+    context) or None (node 0 is the root, accepted as it is).  Out: path [rows], n_accepted,
     next_tokens, kept_lens, kept_blocks [B].
     """
     rc = (_binding or _native()).tree_accept(parents, tokens, targets, cu_q, start_pos, path, n_accepted, next_tokens,

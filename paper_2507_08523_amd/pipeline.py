@@ -318,6 +318,7 @@ class DeviceTables:
             self.n_accepted, self.next_tokens = empty(self.B), empty(self.B)
             self.kept_lens, self.kept_blocks = empty(self.B), empty(self.B)
             self._accept_status = empty(1)
+            self._row_ids = dev(np.arange(self.B))
         if self.shared:
             self.copy_src, self.copy_dst = empty(self.B).fill_(-1), empty(self.B).fill_(-1)
 
@@ -325,7 +326,7 @@ class DeviceTables:
         """Every request r gets new_lens[r] (device int32, at most max_new) tokens.
 
         The rows of the returned batch are the new tokens', in request order,
-        ``max_rows`` at most; its views hold until the next extend or release."""
+        ``max_rows`` at most; its views hold until the next extend, fork or release."""
         import torch
 
         torch.add(self.seq_lens, 0, out=self.start_pos)
@@ -374,12 +375,24 @@ class DeviceTables:
     def fork(self, sources):
         """Row r holds row sources[r]'s tokens from now on, where that is another row (device int32
         [B]; rows forked from name themselves, as do those that stay; what a fork's row held has
-        been released).  Returns the block pairs that ``pc.copy_blocks`` copies, in every layer."""
+        been released).  Returns the block pairs that ``pc.copy_blocks`` copies, in every layer.
+
+        Rows forked from and rows forked over have no draft from then on: they keep all the tokens that they
+        hold, and accept finds nothing of them (``n_accepted`` 0)."""
+        import torch
+
         if not self.shared:
             raise ilpc.ILPCError(ilpc.EINVAL, "fork: DeviceTables was made without shared")
         pc = self.pc
         ilpc.fork_tables(self.block_tables, self.seq_lens, sources, pc.holds, pc.num_blocks, pc.free_ids,
                          pc.free_taken, self.copy_src, self.copy_dst, pc.free_taken, self.status, pc.k_pool.shape[0])
+        if self.max_nodes > 0:
+            # The blocks of an open draft may be other rows' as well now, or the draft that of a row that was here
+            # before: a path must neither cut nor move them.  (Index B: rows that stay, or a refused fork's.)
+            forks = (sources != self._row_ids) & (self.status == 0)
+            ended = torch.zeros(self.B + 1, dtype=torch.bool, device=pc.device)
+            ended.scatter_(0, torch.where(forks, sources, self.B).long(), True)
+            self.start_pos.masked_fill_(ended[:-1] | forks, -1)
         return self.copy_src, self.copy_dst
 
     def release(self, ended):

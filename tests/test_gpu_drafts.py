@@ -817,3 +817,136 @@ def test_what_accept_itself_refuses_is_added():
     tab.extend(dev([0]), 20)
     torch.cuda.synchronize()
     assert ints(tab.status) == [0] and ints(tab.seq_lens) == [20]
+
+
+# -- forks beside drafts ---------------------------------------------------------------
+
+def conserved(pc, tab):
+    """Every spare block is free or held by as many rows as its count says."""
+    torch.cuda.synchronize()
+    rows, lens, held = ints(tab.block_tables), ints(tab.seq_lens), {}
+    for row, n in zip(rows, lens):
+        for b in row[:-(-n // 16)]:
+            held[b] = held.get(b, 0) + 1
+    nb, first, taken = pc.k_pool.shape[0], pc.num_blocks, ints(pc.free_taken)[0]
+    assert sorted([b for b in held if b >= first] + ints(pc.free_ids)[taken:]) == list(range(first, nb))
+    assert ints(pc.holds)[:nb - first] == [max(held.get(b, 0) - 1, 0) for b in range(first, nb)]
+
+
+def rows_of_cache(pc, tab, r):
+    at = torch.arange(ints(tab.seq_lens)[r], device="cuda")
+    blk, off = tab.block_tables[r].long()[at // 16], at % 16
+    return pc.k_pool[blk, :, off].clone(), pc.v_pool[blk, :, :, off].clone()
+
+
+def drafting(lens, B=5, N=24):
+    """A table of B rows that hold `lens` tokens, over a cache of random bits."""
+    pc = pipeline.PagedPrefixCache(2, 64, 4, 12, B, 12, spare_blocks=50)
+    for pool, x in zip((pc.k_pool, pc.v_pool), pools(54, 2, 64)):
+        pool.copy_(x)
+    tab = pipeline.DeviceTables(pc, np.full((B, 12), -1, np.int32), [0] * B, B * 40, max_nodes=N, shared=True)
+    tab.extend(dev(lens), 64)
+    return pc, tab, dict(par=dev(list(range(-1, 39)) * B), tok=dev([3] * 40 * B), yes=dev([3] * 40 * B), no=dev([4] * 40 * B))
+
+
+@pytest.mark.parametrize("picks", ["yes", "no"])
+@pytest.mark.parametrize("rooted", [False, True])
+def test_a_fork_ends_the_open_drafts_of_its_rows(picks, rooted):
+    # rows 0 and 1 are forked from while their drafts are open: their blocks are the forks' as well
+    pc, tab, d = drafting([37, 16, 20, 0, 0])
+    new = [24, 24, 21, 0, 0]
+    batch = tab.extend(dev(new), 24)
+    par = dev(sum((list(range(-1, n - 1)) for n in new), []) + [0] * (tab.max_rows - sum(new)))
+    if picks == "yes":  # a path that leaves nodes out: its rows would move
+        par[2:24], par[26:48], par[50:69] = 0, 0, 0
+        pick, tok = dev([7] * tab.max_rows), dev([3] * tab.max_rows)
+        for a, n in zip((0, 24, 48), new):
+            tok[a + n - 1] = 7
+    else:
+        pick, tok = d["no"], d["tok"]
+    pc.copy_blocks(*tab.fork(dev([0, 1, 2, 0, 1])))
+    torch.cuda.synchronize()
+    assert ints(tab.status) == [0]
+    conserved(pc, tab)
+    before = [rows_of_cache(pc, tab, r) for r in (0, 1, 3, 4)]
+    tab.accept(par, tok, pick, dev([3] * 5) if rooted else None)
+    pc.compact(batch, tab.path, tab.n_accepted)
+    torch.cuda.synchronize()
+    n2 = {"yes": 2, "no": 1}[picks]
+    assert ints(tab.status) == [0] and ints(tab.seq_lens) == [61, 40, 20 + n2, 61, 40]
+    assert ints(tab.n_accepted) == [0, 0, n2, 0, 0] and ints(tab.path)[:48] == [-1] * 48
+    assert ints(tab.next_tokens)[3:] == [3 if rooted else -1] * 2
+    conserved(pc, tab)
+    for r, (k, v) in zip((0, 1, 3, 4), before):
+        assert all(same_bits(a, b) for a, b in zip(rows_of_cache(pc, tab, r), (k, v))), r
+    # the next draft of these rows is a draft again
+    tab.extend(dev([20, 20, 0, 20, 0]), 20)
+    chain = dev(list(range(-1, 19)) * 3 + [0] * (tab.max_rows - 60))
+    tab.accept(chain, d["tok"], d["no"])
+    torch.cuda.synchronize()
+    assert ints(tab.status) == [0] and ints(tab.seq_lens) == [62, 41, 20 + n2, 62, 40]
+    conserved(pc, tab)
+
+
+@pytest.mark.parametrize("picks", ["yes", "no"])
+def test_a_row_forked_over_while_its_draft_is_open_keeps_its_sources_tokens(picks):
+    for lens in ([20, 60, 5, 0, 0], [20, 64, 5, 0, 0], [50, 49, 5, 0, 0]):
+        pc, tab, d = drafting(lens)
+        batch = tab.extend(dev([18, 0, 18, 0, 0]), 18)
+        tab.release(dev([1, 0, 0, 0, 0]))
+        pc.copy_blocks(*tab.fork(dev([1, 1, 2, 3, 4])))
+        torch.cuda.synchronize()
+        before = [rows_of_cache(pc, tab, r) for r in (0, 1)]
+        assert all(same_bits(a, b) for a, b in zip(*before))
+        chain = dev(list(range(-1, 17)) * 2 + [0] * (tab.max_rows - 36))
+        tab.accept(chain, d["tok"], d[picks])
+        pc.compact(batch, tab.path, tab.n_accepted)
+        torch.cuda.synchronize()
+        k = 18 if picks == "yes" else 1
+        assert ints(tab.status) == [0] and ints(tab.seq_lens) == [lens[1], lens[1], 5 + k, 0, 0]
+        conserved(pc, tab)
+        for r in (0, 1):
+            assert all(same_bits(a, b) for a, b in zip(rows_of_cache(pc, tab, r), before[r])), r
+        tab.release(dev([1] * 5))
+        torch.cuda.synchronize()
+        assert ints(pc.free_taken) == [0] and not any(ints(pc.holds))
+
+
+def test_a_path_of_before_moves_nothing_in_a_row_forked_over():
+    pc, tab, d = drafting([20, 52, 5, 0, 0])
+    batch = tab.extend(dev([24, 0, 0, 0, 0]), 24)
+    par = dev([-1, 0] + [0] * 21 + [0] + [0] * (tab.max_rows - 24))
+    tok, pick = dev([3] * tab.max_rows), dev([9] * tab.max_rows)
+    tok[23] = 9  # nodes 0 and 23 stay
+    tab.accept(par, tok, pick)
+    tab.release(dev([1, 0, 0, 0, 0]))
+    pc.copy_blocks(*tab.fork(dev([1, 1, 2, 3, 4])))
+    torch.cuda.synchronize()
+    before = [rows_of_cache(pc, tab, r) for r in (0, 1)]
+    pc.compact(batch, tab.path, tab.n_accepted)
+    torch.cuda.synchronize()
+    conserved(pc, tab)
+    for r in (0, 1):
+        assert all(same_bits(a, b) for a, b in zip(rows_of_cache(pc, tab, r), before[r])), r
+
+
+def test_a_refused_fork_ends_no_draft():
+    pc, tab, d = drafting([20, 33, 5, 0, 0])
+    tab.extend(dev([20, 20, 20, 0, 0]), 20)
+    for bad in ([0, 1, 2, 7, 4], [0, 1, 2, -1, 0], [0, 0, 2, 1, 4]):
+        tab.fork(dev(bad))
+        torch.cuda.synchronize()
+        assert ints(tab.status) == [ilpc.BAD_VALUE] and ints(tab.start_pos) == [20, 33, 5, 0, 0]
+    tab.fork(dev([0, 1, 2, 3, 4]))
+    tab.accept(dev(list(range(-1, 19)) * 3 + [0] * (tab.max_rows - 60)), d["tok"], d["no"])
+    torch.cuda.synchronize()
+    assert ints(tab.status) == [0] and ints(tab.seq_lens) == [21, 34, 6, 0, 0] and ints(tab.n_accepted) == [1, 1, 1, 0, 0]
+    conserved(pc, tab)
+
+
+def test_requests_without_a_draft_keep_all():
+    par, tok = [-1, 0, 1, -1, 0], [3] * 5
+    for root, nxt in ((None, [3, -1, -1]), ([3, 8, 9], [3, 8, 9])):
+        got = run_accept(par + [0], tok + [0], tok + [0], [0, 3, 5, 5], [7, -1, -1 << 31], root)
+        most = (1 << 31) - 1
+        assert got == [[0, 1, 2, -1, -1, 9], [3, 0, 0], nxt, [10, most, most], [1, most, most]]
