@@ -560,7 +560,8 @@ int ilpc_paged_diff_attn(const uint16_t* q, int64_t q_stride, int32_t n_rows, co
  * sees, ilpc_paged_tree_attn attends, ilpc_tree_accept finds the nodes that the
  * target model's picks confirm, ilpc_kv_compact moves their K/V rows to the front;
  * blocks behind them go back by ilpc_release_tables (first_block = kept_blocks,
- * seq_lens = the lengths with all nodes).  Rows of request r are cu_q[r] ..
+ * seq_lens = the lengths with all nodes).  No call takes blocks from the free list, copies
+ * them or shares them between the two: moved rows come from blocks that go back.  Rows of request r are cu_q[r] ..
  * cu_q[r+1]-1 in all of them; requests with rows outside [0, n_rows) are taken as
  * having none.  B <= 2^20 (ILPC_EUNSUP).
  */

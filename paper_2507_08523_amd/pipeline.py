@@ -247,8 +247,9 @@ class PagedPrefixCache:
                              batch.max_q_len, scale, masks, out, workspace, stream)
 
     def compact(self, batch: DeviceBatch, path, n_accepted, stream=None):
-        """K/V rows of a draft's accepted nodes to its front, before the next extend on this cache
-        (DeviceTables.accept's path; in every layer's pools)."""
+        """K/V rows of a draft's accepted nodes to its front (DeviceTables.accept's path; in every layer's
+        pools).  Rows come from blocks that accept has given back as well, so that every layer's compact is
+        queued before the next extend, fork, copy_blocks or release of any batch on this cache."""
         ilpc.kv_compact(self.k_pool, self.v_pool, batch.block_tables, batch.cu_q, batch.start_pos, path, n_accepted,
                         stream)
 
@@ -288,6 +289,11 @@ class DeviceTables:
     ``pc.compact`` moves its K/V rows.  With ``shared`` rows can be forks of others
     (``fork``, then ``pc.copy_blocks``), and blocks go back once no row holds them.  A
     batch's forks end before the host gives its prompts back (``pc.release``).
+
+    The tables run ahead of the pools: what a call leaves to be done in every layer's
+    pools is queued before the next call on tables of this cache that takes blocks or
+    gives them back -- append and attention behind extend, ``pc.compact`` behind accept
+    (from blocks that are free already), ``pc.copy_blocks`` behind fork.
     """
 
     def __init__(self, pc: PagedPrefixCache, tables, seq_lens, max_rows: int, max_nodes: int = 0, shared: bool = False):
@@ -355,7 +361,8 @@ class DeviceTables:
         """Of the last extend's drafted tokens the path that the target's picks confirm stays
         (ilpc.tree_accept; all device int32 [max_rows], root_targets [B]): ``path``, ``n_accepted`` and
         ``next_tokens`` say which and what follows, the lengths end behind it, and blocks that it does
-        not reach are free again.  ``pc.compact`` then moves the K/V rows.  ``status`` keeps the bits of
+        not reach are free again.  ``pc.compact`` then moves the K/V rows, in every layer, before the next
+        extend, fork or release takes those blocks or shares the rows unmoved.  ``status`` keeps the bits of
         a refused extend, whose batch has no draft (``n_accepted`` 0)."""
         import torch
 
@@ -378,7 +385,8 @@ class DeviceTables:
         been released).  Returns the block pairs that ``pc.copy_blocks`` copies, in every layer.
 
         Rows forked from and rows forked over have no draft from then on: they keep all the tokens that they
-        hold, and accept finds nothing of them (``n_accepted`` 0)."""
+        hold, and accept finds nothing of them (``n_accepted`` 0).  So a draft is accepted, and its rows moved
+        (``pc.compact``, every layer), before its request is forked from."""
         import torch
 
         if not self.shared:

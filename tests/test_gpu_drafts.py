@@ -950,3 +950,92 @@ def test_requests_without_a_draft_keep_all():
         got = run_accept(par + [0], tok + [0], tok + [0], [0, 3, 5, 5], [7, -1, -1 << 31], root)
         most = (1 << 31) - 1
         assert got == [[0, 1, 2, -1, -1, 9], [3, 0, 0], nxt, [10, most, most], [1, most, most]]
+
+
+@pytest.mark.parametrize("captured", [False, True])
+@pytest.mark.parametrize("lens", [[37, 5, 64], [16, 48, 0]])
+def test_drafts_compacted_then_forked_then_drafted_again(lens, captured):
+    # accept, compact, (release,) fork, copy_blocks, extend: each row's cache stays that of its accepted tokens
+    Hkv, D, B, N = 2, 64, 6, 20
+    rng = np.random.default_rng(sum(lens))
+    m = Model(Hkv, D)
+    pc = pipeline.PagedPrefixCache(Hkv, D, 16, 24, B, 10, spare_blocks=100)
+    live = [rng.integers(0, m.vocab, n).astype(np.int32) for n in lens if n]
+    c, t = pc.match(live)
+    k, v = m.kv(np.concatenate(live), np.concatenate([np.arange(len(p)) for p in live]))
+    pc.append(pc.upload_prefill(c, t, [len(p) for p in live]), k.cuda(), v.cuda())
+    tables = np.full((B, 24), -1, np.int32)
+    tables[:len(live)] = t
+    tab = pipeline.DeviceTables(pc, tables, [len(p) for p in live] + [0] * (B - len(live)), B * N, max_nodes=N, shared=True)
+    seqs = [list(p) for p in live] + [[]] * (B - len(live))
+    R = tab.max_rows
+    d = {k: dev([0] * R) for k in ("par", "tok", "pick")}
+    new, ended, src = dev([0] * B), dev([0] * B), dev(range(B))
+    kv = [torch.zeros(R, Hkv, D, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+
+    def draft():
+        batch = tab.extend(new, N)
+        pc.append_slots(tab.slot_map, *kv)
+        tab.accept(d["par"], d["tok"], d["pick"])
+        pc.compact(batch, tab.path, tab.n_accepted)
+
+    def fork():
+        tab.release(ended)
+        pc.copy_blocks(*tab.fork(src))
+
+    calls = dict(draft=draft, fork=fork)
+    if captured:
+        for name, call in list(calls.items()):
+            call()  # (without new tokens, ended rows or forks, which changes nothing)
+            torch.cuda.synchronize()
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g):
+                call()
+            calls[name] = g.replay
+    for it in range(14):
+        sizes, par, tok, pick, pos = [], [], [], [], []
+        for r in range(B):
+            n = int(rng.integers(0, N + 1)) if seqs[r] else 0
+            p = random_tree(n, rng, 2)
+            tk = rng.integers(0, m.vocab, n).tolist()
+            sizes.append(n)
+            par, tok, pick = par + p, tok + tk, pick + picks_for(p, tk, rng, vocab=m.vocab)
+            pos += [len(seqs[r]) + len(a) - 1 for a in tree_ref.ancestors(p)]
+        n = len(par)
+        new.copy_(dev(sizes))
+        for key, x in (("par", par), ("tok", tok), ("pick", pick)):
+            d[key][:n] = dev(x)
+        for to, x in zip(kv, m.kv(tok, pos)):
+            to[:n], to[n:] = x.cuda(), float("nan")
+        calls["draft"]()
+        torch.cuda.synchronize()
+        assert ints(tab.status) == [0]
+        at = 0
+        for r in range(B):
+            path, _ = tree_ref.accept_ref(*(x[at:at + sizes[r]] for x in (par, tok, pick)))
+            seqs[r] = seqs[r] + [tok[at + i] for i in path]
+            at += sizes[r]
+        if it % 3 != 2:
+            ends = [r for r in range(B) if seqs[r] and rng.random() < 0.35][:B - 2]
+            for r in ends:
+                seqs[r] = []
+            on = [r for r in range(B) if seqs[r]]
+            of = [r if seqs[r] or not on or rng.random() < 0.3 else int(rng.choice(on)) for r in range(B)]
+            ended.copy_(dev([int(r in ends) for r in range(B)])), src.copy_(dev(of))
+            calls["fork"]()
+            torch.cuda.synchronize()
+            assert ints(tab.status) == [0]
+            seqs = [list(seqs[s]) for s in of]
+        assert ints(tab.seq_lens) == [len(s) for s in seqs]
+        for r, s in enumerate(seqs):
+            if s:
+                k, v = m.kv(s, np.arange(len(s)))
+                got = rows_of_cache(pc, tab, r)
+                assert same_bits(got[0], k.cuda()) and same_bits(got[1], v.cuda()), (it, r)
+        conserved(pc, tab)
+        if not any(seqs):
+            break
+    assert it > 3
+    tab.release(dev([1] * B))
+    torch.cuda.synchronize()
+    assert ints(pc.free_taken) == [0] and not any(ints(pc.holds))
