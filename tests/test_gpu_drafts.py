@@ -1039,3 +1039,93 @@ def test_drafts_compacted_then_forked_then_drafted_again(lens, captured):
     tab.release(dev([1] * B))
     torch.cuda.synchronize()
     assert ints(pc.free_taken) == [0] and not any(ints(pc.holds))
+
+
+# -- replays ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("words", [1, 3])
+def test_replays_alone_write_masks_and_paths(words):
+    # (outputs are spoiled before each replay, and read before anything else runs)
+    rng = np.random.default_rng(words)
+    sizes, n = ([12, 8], 20) if words == 1 else ([150, 40], 190)
+    par, tok, pick, start = dev([-1] * n), dev(range(n)), dev([0] * n), dev([3, 40])
+    cu, masks, pos = dev([0, sizes[0], n]), dev(np.zeros((n, words)), np.int64), dev([0] * n)
+    outs = [dev([0] * n)] + [dev([0, 0]) for _ in range(4)]
+
+    def calls():
+        ilpc.tree_masks(par, cu, masks, pos, start)
+        ilpc.tree_accept(par, tok, pick, cu, start, *outs)
+
+    calls()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        calls()
+    for k in range(5):
+        trees = [random_tree(s, rng, 1 + k % 3) for s in sizes]
+        p, s = sum(trees, []), rng.integers(0, 900, 2).tolist()
+        t = picks_for(p[:sizes[0]], list(range(sizes[0])), rng) + picks_for(p[sizes[0]:], list(range(sizes[0], n)), rng)
+        for x, y in ((par, p), (pick, t), (start, s)):
+            x.copy_(dev(y))
+        for x in [masks, pos] + outs:
+            x.fill_(-77)
+        g.replay()
+        torch.cuda.synchronize()
+        want_m, want_p, path, rest = [], [], [], [[], [], [], []]
+        for at, tree, st in zip((0, sizes[0]), trees, s):
+            m, q = tree_ref.masks_ref(tree, st, words)
+            want_m += [signed(x) for x in m]
+            want_p += q
+            got, nxt = tree_ref.accept_ref(tree, list(range(at, at + len(tree))), t[at:at + len(tree)])
+            path += got + [-1] * (len(tree) - len(got))
+            for o, x in zip(rest, (len(got), nxt, st + len(got), -(-(st + len(got)) // 16))):
+                o.append(x)
+        assert ints(masks) == want_m and ints(pos) == want_p and [ints(o) for o in outs] == [path] + rest
+        torch.zeros(1000, device="cuda").sum().item()  # (eager work between replays)
+
+
+@pytest.mark.parametrize("B,live,hi", [(40, 5, 300), (400, 30, 500)])
+def test_replays_alone_fork_copy_and_release(B, live, hi):
+    # of one launch each and of two
+    rng = np.random.default_rng(B)
+    s = Rows(B, live, hi, 2, B + 200, 5)
+    kp, vp = pools(s.nb, 2, 64)
+    src, ended, d = dev(range(B)), dev([0] * B), s.d
+
+    def calls():
+        ilpc.fork_tables(d["bt"], d["lens"], src, d["holds"], 2, d["free"], d["taken"], d["src"], d["dst"], d["taken"],
+                         d["status"], s.nb)
+        ilpc.copy_blocks(kp, vp, d["src"], d["dst"])
+        ilpc.release_shared(d["bt"], ended, d["holds"], 2, d["free"], d["taken"], d["taken"], d["out"], s.nb)
+
+    calls()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        calls()
+    free_rows = set(range(live, B))
+    for k in range(5):
+        # some empty rows become forks, and some rows that hold something end
+        sources = [int(rng.integers(0, live)) if r in free_rows and rng.random() < 0.5 else r for r in range(B)]
+        *rest, taken, st = tree_ref.fork_ref(s.tables, s.lens, sources, s.holds, 2, s.free, s.taken, s.nb)
+        s.tables, s.lens, s.holds, cs, cd = rest
+        ends = [n if r >= live and rng.random() < 0.6 else 0 for r, n in enumerate(s.lens)]
+        s.holds, s.free, s.taken, st2 = tree_ref.release_shared_ref(s.tables, ends, s.holds, 2, s.free, taken, s.nb)
+        assert (st, st2) == (0, 0)
+        src.copy_(dev(sources)), ended.copy_(dev(ends))
+        for x in ("src", "dst", "status", "out"):
+            d[x].fill_(-77)
+        wk, wv = kp.clone(), vp.clone()
+        for a, b in zip(cs, cd):
+            if a >= 0 and b >= 0:
+                wk[b], wv[b] = kp[a], vp[a]
+        g.replay()
+        torch.cuda.synchronize()
+        assert ints(d["status"]) == [0] and ints(d["out"]) == [0]
+        s.state((cs, cd))
+        assert same_bits(kp, wk) and same_bits(vp, wv)
+        # the rows that ended hold nothing from here on
+        s.lens = [0 if e else n for e, n in zip(ends, s.lens)]
+        d["lens"].copy_(dev(s.lens))
+        free_rows = {r for r in range(live, B) if s.lens[r] == 0}
+    assert any(s.holds)
