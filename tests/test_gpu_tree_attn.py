@@ -427,3 +427,54 @@ def test_the_binding_refuses():
     call(scale=b.scale, workspace=ws, stream=torch.cuda.current_stream())
     torch.cuda.synchronize()
     assert torch.equal(out, want)
+
+
+def permuted(b, order):
+    """The batch with its requests in another order: the same blocks, rows and masks."""
+    c = object.__new__(Batch)
+    c.__dict__.update(b.__dict__)
+    at = np.concatenate([[0], np.cumsum(b.new)])
+    rows = torch.from_numpy(np.concatenate([np.arange(at[r], at[r + 1]) for r in order])).cuda()
+    idx = torch.tensor(order, device="cuda")
+    c.q, c.masks = b.q[rows].contiguous(), b.masks[rows].contiguous()
+    c.bt, c.L = b.bt[idx].contiguous(), b.L[idx].contiguous()
+    c.new = [b.new[r] for r in order]
+    c.cu = torch.tensor(np.concatenate([[0], np.cumsum(c.new)]), dtype=torch.int32, device="cuda")
+    return c, rows
+
+
+SHAPES = {  # kernel -> (tokens before, nodes) of the batch that it takes
+    "stream": ([40, 0, 250, 7, 100, 31], [24, 3, 17, 0, 20, 24]),
+    "stream and join": ([4000, 0, 2500, 700, 1, 3333], [24, 3, 17, 0, 20, 24]),
+    "tiles": ([90, 0, 40, 64, 65], [33, 40, 1, 64, 17]),
+    "tiles, two groups": ([1000, 0, 40, 700, 65], [33, 40, 1, 64, 17])}
+
+
+def batch_of(kind, D, seed):
+    before, nodes = SHAPES[kind]
+    if "tiles" in kind:
+        return trees(**wide(before, nodes, 32, 4, D, "two" in kind), seed=seed)
+    return trees(before, nodes, seed=seed, Hq=8, Hkv=2, D=D)
+
+
+@pytest.mark.parametrize("kind", list(SHAPES))
+@pytest.mark.parametrize("D", [64, 128])
+def test_a_requests_rows_are_the_same_bits_at_any_place_of_the_batch(kind, D):
+    b = batch_of(kind, D, 14)
+    need = ilpc.tree_attn_workspace_bytes(len(b.new), b.max_q, b.Hq, b.Hkv, D, b.bt.shape[1])
+    assert (need > 0) == (kind == "stream and join")
+    first = b.run()
+    rng = np.random.default_rng(1)
+    for _ in range(3):
+        c, rows = permuted(b, rng.permutation(len(b.new)).tolist())
+        out = c.run()
+        torch.cuda.synchronize()
+        assert torch.equal(out, first[rows])
+    # other neighbours, of the same largest sizes
+    n = b.new[0]
+    b.q[n:] = (b.q[n:].flip(0) * 1.5).to(torch.bfloat16)
+    b.bt[1:] = b.bt[1:].flip(0)
+    again = b.run()
+    torch.cuda.synchronize()
+    assert torch.equal(again[:n], first[:n])
+    b.check(first, rows_of=[0])
