@@ -18,6 +18,7 @@ import numpy as np
 from . import ilpc
 
 BLOCK = ilpc.BLOCK
+MAX_NODES = 1024  # of a request's draft (16 mask words)
 
 
 @dataclass
@@ -283,7 +284,7 @@ class DeviceTables:
     (0: nothing), and what accepts behind it did: a refused extend changes nothing, and
     the append, attention and accept queued behind it do nothing.
 
-    A step of speculative decoding (``max_nodes`` > 0) extends by drafted tokens, a tree
+    A step of speculative decoding (``max_nodes`` > 0, at most 1024) extends by drafted tokens, a tree
     a request: ``tree`` makes the masks that ``pc.attend_tree`` reads, ``accept`` keeps
     the path that the target's picks confirm and gives the blocks behind it back, and
     ``pc.compact`` moves its K/V rows.  With ``shared`` rows can be forks of others
@@ -299,6 +300,8 @@ class DeviceTables:
     def __init__(self, pc: PagedPrefixCache, tables, seq_lens, max_rows: int, max_nodes: int = 0, shared: bool = False):
         import torch
 
+        if int(max_nodes) > MAX_NODES:
+            raise ilpc.ILPCError(ilpc.EUNSUP, f"DeviceTables: max_nodes {int(max_nodes)} > {MAX_NODES}")
         tables = np.ascontiguousarray(tables, dtype=np.int32)
         L = np.ascontiguousarray(seq_lens, dtype=np.int32)
         if tables.ndim != 2 or tables.shape[1] != pc.max_blocks or L.shape != (tables.shape[0],):

@@ -3,11 +3,13 @@ before anything is launched, in the library and in the binding."""
 import ctypes
 import os
 import re
+from types import SimpleNamespace
 
+import numpy as np
 import pytest
 import torch
 
-from paper_2507_08523_amd import ilpc
+from paper_2507_08523_amd import ilpc, pipeline
 
 P = 1 << 20  # stands for a device pointer in calls that are refused before it is used
 
@@ -124,3 +126,11 @@ def test_the_committed_profile_names_the_current_kernel_code(monkeypatch):
     for name, sha in named.items():
         monkeypatch.setattr(bench, "KERNEL_SRC", os.path.join(bench.ROOT, "paper_2507_08523_amd", "csrc", name))
         assert bench.kernel_source_sha() == sha, name
+
+
+@pytest.mark.parametrize("n", [1025, 4096])
+def test_tables_refuse_longer_drafts_than_the_calls_take(n):
+    pc = SimpleNamespace(max_blocks=4)  # (refused before anything of it is used)
+    with pytest.raises(ilpc.ILPCError, match="max_nodes") as e:
+        pipeline.DeviceTables(pc, np.full((2, 4), -1, np.int32), [0, 0], 8, max_nodes=n)
+    assert e.value.code == ilpc.EUNSUP
