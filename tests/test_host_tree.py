@@ -134,3 +134,15 @@ def test_tables_refuse_longer_drafts_than_the_calls_take(n):
     with pytest.raises(ilpc.ILPCError, match="max_nodes") as e:
         pipeline.DeviceTables(pc, np.full((2, 4), -1, np.int32), [0, 0], 8, max_nodes=n)
     assert e.value.code == ilpc.EUNSUP
+
+
+def test_the_committed_profile_names_the_headers_code(monkeypatch):
+    # (tree_attn.h has the mask window, diff_attn.h the operand layouts)
+    import bench
+
+    with open(os.path.join(bench.ROOT, "profiles", "tree_attn_kernel_trace.txt"), encoding="utf-8") as f:
+        named = dict(re.findall(r"^# code of (\w+\.h): ([0-9a-f]{16})$", f.read(), re.M))
+    assert sorted(named) == ["diff_attn.h", "tree_attn.h"]
+    for name, sha in named.items():
+        monkeypatch.setattr(bench, "KERNEL_SRC", os.path.join(bench.ROOT, "paper_2507_08523_amd", "csrc", name))
+        assert bench.kernel_source_sha() == sha, name
