@@ -577,7 +577,8 @@ int ilpc_paged_diff_attn(const uint16_t* q, int64_t q_stride, int32_t n_rows, co
  * masks      [device] uint64 [n_rows, mask_words], 8-byte aligned, out;
  *            1 <= mask_words <= 16 (ILPC_EUNSUP); nodes at or past 64 * mask_words
  *            see no node
- * positions  [device] int32 [n_rows] or NULL  out: start_pos + the node's depth
+ * positions  [device] int32 [n_rows] or NULL  out: start_pos + the node's depth;
+ *            start_pos for nodes that see no node
  *
  * Rows of no request stay as they are.
  */
@@ -723,7 +724,9 @@ int ilpc_fork_tables(int32_t* block_tables, int32_t max_blocks, int32_t B, int32
  * taken_out  [device] int32 [1]  out: taken - n; may be taken
  * status     [device] int32 [1]  out: 0, or bits: 1 more blocks than were taken, 2 a row
  *            longer than its table, 8 a negative length or taken outside [0, n_free], 16 a
- *            block given back more often than it is held; then nothing is changed
+ *            block given back more often than it is held; then nothing is changed.  (The counts do
+ *            not tell a free block from one held once: one that an earlier call gave back is in the
+ *            list twice, as with ilpc_release_tables.)
  */
 int ilpc_release_shared(const int32_t* block_tables, int32_t max_blocks, int32_t B, const int32_t* seq_lens,
                         int32_t* holds, int32_t first_id, int32_t* free_ids, int32_t n_free, const int32_t* taken,
