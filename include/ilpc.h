@@ -702,14 +702,24 @@ int ilpc_holds_words(int32_t n_blocks, int32_t* words);
  *
  * A shared block is full and stays so: no row may be cut back below the length it
  * was forked at, nor its rows below that moved: a draft that was open when its row was
- * forked from or over is none any more (start_pos < 0 in ilpc_tree_accept and
- * ilpc_kv_compact).  Limits as for ilpc_extend_tables.  Outputs must not overlap other
+ * forked from or over is none any more.  ilpc_fork_tables_drafts is the same call, which
+ * writes that down for ilpc_tree_accept and ilpc_kv_compact:
+ *
+ * start_pos    [device] int32 [B] or NULL  in/out: -1 for rows forked from or over; others, and
+ *              all where the batch is refused, stay
+ *
+ * Limits as for ilpc_extend_tables.  Outputs must not overlap other
  * arguments (taken_out may be taken).
  */
 int ilpc_fork_tables(int32_t* block_tables, int32_t max_blocks, int32_t B, int32_t* seq_lens, const int32_t* sources,
                      int32_t* holds, int32_t first_id, const int32_t* free_ids, int32_t n_free, const int32_t* taken,
                      int32_t num_blocks, int32_t* copy_src, int32_t* copy_dst, int32_t* taken_out, int32_t* status,
                      void* stream);
+int ilpc_fork_tables_drafts(int32_t* block_tables, int32_t max_blocks, int32_t B, int32_t* seq_lens,
+                            const int32_t* sources, int32_t* holds, int32_t first_id, const int32_t* free_ids,
+                            int32_t n_free, const int32_t* taken, int32_t num_blocks, int32_t* copy_src,
+                            int32_t* copy_dst, int32_t* start_pos, int32_t* taken_out, int32_t* status,
+                            void* stream);
 
 /*
  * Blocks of ended rows given back where rows share them: of row r, the first

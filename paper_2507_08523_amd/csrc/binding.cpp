@@ -42,7 +42,7 @@ decltype(&ilpc_tree_attn_workspace_bytes) tree_attn_workspace_bytes = nullptr;
 decltype(&ilpc_paged_tree_attn) paged_tree_attn = nullptr;
 decltype(&ilpc_tree_accept) tree_accept = nullptr;
 decltype(&ilpc_kv_compact) kv_compact = nullptr;
-decltype(&ilpc_fork_tables) fork_tables = nullptr;
+decltype(&ilpc_fork_tables_drafts) fork_tables = nullptr;
 decltype(&ilpc_release_shared) release_shared = nullptr;
 decltype(&ilpc_copy_blocks) copy_blocks = nullptr;
 
@@ -555,7 +555,7 @@ bool holds_fit(const at::Tensor& holds, int64_t num_blocks, int64_t first) {
 }
 
 // fork_tables(block_tables, seq_lens, sources, holds, first_id, free_ids, taken, copy_src, copy_dst, taken_out, status,
-//             num_blocks, stream)
+//             num_blocks, start_pos, stream)
 PyObject* py_fork_tables(PyObject*, PyObject* const* argv, Py_ssize_t n) {
   return guarded([&]() -> int {
     Args a{argv, n};
@@ -565,19 +565,23 @@ PyObject* py_fork_tables(PyObject*, PyObject* const* argv, Py_ssize_t n) {
     const at::Tensor *free = ints(1), *taken = ints(1), *from = ints(1), *to = ints(1), *out = ints(1),
                      *status = ints(1);
     const int32_t nb = a.integer();
+    const at::Tensor* start = a.tensor_or_none(at::kInt, 1);
     PyObject* so = a.next();
     if (!a.ok) return kNotHere;
     const int64_t B = src->size(0);
     if (bt->size(0) != B || seq->size(0) != B || from->size(0) != B || to->size(0) != B || taken->size(0) != 1 ||
-        out->size(0) != 1 || status->size(0) != 1 || !holds_fit(*holds, nb, first))
+        out->size(0) != 1 || status->size(0) != 1 || (start && start->size(0) != B) ||
+        !holds_fit(*holds, nb, first))
       return kNotHere;
-    if (!apart({bt, seq, holds, from, to, status, out},
-               {src, free, out->data_ptr() == taken->data_ptr() ? nullptr : taken}))
+    const at::Tensor* had = out->data_ptr() == taken->data_ptr() ? nullptr : taken;
+    if (start ? !apart({bt, seq, holds, from, to, status, out, start}, {src, free, had})
+              : !apart({bt, seq, holds, from, to, status, out}, {src, free, had}))
       return kNotHere;
     void* s;
-    if (!placed({bt, seq, src, holds, free, taken, from, to, out, status}, so, &s)) return kNotHere;
+    if (!placed({bt, seq, src, holds, free, taken, from, to, out, status, start}, so, &s)) return kNotHere;
     return call(fork_tables, i32(bt), int32_t(bt->size(1)), int32_t(B), i32(seq), i32(src), i32(holds), first,
-                i32(free), int32_t(free->size(0)), i32(taken), nb, i32(from), i32(to), i32(out), i32(status), s);
+                i32(free), int32_t(free->size(0)), i32(taken), nb, i32(from), i32(to), start ? i32(start) : nullptr,
+                i32(out), i32(status), s);
   });
 }
 

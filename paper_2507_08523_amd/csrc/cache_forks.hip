@@ -74,13 +74,14 @@ __device__ __forceinline__ void fork_entry(int r, int j, int src, int len, int o
 // Checks, lengths and copies, by one workgroup: a thread takes a run of rows.  The batch
 // is forked whole or not at all, so that nothing is written before all rows are known
 // to be right.  FILL: the same workgroup writes the rows.  Bound by its round trips (sources,
-// lengths, ids): 3.9 us for 512 rows; 4.2 with FILL for 16 rows of up to 38 blocks.
+// lengths, ids): 3.9 us for 512 rows; 4.2 with FILL for 16 rows of up to 38 blocks.  draft_start (or NULL): -1, no
+// draft, for rows forked from or over, by whichever of their forks comes last.
 template <bool FILL>
 __global__ __launch_bounds__(kThreads) void fork_scan_kernel(
     int32_t* block_tables, int max_blocks, int B, int32_t* seq_lens, const int32_t* __restrict__ sources,
     int32_t* holds, int first_id, const int32_t* __restrict__ free_ids, int n_free, const int32_t* taken,
-    int num_blocks, int32_t* __restrict__ copy_src, int32_t* __restrict__ copy_dst, int32_t* taken_out,
-    int32_t* __restrict__ status) {
+    int num_blocks, int32_t* __restrict__ copy_src, int32_t* __restrict__ copy_dst, int32_t* draft_start,
+    int32_t* taken_out, int32_t* __restrict__ status) {
   const int per = (B + kThreads - 1) / kThreads;
   const int r0 = min(int(threadIdx.x) * per, B), r1 = min(r0 + per, B);
   const int64_t had = *taken;
@@ -111,6 +112,7 @@ __global__ __launch_bounds__(kThreads) void fork_scan_kernel(
           to = free_ids[at++];
         }
         seq_lens[r] = len;  // (sources stay: no other row's length comes from here)
+        if (draft_start) draft_start[r] = draft_start[s] = -1;
       }
     }
     copy_src[r] = from;
@@ -336,10 +338,11 @@ constexpr int kOneFork = 4096, kOneRelease = 4096;
 
 }  // namespace
 
-extern "C" int ilpc_fork_tables(int32_t* block_tables, int32_t max_blocks, int32_t B, int32_t* seq_lens,
-                                const int32_t* sources, int32_t* holds, int32_t first_id, const int32_t* free_ids,
-                                int32_t n_free, const int32_t* taken, int32_t num_blocks, int32_t* copy_src,
-                                int32_t* copy_dst, int32_t* taken_out, int32_t* status, void* stream) {
+extern "C" int ilpc_fork_tables_drafts(int32_t* block_tables, int32_t max_blocks, int32_t B, int32_t* seq_lens,
+                                       const int32_t* sources, int32_t* holds, int32_t first_id,
+                                       const int32_t* free_ids, int32_t n_free, const int32_t* taken,
+                                       int32_t num_blocks, int32_t* copy_src, int32_t* copy_dst, int32_t* start_pos,
+                                       int32_t* taken_out, int32_t* status, void* stream) {
   static const char* fn = "ilpc_fork_tables";
   using ilpc::set_error;
   const int rc = check_sizes(fn, B, max_blocks, n_free, num_blocks, first_id);
@@ -351,7 +354,7 @@ extern "C" int ilpc_fork_tables(int32_t* block_tables, int32_t max_blocks, int32
   const bool one = int64_t(B) * max_blocks <= kOneFork;
   auto launch_scan = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, dim3(1), dim3(kThreads), 0, s, block_tables, max_blocks, B, seq_lens, sources, holds,
-                       first_id, free_ids, n_free, taken, num_blocks, copy_src, copy_dst, taken_out, status);
+                       first_id, free_ids, n_free, taken, num_blocks, copy_src, copy_dst, start_pos, taken_out, status);
   };
   if (one) launch_scan(fork_scan_kernel<true>);
   else launch_scan(fork_scan_kernel<false>);
@@ -361,6 +364,14 @@ extern "C" int ilpc_fork_tables(int32_t* block_tables, int32_t max_blocks, int32
   hipLaunchKernelGGL(fork_fill_kernel, dim3(unsigned(B), parts), dim3(kFillThreads), 0, s, block_tables, max_blocks,
                      seq_lens, sources, holds, first_id, num_blocks, copy_dst, status);
   return launch_status(fn);
+}
+
+extern "C" int ilpc_fork_tables(int32_t* block_tables, int32_t max_blocks, int32_t B, int32_t* seq_lens,
+                                const int32_t* sources, int32_t* holds, int32_t first_id, const int32_t* free_ids,
+                                int32_t n_free, const int32_t* taken, int32_t num_blocks, int32_t* copy_src,
+                                int32_t* copy_dst, int32_t* taken_out, int32_t* status, void* stream) {
+  return ilpc_fork_tables_drafts(block_tables, max_blocks, B, seq_lens, sources, holds, first_id, free_ids, n_free,
+                                 taken, num_blocks, copy_src, copy_dst, nullptr, taken_out, status, stream);
 }
 
 extern "C" int ilpc_release_shared(const int32_t* block_tables, int32_t max_blocks, int32_t B, const int32_t* seq_lens,

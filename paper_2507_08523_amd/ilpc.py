@@ -76,6 +76,8 @@ _SIGS = [
     ("ilpc_kv_compact", _i32, [_vp, _vp, _i32, _vp, _i32, _vp, _vp, _i32, _i32, _vp, _vp, _i32, _i32, _i32, _vp]),
     ("ilpc_holds_words", _i32, [_i32, ctypes.POINTER(_i32)]),
     ("ilpc_fork_tables", _i32, [_vp, _i32, _i32, _vp, _vp, _vp, _i32, _vp, _i32, _vp, _i32, _vp, _vp, _vp, _vp, _vp]),
+    ("ilpc_fork_tables_drafts", _i32, [_vp, _i32, _i32, _vp, _vp, _vp, _i32, _vp, _i32, _vp, _i32, _vp, _vp, _vp, _vp,
+                                       _vp, _vp]),
     ("ilpc_release_shared", _i32, [_vp, _i32, _i32, _vp, _vp, _i32, _vp, _i32, _vp, _i32, _vp, _vp, _vp]),
     ("ilpc_copy_blocks", _i32, [_vp, _vp, _i32, _vp, _vp, _i32, _i32, _i32, _i32, _vp]),
     ("ilpc_chunk_schedule", _i32, [_vp, _i32, _i32, _i32, _vp, _vp, _vp, _vp, ctypes.POINTER(_i32),
@@ -151,7 +153,7 @@ def _native():
             "ilpc_paged_prefill_attn_cascade", "ilpc_extend_tables", "ilpc_release_tables", "ilpc_kv_append_slots",
             "ilpc_diff_attn_workspace_bytes", "ilpc_paged_diff_attn", "ilpc_tree_masks",
             "ilpc_tree_attn_workspace_bytes", "ilpc_paged_tree_attn", "ilpc_tree_accept", "ilpc_kv_compact",
-            "ilpc_fork_tables", "ilpc_release_shared", "ilpc_copy_blocks")))
+            "ilpc_fork_tables_drafts", "ilpc_release_shared", "ilpc_copy_blocks")))
         _binding = mod
     return _binding
 
@@ -1001,17 +1003,18 @@ def _holds(fn, holds, num_blocks, first_id):
 
 
 def fork_tables(block_tables, seq_lens, sources, holds, first_id: int, free_ids, taken, copy_src, copy_dst, taken_out,
-                status, num_blocks: int, stream=None):
+                status, num_blocks: int, stream=None, start_pos=None):
     """Rows of a batch become forks of others: r of sources[r] where that is another row
     (see the C header).
 
     All int32 device tensors: block_tables [B, max_blocks] and seq_lens [B] (in/out),
     sources [B], holds [holds_words(num_blocks - first_id)] (in/out), free_ids [n],
     taken [1]; out: copy_src and copy_dst [B] (copy_blocks'), taken_out [1] (may be
-    taken), status [1].
+    taken), status [1].  start_pos [B] or None (in/out): that of the rows' drafts, -1 for
+    rows forked from or over, which have none any more (tree_accept, kv_compact).
     """
     rc = (_binding or _native()).fork_tables(block_tables, seq_lens, sources, holds, first_id, free_ids, taken,
-                                             copy_src, copy_dst, taken_out, status, num_blocks, stream)
+                                             copy_src, copy_dst, taken_out, status, num_blocks, start_pos, stream)
     if rc is not None:
         return _check(rc)
 
@@ -1020,18 +1023,19 @@ def fork_tables(block_tables, seq_lens, sources, holds, first_id: int, free_ids,
     p = _ints(fn, block_tables=(block_tables, (B, -1)), seq_lens=(seq_lens, (B,)), sources=(sources, (B,)),
               free_ids=(free_ids, (-1,)), taken=(taken, (1,)), copy_src=(copy_src, (B,)), copy_dst=(copy_dst, (B,)),
               taken_out=(taken_out, (1,)), status=(status, (1,)))
+    sp = _ints(fn, start_pos=(start_pos, (B,)))[0] if start_pos is not None else None
     hp = _holds(fn, holds, int(num_blocks), int(first_id))
     outs = [("block_tables", block_tables), ("seq_lens", seq_lens), ("holds", holds), ("copy_src", copy_src),
-            ("copy_dst", copy_dst), ("status", status)]
+            ("copy_dst", copy_dst), ("status", status)] + ([("start_pos", start_pos)] if start_pos is not None else [])
     ins = [("sources", sources), ("free_ids", free_ids)]
     _taken(outs, ins, taken_out, taken)
     _apart(fn, outs, ins)
-    ctx, s = _at((sources, block_tables, seq_lens, holds, free_ids, taken, copy_src, copy_dst, taken_out, status),
-                 stream)
+    ctx, s = _at((sources, block_tables, seq_lens, holds, free_ids, taken, copy_src, copy_dst, taken_out, status,
+                  start_pos), stream)
     with ctx:
-        _check(load().ilpc_fork_tables(p[0], block_tables.shape[1], B, p[1], p[2], hp, int(first_id), p[3],
-                                       free_ids.shape[0], p[4], int(num_blocks), p[5], p[6], p[7], p[8],
-                                       ctypes.c_void_p(s.cuda_stream)))
+        _check(load().ilpc_fork_tables_drafts(p[0], block_tables.shape[1], B, p[1], p[2], hp, int(first_id), p[3],
+                                              free_ids.shape[0], p[4], int(num_blocks), p[5], p[6], sp, p[7], p[8],
+                                              ctypes.c_void_p(s.cuda_stream)))
 
 
 def release_shared(block_tables, seq_lens, holds, first_id: int, free_ids, taken, taken_out, status, num_blocks: int,

@@ -327,7 +327,6 @@ class DeviceTables:
             self.n_accepted, self.next_tokens = empty(self.B), empty(self.B)
             self.kept_lens, self.kept_blocks = empty(self.B), empty(self.B)
             self._accept_status = empty(1)
-            self._row_ids = dev(np.arange(self.B))
         if self.shared:
             self.copy_src, self.copy_dst = empty(self.B).fill_(-1), empty(self.B).fill_(-1)
 
@@ -390,20 +389,14 @@ class DeviceTables:
         Rows forked from and rows forked over have no draft from then on: they keep all the tokens that they
         hold, and accept finds nothing of them (``n_accepted`` 0).  So a draft is accepted, and its rows moved
         (``pc.compact``, every layer), before its request is forked from."""
-        import torch
-
         if not self.shared:
             raise ilpc.ILPCError(ilpc.EINVAL, "fork: DeviceTables was made without shared")
         pc = self.pc
+        # (drafts end: their blocks may be other rows' as well now, or the draft be that of a row that was here before,
+        # and a path must neither cut nor move them)
         ilpc.fork_tables(self.block_tables, self.seq_lens, sources, pc.holds, pc.num_blocks, pc.free_ids,
-                         pc.free_taken, self.copy_src, self.copy_dst, pc.free_taken, self.status, pc.k_pool.shape[0])
-        if self.max_nodes > 0:
-            # The blocks of an open draft may be other rows' as well now, or the draft that of a row that was here
-            # before: a path must neither cut nor move them.  (Index B: rows that stay, or a refused fork's.)
-            forks = (sources != self._row_ids) & (self.status == 0)
-            ended = torch.zeros(self.B + 1, dtype=torch.bool, device=pc.device)
-            ended.scatter_(0, torch.where(forks, sources, self.B).long(), True)
-            self.start_pos.masked_fill_(ended[:-1] | forks, -1)
+                         pc.free_taken, self.copy_src, self.copy_dst, pc.free_taken, self.status, pc.k_pool.shape[0],
+                         start_pos=self.start_pos if self.max_nodes > 0 else None)
         return self.copy_src, self.copy_dst
 
     def release(self, ended):

@@ -1129,3 +1129,34 @@ def test_replays_alone_fork_copy_and_release(B, live, hi):
         d["lens"].copy_(dev(s.lens))
         free_rows = {r for r in range(live, B) if s.lens[r] == 0}
     assert any(s.holds)
+
+
+# -- drafts' starts in the fork's own call ---------------------------------------------
+
+@pytest.mark.parametrize("general", [False, True])
+@pytest.mark.parametrize("B,live,hi", [(1, 1, 20), (12, 4, 100), (300, 40, 700), (3000, 5, 33)])
+def test_forks_write_down_whose_drafts_have_ended(B, live, hi, general):
+    rng = np.random.default_rng(B)
+    for share in (0.0, 0.5, 1.0):
+        s = Rows(B, live, hi, 2, B + 8, B)
+        src = [int(rng.integers(0, live)) if r >= live and rng.random() < share else r for r in range(B)]
+        d, start = s.d, rng.integers(0, 99, B).tolist()
+        at = dev(start + [5])[:B]
+        num = np.int64(s.nb) if general else s.nb  # (what is no plain int goes by way of ctypes)
+        fork = lambda to, of=None: ilpc.fork_tables(  # noqa: E731
+            d["bt"], d["lens"], dev(of or src), d["holds"], 2, d["free"], d["taken"], d["src"], d["dst"], d["taken"],
+            d["status"], num, start_pos=to)
+        if B > 1:
+            fork(at, src[:-1] + [B])
+            torch.cuda.synchronize()
+            assert ints(d["status"]) == [ilpc.BAD_VALUE] and ints(at) == start
+        fork(at)
+        s.tables, s.lens, s.holds, cs, cd, s.taken, st = tree_ref.fork_ref(s.tables, s.lens, src, s.holds, 2, s.free, s.taken,
+                                                                          s.nb)
+        s.state((cs, cd))
+        touched = {r for r in range(B) if src[r] != r} | {x for r, x in enumerate(src) if x != r}
+        assert st == 0 and ints(d["status"]) == [0] and ints(at) == [-1 if r in touched else x for r, x in enumerate(start)]
+        for bad in (at.long(), dev(start + [1]), d["lens"], d["src"]):
+            with pytest.raises(ilpc.ILPCError):
+                fork(bad)
+        s.state((cs, cd))

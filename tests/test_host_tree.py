@@ -146,3 +146,16 @@ def test_the_committed_profile_names_the_headers_code(monkeypatch):
     for name, sha in named.items():
         monkeypatch.setattr(bench, "KERNEL_SRC", os.path.join(bench.ROOT, "paper_2507_08523_amd", "csrc", name))
         assert bench.kernel_source_sha() == sha, name
+
+
+fork_drafts = caller("ilpc_fork_tables_drafts", bt=P, mb=4, B=3, seq=P, src=P, holds=P, first=2, free=P, n_free=8, taken=P,
+                     nb=64, cs=P, cd=P, start=P, out=P, status=P)
+
+
+@pytest.mark.parametrize("kw,rc", [
+    *[({k: None}, EINVAL) for k in ("bt", "seq", "src", "holds", "free", "taken", "cs", "cd", "out", "status")],
+    *[({k: -1}, EINVAL) for k in ("B", "n_free", "nb", "first")], (dict(mb=0), EINVAL), (dict(first=65), EINVAL),
+    (dict(B=(1 << 20) + 1), EUNSUP), (dict(mb=(1 << 24) + 1), EUNSUP), (dict(nb=1 << 27), EUNSUP),
+    (dict(start=None, B=(1 << 20) + 1), EUNSUP)])
+def test_forks_beside_drafts_are_refused_alike(kw, rc):
+    assert fork_drafts(**kw) == rc, ilpc.load().ilpc_last_error()
