@@ -613,6 +613,9 @@ int ilpc_tree_attn_workspace_bytes(int32_t B, int32_t max_q_len, int32_t Hq, int
  *              that is 0).  Calls that may run concurrently, captured graphs
  *              among them, need separate ones.
  *
+ * How the work is cut goes by the batch's shape and by max_blocks: a table much wider than
+ * its contexts costs short ones time (and bytes of workspace).
+ *
  * K and V of a node that none of its request's rows sees may be anything (slots
  * that hold no token); V of the others is finite.  Requests with q_len_r > L_r are
  * not computed; otherwise the bounds rules of ilpc_paged_prefill_attn hold.  At

@@ -406,7 +406,7 @@ struct Plan {
 
 // What few tiles wait for is a wave's steps, about 1 us each one after the other: four waves to a tile,
 // and more workgroups while there are compute units without one; but their states' join is
-// a launch more (3 us, and more for many columns), so that contexts up to about 1.2 K
+// a launch more (3 us, and more for many columns), so that tables of up to about 1.2 K
 // keys are not cut, and a tile's range count goes as the root of its steps: the steps fall as 1 / ranges
 // and the join's reads grow with them.  us (waves x groups; 8 kv heads, D 128 where not said):
 //   tiles, keys       8, 300    4x1 8.6, 4x4 10.4             8, 1000    4x8 10.6, 4x4 11.7, 8x1 12.3
@@ -418,7 +418,7 @@ struct Plan {
 //   256, 2000         4x1 22.9, 4x2 27.9                      D 64: 32, 1000  8x1 9.0, 4x8 9.8, 4x1 10.0
 //   D 64: 128, 2500   8x1 14.5, 4x4 16.1, 4x1 18.2            D 64: 32, 3000  4x8 10.8, 8x1 14.9
 // A compute unit holds two workgroups of the kernel above.  From more than two tiles of 32 to a unit on, and in
-// contexts up to 320 keys from more than one (D 128), columns are taken 128 at a time on LDS tiles, where a pair has
+// tables of up to 320 keys from more than one (D 128), columns are taken 128 at a time on LDS tiles, where a pair has
 // more than one tile of 32 (here, there):
 //   280, 150    10.1, 9.8       384, 110    8.9, 7.6         400, 290    11.9, 11.8     400, 490    14.6, 14.5
 //   512, 230    11.9, 10.7      512, 320    12.6, 13.2       512, 2000   32.6, 36.2     400, 2000   30.5, 34.0
@@ -435,6 +435,20 @@ struct Plan {
 //   904, 150    19.1, 18.0, 19.5  904, 2000  165, 167, 171       1024, 500  51.2, 49.1, 48.2   2400, 100  34.0, 34.5, 38.5
 //   D 64: 400, 150  8.7, 6.4, 6.8     520, 1000  28.9, 29.6, 27.5     900, 150  9.9, 9.3, 10.4
 // Where a pair has more tiles, they share its keys from L2: 384 of 500 keys 23.3, 15.4, 14.0.
+// Between half as many tiles as compute units and as many, no rule cuts the keys (waves x groups):
+//   one tile of 32 a pair   136, 2000   4x1 24.5, 8x1 25.7, 4x2 35.0    136, 8000   4x1 101, 8x1 102, 4x2 134
+//                           192, 4000   4x1 70.5, 8x1 71.5, 4x2 84.1    256, 8000   4x1 180, 8x1 179, 4x2 193
+//   eight tiles a pair      192, 1000   4x1 13.3, 8x1 14.7, 4x2 20.2    192, 4000   4x1 33.5, 8x1 28.5, 4x2 33.6
+//                           192, 16000  4x1 116, 8x1 88.3, 4x2 94.1     256, 8000   4x1 65.2, 8x1 55.9, 4x2 61.2
+//   D 64, one tile          136, 4000   4x1 27.1, 8x1 25.1, 4x2 33.1    192, 2000   4x1 18.5, 8x1 18.8, 4x2 23.1
+// so that what the rules leave there is eight waves for pairs of several tiles from 2 K keys on.  At 128 tiles, one
+// a pair, the cut that several tiles gain by costs: 2000 keys 4x1 23.5, 8x2 28.6 (taken); 8000 98.7, 98.6.
+// `steps` goes by the table's width, which bounds the contexts (their lengths are on the device), and the sides
+// above had tables as wide as their contexts.  In wider ones short contexts get workgroups and a join that they do
+// not need; us by the width in blocks: 4 requests of 72 to 80 keys, 4 heads of D 64 on one: 6 5.5, 128 8.9, 512 9.9,
+// 2048 14.0; one request of 308 keys, 32 heads on 8: 21 7.6, 256 10.1, 1024 14.1, 2048 18.5; 64 of 216 to 266, 64 on
+// 8: 18 25.9, 128 23.6, from 256 on 21.3.  Longer or more ones do not depend on it: one of 4160 keys 261 19.6, 2048
+// 18.7; 32 of 570 to 1050 23.3 to 23.9.
 Plan make_plan(int64_t B, int64_t max_q_len, int Hq, int Hkv, int D, int64_t max_blocks) {
   const int64_t cus = ilpc::device_cus(), cols = max_q_len * (Hq / Hkv), pairs = B * Hkv;
   const int64_t steps = (max_blocks * kBlock + kStepKeys - 1) / kStepKeys;

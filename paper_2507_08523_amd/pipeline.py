@@ -243,7 +243,8 @@ class PagedPrefixCache:
 
     def attend_tree(self, batch: DeviceBatch, q, out, scale: float, masks, workspace=None, stream=None):
         """Attention of each request's newest tokens as a tree: all keys before them, and of
-        themselves those that a row's mask names (DeviceTables.tree, ilpc.paged_tree_attn)."""
+        themselves those that a row's mask names (DeviceTables.tree, ilpc.paged_tree_attn).  The work is cut
+        by the tables' width, ``max_blocks``: one far beyond the contexts costs short ones time."""
         ilpc.paged_tree_attn(q, self.k_pool, self.v_pool, batch.block_tables, batch.cu_q, batch.seq_lens,
                              batch.max_q_len, scale, masks, out, workspace, stream)
 
